@@ -346,6 +346,95 @@ dsmoe_status dsmoe_moa_forward(const dsmoe_layer_desc* desc, const dsmoe_moa_arg
                                void* workspace, size_t ws_bytes, int32_t* dev_status, dsmoe_stream stream);
 
 /*
+ * Attention against a key/value cache as steps of their own, for servers of the model whose caches are bounded, shared or thinned out (the
+ * paper has no counterpart: dsmoe_moa_forward attends to the whole cache).  One layout for all four calls:
+ *
+ *   queries  q[t, j, g, :]   bf16, token t < T, key/value head j < n_head, member g < group of the query heads that share it (the attention
+ *            layer: the experts that a token selected).  q_stride: elements between tokens, heads and members (0 allowed: broadcast);
+ *            d_head is contiguous.  out: bf16, o_stride likewise; no two rows may overlap.
+ *   caches   K, V [n_seq][n_head][L][d_head] bf16 by kv_stride (sequence, head, position; one for both), so that a cache that is stored by
+ *            position or is part of a larger one can be passed as it is.
+ *   tok_seq  device int32 [T], the sequence of each token, or NULL (all 0);  pos  device int32 [T]: token t sees keys 0 .. pos[t] of its
+ *            sequence's cache; -1: none (a padded entry of the batch: zeros in out, -inf in lse).
+ *   lse      fp32 [T][n_head][group] or NULL: the natural logarithm of the sum of the exponentials of a row's logits.
+ *
+ * All strides are multiples of 8 elements, addresses of 16 bytes.  d_head a multiple of 32 up to 256, group up to 64, otherwise
+ * DSMOE_ERR_UNSUPPORTED.  The memory from out's first element to its last must not overlap q's or the caches'.  Products of bf16 are added in fp32, softmax statistics are fp32, and out is
+ * rounded once.  Keys that a token does not see may hold anything, numbers or not.  A tok_seq or pos entry out of range is clamped and reported
+ * as DSMOE_ERR_INVALID_ARG in *dev_status.  workspace: dsmoe_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one
+ * call to the next.  Results do not change from run to run.
+ */
+typedef struct dsmoe_attention_desc {
+    int32_t T, n_head, group, d_head, n_seq, L;
+    float scale;                 /* logits are scale * <q, k> */
+    int64_t q_stride[3];         /* token, head, member */
+    int64_t o_stride[3];         /* token, head, member */
+    int64_t kv_stride[3];        /* sequence, head, position */
+} dsmoe_attention_desc;
+
+typedef enum { DSMOE_ATTENTION_WINDOW = 0, DSMOE_ATTENTION_PREFIX = 1, DSMOE_ATTENTION_TALLY = 2 } dsmoe_attention_kind;
+
+/* Bytes of scratch for one of the three attention calls with this desc.  prefix_len: of DSMOE_ATTENTION_PREFIX, otherwise ignored. */
+dsmoe_status dsmoe_attention_workspace_size(const dsmoe_attention_desc* desc, int kind, int prefix_len, size_t* bytes);
+
+/*
+ * Attention with a sliding window and sinks: token t at position p = pos[t] sees key l iff 0 <= l <= p and (p - l < window or l < sinks).
+ *   window >= 1, sinks >= 0.
+ *   rolling 0: position l lies in slot l of the cache, pos[t] < L.  rolling 1: the cache keeps the first `sinks` positions and the latest
+ *   others: position l lies in slot l (l < sinks) or sinks + (l - sinks) % (L - sinks); pos[t] has no bound, window <= L - sinks.  The caller
+ *   sees to it that the keys that the call's tokens see are all there: with n neighbouring tokens of a sequence in one call, window + n - 1
+ *   <= L - sinks.
+ */
+dsmoe_status dsmoe_window_attention(const dsmoe_attention_desc* desc, int window, int sinks, int rolling, const void* q, const void* K,
+                                    const void* V, const int32_t* tok_seq, const int32_t* pos, void* out, float* lse, void* workspace,
+                                    size_t ws_bytes, int32_t* dev_status, dsmoe_stream stream);
+
+/*
+ * Attention of a batch whose sequences begin with the same prefix, which is held and read once for all: every token sees the P keys of the prefix
+ * Kp, Vp [n_head][P][d_head] (prefix_stride: elements between heads and positions), then keys 0 .. pos[t] of its sequence's own cache (pos[t]
+ * counts from there; -1: the prefix alone).  P >= 0.
+ */
+typedef struct dsmoe_prefix {
+    const void* Kp;
+    const void* Vp;
+    int32_t P;
+    int64_t stride[2];           /* head, position */
+} dsmoe_prefix;
+dsmoe_status dsmoe_prefix_attention(const dsmoe_attention_desc* desc, const dsmoe_prefix* prefix, const void* q, const void* K, const void* V,
+                                    const int32_t* tok_seq, const int32_t* pos, void* out, float* lse, void* workspace, size_t ws_bytes,
+                                    int32_t* dev_status, dsmoe_stream stream);
+
+/*
+ * Attention (token t sees keys 0 .. pos[t]) that also adds up the weight that each key gets, which is what dsmoe_cache_evict goes by:
+ *   tally_out[s][j][l] = tally_in[s][j][l] + sum over tokens t of sequence s and members g of the softmax weight of key l.
+ *   tally_in, tally_out: fp32 [n_seq][n_head][L]; tally_in NULL: zeros; they may be the same.  tally_out is written in full.
+ */
+dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void* q, const void* K, const void* V, const int32_t* tok_seq,
+                                   const int32_t* pos, void* out, float* lse, const float* tally_in, float* tally_out, void* workspace,
+                                   size_t ws_bytes, int32_t* dev_status, dsmoe_stream stream);
+
+/*
+ * Thins a cache out.  Sequence s holds n = len[s] keys; if n > keep, of each (sequence, head) stay the first `sinks`, the last `recent` and,
+ * of the others, the keep - sinks - recent with the largest tally (ties: the lower index; a tally that is no number comes last); otherwise all.
+ * What stays is closed up in its order into K_out, V_out, tally_out.  desc: n_head, d_head, n_seq, L and kv_stride (the cache K, V) alone.
+ *   len int32 [n_seq] device; tally fp32 [n_seq][n_head][L]; kept int32 [n_seq][n_head][keep]: the indices, -1 behind them;
+ *   len_out int32 [n_seq]: min(n, keep), may be len.
+ *   K_out, V_out: bf16, room for keep positions by out_stride (sequence, head, position); tally_out: fp32, heads tally_pitch (>= keep) apart.
+ *   Rows behind the last one that stays are left as they were.  K_out = K and V_out = V with the same strides: in place; likewise tally_out =
+ *   tally with tally_pitch = L.  Otherwise the memory from their first elements to their last must not overlap that of K, V and tally.
+ *   workspace: dsmoe_evict_workspace_size bytes.
+ */
+typedef struct dsmoe_evict_args {
+    int32_t keep, sinks, recent;     /* 1 <= keep <= L, sinks + recent <= keep */
+    int64_t out_stride[3];
+    int64_t tally_pitch;
+} dsmoe_evict_args;
+dsmoe_status dsmoe_evict_workspace_size(const dsmoe_attention_desc* desc, size_t* bytes);
+dsmoe_status dsmoe_cache_evict(const dsmoe_attention_desc* desc, const dsmoe_evict_args* args, const int32_t* len, const float* tally,
+                               const void* K, const void* V, int32_t* kept, int32_t* len_out, float* tally_out, void* K_out, void* V_out,
+                               void* workspace, size_t ws_bytes, int32_t* dev_status, dsmoe_stream stream);
+
+/*
  * Measurement aid (no counterpart in the paper): a ring of CUDA event pairs on the caller's stream.
  * After dsmoe_timing_enable(n_pairs) (n_pairs > 0; events are created here, so call it outside any
  * timed region), every launch of an expert-MLP tensor-core kernel is bracketed by the next pair until

@@ -17,6 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdsmoe.so")
 
 F32, BF16 = 0, 1
+ATTENTION_WINDOW, ATTENTION_PREFIX, ATTENTION_TALLY = 0, 1, 2
 SELECT_THRESHOLD, SELECT_TOPK, SELECT_ALL, SELECT_THRESHOLD_TOPK = 0, 1, 2, 3
 
 EXPORTS = (
@@ -25,6 +26,8 @@ EXPORTS = (
     "dsmoe_layer_forward", "dsmoe_layer_forward_host", "dsmoe_layer_forward_host_async", "dsmoe_timing_enable", "dsmoe_timing_read",
     "dsmoe_select_static", "dsmoe_workspace_size_packed", "dsmoe_workspace_size_stages", "dsmoe_stats",
     "dsmoe_mi_loss", "dsmoe_dense_backward", "dsmoe_moa_forward",
+    "dsmoe_attention_workspace_size", "dsmoe_window_attention", "dsmoe_prefix_attention", "dsmoe_tally_attention",
+    "dsmoe_evict_workspace_size", "dsmoe_cache_evict",
 )
 
 
@@ -40,15 +43,30 @@ class MoaArgs(ctypes.Structure):
                 ("Kc", ctypes.c_void_p), ("Vc", ctypes.c_void_p), ("tok_seq", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
 
 
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("n_head", ctypes.c_int32), ("group", ctypes.c_int32), ("d_head", ctypes.c_int32),
+                ("n_seq", ctypes.c_int32), ("L", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3), ("kv_stride", ctypes.c_int64 * 3)]
+
+
+class Prefix(ctypes.Structure):
+    _fields_ = [("Kp", ctypes.c_void_p), ("Vp", ctypes.c_void_p), ("P", ctypes.c_int32), ("stride", ctypes.c_int64 * 2)]
+
+
+class EvictArgs(ctypes.Structure):
+    _fields_ = [("keep", ctypes.c_int32), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("out_stride", ctypes.c_int64 * 3), ("tally_pitch", ctypes.c_int64)]
+
+
 class DsmoeError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
         super().__init__(f"{where}: {status_string(code)} (status {code})")
 
 
-# Arguments of the entry points by letter: d(escriptor), p(ointer), n (size_t), i(nt).  Declared once, so that a call passes plain numbers:
+# Arguments of the entry points by letter: d(escriptor), a(ttention descriptor), p(ointer), n (size_t), i(nt).  Declared once, so that a call passes plain numbers:
 # building a ctypes object for each of a call's dozen arguments cost as much host time as the call's launches.
-_ARGTYPES = {"d": ctypes.POINTER(LayerDesc), "p": ctypes.c_void_p, "n": ctypes.c_size_t, "i": ctypes.c_int}
+_ARGTYPES = {"d": ctypes.POINTER(LayerDesc), "a": ctypes.POINTER(AttentionDesc), "p": ctypes.c_void_p, "n": ctypes.c_size_t, "i": ctypes.c_int}
 _SIGNATURES = {
     "dsmoe_workspace_size": "dp", "dsmoe_workspace_size_packed": "dp", "dsmoe_workspace_size_stages": "dp", "dsmoe_packed_size": "dp",
     "dsmoe_router": "dppppp", "dsmoe_select": "dppppppnp", "dsmoe_select_static": "dpppppp", "dsmoe_permute": "dpppppppppnp",
@@ -56,6 +74,8 @@ _SIGNATURES = {
     "dsmoe_layer_forward": "dppppppppppnpp", "dsmoe_layer_forward_host": "dppppppppppnpp",
     "dsmoe_layer_forward_host_async": "dppppppppppnpp", "dsmoe_stats": "dpppp", "dsmoe_mi_loss": "dppppnp",
     "dsmoe_dense_backward": "dppppppppppnpp", "dsmoe_moa_forward": "dpppppppppnpp",
+    "dsmoe_attention_workspace_size": "aiip", "dsmoe_window_attention": "aiii" + "p" * 8 + "npp", "dsmoe_prefix_attention": "ap" + "p" * 8 + "npp",
+    "dsmoe_tally_attention": "a" + "p" * 10 + "npp", "dsmoe_evict_workspace_size": "ap", "dsmoe_cache_evict": "ap" + "p" * 10 + "npp",
     "dsmoe_timing_enable": "i", "dsmoe_timing_read": "pip",
 }
 
@@ -248,6 +268,102 @@ def dsmoe_moa_forward(desc, n_head, scale, Kc, Vc, tok_seq, pos, x, Wr, br, pack
                                    _ptr(out), _ptr(mask_out), _ptr(counts_out), _ptr(workspace),
                                    workspace.numel() if workspace is not None else 0,
                                    _ptr(dev_status), _stream(stream)), "dsmoe_moa_forward")
+
+
+def make_attention_desc(q, K, scale=1.0, out=None) -> AttentionDesc:
+    """Sizes and strides of a call's queries [T, n_head, group, d_head] (or a view of them in another order), key cache [n_seq, n_head, L,
+    d_head] and outputs (``None``: contiguous).  ``q`` is ``None`` for ``dsmoe_cache_evict``.  Tensors passed along with it must have these
+    shapes and strides."""
+    n_seq, n_head, L, d_head = K.shape
+    T, group = (0, 1) if q is None else (q.shape[0], q.shape[2])
+    desc = AttentionDesc(T, n_head, group, d_head, n_seq, L, float(scale))
+    desc.kv_stride[:] = K.stride()[:3]
+    o_stride = (n_head * group * d_head, group * d_head, d_head)
+    if q is not None:
+        assert q.shape == (T, n_head, group, d_head) and (out is None or out.shape == q.shape)
+        desc.q_stride[:] = q.stride()[:3]
+        if out is not None:
+            o_stride = out.stride()[:3]
+        desc.layout = q.shape, q.stride(), o_stride + (1,)
+    desc.o_stride[:] = o_stride
+    desc.cache_layout = K.shape, K.stride()
+    return desc
+
+
+def _cache_ptrs(desc, K, V):
+    shape, stride = desc.cache_layout
+    if not (K.dtype == V.dtype == torch.bfloat16 and K.shape == V.shape == shape and K.stride() == V.stride() == stride and stride[3] == 1):
+        raise ValueError("caches are bf16 tensors of the descriptor's shape and strides, d_head contiguous")
+    return K.data_ptr(), V.data_ptr()
+
+
+def _attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse):
+    shape, q_stride, o_stride = desc.layout
+    if not (q.dtype == out.dtype == torch.bfloat16 and q.shape == out.shape == shape and q.stride() == q_stride and out.stride() == o_stride
+            and q_stride[3] == 1):
+        raise ValueError("queries and outputs are bf16 tensors of the descriptor's shape and strides, d_head contiguous")
+    return (q.data_ptr(), *_cache_ptrs(desc, K, V), _ptr(tok_seq), _ptr(pos), out.data_ptr(), _ptr(lse))
+
+
+def dsmoe_attention_workspace_size(desc: AttentionDesc, kind: int, prefix_len: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dsmoe_attention_workspace_size(ctypes.byref(desc), int(kind), int(prefix_len), ctypes.byref(n)),
+           "dsmoe_attention_workspace_size")
+    return n.value
+
+
+def dsmoe_window_attention(desc, window, sinks, rolling, q, K, V, tok_seq, pos, out, lse, workspace, dev_status=None, stream=None):
+    """Attention with a sliding window and sinks.  q, out: [T, n_head, group, d_head]; K, V: [n_seq, n_head, L, d_head]; lse: [T, n_head,
+    group] fp32 or ``None``."""
+    _check(lib().dsmoe_window_attention(ctypes.byref(desc), window, sinks, rolling, *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse),
+                                        _ptr(workspace), workspace.numel() if workspace is not None else 0, _ptr(dev_status),
+                                        _stream(stream)), "dsmoe_window_attention")
+
+
+def dsmoe_prefix_attention(desc, Kp, Vp, q, K, V, tok_seq, pos, out, lse, workspace, dev_status=None, stream=None):
+    """Attention behind a prefix Kp, Vp [n_head, P, d_head] that all tokens share."""
+    if not (Kp.dtype == Vp.dtype == torch.bfloat16 and Kp.shape == Vp.shape == (desc.n_head, Kp.shape[1], desc.d_head)
+            and Kp.stride() == Vp.stride() and Kp.stride(2) == 1):
+        raise ValueError("prefixes are bf16 tensors [n_head, P, d_head] of one layout, d_head contiguous")
+    prefix = Prefix(Kp.data_ptr(), Vp.data_ptr(), Kp.shape[1])
+    prefix.stride[:] = Kp.stride()[:2]
+    _check(lib().dsmoe_prefix_attention(ctypes.byref(desc), ctypes.byref(prefix), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse),
+                                        _ptr(workspace), workspace.numel() if workspace is not None else 0, _ptr(dev_status),
+                                        _stream(stream)), "dsmoe_prefix_attention")
+
+
+def dsmoe_tally_attention(desc, q, K, V, tok_seq, pos, out, lse, tally_in, tally_out, workspace, dev_status=None, stream=None):
+    """Attention that adds the keys' weights to tallies [n_seq, n_head, L] fp32."""
+    if tally_out.shape != desc.cache_layout[0][:3]:
+        raise ValueError("tallies are [n_seq, n_head, L]")
+    _check(lib().dsmoe_tally_attention(ctypes.byref(desc), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse), _ptr(tally_in),
+                                       _ptr(tally_out), _ptr(workspace), workspace.numel() if workspace is not None else 0,
+                                       _ptr(dev_status), _stream(stream)), "dsmoe_tally_attention")
+
+
+def dsmoe_evict_workspace_size(desc: AttentionDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dsmoe_evict_workspace_size(ctypes.byref(desc), ctypes.byref(n)), "dsmoe_evict_workspace_size")
+    return n.value
+
+
+def dsmoe_cache_evict(desc, keep, sinks, recent, length, tally, K, V, kept, len_out, tally_out, K_out, V_out, workspace, dev_status=None,
+                      stream=None):
+    """Thins a cache out to ``keep`` keys a sequence and head.  K_out, V_out: [n_seq, n_head, at least keep, d_head], or K and V themselves;
+    tally_out: [n_seq, n_head, at least keep], or tally."""
+    if not (K_out.dtype == V_out.dtype == torch.bfloat16 and K_out.stride() == V_out.stride() and K_out.stride(3) == 1
+            and K_out.shape == V_out.shape and K_out.shape[2] >= keep and K_out.shape[:2] == tally_out.shape[:2] == desc.cache_layout[0][:2]
+            and K_out.shape[3] == desc.d_head):
+        raise ValueError("K_out, V_out and tally_out have room for `keep` keys of every sequence and head, K_out and V_out one layout")
+    if tally.shape != desc.cache_layout[0][:3] or kept.shape != (desc.n_seq, desc.n_head, keep):
+        raise ValueError("tally is [n_seq, n_head, L], kept is [n_seq, n_head, keep]")
+    args = EvictArgs(int(keep), int(sinks), int(recent))
+    args.out_stride[:] = K_out.stride()[:3]
+    args.tally_pitch = tally_out.shape[2]
+    _check(lib().dsmoe_cache_evict(ctypes.byref(desc), ctypes.byref(args), _ptr(length), _ptr(tally), *_cache_ptrs(desc, K, V), _ptr(kept),
+                                   _ptr(len_out), _ptr(tally_out), K_out.data_ptr(), V_out.data_ptr(), _ptr(workspace),
+                                   workspace.numel() if workspace is not None else 0, _ptr(dev_status), _stream(stream)),
+           "dsmoe_cache_evict")
 
 
 def dsmoe_timing_enable(n_pairs: int):

@@ -1,0 +1,334 @@
+// C entry points of the attention steps on a key/value cache: argument checks, workspace, and which kernels a call takes.
+#include <math.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "cache_attention.cuh"
+
+namespace dsmoe {
+
+namespace {
+
+bool strides_ok(const int64_t* s, int n) {
+    for (int i = 0; i < n; ++i)
+        if (s[i] < 0 || (s[i] & 7)) return false;
+    return true;
+}
+
+// Whether rows of `row` elements at these strides are apart from one another: each stride, in their order, spans what lies within it
+bool rows_apart(const int64_t* stride, const int64_t* n, int64_t row) {
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+    int64_t span = row;
+    for (int i : order) {
+        if (n[i] <= 1) continue;
+        if (stride[i] < span) return false;
+        if (stride[i] > (INT64_MAX / 4) / n[i]) return false;
+        span += stride[i] * (n[i] - 1);
+    }
+    return true;
+}
+
+// The bytes that rows at these strides lie in
+struct Extent {
+    uintptr_t begin, end;
+    bool meets(const Extent& o) const { return begin < o.end && o.begin < end; }
+};
+Extent extent(const void* p, const int64_t* stride, const int64_t* n, int64_t row, int64_t size) {
+    int64_t last = row;
+    for (int i = 0; i < 3; ++i) last += stride[i] * (n[i] - 1);
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return Extent{a, a + (uintptr_t)(last * size)};
+}
+
+dsmoe_status check_cache(const dsmoe_attention_desc* d) {
+    if (!d) return DSMOE_ERR_INVALID_ARG;
+    if (d->n_head <= 0 || d->d_head <= 0 || d->n_seq <= 0 || d->L <= 0) return DSMOE_ERR_INVALID_ARG;
+    if (!strides_ok(d->kv_stride, 3)) return DSMOE_ERR_INVALID_ARG;
+    if (d->d_head % 32 || d->d_head > 256) return DSMOE_ERR_UNSUPPORTED;
+    if ((long long)d->n_seq * d->n_head > INT_MAX / 4) return DSMOE_ERR_UNSUPPORTED;
+    for (int i = 0; i < 3; ++i)
+        if (d->kv_stride[i] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
+    return DSMOE_OK;
+}
+
+dsmoe_status check_attention(const dsmoe_attention_desc* d) {
+    DSMOE_TRY(check_cache(d));
+    if (d->T < 0 || d->group <= 0 || !isfinite(d->scale)) return DSMOE_ERR_INVALID_ARG;
+    if (!strides_ok(d->q_stride, 3) || !strides_ok(d->o_stride, 3)) return DSMOE_ERR_INVALID_ARG;
+    if (d->group > 64) return DSMOE_ERR_UNSUPPORTED;
+    if ((double)d->T * d->n_head * d->group > (double)INT_MAX / 2) return DSMOE_ERR_UNSUPPORTED;
+    for (int i = 0; i < 3; ++i)
+        if (d->q_stride[i] > (1ll << 40) || d->o_stride[i] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
+    const int64_t n[3] = {d->T, d->n_head, d->group};
+    if (!rows_apart(d->o_stride, n, d->d_head)) return DSMOE_ERR_INVALID_ARG;
+    return DSMOE_OK;
+}
+
+dsmoe_status check_attention_call(const dsmoe_attention_desc* d, const void* q, const void* K, const void* V, const int32_t* pos, const void* out) {
+    if (!q || !K || !V || !pos || !out) return DSMOE_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return DSMOE_ERR_INVALID_ARG;
+    const int64_t n[3] = {d->T, d->n_head, d->group}, c[3] = {d->n_seq, d->n_head, d->L};
+    const Extent o = extent(out, d->o_stride, n, d->d_head, 2);
+    if (o.meets(extent(q, d->q_stride, n, d->d_head, 2)) || o.meets(extent(K, d->kv_stride, c, d->d_head, 2)) ||
+        o.meets(extent(V, d->kv_stride, c, d->d_head, 2)))
+        return DSMOE_ERR_INVALID_ARG;
+    return DSMOE_OK;
+}
+
+AttnView view_of(const dsmoe_attention_desc& d, const void* q, const void* K, const void* V, const int32_t* tok_seq, const int32_t* pos, void* out,
+                 float* lse, int32_t* dev_status) {
+    AttnView A{};
+    A.T = d.T;
+    A.n_head = d.n_head;
+    A.group = d.group;
+    A.fold = 1;
+    A.row_tiles = ceil_div(d.group, 16);
+    A.d_head = d.d_head;
+    A.n_seq = d.n_seq;
+    A.L = d.L;
+    A.window = INT_MAX;
+    A.scale_log2 = d.scale * 1.4426950408889634f;
+    A.q = static_cast<const __nv_bfloat16*>(q);
+    A.q_t = d.q_stride[0], A.q_h = d.q_stride[1], A.q_g = d.q_stride[2];
+    A.K = static_cast<const __nv_bfloat16*>(K);
+    A.V = static_cast<const __nv_bfloat16*>(V);
+    A.kv_s = d.kv_stride[0], A.kv_h = d.kv_stride[1], A.kv_p = d.kv_stride[2];
+    A.tok_seq = tok_seq;
+    A.pos = pos;
+    A.out = static_cast<__nv_bfloat16*>(out);
+    A.o_t = d.o_stride[0], A.o_h = d.o_stride[1], A.o_g = d.o_stride[2];
+    A.lse = lse;
+    A.dev_status = dev_status;
+    return A;
+}
+
+// The tokens of a prefix taken as one
+AttnView folded_view(const AttnView& A, const dsmoe_prefix& p) {
+    AttnView F = A;
+    F.fold = A.T;
+    F.T = 1;
+    F.row_tiles = (int)(((long long)A.T * A.group + 15) / 16);
+    F.n_seq = 1;
+    F.L = p.P;
+    F.K = static_cast<const __nv_bfloat16*>(p.Kp);
+    F.V = static_cast<const __nv_bfloat16*>(p.Vp);
+    F.kv_s = 0, F.kv_h = p.stride[0], F.kv_p = p.stride[1];
+    F.tok_seq = F.pos = nullptr;
+    return F;
+}
+
+// Workspace of a call: the own caches' parts (of one chunk of kListTokens tokens at a time), the folded tokens' parts, the rows' sums
+struct AttnWs {
+    size_t slots, head, f_slots, f_head, ml, total;
+    int ctas, f_ctas;
+};
+AttnWs attention_ws(const AttnView& A, const AttnView* F, bool keep_parts, bool wants_ml) {
+    AttnWs w{};
+    size_t off = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align_up(off + bytes, 256);
+        return at;
+    };
+    const size_t tokens = (size_t)(A.T < kListTokens ? A.T : kListTokens), pairs = tokens * A.n_head * A.row_tiles;
+    w.ctas = stream_ctas(A);
+    w.head = take(pairs * sizeof(int2));
+    w.slots = take((2 * (size_t)w.ctas + (keep_parts ? pairs : 0)) * part_bytes(A.d_head));
+    if (F) {
+        const size_t f_pairs = (size_t)F->n_head * F->row_tiles;
+        w.f_ctas = stream_ctas(*F);
+        w.f_head = take(f_pairs * sizeof(int2));
+        w.f_slots = take((2 * (size_t)w.f_ctas + f_pairs) * part_bytes(A.d_head));
+    }
+    if (wants_ml) w.ml = take((size_t)A.T * A.n_head * A.group * sizeof(float2));
+    w.total = off;
+    return w;
+}
+
+// Attention of all tokens against their own caches, and the sum with what is there of the prefix (F nullptr: nothing)
+dsmoe_status attend(const AttnView& all, const AttnView* F, const AttnWs& w, char* ws, cudaStream_t s) {
+    PartPlan folded{};
+    if (F) {
+        folded = PartPlan{reinterpret_cast<float*>(ws + w.f_slots), reinterpret_cast<int2*>(ws + w.f_head), w.f_ctas, true};
+        DSMOE_TRY(launch_stream_attention(*F, folded, s));
+    }
+    for (int t0 = 0; t0 < all.T; t0 += kListTokens) {
+        AttnView A = all;
+        A.T = std::min(kListTokens, all.T - t0);
+        A.q += t0 * A.q_t;
+        A.out += t0 * A.o_t;
+        if (A.tok_seq) A.tok_seq += t0;
+        A.pos += t0;
+        const size_t rows = (size_t)t0 * A.n_head * A.group;
+        if (A.lse) A.lse += rows;
+        if (A.ml) A.ml += rows;
+        const PartPlan P{reinterpret_cast<float*>(ws + w.slots), reinterpret_cast<int2*>(ws + w.head), std::min(w.ctas, stream_ctas(A)), F != nullptr};
+        DSMOE_TRY(launch_stream_attention(A, P, s));
+        DSMOE_TRY(launch_attention_sum(A, P, folded, F ? F->row_tiles : 0, t0, TileParts{}, s));
+    }
+    return DSMOE_OK;
+}
+
+dsmoe_status check_window(const dsmoe_attention_desc* d, int window, int sinks, int rolling) {
+    if (window < 1 || sinks < 0 || (rolling != 0 && rolling != 1)) return DSMOE_ERR_INVALID_ARG;
+    if (rolling && (sinks >= d->L || window > d->L - sinks)) return DSMOE_ERR_INVALID_ARG;
+    return DSMOE_OK;
+}
+
+dsmoe_status check_prefix(const dsmoe_attention_desc* d, const dsmoe_prefix* p, const void* out) {
+    if (!p || p->P < 0) return DSMOE_ERR_INVALID_ARG;
+    if (p->P == 0) return DSMOE_OK;
+    if (!p->Kp || !p->Vp || !aligned16(p->Kp) || !aligned16(p->Vp) || !strides_ok(p->stride, 2)) return DSMOE_ERR_INVALID_ARG;
+    if (p->stride[0] > (1ll << 40) || p->stride[1] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
+    const int64_t n[3] = {d->T, d->n_head, d->group}, c[3] = {1, d->n_head, p->P}, st[3] = {0, p->stride[0], p->stride[1]};
+    const Extent o = extent(out, d->o_stride, n, d->d_head, 2);
+    if (o.meets(extent(p->Kp, st, c, d->d_head, 2)) || o.meets(extent(p->Vp, st, c, d->d_head, 2))) return DSMOE_ERR_INVALID_ARG;
+    return DSMOE_OK;
+}
+
+}  // namespace
+
+}  // namespace dsmoe
+
+using namespace dsmoe;
+
+extern "C" {
+
+dsmoe_status dsmoe_attention_workspace_size(const dsmoe_attention_desc* desc, int kind, int prefix_len, size_t* bytes) {
+    DSMOE_TRY(check_attention(desc));
+    if (!bytes || kind < DSMOE_ATTENTION_WINDOW || kind > DSMOE_ATTENTION_TALLY) return DSMOE_ERR_INVALID_ARG;
+    if (kind == DSMOE_ATTENTION_PREFIX && prefix_len < 0) return DSMOE_ERR_INVALID_ARG;
+    const AttnView A = view_of(*desc, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+    if (desc->T == 0) {
+        *bytes = 0;
+    } else if (kind == DSMOE_ATTENTION_PREFIX && prefix_len > 0) {
+        dsmoe_prefix p{};
+        p.P = prefix_len;
+        const AttnView F = folded_view(A, p);
+        *bytes = attention_ws(A, &F, true, false).total;
+    } else {
+        *bytes = attention_ws(A, nullptr, false, kind == DSMOE_ATTENTION_TALLY).total;
+    }
+    return DSMOE_OK;
+}
+
+dsmoe_status dsmoe_window_attention(const dsmoe_attention_desc* desc, int window, int sinks, int rolling, const void* q, const void* K,
+                                    const void* V, const int32_t* tok_seq, const int32_t* pos, void* out, float* lse, void* workspace,
+                                    size_t ws_bytes, int32_t* dev_status, dsmoe_stream stream) {
+    DSMOE_TRY(check_attention(desc));
+    DSMOE_TRY(check_window(desc, window, sinks, rolling));
+    if (desc->T == 0) return DSMOE_OK;
+    DSMOE_TRY(check_attention_call(desc, q, K, V, pos, out));
+    AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
+    // (the workspace is that of a window as wide as the cache: the most CTAs that any window can have)
+    const AttnWs w = attention_ws(A, nullptr, false, false);
+    if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
+    A.window = window;
+    A.sinks = sinks;
+    A.ring = rolling ? desc->L - sinks : 0;
+    return attend(A, nullptr, w, static_cast<char*>(workspace), (cudaStream_t)stream);
+}
+
+dsmoe_status dsmoe_prefix_attention(const dsmoe_attention_desc* desc, const dsmoe_prefix* prefix, const void* q, const void* K, const void* V,
+                                    const int32_t* tok_seq, const int32_t* pos, void* out, float* lse, void* workspace, size_t ws_bytes,
+                                    int32_t* dev_status, dsmoe_stream stream) {
+    DSMOE_TRY(check_attention(desc));
+    if (!prefix || prefix->P < 0) return DSMOE_ERR_INVALID_ARG;
+    if (desc->T == 0) return DSMOE_OK;
+    DSMOE_TRY(check_attention_call(desc, q, K, V, pos, out));
+    DSMOE_TRY(check_prefix(desc, prefix, out));
+    const AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
+    const bool shared = prefix->P > 0;
+    const AttnView F = folded_view(A, *prefix);
+    const AttnWs w = attention_ws(A, shared ? &F : nullptr, shared, false);
+    if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
+    return attend(A, shared ? &F : nullptr, w, static_cast<char*>(workspace), (cudaStream_t)stream);
+}
+
+dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void* q, const void* K, const void* V, const int32_t* tok_seq,
+                                   const int32_t* pos, void* out, float* lse, const float* tally_in, float* tally_out, void* workspace,
+                                   size_t ws_bytes, int32_t* dev_status, dsmoe_stream stream) {
+    DSMOE_TRY(check_attention(desc));
+    if (!tally_out) return DSMOE_ERR_INVALID_ARG;
+    const size_t cells = (size_t)desc->n_seq * desc->n_head * desc->L;
+    if (tally_in && tally_in != tally_out && tally_in < tally_out + cells && tally_out < tally_in + cells) return DSMOE_ERR_INVALID_ARG;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (desc->T > 0) {
+        DSMOE_TRY(check_attention_call(desc, q, K, V, pos, out));
+    } else {                                            // no token: the tallies are handed on
+        if (tally_in == tally_out) return DSMOE_OK;
+        if (tally_in) DSMOE_CUDA_TRY(cudaMemcpyAsync(tally_out, tally_in, cells * 4, cudaMemcpyDeviceToDevice, s));
+        else DSMOE_CUDA_TRY(cudaMemsetAsync(tally_out, 0, cells * 4, s));
+        return DSMOE_OK;
+    }
+    AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
+    const AttnWs w = attention_ws(A, nullptr, false, true);
+    if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
+    A.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + w.ml);
+    DSMOE_TRY(attend(A, nullptr, w, static_cast<char*>(workspace), s));
+    return launch_tally(A, tally_in, tally_out, s);
+}
+
+dsmoe_status dsmoe_evict_workspace_size(const dsmoe_attention_desc* desc, size_t* bytes) {
+    DSMOE_TRY(check_cache(desc));
+    if (!bytes) return DSMOE_ERR_INVALID_ARG;
+    *bytes = align_up((size_t)desc->n_seq * desc->n_head * 4, 256);
+    return DSMOE_OK;
+}
+
+dsmoe_status dsmoe_cache_evict(const dsmoe_attention_desc* desc, const dsmoe_evict_args* args, const int32_t* len, const float* tally,
+                               const void* K, const void* V, int32_t* kept, int32_t* len_out, float* tally_out, void* K_out, void* V_out,
+                               void* workspace, size_t ws_bytes, int32_t* dev_status, dsmoe_stream stream) {
+    DSMOE_TRY(check_cache(desc));
+    if (!args || !len || !tally || !K || !V || !kept || !len_out || !tally_out || !K_out || !V_out) return DSMOE_ERR_INVALID_ARG;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(K_out) || !aligned16(V_out)) return DSMOE_ERR_INVALID_ARG;
+    const dsmoe_evict_args& a = *args;
+    if (a.keep < 1 || a.keep > desc->L || a.sinks < 0 || a.recent < 0 || (long long)a.sinks + a.recent > a.keep) return DSMOE_ERR_INVALID_ARG;
+    if (!strides_ok(a.out_stride, 3) || a.tally_pitch < a.keep) return DSMOE_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i)
+        if (a.out_stride[i] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
+    if (a.tally_pitch > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
+    const int64_t n[3] = {desc->n_seq, desc->n_head, desc->L}, m[3] = {desc->n_seq, desc->n_head, a.keep};
+    const bool in_place = K_out == K;
+    if (in_place != (V_out == V) || K_out == V_out) return DSMOE_ERR_INVALID_ARG;
+    if (!rows_apart(a.out_stride, m, desc->d_head)) return DSMOE_ERR_INVALID_ARG;
+    const Extent ek = extent(K, desc->kv_stride, n, desc->d_head, 2), ev = extent(V, desc->kv_stride, n, desc->d_head, 2);
+    const Extent ok = extent(K_out, a.out_stride, m, desc->d_head, 2), ov = extent(V_out, a.out_stride, m, desc->d_head, 2);
+    if (in_place) {
+        for (int i = 0; i < 3; ++i)
+            if (a.out_stride[i] != desc->kv_stride[i]) return DSMOE_ERR_INVALID_ARG;
+        if (!rows_apart(desc->kv_stride, n, desc->d_head)) return DSMOE_ERR_INVALID_ARG;
+    } else if (ok.meets(ek) || ok.meets(ev) || ov.meets(ek) || ov.meets(ev)) {
+        return DSMOE_ERR_INVALID_ARG;
+    }
+    const int64_t pairs = (int64_t)desc->n_seq * desc->n_head;
+    if (tally_out == tally) {
+        if (a.tally_pitch != desc->L) return DSMOE_ERR_INVALID_ARG;
+    } else if (tally < tally_out + (pairs - 1) * a.tally_pitch + a.keep && tally_out < tally + pairs * desc->L) {
+        return DSMOE_ERR_INVALID_ARG;
+    }
+    if (!workspace || !aligned16(workspace) || ws_bytes < (size_t)pairs * 4) return DSMOE_ERR_WORKSPACE;
+    EvictView E{};
+    E.n_seq = desc->n_seq, E.n_head = desc->n_head, E.L = desc->L, E.d_head = desc->d_head;
+    E.keep = a.keep, E.sinks = a.sinks, E.recent = a.recent;
+    E.len = len;
+    E.tally = tally;
+    E.K = static_cast<const __nv_bfloat16*>(K);
+    E.V = static_cast<const __nv_bfloat16*>(V);
+    E.kv_s = desc->kv_stride[0], E.kv_h = desc->kv_stride[1], E.kv_p = desc->kv_stride[2];
+    E.kept = kept;
+    E.len_out = len_out;
+    E.tally_out = tally_out;
+    E.tally_pitch = a.tally_pitch;
+    E.K_out = static_cast<__nv_bfloat16*>(K_out);
+    E.V_out = static_cast<__nv_bfloat16*>(V_out);
+    E.o_s = a.out_stride[0], E.o_h = a.out_stride[1], E.o_p = a.out_stride[2];
+    E.in_place = in_place;
+    E.count = static_cast<int32_t*>(workspace);
+    E.dev_status = dev_status;
+    return launch_evict(E, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,168 @@
+"""The attention steps on a key/value cache: the plain forms that the GPU tests compare with, and what the calls refuse (no GPU needed)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2404_05567_b200 as dm
+from cache_attention_reference import attention, evict, visible
+from paper_2404_05567_b200 import build as dm_build
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    dm_build.build()
+
+
+def test_visible_keys():
+    assert visible(5) == [0, 1, 2, 3, 4, 5] and visible(-1) == [] and visible(-1, 3, 2) == []
+    assert visible(9, 3, 0) == [7, 8, 9] and visible(9, 3, 2) == [0, 1, 7, 8, 9] and visible(2, 3, 2) == [0, 1, 2]
+
+
+def test_plain_attention():
+    """Two keys with equal logits; a key that outweighs; nothing visible."""
+    K, V = np.array([[1.0, 0], [1, 0], [0, 90]]), np.array([[2.0], [4], [7]])
+    V = np.repeat(V, 2, 1)
+    out, lse, p, _, _ = attention(np.array([[3.0, 0]]), K, V, 1.0, [0, 1])
+    assert np.allclose(out, 3) and np.allclose(lse, 3 + np.log(2)) and np.allclose(p, 0.5)
+    assert np.allclose(attention(np.array([[0.0, 1]]), K, V, 1.0, [0, 1, 2])[0], 7)
+    out, lse = attention(np.ones((1, 2)), K, V, 1.0, [])[:2]
+    assert (out == 0).all() and lse[0] == -np.inf
+
+
+def test_plain_eviction():
+    t = np.array([5, 1, 3, 3, 0, 9, 2], dtype=np.float32)
+    assert evict(t, 7, 7, 0, 0) == list(range(7)) and evict(t, 3, 4, 1, 1) == [0, 1, 2]
+    assert evict(t, 7, 3, 0, 0) == [0, 2, 5] and evict(t, 7, 4, 1, 1) == [0, 2, 5, 6] and evict(t, 7, 3, 1, 2) == [0, 5, 6]
+    assert evict(np.array([np.nan, -np.inf, 0, np.nan], dtype=np.float32), 4, 2, 0, 0) == [1, 2]
+
+
+def _desc(**kw):
+    a = dict(T=4, n_head=2, group=3, d_head=64, n_seq=2, L=32, scale=0.125)
+    strides = {k: kw.pop(k) for k in ("q_stride", "o_stride", "kv_stride") if k in kw}
+    a.update(kw)
+    d = dm.AttentionDesc(*a.values())
+    row = a["n_head"] * a["group"] * a["d_head"]
+    d.q_stride[:] = d.o_stride[:] = (row, a["group"] * a["d_head"], a["d_head"])
+    d.kv_stride[:] = (a["n_head"] * a["L"] * a["d_head"], a["L"] * a["d_head"], a["d_head"])
+    for k, v in strides.items():
+        getattr(d, k)[:] = v
+    return d
+
+
+def _size(d, kind=0, P=0):
+    n = ctypes.c_size_t(0)
+    return dm.lib().dsmoe_attention_workspace_size(ctypes.byref(d), kind, P, ctypes.byref(n)), n.value
+
+
+def test_descriptors_that_are_refused():
+    assert _size(_desc())[0] == 0
+    for kw in (dict(T=-1), dict(n_head=0), dict(group=0), dict(d_head=0), dict(n_seq=0), dict(L=0), dict(scale=float("nan")),
+               dict(scale=float("inf")), dict(q_stride=(384, 192, 4)), dict(q_stride=(-384, 192, 64)), dict(kv_stride=(4096, 2048, 63)),
+               dict(o_stride=(384, 192, 32)), dict(o_stride=(0, 192, 64)), dict(o_stride=(384, 0, 64)), dict(o_stride=(380, 192, 64)),
+               dict(o_stride=(128, 64, 64))):
+        assert _size(_desc(**kw))[0] == 1, kw
+    for kw in (dict(d_head=48), dict(d_head=288), dict(group=65), dict(T=2 ** 30), dict(kv_stride=(2 ** 41, 2048, 64))):
+        assert _size(_desc(**kw))[0] == 2, kw
+    for kw in (dict(q_stride=(0, 0, 0)), dict(o_stride=(384, 64, 128)), dict(o_stride=(64, 64 * 4 * 3, 64 * 4)), dict(T=0, o_stride=(0, 192, 64)),
+               dict(T=1, o_stride=(0, 192, 64))):
+        assert _size(_desc(**kw))[0] == 0, kw
+    assert _size(_desc(), 3)[0] == 1 and _size(_desc(), -1)[0] == 1 and _size(_desc(), 1, -1)[0] == 1
+    assert _size(_desc(T=0)) == (0, 0)
+    assert dm.lib().dsmoe_attention_workspace_size(None, 0, 0, ctypes.byref(ctypes.c_size_t(0))) == 1
+    # more to hold: a prefix, the rows' sums
+    assert _size(_desc(), 1, 1000)[1] > _size(_desc(), 1, 0)[1] >= _size(_desc(), 0)[1]
+    assert _size(_desc(), 2)[1] > _size(_desc(), 0)[1]
+
+
+A = 1 << 20       # addresses far apart, never looked at on the host
+
+
+def _call(name, d, more=(), q=A, K=2 * A, V=3 * A, seq=4 * A, pos=5 * A, out=6 * A, lse=None, tail=(), ws=8 * A, n=1 << 40):
+    return getattr(dm.lib(), name)(ctypes.byref(d) if d is not None else None, *more, q, K, V, seq, pos, out, lse, *tail, ws, n, None, None)
+
+
+CALLS = [("dsmoe_window_attention", (16, 2, 0), ()), ("dsmoe_tally_attention", (), (None, 9 * A))]
+
+
+@pytest.mark.parametrize("name,more,tail", CALLS)
+def test_calls_that_are_refused(name, more, tail):
+    d = _desc()
+    for kw in (dict(q=None), dict(K=None), dict(V=None), dict(pos=None), dict(out=None), dict(q=A + 8), dict(K=2 * A + 2), dict(V=3 * A + 4),
+               dict(out=6 * A + 8), dict(out=A), dict(out=A + 16), dict(out=2 * A + 4096), dict(out=3 * A)):
+        assert _call(name, d, more, tail=tail, **kw) == 1, kw
+    assert _call(name, None, more, tail=tail) == 1
+    assert _call(name, _desc(d_head=40), more, tail=tail) == 2
+    need = _size(d, 2 if "tally" in name else 0)[1]
+    for kw in (dict(ws=None), dict(ws=8 * A + 8), dict(n=need - 1), dict(n=0)):
+        assert _call(name, d, more, tail=tail, **kw) == 3, kw
+
+
+def test_windows_that_are_refused():
+    for window, sinks, rolling in ((0, 0, 0), (-1, 0, 0), (4, -1, 0), (4, 0, 2), (4, 0, -1), (31, 2, 1), (1, 32, 1), (33, 0, 1)):
+        assert _call("dsmoe_window_attention", _desc(), (window, sinks, rolling)) == 1, (window, sinks, rolling)
+    assert _call("dsmoe_window_attention", _desc(T=0), (4, 1, 0), q=None, out=None, ws=None, n=0) == 0
+
+
+def test_prefixes_that_are_refused():
+    def go(d=None, Kp=10 * A, Vp=11 * A, P=8, stride=(512, 64), **kw):
+        p = dm.Prefix(Kp, Vp, P)
+        p.stride[:] = stride
+        return _call("dsmoe_prefix_attention", d or _desc(), (ctypes.byref(p),), **kw)
+    for kw in (dict(P=-1), dict(Kp=None), dict(Vp=None), dict(Kp=10 * A + 2), dict(stride=(512, 60)), dict(stride=(-512, 64)), dict(out=10 * A),
+               dict(out=11 * A + 64), dict(q=None), dict(out=A)):
+        assert go(**kw) == 1, kw
+    assert _call("dsmoe_prefix_attention", _desc(), (None,)) == 1
+    assert go(stride=(2 ** 41, 64)) == 2
+    assert go(n=_size(_desc(), 1, 8)[1] - 1) == 3
+    assert go(d=_desc(T=0), q=None, ws=None, n=0) == 0
+
+
+def test_tallies_that_are_refused():
+    d = _desc()                                        # 2 * 2 * 32 tallies: 512 bytes
+    for tail in ((None, None), (9 * A, 9 * A + 4), (9 * A + 508, 9 * A), (9 * A, 9 * A + 508)):
+        assert _call("dsmoe_tally_attention", d, (), tail=tail) == 1, tail
+    assert _call("dsmoe_tally_attention", _desc(T=0), (), tail=(9 * A, 9 * A), ws=None, n=0) == 0
+
+
+def test_evictions_that_are_refused():
+    def go(d=None, keep=16, sinks=2, recent=4, out_stride=(2048, 1024, 64), pitch=16, length=A, tally=2 * A, K=3 * A, V=4 * A, kept=5 * A,
+           len_out=6 * A, tally_out=7 * A, K_out=8 * A, V_out=9 * A, ws=10 * A, n=1 << 20):
+        a = dm.EvictArgs(keep, sinks, recent)
+        a.out_stride[:] = out_stride
+        a.tally_pitch = pitch
+        return dm.lib().dsmoe_cache_evict(ctypes.byref(d or _desc()), ctypes.byref(a), length, tally, K, V, kept, len_out, tally_out, K_out, V_out,
+                                          ws, n, None, None)
+    same = dict(out_stride=(4096, 2048, 64), pitch=32)
+    for kw in (dict(keep=0), dict(keep=33, pitch=33), dict(sinks=-1), dict(recent=-1), dict(sinks=10, recent=7), dict(pitch=15),
+               dict(out_stride=(2048, 1024, 60)), dict(out_stride=(2048, 512, 64)), dict(out_stride=(0, 1024, 64)), dict(length=None),
+               dict(tally=None), dict(K=None), dict(V=None), dict(kept=None), dict(len_out=None), dict(tally_out=None), dict(K_out=None),
+               dict(V_out=None), dict(K=3 * A + 2), dict(V_out=9 * A + 8), dict(K_out=3 * A), dict(V_out=4 * A), dict(V_out=8 * A),
+               dict(K_out=3 * A, V_out=4 * A), dict(K_out=3 * A + 64), dict(K_out=4 * A, V_out=3 * A, **same), dict(tally_out=2 * A),
+               dict(tally_out=2 * A + 4, pitch=32)):
+        assert go(**kw) == 1, kw
+    assert go(out_stride=(2 ** 41, 1024, 64)) == 2
+    assert go(ws=None) == 3 and go(ws=10 * A + 4) == 3 and go(n=8) == 3
+    n = ctypes.c_size_t(0)
+    assert dm.lib().dsmoe_evict_workspace_size(None, ctypes.byref(n)) == 1
+    assert dm.lib().dsmoe_evict_workspace_size(ctypes.byref(_desc()), None) == 1
+    assert dm.dsmoe_evict_workspace_size(_desc()) >= 16
+
+
+def test_the_binding_checks_shapes_and_types():
+    q = torch.zeros((4, 2, 3, 64), dtype=torch.bfloat16)
+    K = torch.zeros((2, 2, 32, 64), dtype=torch.bfloat16)
+    desc = dm.make_attention_desc(q, K, 0.125)
+    assert _size(desc)[0] == 0
+    args = lambda **kw: {**dict(q=q, K=K, V=K.clone(), tok_seq=None, pos=torch.zeros(4, dtype=torch.int32), out=torch.zeros_like(q), lse=None), **kw}
+    for kw in (dict(q=q.float()), dict(q=q[:3]), dict(out=q.transpose(1, 2)), dict(K=K[:, :, :31]), dict(V=K.float()), dict(V=K.transpose(1, 2))):
+        with pytest.raises(ValueError):
+            dm.dsmoe_window_attention(desc, 4, 0, False, *args(**kw).values(), None)
+    with pytest.raises(ValueError):
+        dm.dsmoe_prefix_attention(desc, K[0, :, :, :32], K[0, :, :, :32], *args().values(), None)
+    with pytest.raises(ValueError):
+        dm.dsmoe_tally_attention(desc, *args().values(), None, torch.zeros((2, 2, 31)), None)
+    with pytest.raises(ValueError):
+        dm.dsmoe_cache_evict(desc, 8, 0, 0, None, torch.zeros((2, 2, 32)), K, K.clone(), torch.zeros((2, 2, 7), dtype=torch.int32), None,
+                             torch.zeros((2, 2, 8)), K[:, :, :8].clone(), K[:, :, :8].clone(), None)
