@@ -119,13 +119,33 @@ AttnView folded_view(const AttnView& A, const dsmoe_prefix& p) {
     return F;
 }
 
-// Workspace of a call: the own caches' parts (of one chunk of kListTokens tokens at a time), the folded tokens' parts, the rows' sums
-struct AttnWs {
-    size_t slots, head, f_slots, f_head, ml, total;
+// Which kernels a call takes, and its workspace.
+//
+// The prefix: on the 128-row kernel from 33 rows on (two 16-row tiles of the stream kernel read it twice; with more rows the stream kernel is bound by
+// its MMAs), its keys cut so that all SMs have some.  The own caches: where there are more tokens than sequences, on the 128-row kernel, which
+// leaves tokens alone that have too few neighbours of their sequence (is_streams); otherwise, and for those, on the stream kernel.
+constexpr int kPrefixStreamRows = 32, kOwnTileRows = 64, kMaxSplits = 64;
+
+struct AttnPlan {
+    size_t slots, head, f_slots, f_head, ml, tile_o, tile_ml, total;
     int ctas, f_ctas;
+    int prefix_splits;                    // 0: the prefix is not the 128-row kernel's
+    int own_splits;                       // ... the own caches
 };
-AttnWs attention_ws(const AttnView& A, const AttnView* F, bool keep_parts, bool wants_ml) {
-    AttnWs w{};
+
+// Parts into which the 128-row kernel's keys are cut: as many as fill the SMs, two tiles of keys or more in each
+int tile_splits(const AttnView& A, long long keys) {
+    const long long ctas = (long long)tile_blocks(A.T, A.group) * A.n_head, tiles = (keys + 127) / 128;
+    return (int)std::max(1ll, std::min({(long long)sm_count() / ctas, tiles / 2, (long long)kMaxSplits}));
+}
+
+bool own_on_tiles(const AttnView& A) {
+    return tile_supported(A) && (A.tok_seq ? A.T > A.n_seq : A.T > 1) && (long long)A.T * A.group >= kOwnTileRows;
+}
+
+// F: the folded prefix or nullptr; may_tile: the prefix's strides allow it, as far as known.
+AttnPlan attention_plan(const AttnView& A, const AttnView* F, bool may_tile, bool wants_ml) {
+    AttnPlan w{};
     size_t off = 0;
     const auto take = [&](size_t bytes) {
         const size_t at = off;
@@ -133,26 +153,55 @@ AttnWs attention_ws(const AttnView& A, const AttnView* F, bool keep_parts, bool 
         return at;
     };
     const size_t tokens = (size_t)(A.T < kListTokens ? A.T : kListTokens), pairs = tokens * A.n_head * A.row_tiles;
+    const size_t rows = (size_t)A.T * A.n_head * A.group;
     w.ctas = stream_ctas(A);
     w.head = take(pairs * sizeof(int2));
-    w.slots = take((2 * (size_t)w.ctas + (keep_parts ? pairs : 0)) * part_bytes(A.d_head));
+    // (whole pairs leave parts too where there is something to add them to)
+    w.slots = take((2 * (size_t)w.ctas + pairs) * part_bytes(A.d_head));
+    if (wants_ml) w.ml = take(rows * sizeof(float2));
+    if (own_on_tiles(A)) w.own_splits = tile_splits(A, A.L);
+    size_t folded = off;
     if (F) {
         const size_t f_pairs = (size_t)F->n_head * F->row_tiles;
         w.f_ctas = stream_ctas(*F);
         w.f_head = take(f_pairs * sizeof(int2));
         w.f_slots = take((2 * (size_t)w.f_ctas + f_pairs) * part_bytes(A.d_head));
+        const bool wide = A.d_head == 64 || A.d_head == 96 || A.d_head == 128;
+        if (may_tile && wide && (long long)A.T * A.group > kPrefixStreamRows) w.prefix_splits = tile_splits(A, F->L);
+        // (one of the two; which, the prefix's strides may decide)
+        if (w.prefix_splits) std::swap(folded, off);
+        else folded = off;
     }
-    if (wants_ml) w.ml = take((size_t)A.T * A.n_head * A.group * sizeof(float2));
-    w.total = off;
+    const size_t parts = (size_t)w.prefix_splits + w.own_splits;
+    w.tile_ml = take(parts * rows * 2 * 4);
+    w.tile_o = take(parts * rows * A.d_head * 4);
+    w.total = std::max(off, folded);
     return w;
 }
 
-// Attention of all tokens against their own caches, and the sum with what is there of the prefix (F nullptr: nothing)
-dsmoe_status attend(const AttnView& all, const AttnView* F, const AttnWs& w, char* ws, cudaStream_t s) {
+// Attention of all tokens: the prefix (F, on the 128-row kernel as N), the own caches, the sum
+dsmoe_status attend(const AttnView& all, const AttnView* F, const AttnView* N, const AttnPlan& w, char* ws, cudaStream_t s) {
+    const size_t rows = (size_t)all.T * all.n_head * all.group;
+    float* const o = reinterpret_cast<float*>(ws + w.tile_o);
+    float* const ml = reinterpret_cast<float*>(ws + w.tile_ml);
+    const bool one_sequence = !all.tok_seq || all.n_seq == 1;
     PartPlan folded{};
-    if (F) {
+    TileParts parts{0, rows, o, ml};
+    if (w.prefix_splits) {
+        DSMOE_TRY(launch_tile_attention(*N, TilePlan{w.prefix_splits, o, ml}, s));
+        parts.n = w.prefix_splits;
+    } else if (F) {
         folded = PartPlan{reinterpret_cast<float*>(ws + w.f_slots), reinterpret_cast<int2*>(ws + w.f_head), w.f_ctas, true};
         DSMOE_TRY(launch_stream_attention(*F, folded, s));
+    }
+    if (w.own_splits) {
+        // a narrow window needs fewer parts than the workspace has room for
+        const long long keys = all.window < all.L ? (long long)all.window + all.sinks + tile_span(all.group) : all.L;
+        const int splits = std::min(w.own_splits, tile_splits(all, keys));
+        const bool direct = splits == 1 && !F;
+        DSMOE_TRY(launch_tile_attention(all, direct ? TilePlan{1, nullptr, nullptr} : TilePlan{splits, o + parts.n * rows * all.d_head, ml + parts.n * rows * 2}, s));
+        if (!direct) parts.n += splits;
+        if (direct && one_sequence) return DSMOE_OK;
     }
     for (int t0 = 0; t0 < all.T; t0 += kListTokens) {
         AttnView A = all;
@@ -161,12 +210,18 @@ dsmoe_status attend(const AttnView& all, const AttnView* F, const AttnWs& w, cha
         A.out += t0 * A.o_t;
         if (A.tok_seq) A.tok_seq += t0;
         A.pos += t0;
-        const size_t rows = (size_t)t0 * A.n_head * A.group;
-        if (A.lse) A.lse += rows;
-        if (A.ml) A.ml += rows;
-        const PartPlan P{reinterpret_cast<float*>(ws + w.slots), reinterpret_cast<int2*>(ws + w.head), std::min(w.ctas, stream_ctas(A)), F != nullptr};
-        DSMOE_TRY(launch_stream_attention(A, P, s));
-        DSMOE_TRY(launch_attention_sum(A, P, folded, F ? F->row_tiles : 0, t0, TileParts{}, s));
+        const size_t row0 = (size_t)t0 * A.n_head * A.group;
+        if (A.lse) A.lse += row0;
+        if (A.ml) A.ml += row0;
+        if (w.own_splits) {
+            A.token0 = t0;
+            A.all_T = all.T;
+        }
+        PartPlan P{reinterpret_cast<float*>(ws + w.slots), reinterpret_cast<int2*>(ws + w.head), std::min(w.ctas, stream_ctas(A)), F || parts.n > 0};
+        if (w.own_splits && one_sequence) P = PartPlan{};
+        else DSMOE_TRY(launch_stream_attention(A, P, s));
+        const TileParts M{parts.n, rows, parts.o + row0 * all.d_head, parts.ml + row0 * 2};
+        DSMOE_TRY(launch_attention_sum(A, P, folded, F ? F->row_tiles : 0, t0, M, s));
     }
     return DSMOE_OK;
 }
@@ -207,9 +262,10 @@ dsmoe_status dsmoe_attention_workspace_size(const dsmoe_attention_desc* desc, in
         dsmoe_prefix p{};
         p.P = prefix_len;
         const AttnView F = folded_view(A, p);
-        *bytes = attention_ws(A, &F, true, false).total;
+        // (with and without sequence numbers, and whatever the prefix's strides turn out to be)
+        *bytes = std::max(attention_plan(A, &F, true, false).total, attention_plan(A, &F, false, false).total);
     } else {
-        *bytes = attention_ws(A, nullptr, false, kind == DSMOE_ATTENTION_TALLY).total;
+        *bytes = attention_plan(A, nullptr, false, kind == DSMOE_ATTENTION_TALLY).total;
     }
     return DSMOE_OK;
 }
@@ -223,12 +279,12 @@ dsmoe_status dsmoe_window_attention(const dsmoe_attention_desc* desc, int window
     DSMOE_TRY(check_attention_call(desc, q, K, V, pos, out));
     AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
     // (the workspace is that of a window as wide as the cache: the most CTAs that any window can have)
-    const AttnWs w = attention_ws(A, nullptr, false, false);
+    const AttnPlan w = attention_plan(A, nullptr, false, false);
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
     A.window = window;
     A.sinks = sinks;
     A.ring = rolling ? desc->L - sinks : 0;
-    return attend(A, nullptr, w, static_cast<char*>(workspace), (cudaStream_t)stream);
+    return attend(A, nullptr, nullptr, w, static_cast<char*>(workspace), (cudaStream_t)stream);
 }
 
 dsmoe_status dsmoe_prefix_attention(const dsmoe_attention_desc* desc, const dsmoe_prefix* prefix, const void* q, const void* K, const void* V,
@@ -242,9 +298,13 @@ dsmoe_status dsmoe_prefix_attention(const dsmoe_attention_desc* desc, const dsmo
     const AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
     const bool shared = prefix->P > 0;
     const AttnView F = folded_view(A, *prefix);
-    const AttnWs w = attention_ws(A, shared ? &F : nullptr, shared, false);
+    AttnView N = F;                                     // the same, tokens not folded
+    N.T = A.T;
+    N.fold = 1;
+    N.row_tiles = A.row_tiles;
+    const AttnPlan w = attention_plan(A, shared ? &F : nullptr, shared && tile_supported(N), false);
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
-    return attend(A, shared ? &F : nullptr, w, static_cast<char*>(workspace), (cudaStream_t)stream);
+    return attend(A, shared ? &F : nullptr, &N, w, static_cast<char*>(workspace), (cudaStream_t)stream);
 }
 
 dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void* q, const void* K, const void* V, const int32_t* tok_seq,
@@ -264,10 +324,10 @@ dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void*
         return DSMOE_OK;
     }
     AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
-    const AttnWs w = attention_ws(A, nullptr, false, true);
+    const AttnPlan w = attention_plan(A, nullptr, false, true);
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
     A.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + w.ml);
-    DSMOE_TRY(attend(A, nullptr, w, static_cast<char*>(workspace), s));
+    DSMOE_TRY(attend(A, nullptr, nullptr, w, static_cast<char*>(workspace), s));
     return launch_tally(A, tally_in, tally_out, s);
 }
 

@@ -79,7 +79,9 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
             mine[i] = 0;
             if (t < T) {
                 bool bad = false;
-                mine[i] = (long long)sight_of(A, t, &bad).units() * heads;
+                if (is_streams(A, t)) mine[i] = (long long)sight_of(A, t, &bad).units() * heads;
+                else if (blockIdx.x == 0)
+                    for (int h = 0; h < heads; ++h) P.head[(long long)t * heads + h] = make_int2(0, 0);
                 if (bad && blockIdx.x == 0) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
             }
             sum += mine[i];
@@ -104,7 +106,9 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         __syncthreads();
     }
     // Equal runs; no CTA without a unit per warp, as far as there are so many
-    const long long total = base_s[T], wanted = (total + WARPS - 1) / WARPS;
+    const long long total = base_s[T];
+    if (total == 0) return;
+    const long long wanted = (total + WARPS - 1) / WARPS;
     const int n_cta = (int)(wanted < (long long)gridDim.x ? wanted : (long long)gridDim.x);
     if ((int)blockIdx.x >= n_cta) return;
     const long long share = total / n_cta, extra = total - share * n_cta;
@@ -120,8 +124,9 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         int t, h, k, units;
         Sight s;
     };
-    const auto look = [&](Cursor& c) {
+    const auto look = [&](Cursor& c) {                  // (tokens without units are passed over)
         bool bad = false;
+        while (c.t < T && base_s[c.t + 1] == base_s[c.t]) ++c.t;
         if (c.t < T) {
             c.s = sight_of(A, c.t, &bad);
             c.units = c.s.units();
@@ -399,8 +404,9 @@ __global__ void __launch_bounds__(128) attention_sum_kernel(const __grid_constan
         float nx = 0.f, ny = 0.f, den = 0.f;
         const auto add = [&](const float2 ml, const float2 v) {
             const float wgt = exp2_fast(ml.x - z);
-            nx = fmaf(wgt, v.x, nx);
-            ny = fmaf(wgt, v.y, ny);
+            const bool any = ml.x != -INFINITY;         // (a part without keys may hold anything else)
+            nx = fmaf(wgt, any ? v.x : 0.f, nx);
+            ny = fmaf(wgt, any ? v.y : 0.f, ny);
             den = fmaf(wgt, ml.y, den);
         };
 #pragma unroll 4

@@ -1,0 +1,655 @@
+// Attention of many rows that share their keys (prompts; a batch's shared prefix) on the 5th-generation tensor cores.
+//
+// A CTA owns up to 256 rows (neighbouring tokens' query heads of one key/value head) as two tiles of 128, and walks the keys that any of them sees in
+// tiles of 128 keys, which both tiles use.  Per tile of rows and keys: S = Q.K^T into tensor memory; a thread per row takes the row's logits
+// from there, its weights 2^(logit - m) go back as bf16 where the logits lay, and O += P.V with P as the operand in tensor memory and V as it
+// lies in memory (N-major).  The running maximum moves only when a logit passes it by more than 2^8: until then the weights are at most 256, the
+// sums lose nothing, and O needs no rescaling; then the row's threads rescale it in tensor memory.  Roles: warp 0 copies (TMA, a ring of
+// tiles), warp 1 issues the MMAs, warp 2 clears the values behind a stretch's last key (0 times what is no number is no number), warps 4-7
+// and 8-11 are the two tiles' rows.  While one tile's threads are at their weights the tensor pipe works for the other one.
+//
+// What a CTA's tokens see: tokens of one sequence that follow one another are a run; a run's keys are at most three stretches of slots (sinks, and
+// the window, cut in two where a ring ends).  Runs too short to fill a tile are left to attention_stream_kernel.
+// A value that is not finite reaches all rows of a tile, also those that do not see it: rows that come out as no numbers are done again, one by one.
+#include "cache_attention.cuh"
+#include "tensor_maps.cuh"
+#include "umma.cuh"
+
+namespace dsmoe {
+
+namespace {
+
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 384, kMaxRuns = 16, kMaxStretches = 3 * kMaxRuns;
+
+template <int DH>
+struct TileGeo {
+    static constexpr int HALVES = (DH + 63) / 64;                      // 128-byte pieces of a row
+    static constexpr uint32_t PIECE = kTileRows * 128, TILE = HALVES * PIECE;
+    static constexpr int STAGES = HALVES == 1 ? 4 : 2;
+    static constexpr uint32_t Q = 0, K = 2 * TILE, V = K + STAGES * TILE, END = V + STAGES * TILE;
+    static constexpr int SMEM = (int)END + 1024;
+};
+
+struct Stretch {
+    int run, seq, slot0, pos0, n, tile0;  // n keys of a run's, from slot0 / position pos0 on; tile0: tiles before
+};
+
+struct TileShared {
+    uint64_t k_full[4], k_empty[4], v_full[4], v_clear[4], v_empty[4], s_full[2], p_full[2], o_done[2];
+    uint32_t tmem;
+    volatile int abort_flag;
+    int n_tiles, n_stretches, n_runs;
+    int begin, end;                       // this CTA's tiles
+    int redo_n;
+    int seq[2 * kTileRows], first[2 * kTileRows], last[2 * kTileRows], run[2 * kTileRows];
+    int run_len[2 * kTileRows], run_lo[2 * kTileRows], run_hi[2 * kTileRows];
+    int redo[2 * kTileRows];
+    Stretch st[kMaxStretches];
+};
+
+__device__ __forceinline__ float exp2_fast(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// Operand B = V as it lies in memory, [128 keys][64 columns] in the 128-byte swizzle: N-major.  Eight keys are 1024 bytes, the next 64 columns
+// begin 128 rows further on.
+__device__ __forceinline__ uint64_t make_desc_values(uint32_t smem_addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFF) >> 4);
+    d |= (uint64_t)((kTileKeys * 128) >> 4) << 16;                     // leading byte offset: between 64-column groups
+    d |= (uint64_t)(1024 >> 4) << 32;                                  // stride byte offset: between groups of 8 keys
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z, int w) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+
+struct TileArgs {
+    AttnView A;
+    int tile_tokens;                      // tokens of a 128-row tile
+    int least_run;
+    int blocks, splits;
+    int at_pos, at_head, at_seq;          // which of the tensor map's dimensions 1 .. 3 are positions, heads, sequences
+    float *o, *ml;                        // parts [split][T * n_head * group][DH], [..][2]; nullptr: out and lse are written
+};
+
+// Key tile i: the stretch that holds it (the caller's `at` only grows), its first key there
+struct Tile {
+    int run, seq, slot, pos, n;           // n: keys of the tile, up to 128
+};
+__device__ __forceinline__ Tile tile_at(const TileShared& S, int i, int& at) {
+    while (at + 1 < S.n_stretches && S.st[at + 1].tile0 <= i) ++at;
+    const Stretch& s = S.st[at];
+    const int k = (i - s.tile0) * kTileKeys;
+    return Tile{s.run, s.seq, s.slot0 + k, s.pos0 + k, min(kTileKeys, s.n - k)};
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kTileThreads, 1)
+attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const __grid_constant__ TileArgs P) {
+    using G = TileGeo<DH>;
+    constexpr int CH = DH / 8, KS = DH / 16, STAGES = G::STAGES;
+    extern __shared__ unsigned char tile_smem[];
+    __shared__ TileShared S;
+    const AttnView& A = P.A;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t raw = ptx::smem_u32(tile_smem), base = (raw + 1023u) & ~1023u;
+    unsigned char* const smem = tile_smem + (base - raw);
+    // the blocks with the most keys (the last tokens) go first
+    const int j = (int)(blockIdx.x % A.n_head), split = (int)(blockIdx.x / A.n_head) % P.splits;
+    const int block = P.blocks - 1 - (int)(blockIdx.x / A.n_head / P.splits);
+    const int span = 2 * P.tile_tokens, tg0 = block * span, ng = min(A.T - tg0, span);
+    const int tiles_of_rows = ng > P.tile_tokens ? 2 : 1;
+    if (tid == 0) {
+        for (int i = 0; i < STAGES; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&S.k_full[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&S.k_empty[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&S.v_full[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&S.v_clear[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&S.v_empty[i]), 1);
+        }
+        for (int r = 0; r < 2; ++r) {
+            ptx::mbar_init(ptx::smem_u32(&S.s_full[r]), 1);
+            ptx::mbar_init(ptx::smem_u32(&S.p_full[r]), kTileRows);
+            ptx::mbar_init(ptx::smem_u32(&S.o_done[r]), 1);
+        }
+        S.abort_flag = 0;
+        S.redo_n = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(ptx::smem_u32(&S.tmem), 512);
+        ptx::tmem_relinquish();
+    }
+    chain_wait();
+    // ---- what the tokens see, and the runs
+    bool bad = false;
+    if (tid < ng) {
+        const Sight s = sight_of(A, tg0 + tid, &bad);
+        S.seq[tid] = s.seq;
+        S.last[tid] = s.last;
+        S.first[tid] = max(0, s.last >= A.window ? s.last - A.window + 1 : 0);
+        S.run_len[tid] = 0;
+        S.run_lo[tid] = 0x7fffffff;
+        S.run_hi[tid] = -1;
+    }
+    if (bad) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
+    __syncthreads();
+    if (warp == 0) {                      // a token's run: how many runs begin at or before it, less one
+        int before = 0;
+        for (int c = 0; c < ng; c += 32) {
+            const int t = c + lane;
+            const bool begins = t < ng && t > 0 && S.seq[t] != S.seq[t - 1];
+            const uint32_t votes = __ballot_sync(0xffffffffu, begins);
+            if (t < ng) S.run[t] = before + __popc(votes & (0xffffffffu >> (31 - lane)));
+            before += __popc(votes);
+        }
+        if (lane == 0) S.n_runs = before + 1;
+    }
+    __syncthreads();
+    if (tid < ng) {
+        const int r = S.run[tid];
+        atomicAdd(&S.run_len[r], 1);
+        if (S.last[tid] >= 0) {
+            atomicMin(&S.run_lo[r], S.first[tid]);
+            atomicMax(&S.run_hi[r], S.last[tid]);
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        int n = 0, tiles = 0, t = 0;
+        const auto put = [&](int run, int seq, int pos0, int count) {
+            while (count > 0) {           // (in a ring, up to its end and then from its beginning)
+                const int slot = slot_of(A, pos0), m = A.ring && pos0 >= A.sinks ? min(count, A.L - slot) : count;
+                S.st[n++] = Stretch{run, seq, slot, pos0, m, tiles};
+                tiles += (m + kTileKeys - 1) / kTileKeys;
+                pos0 += m;
+                count -= m;
+                if (n == kMaxStretches) return;
+            }
+        };
+        for (int r = 0; r < S.n_runs; ++r) {
+            const int len = S.run_len[r], lo = S.run_lo[r], hi = S.run_hi[r];
+            const bool mine = S.n_runs == 1 || len >= P.least_run;
+            if (mine && hi >= 0 && n + 3 <= kMaxStretches) {
+                const int sinks = min(A.sinks, hi + 1);
+                if (lo <= sinks) {
+                    put(r, S.seq[t], 0, hi + 1);
+                } else {
+                    put(r, S.seq[t], 0, sinks);
+                    put(r, S.seq[t], lo, hi + 1 - lo);
+                }
+            }
+            t += len;
+        }
+        S.n_stretches = n;
+        S.n_tiles = tiles;
+        S.begin = (int)((long long)tiles * split / P.splits);
+        S.end = (int)((long long)tiles * (split + 1) / P.splits);
+    }
+    // ---- queries, in the swizzle's order; rows that are none are zeros
+    for (int idx = tid; idx < tiles_of_rows * kTileRows * CH; idx += kTileThreads) {
+        const int row = idx / CH, ch = idx % CH, r = row >> 7, at = row & 127;
+        const int tl = r * P.tile_tokens + at / A.group, m = at % A.group;
+        const bool real = at < P.tile_tokens * A.group && tl < ng;
+        const __nv_bfloat16* q = A.q + (tg0 + (real ? tl : 0)) * A.q_t + j * A.q_h + m * A.q_g + ch * 8;
+        const uint32_t dst = base + G::Q + r * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + at * 128 + (((ch & 7) ^ (at & 7)) << 4));
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(q), "r"(real ? 16u : 0u) : "memory");
+    }
+    ptx::cp_async_commit();
+    ptx::cp_async_wait<0>();
+    ptx::fence_proxy_async();
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = S.tmem;
+    const int begin = S.begin, n = S.end - S.begin;
+
+    if (warp == 0) {
+        // ---- copies
+        if (ptx::elect_one()) {
+            int at = 0, issued = 0;
+            const auto load = [&](const CUtensorMap* map, uint32_t dst, uint64_t* bar, const Tile& t) {
+                const uint32_t b = ptx::smem_u32(bar);
+                ptx::mbar_expect_tx(b, G::TILE);
+                int c[4];
+                c[P.at_pos] = t.slot, c[P.at_head] = j, c[P.at_seq] = t.seq;
+#pragma unroll
+                for (int h = 0; h < G::HALVES; ++h) tma_load_4d(dst + h * G::PIECE, map, b, h * 64, c[1], c[2], c[3]);
+            };
+            for (int i = 0; i < n; ++i) {
+                const int s = i % STAGES;
+                const uint32_t parity = (uint32_t)((i / STAGES) & 1) ^ 1u;
+                const Tile t = tile_at(S, begin + i, at);
+                if (i >= STAGES && !ptx::mbar_wait(ptx::smem_u32(&S.k_empty[s]), parity, &S.abort_flag)) break;
+                load(&mapK, base + G::K + s * G::TILE, &S.k_full[s], t);
+                if (i >= STAGES && !ptx::mbar_wait(ptx::smem_u32(&S.v_empty[s]), parity, &S.abort_flag)) break;
+                load(&mapV, base + G::V + s * G::TILE, &S.v_full[s], t);
+                issued = i + 1;
+            }
+            if (S.abort_flag) {           // copies in flight end before the CTA does
+                int none = 0;
+                for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i) {
+                    ptx::mbar_wait(ptx::smem_u32(&S.k_full[i % STAGES]), (uint32_t)((i / STAGES) & 1), &none);
+                    ptx::mbar_wait(ptx::smem_u32(&S.v_full[i % STAGES]), (uint32_t)((i / STAGES) & 1), &none);
+                }
+                if (issued < n) ptx::mbar_wait(ptx::smem_u32(&S.k_full[issued % STAGES]), (uint32_t)((issued / STAGES) & 1), &none);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---- MMAs
+        if (ptx::elect_one()) {
+            const uint32_t idesc_s = ptx::make_idesc_bf16(kTileRows, kTileKeys), idesc_o = ptx::make_idesc_bf16(kTileRows, DH) | (1u << 16);
+            const auto logits = [&](int i, int r) {
+                const uint32_t q0 = base + G::Q + r * G::TILE, k0 = base + G::K + (i % STAGES) * G::TILE;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+                    ptx::umma_bf16(tmem + r * 128, ptx::make_desc_k_sw128(q0 + (k >> 2) * G::PIECE + (k & 3) * 32),
+                                   ptx::make_desc_k_sw128(k0 + (k >> 2) * G::PIECE + (k & 3) * 32), idesc_s, (uint32_t)(k != 0));
+                ptx::umma_commit(ptx::smem_u32(&S.s_full[r]));
+            };
+            bool ok = true;
+            if (n > 0) {
+                ok = ptx::mbar_wait(ptx::smem_u32(&S.k_full[0]), 0, &S.abort_flag);
+                if (ok) {
+                    for (int r = 0; r < tiles_of_rows; ++r) logits(0, r);
+                    ptx::umma_commit(ptx::smem_u32(&S.k_empty[0]));
+                }
+            }
+            for (int i = 0; ok && i < n; ++i) {
+                const int s = i % STAGES;
+                ok = ptx::mbar_wait(ptx::smem_u32(&S.v_clear[s]), (uint32_t)((i / STAGES) & 1), &S.abort_flag);
+                if (ok && i + 1 < n)
+                    ok = ptx::mbar_wait(ptx::smem_u32(&S.k_full[(i + 1) % STAGES]), (uint32_t)(((i + 1) / STAGES) & 1), &S.abort_flag);
+                for (int r = 0; ok && r < tiles_of_rows; ++r) {
+                    ok = ptx::mbar_wait(ptx::smem_u32(&S.p_full[r]), (uint32_t)(i & 1), &S.abort_flag);
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+                    const uint32_t v0 = base + G::V + s * G::TILE;
+#pragma unroll
+                    for (int k = 0; k < kTileKeys / 16; ++k)
+                        umma_bf16_ts(tmem + 256 + r * 128, tmem + r * 128 + k * 8, make_desc_values(v0 + k * 2048), idesc_o,
+                                     (uint32_t)(i != 0 || k != 0));
+                    ptx::umma_commit(ptx::smem_u32(&S.o_done[r]));
+                    if (i + 1 < n) logits(i + 1, r);
+                }
+                if (!ok) break;
+                ptx::umma_commit(ptx::smem_u32(&S.v_empty[s]));
+                if (i + 1 < n) ptx::umma_commit(ptx::smem_u32(&S.k_empty[(i + 1) % STAGES]));
+            }
+        }
+        __syncwarp();
+    } else if (warp == 2) {
+        // ---- values that are no keys': zeros
+        int at = 0;
+        for (int i = 0; i < n; ++i) {
+            const Tile t = tile_at(S, begin + i, at);
+            if (!__all_sync(0xffffffffu, ptx::mbar_wait(ptx::smem_u32(&S.v_full[i % STAGES]), (uint32_t)((i / STAGES) & 1), &S.abort_flag))) break;
+            unsigned char* const v = smem + G::V + (i % STAGES) * G::TILE;
+            for (int idx = lane; idx < (kTileKeys - t.n) * 8 * G::HALVES; idx += 32) {
+                const int piece = idx % (8 * G::HALVES), row = t.n + idx / (8 * G::HALVES);
+                *reinterpret_cast<uint4*>(v + (piece >> 3) * G::PIECE + row * 128 + (piece & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            ptx::fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&S.v_clear[i % STAGES]));        // (of every tile: the MMAs wait for it alone)
+        }
+        __syncwarp();
+    }
+    if (warp >= 4) {
+        // ---- rows
+        const int r = (warp - 4) >> 2, at = tid - 128 - r * 128;          // row tile, row of it = lane of tensor memory
+        const int tl = r * P.tile_tokens + at / A.group, m_of = at % A.group;
+        const bool real = at < P.tile_tokens * A.group && tl < ng;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + lanes + r * 128, tO = tmem + lanes + 256 + r * 128;
+        const bool taken = real && (S.n_runs == 1 || S.run_len[S.run[tl]] >= P.least_run);
+        const int run = taken ? S.run[tl] : -1, last = taken ? S.last[tl] : -1, first = taken ? S.first[tl] : 0;
+        const float sl2 = A.scale_log2;
+        float m = -INFINITY, l = 0.f;
+        bool alive = true;
+        int stretch = 0;
+        if (r < tiles_of_rows) {
+            for (int i = 0; i < n; ++i) {
+                const Tile t = tile_at(S, begin + i, stretch);
+                // keys a .. b of the tile are this row's, and those before c
+                const bool in = t.run == run;               // (the same sequence may have two runs in this block)
+                const int b = in ? min(last - t.pos, t.n - 1) : -1, a = first - t.pos, c = A.sinks - t.pos;
+                const bool full = __all_sync(0xffffffffu, b == kTileKeys - 1 && (a <= 0 || c >= kTileKeys)) && sl2 > 0.f;
+                alive = ptx::mbar_wait(ptx::smem_u32(&S.s_full[r]), (uint32_t)(i & 1), &S.abort_flag);
+                alive = __all_sync(0xffffffffu, alive);
+                if (!alive) break;
+                ptx::tc_fence_after();
+                uint32_t v[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) ptx::tmem_ld32(tS + q * 32, v[q]);
+                ptx::tmem_ld_wait();
+                float top = -INFINITY, scale = sl2;
+                if (full) {
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(v[q][k]));
+                    top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
+                } else {
+                    scale = 1.f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const int x = q * 32 + k;
+                            const float y = x <= b && (x >= a || x < c) ? __uint_as_float(v[q][k]) * sl2 : -INFINITY;
+                            v[q][k] = __float_as_uint(y);
+                            top = fmaxf(top, y);
+                        }
+                }
+                // the maximum moves if it has to
+                const bool moves = top > m + 8.f || m == -INFINITY;
+                const float was = m;
+                if (moves) m = fmaxf(m, top);
+                if (__any_sync(0xffffffffu, moves && was != -INFINITY)) {
+                    const float f = moves && was != -INFINITY ? exp2_fast(was - m) : 1.f;
+                    l *= f;
+                    alive = i == 0 || ptx::mbar_wait(ptx::smem_u32(&S.o_done[r]), (uint32_t)((i - 1) & 1), &S.abort_flag);
+                    alive = __all_sync(0xffffffffu, alive);
+                    if (!alive) break;
+                    ptx::tc_fence_after();
+#pragma unroll 1
+                    for (int q = 0; q < DH / 16; ++q) {
+                        uint32_t o[16];
+                        ptx::tmem_ld16(tO + q * 16, o);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                        tmem_st16(tO + q * 16, o);
+                    }
+                }
+                const float z = m == -INFINITY ? 0.f : m;
+                float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float p0 = exp2_fast(fmaf(__uint_as_float(v[q][2 * k]), scale, -z));
+                        const float p1 = exp2_fast(fmaf(__uint_as_float(v[q][2 * k + 1]), scale, -z));
+                        s4[(2 * k) & 3] += p0;
+                        s4[(2 * k + 1) & 3] += p1;
+                        pk[k] = pack2(p0, p1);
+                    }
+                    tmem_st16(tS + q * 16, pk);
+                }
+                l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                tmem_st_wait();
+                ptx::tc_fence_before();
+                ptx::mbar_arrive(ptx::smem_u32(&S.p_full[r]));
+            }
+            if (alive && n > 0) {
+                alive = ptx::mbar_wait(ptx::smem_u32(&S.o_done[r]), (uint32_t)((n - 1) & 1), &S.abort_flag);
+                alive = __all_sync(0xffffffffu, alive);
+            }
+            ptx::tc_fence_after();
+            if (!alive && lane == 0) report_status(A.dev_status, DSMOE_ERR_TIMEOUT);
+        }
+        const long long row = ((long long)(tg0 + tl) * A.n_head + j) * A.group + m_of;
+        if (alive && r < tiles_of_rows) {
+            const float inv = P.o ? 1.f : l == 0.f ? 0.f : 1.f / l;
+            float check = l * 0.f;
+            // through shared memory (the queries' place: every S is done), so that a store writes whole rows
+            unsigned char* const stage = smem + G::Q + r * G::TILE + (warp & 3) * 32 * (G::TILE / kTileRows);
+            constexpr int LINE = (int)(G::TILE / kTileRows);              // bytes of staging a row: 128 or 256
+            constexpr int COLS = LINE / 4;                                // fp32 columns at a time
+            if (P.o) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < DH; c0 += COLS) {
+                    __syncwarp();
+#pragma unroll
+                    for (int q = 0; q < COLS / 32; ++q) {
+                        uint32_t o[32];
+                        if (c0 + q * 32 < DH) {
+                            if (n > 0) {
+                                ptx::tmem_ld32(tO + c0 + q * 32, o);
+                                ptx::tmem_ld_wait();
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) o[k] = 0u;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                check = fmaf(__uint_as_float(o[4 * k]) + __uint_as_float(o[4 * k + 1]) + __uint_as_float(o[4 * k + 2]) +
+                                                 __uint_as_float(o[4 * k + 3]), 0.f, check);
+                                const int ch = q * 8 + k;
+                                *reinterpret_cast<uint4*>(stage + lane * LINE + ((ch ^ (lane & 7)) << 4)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    const int chunks = min(COLS, DH - c0) / 4;
+                    for (int idx = lane; idx < 32 * chunks; idx += 32) {
+                        const int rw = idx / chunks, ch = idx % chunks;
+                        const long long to = __shfl_sync(0xffffffffu, real ? row : -1ll, rw);
+                        if (to >= 0)
+                            *reinterpret_cast<uint4*>(P.o + ((size_t)split * A.T * A.n_head * A.group + to) * DH + c0 + ch * 4) =
+                                *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw & 7)) << 4));
+                    }
+                }
+            } else {
+#pragma unroll 1
+                for (int q = 0; q < DH / 32; ++q) {
+                    uint32_t o[32];
+                    if (n > 0) {
+                        ptx::tmem_ld32(tO + q * 32, o);
+                        ptx::tmem_ld_wait();
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = 0u;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = __uint_as_float(o[8 * k + 2 * e]), y = __uint_as_float(o[8 * k + 2 * e + 1]);
+                            check = fmaf(x + y, 0.f, check);
+                            w[e] = pack2(x * inv, y * inv);
+                        }
+                        const int ch = q * 4 + k;
+                        *reinterpret_cast<uint4*>(stage + lane * LINE + ((ch ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                __syncwarp();
+                const bool good = taken && check == 0.f;
+                const long long dst = good ? (tg0 + tl) * A.o_t + j * A.o_h + m_of * A.o_g : -1ll;
+                for (int idx = lane; idx < 32 * CH; idx += 32) {
+                    const int rw = idx / CH, ch = idx % CH;
+                    const long long to = __shfl_sync(0xffffffffu, dst, rw);
+                    if (to >= 0)
+                        *reinterpret_cast<uint4*>(A.out + to + ch * 8) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw & 7)) << 4));
+                }
+            }
+            if (taken && check != 0.f) {
+                S.redo[atomicAdd(&S.redo_n, 1)] = r * kTileRows + at;
+            } else if (P.o) {
+                if (real) *reinterpret_cast<float2*>(P.ml + ((size_t)split * A.T * A.n_head * A.group + row) * 2) = make_float2(l == 0.f ? -INFINITY : m, l);
+            } else if (taken) {
+                const float z = m == -INFINITY ? 0.f : m;
+                if (A.lse) A.lse[row] = (z + log2f(l)) * 0.6931471805599453f;
+                if (A.ml) A.ml[row] = make_float2(z, l == 0.f ? 0.f : 1.f / l);
+            }
+        }
+    }
+    chain_next();
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+    // ---- rows that came out as no numbers: a warp per row, a key at a time, over this CTA's tiles
+    for (int x = warp; x < S.redo_n; x += kTileThreads / 32) {
+        constexpr int PER = DH / 32;
+        const int rr = S.redo[x], r = rr / kTileRows, at = rr % kTileRows, tl = r * P.tile_tokens + at / A.group, m_of = at % A.group;
+        const __nv_bfloat16* const q = A.q + (tg0 + tl) * A.q_t + j * A.q_h + m_of * A.q_g;
+        float qv[PER], o[PER], m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            qv[e] = __bfloat162float(q[lane + 32 * e]);
+            o[e] = 0.f;
+        }
+        int stretch = 0;
+        for (int i = 0; i < n; ++i) {
+            const Tile t = tile_at(S, begin + i, stretch);
+            if (t.run != S.run[tl]) continue;
+            for (int k = 0; k < t.n; ++k) {
+                const int pos = t.pos + k;
+                if (pos > S.last[tl] || (pos < S.first[tl] && pos >= A.sinks)) continue;
+                const long long src = t.seq * A.kv_s + j * A.kv_h + slot_of(A, pos) * A.kv_p + lane;
+                float dot = 0.f;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) dot = fmaf(qv[e], __bfloat162float(A.K[src + 32 * e]), dot);
+#pragma unroll
+                for (int w = 16; w > 0; w >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, w);
+                dot *= A.scale_log2;
+                const float top = fmaxf(m, dot), f = m == -INFINITY ? 0.f : exp2_fast(m - top), p = exp2_fast(dot - top);
+                m = top;
+                l = fmaf(l, f, p);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) o[e] = fmaf(o[e], f, p * __bfloat162float(A.V[src + 32 * e]));
+            }
+        }
+        const long long row = ((long long)(tg0 + tl) * A.n_head + j) * A.group + m_of;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if (P.o) P.o[((size_t)split * A.T * A.n_head * A.group + row) * DH + lane + 32 * e] = o[e];
+            else A.out[(tg0 + tl) * A.o_t + j * A.o_h + m_of * A.o_g + lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
+        }
+        if (lane == 0) {
+            const float z = m == -INFINITY ? 0.f : m;
+            if (P.o) {
+                *reinterpret_cast<float2*>(P.ml + ((size_t)split * A.T * A.n_head * A.group + row) * 2) = make_float2(m, l);
+            } else {
+                if (A.lse) A.lse[row] = (z + log2f(l)) * 0.6931471805599453f;
+                if (A.ml) A.ml[row] = make_float2(z, inv);
+            }
+        }
+    }
+}
+
+// K or V as a tensor of four dimensions, d_head and then positions, heads and sequences in the order of their strides
+dsmoe_status make_cache_map(CUtensorMap* m, const AttnView& A, const void* ptr, int (&at)[3]) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return DSMOE_ERR_CUDA;
+    const long long stride[3] = {A.kv_p, A.kv_h, A.kv_s};
+    const cuuint64_t size[3] = {(cuuint64_t)A.L, (cuuint64_t)A.n_head, (cuuint64_t)A.n_seq};
+    int order[3] = {0, 1, 2};
+    for (int a = 0; a < 2; ++a)
+        for (int b = 0; b < 2 - a; ++b) {
+            // (a dimension of one element has no stride to speak of: last)
+            const long long x = size[order[b]] == 1 ? 1ll << 50 : stride[order[b]], y = size[order[b + 1]] == 1 ? 1ll << 50 : stride[order[b + 1]];
+            if (x > y) {
+                const int t = order[b];
+                order[b] = order[b + 1];
+                order[b + 1] = t;
+            }
+        }
+    cuuint64_t dims[4] = {(cuuint64_t)A.d_head}, strides[3];
+    cuuint32_t box[4] = {64, 1, 1, 1};
+    const cuuint32_t es[4] = {1, 1, 1, 1};
+    for (int d = 0; d < 3; ++d) {
+        const int o = order[d];
+        dims[d + 1] = size[o];
+        strides[d] = size[o] == 1 ? (d == 0 ? (cuuint64_t)A.d_head * 2 : strides[d - 1] * dims[d]) : (cuuint64_t)stride[o] * 2;
+        at[o] = d + 1;
+        if (o == 0) box[d + 1] = kTileKeys;
+    }
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DSMOE_OK : DSMOE_ERR_CUDA;
+}
+
+template <int DH>
+dsmoe_status launch_tile(const AttnView& A, const TilePlan& plan, cudaStream_t s) {
+    using G = TileGeo<DH>;
+    static bool attr[kMaxDeviceSlots] = {};
+    int dev = 0;
+    DeviceState* st = nullptr;
+    DSMOE_TRY(device_state(&st, &dev));
+    if (!attr[dev]) {
+        DSMOE_CUDA_TRY(cudaFuncSetAttribute(attention_tile_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
+        attr[dev] = true;
+    }
+    CUtensorMap mapK, mapV;
+    int at[3];
+    DSMOE_TRY(make_cache_map(&mapK, A, A.K, at));
+    DSMOE_TRY(make_cache_map(&mapV, A, A.V, at));
+    TileArgs P{A, kTileRows / A.group, tile_least_run(A.group), tile_blocks(A.T, A.group), plan.splits, at[0], at[1], at[2], plan.o, plan.ml};
+    const long long ctas = (long long)P.blocks * A.n_head * plan.splits;
+    if (ctas > 0x7fffffffll) return DSMOE_ERR_UNSUPPORTED;
+    DSMOE_CUDA_TRY(launch_chained(attention_tile_kernel<DH>, (unsigned)ctas, kTileThreads, G::SMEM, s, mapK, mapV, P));
+    return DSMOE_OK;
+}
+
+}  // namespace
+
+bool tile_supported(const AttnView& A) {
+    if (A.d_head != 64 && A.d_head != 96 && A.d_head != 128) return false;
+    const long long stride[3] = {A.kv_p, A.kv_h, A.kv_s};
+    const int size[3] = {A.L, A.n_head, A.n_seq};
+    for (int d = 0; d < 3; ++d)
+        if (size[d] > 1 && (stride[d] <= 0 || stride[d] >= 1ll << 38)) return false;
+    return true;
+}
+
+dsmoe_status launch_tile_attention(const AttnView& A, const TilePlan& plan, cudaStream_t s) {
+    switch (A.d_head) {
+        case 64: return launch_tile<64>(A, plan, s);
+        case 96: return launch_tile<96>(A, plan, s);
+        case 128: return launch_tile<128>(A, plan, s);
+        default: return DSMOE_ERR_UNSUPPORTED;
+    }
+}
+
+}  // namespace dsmoe

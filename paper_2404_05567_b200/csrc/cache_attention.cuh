@@ -29,6 +29,9 @@ struct AttnView {
     float* lse;                           // nullable
     float2* ml;                           // nullable: (largest logit, 1 / sum) of every row, [T][n_head][group]
     int32_t* dev_status;
+    // The stream kernel beside the 128-row kernel: it attends the tokens that the latter leaves alone.  The call has all_T tokens, of which these
+    // begin at token0 (all_T 0: it attends all tokens).
+    int token0, all_T;
 };
 
 constexpr int kUnit = 16;                 // keys that a warp takes at a time
@@ -65,6 +68,22 @@ __device__ __forceinline__ Sight sight_of(const AttnView& A, int t, bool* bad) {
     }
     return s;
 }
+// The 128-row kernel's blocks of tokens: two tiles of as many tokens as have their rows in 128.  Tokens of one sequence that follow one another
+// there are a run; runs that fill less than a quarter of a tile, unless the block is one, are left to the stream kernel.
+__host__ __device__ static inline int tile_span(int group) { return 2 * (128 / group); }
+__host__ __device__ static inline int tile_least_run(int group) { return (32 + group - 1) / group; }
+__host__ __device__ static inline int tile_blocks(int T, int group) { return (T + tile_span(group) - 1) / tile_span(group); }
+__device__ __forceinline__ int seq_of_token(const AttnView& A, int t) { return A.tok_seq ? min(max(A.tok_seq[t], 0), A.n_seq - 1) : 0; }
+// Whether the stream kernel attends token t (numbered from A.token0)
+__device__ __forceinline__ bool is_streams(const AttnView& A, int t) {
+    if (A.all_T == 0) return true;
+    const int span = tile_span(A.group), least = tile_least_run(A.group), at = A.token0 + t;
+    const int b0 = at / span * span, b1 = min(A.all_T, b0 + span), seq = seq_of_token(A, t);
+    int lo = at, hi = at + 1;
+    while (lo > b0 && hi - lo < least && seq_of_token(A, lo - 1 - A.token0) == seq) --lo;
+    while (hi < b1 && hi - lo < least && seq_of_token(A, hi - A.token0) == seq) ++hi;
+    return hi - lo < least && (lo > b0 || hi < b1);
+}
 // The slot of the cache that holds position l
 __device__ __forceinline__ int slot_of(const AttnView& A, int l) { return !A.ring || l < A.sinks ? l : A.sinks + (l - A.sinks) % A.ring; }
 
@@ -84,6 +103,15 @@ struct TileParts {
     const float* o;
     const float* ml;
 };
+
+// The 128-row kernel: heads of 64, 96 and 128, caches that a tensor map describes.  Its rows' keys are cut into `splits`; o, ml: where their parts
+// go (TileParts), or nullptr with one split: out and lse are written.
+struct TilePlan {
+    int splits;
+    float *o, *ml;
+};
+bool tile_supported(const AttnView& A);
+dsmoe_status launch_tile_attention(const AttnView& A, const TilePlan& plan, cudaStream_t s);
 
 int stream_ctas(const AttnView& A);       // CTAs of launch_stream_attention at most
 dsmoe_status launch_stream_attention(const AttnView& A, const PartPlan& parts, cudaStream_t s);
