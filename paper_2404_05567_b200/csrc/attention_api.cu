@@ -83,7 +83,6 @@ AttnView view_of(const dsmoe_attention_desc& d, const void* q, const void* K, co
     A.T = d.T;
     A.n_head = d.n_head;
     A.group = d.group;
-    A.fold = 1;
     A.row_tiles = ceil_div(d.group, 16);
     A.d_head = d.d_head;
     A.n_seq = d.n_seq;
@@ -104,33 +103,20 @@ AttnView view_of(const dsmoe_attention_desc& d, const void* q, const void* K, co
     return A;
 }
 
-// The tokens of a prefix taken as one
-AttnView folded_view(const AttnView& A, const dsmoe_prefix& p) {
-    AttnView F = A;
-    F.fold = A.T;
-    F.T = 1;
-    F.row_tiles = (int)(((long long)A.T * A.group + 15) / 16);
-    F.n_seq = 1;
-    F.L = p.P;
-    F.K = static_cast<const __nv_bfloat16*>(p.Kp);
-    F.V = static_cast<const __nv_bfloat16*>(p.Vp);
-    F.kv_s = 0, F.kv_h = p.stride[0], F.kv_p = p.stride[1];
-    F.tok_seq = F.pos = nullptr;
-    return F;
-}
-
 // Which kernels a call takes, and its workspace.
 //
 // The prefix: on the 128-row kernel from 33 rows on (two 16-row tiles of the stream kernel read it twice; with more rows the stream kernel is bound by
-// its MMAs), its keys cut so that all SMs have some.  The own caches: where there are more tokens than sequences, on the 128-row kernel, which
-// leaves tokens alone that have too few neighbours of their sequence (is_streams); otherwise, and for those, on the stream kernel.
+// its MMAs), its keys cut so that all SMs have some; with fewer rows on the stream kernel, in one launch with the own caches.  The own caches:
+// where there are more tokens than sequences, on the 128-row kernel, which leaves tokens that have too few neighbours of their sequence; otherwise,
+// and for those, on the stream kernel.
 constexpr int kPrefixStreamRows = 32, kOwnTileRows = 64, kMaxSplits = 64;
 
 struct AttnPlan {
-    size_t slots, head, f_slots, f_head, ml, tile_o, tile_ml, total;
-    int ctas, f_ctas;
+    size_t slots, head, run_head, count, list, ml, row_o, row_ml, total;
+    int ctas, passes;                     // of the stream kernel, at most
     int prefix_splits;                    // 0: the prefix is not the 128-row kernel's
     int own_splits;                       // ... the own caches
+    int row_parts;                        // parts of whole rows
 };
 
 // Parts into which the 128-row kernel's keys are cut: as many as fill the SMs, two tiles of keys or more in each
@@ -143,8 +129,23 @@ bool own_on_tiles(const AttnView& A) {
     return tile_supported(A) && (A.tok_seq ? A.T > A.n_seq : A.T > 1) && (long long)A.T * A.group >= kOwnTileRows;
 }
 
-// F: the folded prefix or nullptr; may_tile: the prefix's strides allow it, as far as known.
-AttnPlan attention_plan(const AttnView& A, const AttnView* F, bool may_tile, bool wants_ml) {
+SharedKeys shared_keys(const AttnView& A, const dsmoe_prefix& p) {
+    return SharedKeys{p.P, (int)(((long long)A.T * A.group + 15) / 16), static_cast<const __nv_bfloat16*>(p.Kp),
+                      static_cast<const __nv_bfloat16*>(p.Vp), p.stride[0], p.stride[1]};
+}
+// The shared keys as a cache of one sequence
+AttnView shared_view(const AttnView& A, const SharedKeys& S) {
+    AttnView N = A;
+    N.n_seq = 1;
+    N.L = S.P;
+    N.K = S.K, N.V = S.V;
+    N.kv_s = 0, N.kv_h = S.kv_h, N.kv_p = S.kv_p;
+    N.tok_seq = N.pos = nullptr;
+    return N;
+}
+
+// may_tile: the prefix's strides allow it
+AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, bool wants_ml) {
     AttnPlan w{};
     size_t off = 0;
     const auto take = [&](size_t bytes) {
@@ -152,78 +153,78 @@ AttnPlan attention_plan(const AttnView& A, const AttnView* F, bool may_tile, boo
         off = align_up(off + bytes, 256);
         return at;
     };
-    const size_t tokens = (size_t)(A.T < kListTokens ? A.T : kListTokens), pairs = tokens * A.n_head * A.row_tiles;
-    const size_t rows = (size_t)A.T * A.n_head * A.group;
-    w.ctas = stream_ctas(A);
-    w.head = take(pairs * sizeof(int2));
-    // (whole pairs leave parts too where there is something to add them to)
-    w.slots = take((2 * (size_t)w.ctas + pairs) * part_bytes(A.d_head));
+    const size_t rows = (size_t)A.T * A.n_head * A.group, blocks = (size_t)tile_blocks(A.T, A.group);
+    w.ctas = stream_ctas(A, S, true);
+    w.passes = ceil_div(A.T, kListTokens);
+    w.slots = take((size_t)w.passes * 2 * w.ctas * part_bytes(A.d_head));
+    w.run_head = take((size_t)w.passes * w.ctas * sizeof(int2));
+    w.head = take((size_t)A.n_head * ((size_t)A.T * A.row_tiles + S.row_tiles) * sizeof(int2));
     if (wants_ml) w.ml = take(rows * sizeof(float2));
-    if (own_on_tiles(A)) w.own_splits = tile_splits(A, A.L);
-    size_t folded = off;
-    if (F) {
-        const size_t f_pairs = (size_t)F->n_head * F->row_tiles;
-        w.f_ctas = stream_ctas(*F);
-        w.f_head = take(f_pairs * sizeof(int2));
-        w.f_slots = take((2 * (size_t)w.f_ctas + f_pairs) * part_bytes(A.d_head));
-        const bool wide = A.d_head == 64 || A.d_head == 96 || A.d_head == 128;
-        if (may_tile && wide && (long long)A.T * A.group > kPrefixStreamRows) w.prefix_splits = tile_splits(A, F->L);
-        // (one of the two; which, the prefix's strides may decide)
-        if (w.prefix_splits) std::swap(folded, off);
-        else folded = off;
+    if (own_on_tiles(A)) {
+        w.own_splits = tile_splits(A, A.L);
+        w.count = take(blocks * 4);
+        w.list = take(blocks * tile_span(A.group) * 4);
     }
-    const size_t parts = (size_t)w.prefix_splits + w.own_splits;
-    w.tile_ml = take(parts * rows * 2 * 4);
-    w.tile_o = take(parts * rows * A.d_head * 4);
-    w.total = std::max(off, folded);
+    if (S.P > 0 && may_tile && (long long)A.T * A.group > kPrefixStreamRows) w.prefix_splits = tile_splits(A, S.P);
+    if (S.P > 0 || w.own_splits > 1) w.row_parts = (S.P > 0 ? std::max(1, w.prefix_splits) : 0) + std::max(1, w.own_splits);
+    w.row_ml = take((size_t)w.row_parts * rows * 2 * 4);
+    w.row_o = take((size_t)w.row_parts * rows * A.d_head * 4);
+    w.total = off;
     return w;
 }
 
-// Attention of all tokens: the prefix (F, on the 128-row kernel as N), the own caches, the sum
-dsmoe_status attend(const AttnView& all, const AttnView* F, const AttnView* N, const AttnPlan& w, char* ws, cudaStream_t s) {
-    const size_t rows = (size_t)all.T * all.n_head * all.group;
-    float* const o = reinterpret_cast<float*>(ws + w.tile_o);
-    float* const ml = reinterpret_cast<float*>(ws + w.tile_ml);
-    const bool one_sequence = !all.tok_seq || all.n_seq == 1;
-    PartPlan folded{};
-    TileParts parts{0, rows, o, ml};
+// Attention of all tokens: the prefix, the own caches, the sum
+dsmoe_status attend(const AttnView& A, const SharedKeys& S, const AttnPlan& w, char* ws, cudaStream_t s) {
+    const size_t rows = (size_t)A.T * A.n_head * A.group;
+    const bool one_sequence = !A.tok_seq || A.n_seq == 1;
+    RowParts parts{0, rows, reinterpret_cast<float*>(ws + w.row_o), reinterpret_cast<float*>(ws + w.row_ml)};
+    const auto next_parts = [&](int n) {                // the next n parts of whole rows
+        const RowParts p{n, rows, parts.o + parts.n * rows * A.d_head, parts.ml + parts.n * rows * 2};
+        parts.n += n;
+        return p;
+    };
+    StreamPlan plan{};
+    plan.passes = w.passes;
+    plan.slots = reinterpret_cast<float*>(ws + w.slots);
+    plan.own = true;
+    int2* const head = reinterpret_cast<int2*>(ws + w.head);
     if (w.prefix_splits) {
-        DSMOE_TRY(launch_tile_attention(*N, TilePlan{w.prefix_splits, o, ml}, s));
-        parts.n = w.prefix_splits;
-    } else if (F) {
-        folded = PartPlan{reinterpret_cast<float*>(ws + w.f_slots), reinterpret_cast<int2*>(ws + w.f_head), w.f_ctas, true};
-        DSMOE_TRY(launch_stream_attention(*F, folded, s));
+        const RowParts p = next_parts(w.prefix_splits);
+        DSMOE_TRY(launch_tile_attention(shared_view(A, S), TilePlan{w.prefix_splits, p.o, p.ml, nullptr, nullptr, nullptr}, s));
+    } else if (S.P > 0) {
+        plan.shared = S;
+        plan.shared_rows = next_parts(1);
     }
+    plan.keep = S.P > 0;
     if (w.own_splits) {
         // a narrow window needs fewer parts than the workspace has room for
-        const long long keys = all.window < all.L ? (long long)all.window + all.sinks + tile_span(all.group) : all.L;
-        const int splits = std::min(w.own_splits, tile_splits(all, keys));
-        const bool direct = splits == 1 && !F;
-        DSMOE_TRY(launch_tile_attention(all, direct ? TilePlan{1, nullptr, nullptr} : TilePlan{splits, o + parts.n * rows * all.d_head, ml + parts.n * rows * 2}, s));
-        if (!direct) parts.n += splits;
-        if (direct && one_sequence) return DSMOE_OK;
-    }
-    for (int t0 = 0; t0 < all.T; t0 += kListTokens) {
-        AttnView A = all;
-        A.T = std::min(kListTokens, all.T - t0);
-        A.q += t0 * A.q_t;
-        A.out += t0 * A.o_t;
-        if (A.tok_seq) A.tok_seq += t0;
-        A.pos += t0;
-        const size_t row0 = (size_t)t0 * A.n_head * A.group;
-        if (A.lse) A.lse += row0;
-        if (A.ml) A.ml += row0;
-        if (w.own_splits) {
-            A.token0 = t0;
-            A.all_T = all.T;
+        const long long keys = A.window < A.L ? (long long)A.window + A.sinks + tile_span(A.group) : A.L;
+        const int splits = std::min(w.own_splits, tile_splits(A, keys));
+        plan.keep = plan.keep || splits > 1;
+        TilePlan tile{splits, nullptr, nullptr, nullptr, nullptr, nullptr};
+        if (plan.keep) {
+            plan.own_rows = next_parts(splits);
+            tile.o = plan.own_rows.o, tile.ml = plan.own_rows.ml;
+            tile.head = head + (size_t)A.n_head * plan.shared.row_tiles;
         }
-        PartPlan P{reinterpret_cast<float*>(ws + w.slots), reinterpret_cast<int2*>(ws + w.head), std::min(w.ctas, stream_ctas(A)), F || parts.n > 0};
-        if (w.own_splits && one_sequence) P = PartPlan{};
-        else DSMOE_TRY(launch_stream_attention(A, P, s));
-        const TileParts M{parts.n, rows, parts.o + row0 * all.d_head, parts.ml + row0 * 2};
-        DSMOE_TRY(launch_attention_sum(A, P, folded, F ? F->row_tiles : 0, t0, M, s));
+        if (!one_sequence) {
+            plan.count = tile.count = reinterpret_cast<int32_t*>(ws + w.count);
+            plan.list = tile.list = reinterpret_cast<int32_t*>(ws + w.list);
+            plan.blocks = tile_blocks(A.T, A.group);
+            plan.span = tile_span(A.group);
+        } else {
+            plan.own = false;
+        }
+        DSMOE_TRY(launch_tile_attention(A, tile, s));
+    } else if (plan.keep) {
+        plan.own_rows = next_parts(1);
     }
-    return DSMOE_OK;
+    plan.ctas = std::min(w.ctas, stream_ctas(A, plan.shared, plan.own));
+    if (plan.keep) plan.head = head;
+    else plan.run_head = reinterpret_cast<int2*>(ws + w.run_head);
+    if (plan.own || plan.shared.P > 0) DSMOE_TRY(launch_stream_attention(A, plan, s));
+    else if (!plan.keep) return DSMOE_OK;
+    return launch_attention_sum(A, plan, parts, s);
 }
 
 dsmoe_status check_window(const dsmoe_attention_desc* d, int window, int sinks, int rolling) {
@@ -258,14 +259,12 @@ dsmoe_status dsmoe_attention_workspace_size(const dsmoe_attention_desc* desc, in
     const AttnView A = view_of(*desc, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
     if (desc->T == 0) {
         *bytes = 0;
-    } else if (kind == DSMOE_ATTENTION_PREFIX && prefix_len > 0) {
-        dsmoe_prefix p{};
-        p.P = prefix_len;
-        const AttnView F = folded_view(A, p);
-        // (with and without sequence numbers, and whatever the prefix's strides turn out to be)
-        *bytes = std::max(attention_plan(A, &F, true, false).total, attention_plan(A, &F, false, false).total);
     } else {
-        *bytes = attention_plan(A, nullptr, false, kind == DSMOE_ATTENTION_TALLY).total;
+        // (with and without sequence numbers, and whatever the prefix's strides turn out to be)
+        dsmoe_prefix p{};
+        if (kind == DSMOE_ATTENTION_PREFIX) p.P = prefix_len;
+        const bool tiles = A.d_head == 64 || A.d_head == 96 || A.d_head == 128;
+        *bytes = attention_plan(A, shared_keys(A, p), tiles, kind == DSMOE_ATTENTION_TALLY).total;
     }
     return DSMOE_OK;
 }
@@ -279,12 +278,12 @@ dsmoe_status dsmoe_window_attention(const dsmoe_attention_desc* desc, int window
     DSMOE_TRY(check_attention_call(desc, q, K, V, pos, out));
     AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
     // (the workspace is that of a window as wide as the cache: the most CTAs that any window can have)
-    const AttnPlan w = attention_plan(A, nullptr, false, false);
+    const AttnPlan w = attention_plan(A, SharedKeys{}, false, false);
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
     A.window = window;
     A.sinks = sinks;
     A.ring = rolling ? desc->L - sinks : 0;
-    return attend(A, nullptr, nullptr, w, static_cast<char*>(workspace), (cudaStream_t)stream);
+    return attend(A, SharedKeys{}, w, static_cast<char*>(workspace), (cudaStream_t)stream);
 }
 
 dsmoe_status dsmoe_prefix_attention(const dsmoe_attention_desc* desc, const dsmoe_prefix* prefix, const void* q, const void* K, const void* V,
@@ -296,15 +295,10 @@ dsmoe_status dsmoe_prefix_attention(const dsmoe_attention_desc* desc, const dsmo
     DSMOE_TRY(check_attention_call(desc, q, K, V, pos, out));
     DSMOE_TRY(check_prefix(desc, prefix, out));
     const AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
-    const bool shared = prefix->P > 0;
-    const AttnView F = folded_view(A, *prefix);
-    AttnView N = F;                                     // the same, tokens not folded
-    N.T = A.T;
-    N.fold = 1;
-    N.row_tiles = A.row_tiles;
-    const AttnPlan w = attention_plan(A, shared ? &F : nullptr, shared && tile_supported(N), false);
+    const SharedKeys S = prefix->P > 0 ? shared_keys(A, *prefix) : SharedKeys{};
+    const AttnPlan w = attention_plan(A, S, S.P > 0 && tile_supported(shared_view(A, S)), false);
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
-    return attend(A, shared ? &F : nullptr, &N, w, static_cast<char*>(workspace), (cudaStream_t)stream);
+    return attend(A, S, w, static_cast<char*>(workspace), (cudaStream_t)stream);
 }
 
 dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void* q, const void* K, const void* V, const int32_t* tok_seq,
@@ -324,10 +318,10 @@ dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void*
         return DSMOE_OK;
     }
     AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
-    const AttnPlan w = attention_plan(A, nullptr, false, true);
+    const AttnPlan w = attention_plan(A, SharedKeys{}, false, true);
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
     A.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + w.ml);
-    DSMOE_TRY(attend(A, nullptr, nullptr, w, static_cast<char*>(workspace), s));
+    DSMOE_TRY(attend(A, SharedKeys{}, w, static_cast<char*>(workspace), s));
     return launch_tally(A, tally_in, tally_out, s);
 }
 

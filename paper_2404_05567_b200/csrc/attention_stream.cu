@@ -58,59 +58,96 @@ struct StreamGeo {
 
 template <int DH>
 __global__ void __launch_bounds__(32 * StreamGeo<DH>::WARPS, 1)
-attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constant__ PartPlan P) {
+attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constant__ StreamPlan P) {
     using G = StreamGeo<DH>;
     constexpr int STRIDE = G::STRIDE, KS = DH / 16, DT = DH / 8, CH = DH / 8, LDO = DH + 8, BUFS = G::BUFS, WARPS = G::WARPS;
     constexpr int THREADS = 32 * WARPS, QN = (16 * CH + THREADS - 1) / THREADS, PER = kListTokens / THREADS;
     extern __shared__ __align__(16) unsigned char as_smem[];
-    __shared__ long long base_s[kListTokens + 1];       // units before token t's
+    __shared__ long long base_s[kListTokens + 2];       // units before entry e's: the shared keys (in the first pass), then tokens
+    __shared__ int token_s[kListTokens];                // left tokens: their numbers
     __shared__ long long warp_sum_s[WARPS];
     __shared__ float ms[WARPS][16], ls[WARPS][16];
     __shared__ uint32_t at_s[WARPS];                    // where each warp's accumulators of the pair are
     __shared__ __align__(16) unsigned char q_s[16 * STRIDE];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
-    const int T = A.T, heads = A.n_head * A.row_tiles;
+    const int own_heads = A.n_head * A.row_tiles, shared_heads = A.n_head * P.shared.row_tiles;
     chain_wait();
-    {
-        long long mine[PER], sum = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int t = tid * PER + i;
-            mine[i] = 0;
-            if (t < T) {
-                bool bad = false;
-                if (is_streams(A, t)) mine[i] = (long long)sight_of(A, t, &bad).units() * heads;
-                else if (blockIdx.x == 0)
-                    for (int h = 0; h < heads; ++h) P.head[(long long)t * heads + h] = make_int2(0, 0);
-                if (bad && blockIdx.x == 0) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
-            }
-            sum += mine[i];
-        }
-        long long incl = sum;
+    if (P.run_head)
+        for (int i = tid; i < P.passes; i += THREADS) P.run_head[(long long)i * P.ctas + blockIdx.x] = make_int2(0, 0);
+
+    // Sum over the CTA's threads of what lies before this one's x; *all: of all
+    const auto scan = [&](long long x, long long* all) {
+        long long incl = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long up = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += up;
         }
+        __syncthreads();
         if (lane == 31) warp_sum_s[warp] = incl;
         __syncthreads();
-        long long before = incl - sum;
-        for (int w = 0; w < warp; ++w) before += warp_sum_s[w];
+        long long before = incl - x, sum = 0;
+        for (int w = 0; w < WARPS; ++w) {
+            if (w < warp) before += warp_sum_s[w];
+            sum += warp_sum_s[w];
+        }
+        *all = sum;
+        return before;
+    };
+
+    for (int pass = 0; pass < P.passes; ++pass) {
+    // ---- the pass's entries and their units
+    const int first = pass == 0 && P.shared.P > 0 ? 1 : 0;          // the first token's entry
+    const int n0 = pass * kListTokens;
+    int n = P.own ? min(kListTokens, A.T - n0) : 0;
+    __syncthreads();
+    if (P.own && P.count) {
+        long long so_far = 0;
+        for (int b0 = 0; b0 < P.blocks; b0 += THREADS) {
+            const int b = b0 + tid, c = b < P.blocks ? P.count[b] : 0;
+            long long sum;
+            const long long at = so_far + scan(c, &sum) - n0;
+            for (int i = 0; i < c; ++i)
+                if (at + i >= 0 && at + i < kListTokens) token_s[at + i] = P.list[(long long)b * P.span + i];
+            so_far += sum;
+        }
+        n = (int)max(0ll, min((long long)kListTokens, so_far - n0));
+        __syncthreads();
+    }
+    const auto token_of = [&](int e) { return P.count ? token_s[e - first] : n0 + e - first; };
+    if (n + first == 0) break;
+    {
+        long long mine[PER], sum = 0, total;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int t = tid * PER + i;
-            if (t < T) base_s[t] = before;
+            const int e = tid * PER + i;
+            mine[i] = 0;
+            if (e < n) {
+                bool bad = false;
+                mine[i] = (long long)sight_of(A, token_of(e + first), &bad).units() * own_heads;
+                if (bad && blockIdx.x == 0) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
+            }
+            sum += mine[i];
+        }
+        const long long shared_units = first ? (long long)((P.shared.P + kUnit - 1) / kUnit) * shared_heads : 0;
+        long long before = scan(sum, &total) + shared_units;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = tid * PER + i;
+            if (e < n) base_s[first + e] = before;
             before += mine[i];
-            if (t == T - 1) base_s[T] = before;
+        }
+        if (tid == 0) {
+            base_s[0] = 0;
+            base_s[first + n] = total + shared_units;
         }
         __syncthreads();
     }
     // Equal runs; no CTA without a unit per warp, as far as there are so many
-    const long long total = base_s[T];
-    if (total == 0) return;
-    const long long wanted = (total + WARPS - 1) / WARPS;
+    const int entries = n + first;
+    const long long total = base_s[entries], wanted = (total + WARPS - 1) / WARPS;
     const int n_cta = (int)(wanted < (long long)gridDim.x ? wanted : (long long)gridDim.x);
-    if ((int)blockIdx.x >= n_cta) return;
+    if ((int)blockIdx.x >= n_cta) continue;
     const long long share = total / n_cta, extra = total - share * n_cta;
     const auto run_start = [&](long long c) { return c * share + (c < extra ? c : extra); };
     const auto run_of = [&](long long u) {              // the CTA whose run holds unit u
@@ -119,38 +156,38 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     };
     const long long u0 = run_start(blockIdx.x), u1 = run_start(blockIdx.x + 1);
 
-    // Where a unit lies: token, its (head, row tile), key block of it
+    // Where a unit lies: entry, its (head, row tile), key block of it
     struct Cursor {
-        int t, h, k, units;
+        int e, h, k, units;
         Sight s;
     };
-    const auto look = [&](Cursor& c) {                  // (tokens without units are passed over)
+    const auto is_shared = [&](int e) { return e < first; };
+    const auto look = [&](Cursor& c) {
         bool bad = false;
-        while (c.t < T && base_s[c.t + 1] == base_s[c.t]) ++c.t;
-        if (c.t < T) {
-            c.s = sight_of(A, c.t, &bad);
-            c.units = c.s.units();
-        }
+        if (c.e >= entries) return;
+        if (is_shared(c.e)) c.s = Sight{0, 0, 0, P.shared.P - 1};
+        else c.s = sight_of(A, token_of(c.e), &bad);
+        c.units = c.s.units();
     };
     const auto settle = [&](Cursor& c) {                // k past the pair's units: on to the pair that holds it
-        while (c.t < T && c.k >= c.units) {
+        while (c.e < entries && c.k >= c.units) {
             c.k -= c.units;
-            if (++c.h == heads) {
+            if (++c.h == (is_shared(c.e) ? shared_heads : own_heads)) {
                 c.h = 0;
-                ++c.t;
+                ++c.e;
                 look(c);
             }
         }
     };
     Cursor seg;
     {
-        int lo = 0, hi = T - 1;                         // the last token whose units begin at or before u0
+        int lo = 0, hi = entries - 1;                   // the last entry whose units begin at or before u0
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (base_s[mid] <= u0) lo = mid;
             else hi = mid - 1;
         }
-        seg.t = lo;
+        seg.e = lo;
         look(seg);
         const long long in = u0 - base_s[lo];
         seg.h = (int)(in / seg.units);
@@ -165,22 +202,24 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     const auto fetch = [&](int buf) {
         if (u_ahead < u1) {
             const Sight& s = ahead.s;
+            const bool sh = is_shared(ahead.e);
             const int su = s.sink_units();
             const int key0 = ahead.k < su ? ahead.k * kUnit : s.first + (ahead.k - su) * kUnit;
             const int nk = ahead.k < su ? s.sinks - key0 : s.last + 1 - key0;       // keys of the unit, if fewer than kUnit
-            const int slot0 = slot_of(A, key0 < 0 ? 0 : key0);
-            const long long head = (long long)s.seq * A.kv_s + (long long)(ahead.h / A.row_tiles) * A.kv_h;
+            const int slot0 = sh ? key0 : slot_of(A, key0);
+            const int j = ahead.h / (sh ? P.shared.row_tiles : A.row_tiles);
+            const long long head = sh ? j * P.shared.kv_h : (long long)s.seq * A.kv_s + j * A.kv_h, step = sh ? P.shared.kv_p : A.kv_p;
+            const __nv_bfloat16 *const K = (sh ? P.shared.K : A.K) + head, *const V = (sh ? P.shared.V : A.V) + head;
             const uint32_t kd = ring0 + (uint32_t)(buf * G::UNIT), vd = kd + (uint32_t)(kUnit * STRIDE);
 #pragma unroll
             for (int i = 0; i < CH * kUnit / 32; ++i) {
                 const int idx = lane + 32 * i, row = idx / CH, ch = idx % CH;
                 int slot = slot0 + (row < nk ? row : 0);
-                // in a unit across the end of the sinks, or of the ring, the slots are not neighbours
-                if (A.ring && slot >= A.L) slot -= A.ring;
-                const long long src = head + (long long)slot * A.kv_p + ch * 8;
+                if (A.ring && !sh && slot >= A.L) slot -= A.ring;      // in a unit across the end of the ring the slots are not neighbours
+                const long long src = slot * step + ch * 8;
                 const uint32_t nbytes = row < nk ? 16u : 0u, dst = (uint32_t)(row * STRIDE + ch * 16);      // past the last key: zeros
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kd + dst), "l"(A.K + src), "r"(nbytes) : "memory");
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd + dst), "l"(A.V + src), "r"(nbytes) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kd + dst), "l"(K + src), "r"(nbytes) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd + dst), "l"(V + src), "r"(nbytes) : "memory");
             }
             ahead.k += WARPS;
             settle(ahead);
@@ -196,21 +235,24 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     long long mine = u0 + warp;                         // this warp's next unit
     uint4 next_q[QN];                                   // a thread's pieces of the next pair's queries; rows that are none are zeros
     const auto ask_queries = [&](const Cursor& c) {
+        const bool sh = is_shared(c.e);
+        const int tiles = sh ? P.shared.row_tiles : A.row_tiles, t0 = sh ? 0 : token_of(c.e);
+        const long long all = sh ? (long long)A.T * A.group : A.group;
 #pragma unroll
         for (int i = 0; i < QN; ++i) {
-            const int idx = tid + i * THREADS, row = (c.h % A.row_tiles) * 16 + idx / CH;
+            const int idx = tid + i * THREADS, row = (c.h % tiles) * 16 + idx / CH;
             next_q[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (idx < 16 * CH && row < A.group * A.fold) {
-                const int t = c.t + row / A.group;
-                next_q[i] = *reinterpret_cast<const uint4*>(A.q + t * A.q_t + (c.h / A.row_tiles) * A.q_h + row % A.group * A.q_g + idx % CH * 8);
-            }
+            if (idx < 16 * CH && row < all)
+                next_q[i] = *reinterpret_cast<const uint4*>(A.q + (t0 + row / A.group) * A.q_t + (c.h / tiles) * A.q_h + row % A.group * A.q_g + idx % CH * 8);
         }
     };
     ask_queries(seg);
     for (long long at = u0; at < u1;) {
-        const int units = seg.units, t = seg.t, j = seg.h / A.row_tiles, row0 = seg.h % A.row_tiles * 16;
+        const bool sh = is_shared(seg.e);
+        const int tiles = sh ? P.shared.row_tiles : A.row_tiles, t = sh ? 0 : token_of(seg.e);
+        const int units = seg.units, j = seg.h / tiles, row0 = seg.h % tiles * 16;
         const long long end = min(u1, at + units - seg.k);
-        const int rows = min(16, A.group * A.fold - row0), first_k = seg.k;
+        const int rows = (int)min(16ll, (sh ? (long long)A.T * A.group : A.group) - row0), first_k = seg.k;
         const Sight& s = seg.s;
         const int su = s.sink_units();
 #pragma unroll
@@ -305,7 +347,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         next.k += (int)(end - at);
         settle(next);
         if (end < u1) ask_queries(next);
-        else chain_next();
+        else if (pass + 1 == P.passes) chain_next();
         // ---- the warps' triples of the pair, through the buffer that each has just finished (the next fetch would fill it)
         l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
         l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
@@ -327,15 +369,17 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
             if (rows > 8) *reinterpret_cast<float2*>(acc + (g + 8) * LDO + dt * 8 + q4 * 2) = make_float2(o[dt][2], o[dt][3]);
         }
         __syncthreads();
-        const bool whole = end - at == units, keep = P.keep_parts;
-        const long long pair = (long long)t * heads + seg.h;
+        const bool whole = end - at == units, begins = first_k == 0;
         // a pair that begins in this run leaves its first part in the run's second slot, one that began before in the first
-        const long long slot_at = whole ? 2ll * P.ctas + pair : 2ll * blockIdx.x + (first_k == 0 ? 1 : 0);
+        const long long slot_at = 2ll * ((long long)pass * P.ctas + blockIdx.x) + (begins ? 1 : 0);
         float* const slot = P.slots + slot_at * 16 * (DH + 2);
-        if (tid == 0 && first_k == 0) {
-            const long long through = run_of(base_s[t] + (long long)(seg.h + 1) * units - 1);
-            P.head[pair] = make_int2((int)slot_at, whole ? (keep ? 1 : 0) : (int)(through - blockIdx.x + 1));
+        if (tid == 0 && begins) {
+            const int parts = whole ? 0 : (int)(run_of(at + units - 1) - blockIdx.x + 1);
+            if (P.keep) P.head[sh ? seg.h : shared_heads + (long long)t * own_heads + seg.h] = make_int2((int)slot_at, parts);
+            else if (!whole) P.run_head[(long long)pass * P.ctas + blockIdx.x] = make_int2(t * own_heads + seg.h, parts);
         }
+        float* const row_o = sh ? P.shared_rows.o : P.own_rows.o;
+        float* const row_ml = sh ? P.shared_rows.ml : P.own_rows.ml;
         for (int idx = tid; idx < rows * (DH / 2); idx += THREADS) {
             const int row = idx / (DH / 2), col = idx % (DH / 2) * 2;
             float M = -INFINITY;
@@ -351,81 +395,130 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
                 ny = fmaf(wgt, v.y, ny);
                 den = fmaf(wgt, ls[w][row], den);
             }
-            if (whole && !keep) {
-                const float inv = den == 0.f ? 0.f : 1.f / den;           // no key: zeros
-                *reinterpret_cast<uint32_t*>(A.out + t * A.o_t + j * A.o_h + (row0 + row) * A.o_g + col) = pack2(nx * inv, ny * inv);
-                if (col == 0) write_sums(A, ((size_t)t * A.n_head + j) * A.group + row0 + row, z, den);
-            } else {
+            const int member = (row0 + row) % A.group, tok = t + (row0 + row) / A.group;
+            const long long r = row_at(A, tok, j, member);
+            if (!whole) {
                 *reinterpret_cast<float2*>(slot + row * DH + col) = make_float2(nx, ny);
                 if (col == 0) *reinterpret_cast<float2*>(slot + 16 * DH + row * 2) = make_float2(M, den);
+                // (the row's whole part: none)
+                if (col == 0 && P.keep && begins) *reinterpret_cast<float2*>(row_ml + r * 2) = make_float2(-INFINITY, 0.f);
+            } else if (P.keep) {
+                *reinterpret_cast<float2*>(row_o + r * DH + col) = make_float2(nx, ny);
+                if (col == 0) *reinterpret_cast<float2*>(row_ml + r * 2) = make_float2(M, den);
+            } else {
+                const float inv = den == 0.f ? 0.f : 1.f / den;           // no key: zeros
+                *reinterpret_cast<uint32_t*>(A.out + tok * A.o_t + j * A.o_h + member * A.o_g + col) = pack2(nx * inv, ny * inv);
+                if (col == 0) write_sums(A, r, z, den);
             }
         }
         __syncthreads();                                // the warps' triples are read before the next fetch overwrites them
         seg = next;
         at = end;
     }
+    ptx::cp_async_wait<0>();
+    }
 }
 
-// A pair's parts: where they are.  The first lies in its first run's second slot, the others in their runs' first ones (a whole one by itself)
-template <int DH>
-struct Parts {
-    const float* slots;
-    int2 head;
-    __device__ __forceinline__ const float* at(int i) const {
-        return slots + (size_t)(i == 0 ? head.x : (head.x & ~1) + 2 * i) * (16 * (DH + 2));
-    }
-    __device__ __forceinline__ float2 sums(int i, int row) const { return *reinterpret_cast<const float2*>(at(i) + 16 * DH + row * 2); }
-    __device__ __forceinline__ float2 values(int i, int row, int col) const { return *reinterpret_cast<const float2*>(at(i) + row * DH + col); }
-};
+// Adds up the parts of a pair's rows, in order: parts of whole rows, those of the shared keys, then those of the token's own.  A CTA per pair, or
+// (no `keep`) per run of the stream kernel's, for the pair that begins there and goes on.  First the weights of all parts, a warp per
+// row, then the sums, a thread per four columns, with sixteen loads under way.
+constexpr int kSumThreads = 256, kSumParts = 448;        // parts at most: whole rows' 2 x 64 + 1, and twice a part per SM
 
-// Adds up a pair's parts, in order: the 128-row kernel's, then those of the folded tokens, then the token's own.  A CTA per pair.
 template <int DH>
-__global__ void __launch_bounds__(128) attention_sum_kernel(const __grid_constant__ AttnView A, const __grid_constant__ PartPlan P,
-                                                            const __grid_constant__ PartPlan F, const int folded_tiles, const int token0,
-                                                            const __grid_constant__ TileParts M) {
+__global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid_constant__ AttnView A, const __grid_constant__ StreamPlan P,
+                                                                    const __grid_constant__ RowParts M) {
+    __shared__ float wgt_s[16][kSumParts];
+    __shared__ float inv_s[16];
     chain_wait();
     chain_next();
-    const int heads = A.n_head * A.row_tiles;
-    const long long pair = blockIdx.x;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int heads = A.n_head * A.row_tiles, shared_heads = A.n_head * P.shared.row_tiles;
+    long long pair = blockIdx.x;
+    int2 own = make_int2(0, 0);                          // first slot, number of parts
+    if (P.keep) {
+        own = P.own ? P.head[shared_heads + pair] : make_int2(0, 0);
+    } else {
+        const int2 h = P.run_head[blockIdx.x];
+        if (h.y == 0) return;
+        pair = h.x;
+        own = make_int2(2 * (int)blockIdx.x + 1, h.y);
+    }
     const int t = (int)(pair / heads), h = (int)(pair % heads), j = h / A.row_tiles, row0 = h % A.row_tiles * 16;
-    const Parts<DH> own{P.slots, P.slots ? P.head[pair] : make_int2(0, 0)};
-    if (own.head.y == 0 && M.n == 0 && !F.slots) return;
     const int rows = min(16, A.group - row0);
-    for (int idx = threadIdx.x; idx < rows * (DH / 2); idx += blockDim.x) {
-        const int row = idx / (DH / 2), col = idx % (DH / 2) * 2;
-        const long long at = ((long long)t * A.n_head + j) * A.group + row0 + row, folded = (long long)(token0 + t) * A.group + row0 + row;
-        const int frow = (int)(folded % 16);
-        const Parts<DH> shared{F.slots, F.slots ? F.head[j * folded_tiles + folded / 16] : make_int2(0, 0)};
-        float top = -INFINITY;
-        for (int i = 0; i < M.n; ++i) top = fmaxf(top, M.ml[(i * M.rows + at) * 2]);
-        for (int i = 0; i < shared.head.y; ++i) top = fmaxf(top, shared.sums(i, frow).x);
-        for (int i = 0; i < own.head.y; ++i) top = fmaxf(top, own.sums(i, row).x);
-        const float z = top == -INFINITY ? 0.f : top;
-        float nx = 0.f, ny = 0.f, den = 0.f;
-        const auto add = [&](const float2 ml, const float2 v) {
-            const float wgt = exp2_fast(ml.x - z);
-            const bool any = ml.x != -INFINITY;         // (a part without keys may hold anything else)
-            nx = fmaf(wgt, any ? v.x : 0.f, nx);
-            ny = fmaf(wgt, any ? v.y : 0.f, ny);
-            den = fmaf(wgt, ml.y, den);
-        };
-#pragma unroll 4
-        for (int i = 0; i < M.n; ++i) {
-            const size_t r = i * M.rows + at;
-            add(*reinterpret_cast<const float2*>(M.ml + r * 2), *reinterpret_cast<const float2*>(M.o + r * DH + col));
+    // the first part lies in its first run's second slot, the others in their runs' first ones
+    const auto slot = [&](int2 head, int i) { return P.slots + (size_t)(i == 0 ? head.x : (head.x & ~1) + 2 * i) * (16 * (DH + 2)); };
+    const auto shared_head = [&](int row) {
+        if (P.shared.P == 0 || !P.keep) return make_int2(0, 0);
+        return P.head[j * P.shared.row_tiles + ((long long)t * A.group + row0 + row) / 16];
+    };
+    // part i of a row: where its (m, l) and values are
+    struct Where {
+        const float *ml, *o;
+    };
+    const auto where = [&](int i, int row, int2 sh) {
+        const long long r = row_at(A, t, j, row0 + row);
+        if (i < M.n) return Where{M.ml + (i * M.rows + r) * 2, M.o + (i * M.rows + r) * DH};
+        i -= M.n;
+        const bool s = i < sh.y;
+        const int at = s ? (int)(((long long)t * A.group + row0 + row) % 16) : row;
+        const float* const p = s ? slot(sh, i) : slot(own, i - sh.y);
+        return Where{p + 16 * DH + at * 2, p + at * DH};
+    };
+    for (int row = warp; row < rows; row += kSumThreads / 32) {
+        const int2 sh = shared_head(row);
+        const int n = M.n + sh.y + own.y;
+        float top = -INFINITY, den = 0.f;
+        for (int i = lane; i < n; i += 32) {
+            const float m = *where(i, row, sh).ml;
+            wgt_s[row][i] = m;
+            top = fmaxf(top, m);
         }
-#pragma unroll 4
-        for (int i = 0; i < shared.head.y; ++i) add(shared.sums(i, frow), shared.values(i, frow, col));
-#pragma unroll 4
-        for (int i = 0; i < own.head.y; ++i) add(own.sums(i, row), own.values(i, row, col));
-        const float inv = den == 0.f ? 0.f : 1.f / den;
-        *reinterpret_cast<uint32_t*>(A.out + t * A.o_t + j * A.o_h + (row0 + row) * A.o_g + col) = pack2(nx * inv, ny * inv);
-        if (col == 0) write_sums(A, at, z, den);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float z = top == -INFINITY ? 0.f : top;
+        for (int i = lane; i < n; i += 32) {
+            const float w = exp2_fast(wgt_s[row][i] - z);
+            wgt_s[row][i] = w;
+            if (w != 0.f) den = fmaf(w, where(i, row, sh).ml[1], den);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+        if (lane == 0) {
+            inv_s[row] = den == 0.f ? 0.f : 1.f / den;
+            write_sums(A, row_at(A, t, j, row0 + row), z, den);
+        }
+    }
+    __syncthreads();
+    for (int idx = tid; idx < rows * (DH / 4); idx += kSumThreads) {
+        const int row = idx / (DH / 4), col = idx % (DH / 4) * 4;
+        const int2 sh = shared_head(row);
+        const int n = M.n + sh.y + own.y;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i0 = 0; i0 < n; i0 += 16) {
+            float4 v[16];
+            float w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                w[k] = i0 + k < n ? wgt_s[row][i0 + k] : 0.f;
+                // (a part of no weight is not looked at: it may hold anything)
+                v[k] = w[k] != 0.f ? *reinterpret_cast<const float4*>(where(i0 + k, row, sh).o + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                sum.x = fmaf(w[k], v[k].x, sum.x);
+                sum.y = fmaf(w[k], v[k].y, sum.y);
+                sum.z = fmaf(w[k], v[k].z, sum.z);
+                sum.w = fmaf(w[k], v[k].w, sum.w);
+            }
+        }
+        const float inv = inv_s[row];
+        *reinterpret_cast<uint2*>(A.out + t * A.o_t + j * A.o_h + (row0 + row) * A.o_g + col) =
+            make_uint2(pack2(sum.x * inv, sum.y * inv), pack2(sum.z * inv, sum.w * inv));
     }
 }
 
 template <int DH>
-dsmoe_status launch_stream(const AttnView& A, const PartPlan& parts, cudaStream_t s) {
+dsmoe_status launch_stream(const AttnView& A, const StreamPlan& plan, cudaStream_t s) {
     static bool attr[kMaxDeviceSlots] = {};
     int dev = 0;
     DeviceState* st = nullptr;
@@ -434,15 +527,14 @@ dsmoe_status launch_stream(const AttnView& A, const PartPlan& parts, cudaStream_
         DSMOE_CUDA_TRY(cudaFuncSetAttribute(attention_stream_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamGeo<DH>::SMEM));
         attr[dev] = true;
     }
-    DSMOE_CUDA_TRY(launch_chained(attention_stream_kernel<DH>, (unsigned)parts.ctas, 32 * StreamGeo<DH>::WARPS, StreamGeo<DH>::SMEM, s, A, parts));
+    DSMOE_CUDA_TRY(launch_chained(attention_stream_kernel<DH>, (unsigned)plan.ctas, 32 * StreamGeo<DH>::WARPS, StreamGeo<DH>::SMEM, s, A, plan));
     return DSMOE_OK;
 }
 
 template <int DH>
-dsmoe_status launch_sum(const AttnView& A, const PartPlan& parts, const PartPlan& folded, int folded_tiles, int token0, const TileParts& more,
-                        cudaStream_t s) {
-    const long long pairs = (long long)A.T * A.n_head * A.row_tiles;
-    DSMOE_CUDA_TRY(launch_chained(attention_sum_kernel<DH>, (unsigned)pairs, 128, 0, s, A, parts, folded, folded_tiles, token0, more));
+dsmoe_status launch_sum(const AttnView& A, const StreamPlan& plan, const RowParts& rows, cudaStream_t s) {
+    const long long ctas = plan.keep ? (long long)A.T * A.n_head * A.row_tiles : (long long)plan.passes * plan.ctas;
+    DSMOE_CUDA_TRY(launch_chained(attention_sum_kernel<DH>, (unsigned)ctas, kSumThreads, 0, s, A, plan, rows));
     return DSMOE_OK;
 }
 
@@ -462,23 +554,22 @@ dsmoe_status launch_sum(const AttnView& A, const PartPlan& parts, const PartPlan
     }
 
 // One CTA per SM, as far as each has a unit per warp in the longest case
-int stream_ctas(const AttnView& A) {
-    const long long seen = A.window < A.L ? (long long)A.window + A.sinks : A.L;
-    const long long units = (seen + kUnit - 1) / kUnit + 1, warps = A.d_head <= 128 ? 8 : 4;
-    const long long pairs = (long long)(A.T < kListTokens ? A.T : kListTokens) * A.n_head * A.row_tiles, most = sm_count();
-    const long long wanted = (pairs * units + warps - 1) / warps;
+int stream_ctas(const AttnView& A, const SharedKeys& shared, bool own) {
+    const long long seen = A.window < A.L ? (long long)A.window + A.sinks : A.L, warps = A.d_head <= 128 ? 8 : 4;
+    long long units = own ? ((seen + kUnit - 1) / kUnit + 1) * ((long long)A.T * A.n_head * A.row_tiles) : 0;
+    units += (long long)((shared.P + kUnit - 1) / kUnit) * A.n_head * shared.row_tiles;
+    const long long wanted = (units + warps - 1) / warps, most = sm_count() < 160 ? sm_count() : 160;      // (kSumParts)
     return (int)(wanted < most ? wanted : most);
 }
 
-dsmoe_status launch_stream_attention(const AttnView& A, const PartPlan& parts, cudaStream_t s) {
-#define DSMOE_CALL(DH) launch_stream<DH>(A, parts, s)
+dsmoe_status launch_stream_attention(const AttnView& A, const StreamPlan& plan, cudaStream_t s) {
+#define DSMOE_CALL(DH) launch_stream<DH>(A, plan, s)
     DSMOE_BY_HEAD(A.d_head, DSMOE_CALL)
 #undef DSMOE_CALL
 }
 
-dsmoe_status launch_attention_sum(const AttnView& A, const PartPlan& parts, const PartPlan& folded, int folded_tiles, int token0,
-                                  const TileParts& more, cudaStream_t s) {
-#define DSMOE_CALL(DH) launch_sum<DH>(A, parts, folded, folded_tiles, token0, more, s)
+dsmoe_status launch_attention_sum(const AttnView& A, const StreamPlan& plan, const RowParts& rows, cudaStream_t s) {
+#define DSMOE_CALL(DH) launch_sum<DH>(A, plan, rows, s)
     DSMOE_BY_HEAD(A.d_head, DSMOE_CALL)
 #undef DSMOE_CALL
 }

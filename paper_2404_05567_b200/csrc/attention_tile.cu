@@ -9,7 +9,8 @@
 // and 8-11 are the two tiles' rows.  While one tile's threads are at their weights the tensor pipe works for the other one.
 //
 // What a CTA's tokens see: tokens of one sequence that follow one another are a run; a run's keys are at most three stretches of slots (sinks, and
-// the window, cut in two where a ring ends).  Runs too short to fill a tile are left to attention_stream_kernel.
+// the window, cut in two where a ring ends).  In blocks of many runs, those too short to be worth a
+// pass of a tile's over their keys are left to attention_stream_kernel.
 // A value that is not finite reaches all rows of a tile, also those that do not see it: rows that come out as no numbers are done again, one by one.
 #include "cache_attention.cuh"
 #include "tensor_maps.cuh"
@@ -19,7 +20,8 @@ namespace dsmoe {
 
 namespace {
 
-constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 384, kMaxRuns = 16, kMaxStretches = 3 * kMaxRuns;
+// A block of up to kFewRuns runs (prompts' ends and beginnings) is taken as it is: each costs a pass over its keys
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 384, kFewRuns = 4, kMaxRuns = 16, kMaxStretches = 3 * kMaxRuns;
 
 template <int DH>
 struct TileGeo {
@@ -111,6 +113,8 @@ struct TileArgs {
     int blocks, splits;
     int at_pos, at_head, at_seq;          // which of the tensor map's dimensions 1 .. 3 are positions, heads, sequences
     float *o, *ml;                        // parts [split][T * n_head * group][DH], [..][2]; nullptr: out and lse are written
+    int32_t *count, *list;                // the tokens that are left: block b's count[b], from list[b * span] on; nullptr: none is
+    int2* head;                           // the stream kernel's, nullable
 };
 
 // Key tile i: the stretch that holds it (the caller's `at` only grows), its first key there
@@ -196,6 +200,19 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         }
     }
     __syncthreads();
+    if (split == 0 && P.head && tid < ng)
+        for (int i = 0; i < A.row_tiles; ++i) P.head[((long long)(tg0 + tid) * A.n_head + j) * A.row_tiles + i] = make_int2(0, 0);
+    if (warp == 1 && split == 0 && j == 0 && P.count) {        // the tokens that are left, in order
+        int n = 0;
+        for (int c = 0; c < ng; c += 32) {
+            const int t = c + lane;
+            const bool left = t < ng && S.n_runs > kFewRuns && S.run_len[S.run[t]] < P.least_run;
+            const uint32_t votes = __ballot_sync(0xffffffffu, left);
+            if (left) P.list[(long long)block * span + n + __popc(votes & ((1u << lane) - 1u))] = tg0 + t;
+            n += __popc(votes);
+        }
+        if (lane == 0) P.count[block] = n;
+    }
     if (tid == 0) {
         int n = 0, tiles = 0, t = 0;
         const auto put = [&](int run, int seq, int pos0, int count) {
@@ -210,7 +227,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         };
         for (int r = 0; r < S.n_runs; ++r) {
             const int len = S.run_len[r], lo = S.run_lo[r], hi = S.run_hi[r];
-            const bool mine = S.n_runs == 1 || len >= P.least_run;
+            const bool mine = !P.count || S.n_runs <= kFewRuns || len >= P.least_run;
             if (mine && hi >= 0 && n + 3 <= kMaxStretches) {
                 const int sinks = min(A.sinks, hi + 1);
                 if (lo <= sinks) {
@@ -344,7 +361,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         const bool real = at < P.tile_tokens * A.group && tl < ng;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + r * 128, tO = tmem + lanes + 256 + r * 128;
-        const bool taken = real && (S.n_runs == 1 || S.run_len[S.run[tl]] >= P.least_run);
+        const bool taken = real && (!P.count || S.n_runs <= kFewRuns || S.run_len[S.run[tl]] >= P.least_run);
         const int run = taken ? S.run[tl] : -1, last = taken ? S.last[tl] : -1, first = taken ? S.first[tl] : 0;
         const float sl2 = A.scale_log2;
         float m = -INFINITY, l = 0.f;
@@ -625,7 +642,8 @@ dsmoe_status launch_tile(const AttnView& A, const TilePlan& plan, cudaStream_t s
     int at[3];
     DSMOE_TRY(make_cache_map(&mapK, A, A.K, at));
     DSMOE_TRY(make_cache_map(&mapV, A, A.V, at));
-    TileArgs P{A, kTileRows / A.group, tile_least_run(A.group), tile_blocks(A.T, A.group), plan.splits, at[0], at[1], at[2], plan.o, plan.ml};
+    TileArgs P{A, kTileRows / A.group, tile_least_run(A.group), tile_blocks(A.T, A.group), plan.splits, at[0], at[1], at[2], plan.o, plan.ml,
+               plan.count, plan.list, plan.head};
     const long long ctas = (long long)P.blocks * A.n_head * plan.splits;
     if (ctas > 0x7fffffffll) return DSMOE_ERR_UNSUPPORTED;
     DSMOE_CUDA_TRY(launch_chained(attention_tile_kernel<DH>, (unsigned)ctas, kTileThreads, G::SMEM, s, mapK, mapV, P));

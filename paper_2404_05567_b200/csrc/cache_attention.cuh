@@ -13,9 +13,7 @@ namespace dsmoe {
 
 struct AttnView {
     int T, n_head, group;
-    // Tokens that see the same keys (a shared prefix) can be taken as one: row r of head j is then member r % group of token r / group, and T is 1
-    int fold;                             // tokens taken as one (1: none)
-    int row_tiles;                        // 16-row tiles of the fold * group rows of a (token, head)
+    int row_tiles;                        // 16-row tiles of the group rows of a (token, head)
     int d_head, n_seq, L;
     int window, sinks, ring;              // ring: slots of the rolling part, 0 if position l lies in slot l
     float scale_log2;
@@ -29,13 +27,10 @@ struct AttnView {
     float* lse;                           // nullable
     float2* ml;                           // nullable: (largest logit, 1 / sum) of every row, [T][n_head][group]
     int32_t* dev_status;
-    // The stream kernel beside the 128-row kernel: it attends the tokens that the latter leaves alone.  The call has all_T tokens, of which these
-    // begin at token0 (all_T 0: it attends all tokens).
-    int token0, all_T;
 };
 
 constexpr int kUnit = 16;                 // keys that a warp takes at a time
-constexpr int kListTokens = 1024;         // tokens whose keys one launch cuts into runs
+constexpr int kListTokens = 1024;         // tokens whose keys are cut into runs at a time
 
 // The keys that a token sees: 0 .. sinks - 1 and first .. last (nothing: last < first and sinks == 0).
 struct Sight {
@@ -69,56 +64,66 @@ __device__ __forceinline__ Sight sight_of(const AttnView& A, int t, bool* bad) {
     return s;
 }
 // The 128-row kernel's blocks of tokens: two tiles of as many tokens as have their rows in 128.  Tokens of one sequence that follow one another
-// there are a run; runs that fill less than a quarter of a tile, unless the block is one, are left to the stream kernel.
+// there are a run; in a block of many runs, those that fill less than a quarter of a tile are left to the stream kernel.
 __host__ __device__ static inline int tile_span(int group) { return 2 * (128 / group); }
 __host__ __device__ static inline int tile_least_run(int group) { return (32 + group - 1) / group; }
 __host__ __device__ static inline int tile_blocks(int T, int group) { return (T + tile_span(group) - 1) / tile_span(group); }
-__device__ __forceinline__ int seq_of_token(const AttnView& A, int t) { return A.tok_seq ? min(max(A.tok_seq[t], 0), A.n_seq - 1) : 0; }
-// Whether the stream kernel attends token t (numbered from A.token0)
-__device__ __forceinline__ bool is_streams(const AttnView& A, int t) {
-    if (A.all_T == 0) return true;
-    const int span = tile_span(A.group), least = tile_least_run(A.group), at = A.token0 + t;
-    const int b0 = at / span * span, b1 = min(A.all_T, b0 + span), seq = seq_of_token(A, t);
-    int lo = at, hi = at + 1;
-    while (lo > b0 && hi - lo < least && seq_of_token(A, lo - 1 - A.token0) == seq) --lo;
-    while (hi < b1 && hi - lo < least && seq_of_token(A, hi - A.token0) == seq) ++hi;
-    return hi - lo < least && (lo > b0 || hi < b1);
-}
 // The slot of the cache that holds position l
 __device__ __forceinline__ int slot_of(const AttnView& A, int l) { return !A.ring || l < A.sinks ? l : A.sinks + (l - A.sinks) % A.ring; }
 
-// Where the parts of a launch lie in the workspace.  Rows of 16 to a (token, head, row tile) = pair.
-struct PartPlan {
-    float* slots;                         // [2 * ctas (+ pairs, keep_parts)][16][d_head + 2]
-    int2* head;                           // [pairs]: first slot, number of parts; 0 parts: the row is written
-    int ctas;                             // CTAs that the slots have room for
-    bool keep_parts;                      // whole pairs leave a part too (something else is still to be added)
-};
-static inline size_t part_bytes(int d_head) { return (size_t)16 * (d_head + 2) * 4; }
+// Row (token t, head j, member m) of the calls' row arrays: lse, ml, whole rows' parts
+__host__ __device__ static inline long long row_at(const AttnView& A, int t, int j, int m) { return ((long long)t * A.n_head + j) * A.group + m; }
 
-// Parts of whole rows from the 128-row kernel: n of them, [n][rows][d_head] and [n][rows][2], a row for each token, head and member
-struct TileParts {
+// Parts of whole rows: n of them, [n][rows][d_head] and [n][rows][2] (m, l), a row for each token, head and member
+struct RowParts {
     int n;
     size_t rows;
-    const float* o;
-    const float* ml;
+    float *o, *ml;
 };
+
+// The keys that all tokens of a call share: they are taken as one token, whose rows are all tokens' members
+struct SharedKeys {
+    int P;                                // 0: none
+    int row_tiles;                        // 16-row tiles of the T * group rows of a head
+    const __nv_bfloat16 *K, *V;
+    long long kv_h, kv_p;
+};
+
+// What launch_stream_attention does: attends all tokens (list nullptr), or those that the 128-row kernel left: count[b] of block b's, list[b * span + i];
+// and, `shared`, the shared keys.  Rows of 16 to a (token, head, row tile) = pair; the shared keys' pairs come first.
+struct StreamPlan {
+    SharedKeys shared;
+    const int32_t *count, *list;
+    int blocks, span;
+    int ctas, passes;                     // passes of kListTokens tokens at most
+    bool own;                             // attends tokens at all
+    // A pair that several CTAs share leaves a part per CTA; one that lies in one CTA's keys is written to out and lse, or (keep) its rows to `own_rows`
+    // and `shared_rows`: something else is still to be added
+    bool keep;
+    float* slots;                         // [passes][2 * ctas][16][d_head + 2]
+    int2* head;                           // keep: [pairs]: first slot, number of parts
+    int2* run_head;                       // otherwise: [passes][ctas]: the pair that begins in that run and goes on, number of parts; or 0 parts
+    RowParts own_rows, shared_rows;       // n = 1
+};
+static inline size_t part_bytes(int d_head) { return (size_t)16 * (d_head + 2) * 4; }
 
 // The 128-row kernel: heads of 64, 96 and 128, caches that a tensor map describes.  Its rows' keys are cut into `splits`; o, ml: where their parts
 // go (TileParts), or nullptr with one split: out and lse are written.
 struct TilePlan {
     int splits;
     float *o, *ml;
+    // own caches of several sequences: the tokens that it leaves are listed here (see StreamPlan), all heads' parts marked as none (or nullptr)
+    int32_t *count, *list;
+    int2* head;
 };
 bool tile_supported(const AttnView& A);
 dsmoe_status launch_tile_attention(const AttnView& A, const TilePlan& plan, cudaStream_t s);
 
-int stream_ctas(const AttnView& A);       // CTAs of launch_stream_attention at most
-dsmoe_status launch_stream_attention(const AttnView& A, const PartPlan& parts, cudaStream_t s);
-// Adds up, into out and lse, what launch_stream_attention left of these tokens in `parts`; of all tokens folded into one in `folded` (slots
-// nullptr: none), the first of these tokens being number `token0` there; and `more`
-dsmoe_status launch_attention_sum(const AttnView& A, const PartPlan& parts, const PartPlan& folded, int folded_tiles, int token0,
-                                  const TileParts& more, cudaStream_t s);
+int stream_ctas(const AttnView& A, const SharedKeys& shared, bool own);       // CTAs of launch_stream_attention at most
+dsmoe_status launch_stream_attention(const AttnView& A, const StreamPlan& plan, cudaStream_t s);
+// Adds up what launch_stream_attention left in parts, into out and lse: without `keep` the pairs that several CTAs share; with it all rows, whose
+// parts `rows` are there too
+dsmoe_status launch_attention_sum(const AttnView& A, const StreamPlan& plan, const RowParts& rows, cudaStream_t s);
 
 // tally_out[s][j][l] = tally_in[s][j][l] (nullptr: 0) + the sum of the softmax weights that the tokens of sequence s gave key l, from A.ml.
 // Causal alone: no window, no ring.
