@@ -1,17 +1,20 @@
 // Eviction from a key/value cache by accumulated attention weight (dsmoe_cache_evict).
 //
 // Of the n keys of a (sequence, head) that holds more than `keep`, the first `sinks`, the last `recent` and those of the others with the
-// largest tally stay, in their order.  evict_select_kernel finds the smallest tally that stays by its bits, eight at a time (a histogram
-// of the candidates that share the bits found so far, then the bin in which the wanted rank falls), and how many of the candidates with exactly
-// that tally stay (the first ones); a last pass in order of the keys writes the indices and the tallies that stay.  evict_move_kernel
-// closes up the rows.
+// largest tally stay, in their order.  A CTA per (sequence, head) finds the smallest tally that stays, and how many of the candidates with exactly
+// that tally do (the first ones); a pass in order of the keys writes the indices and the tallies that stay.  evict_move_kernel closes up the rows.
+//
+// The bound is found by the bits of numbers in the tallies' order, eight at a time: a histogram of the candidates that share the bits found so
+// far, then the bin in which the wanted rank falls, until all of a bin stay.  evict_select_kernel (up to 32768 positions) reads the tallies once
+// and has them in registers; evict_select_long_kernel reads them again for every eight bits.
+// 14 caches of 5001 positions, us: a bit at a time by counting what reaches it, without a histogram, 18; two bits 20; so 14.
 #include "cache_attention.cuh"
 
 namespace dsmoe {
 
 namespace {
 
-constexpr int kSelThreads = 1024, kMoveThreads = 256, kMoveRows = 64;
+constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32, kMoveThreads = 256, kMovePieces = 8;
 
 // Tallies in the order of unsigned numbers: -0 and 0 are alike, what is no number comes before all others
 __device__ __forceinline__ uint32_t rank_bits(float v) {
@@ -20,7 +23,164 @@ __device__ __forceinline__ uint32_t rank_bits(float v) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+// Keys of sequence s, clamped into the cache
+__device__ __forceinline__ int length_of(const EvictView& E, int s) {
+    const int n = E.len[s];
+    if ((n < 0 || n > E.L) && threadIdx.x == 0) report_status(E.dev_status, DSMOE_ERR_INVALID_ARG);
+    return min(max(n, 0), E.L);
+}
+
+// a[0 .. n - 1] (n up to 1024): each becomes the sum of those before it; returns the sum of all
+__device__ __forceinline__ int scan_counts(int* a, int n, int* warp_s) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    __syncthreads();
+    const int x = tid < n ? a[tid] : 0;
+    int incl = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+    }
+    if (lane == 31) warp_s[warp] = incl;
+    __syncthreads();
+    const int w = warp_s[lane];
+    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0), all = __reduce_add_sync(0xffffffffu, w);
+    if (tid < n) a[tid] = before + incl - x;
+    __syncthreads();
+    return all;
+}
+
+// PER: tallies of a thread, tid, tid + 1024 ..
+template <int PER>
 __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_constant__ EvictView E) {
+    __shared__ int counts_s[PER * kSelWarps], scan_s[kSelWarps];
+    __shared__ __align__(16) int hist_s[4][256];         // of the bits from the top, eight at a time; the largest first
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    hist_s[tid >> 8][tid & 255] = 0;
+    chain_wait();
+    const long long pair = blockIdx.x;
+    const int n = length_of(E, (int)(pair / E.n_head));
+    const float* const tally = E.tally + pair * E.L;
+    const bool all = n <= E.keep;
+    const int a = E.sinks, b = n - E.recent;            // candidates: a .. b - 1 (where not all stay)
+    const int want = E.keep - E.sinks - E.recent;       // of the candidates
+    uint32_t bound = 0u;
+    int ties = 0;                                       // candidates with exactly the bound that stay
+    uint32_t stays = 0u;                                // bit i: tally tid + 1024 i
+    __syncthreads();
+    if (all) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) stays |= (uint32_t)(i * kSelThreads + tid < n) << i;
+    } else {
+        uint32_t u[PER];                                // 0: no candidate (or a tally that is no number)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int k = i * kSelThreads + tid;
+            u[i] = k >= a && k < b ? rank_bits(tally[k]) : 0u;
+        }
+        bool tied = true;                               // more have exactly the bound than stay
+        if (want > 0) {
+            int left = want;                            // to find among those that share the bits found so far
+#pragma unroll 1
+            for (int pass = 0; pass < 4 && tied; ++pass) {
+                const int shift = 24 - 8 * pass;
+                int* const hist = hist_s[pass];
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int k = i * kSelThreads + tid;
+                    if (k >= a && k < b && (pass == 0 || (u[i] ^ bound) >> (shift + 8) == 0u)) atomicAdd(hist + (255u - ((u[i] >> shift) & 255u)), 1);
+                }
+                __syncthreads();
+                // the bin in which the left-th largest lies: a lane looks at eight, every warp for itself
+                const int4 x = *reinterpret_cast<const int4*>(hist + 8 * lane), y = *reinterpret_cast<const int4*>(hist + 8 * lane + 4);
+                const int mine[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                int incl = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) incl += mine[i];
+                const int sum = incl;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int up = __shfl_up_sync(0xffffffffu, incl, o);
+                    if (lane >= o) incl += up;
+                }
+                const int holder = __ffs(__ballot_sync(0xffffffffu, incl >= left)) - 1;
+                int before = incl - sum, bin = 0, rest = 0, count = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (before < left && left <= before + mine[i]) {
+                        bin = 255 - 8 * lane - i;
+                        rest = left - before;
+                        count = mine[i];
+                    }
+                    before += mine[i];
+                }
+                bound |= (uint32_t)__shfl_sync(0xffffffffu, bin, holder) << shift;
+                left = __shfl_sync(0xffffffffu, rest, holder);
+                tied = __shfl_sync(0xffffffffu, count, holder) != left;       // otherwise all that share these bits stay
+            }
+            ties = left;
+        } else {
+            bound = 0xffffffffu;
+        }
+        uint32_t tie = 0u;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int k = i * kSelThreads + tid;
+            const bool middle = k >= a && k < b;
+            const bool is_tie = middle && tied && u[i] == bound;
+            tie |= (uint32_t)is_tie << i;
+            stays |= (uint32_t)(k < n && (!middle || (tied ? u[i] > bound : u[i] >= bound))) << i;
+        }
+        if (tied && ties > 0) {                         // (the same for the whole CTA) the first of them
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t votes = __ballot_sync(0xffffffffu, (tie >> i) & 1u);
+                if (lane == 0) counts_s[i * kSelWarps + warp] = __popc(votes);
+            }
+            scan_counts(counts_s, PER * kSelWarps, scan_s);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t votes = __ballot_sync(0xffffffffu, (tie >> i) & 1u);
+                const int rank = counts_s[i * kSelWarps + warp] + __popc(votes & ((1u << lane) - 1u));
+                if (((tie >> i) & 1u) && rank < ties) stays |= 1u << i;
+            }
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const uint32_t votes = __ballot_sync(0xffffffffu, (stays >> i) & 1u);
+        if (lane == 0) counts_s[i * kSelWarps + warp] = __popc(votes);
+    }
+    const int n_kept = scan_counts(counts_s, PER * kSelWarps, scan_s);
+    chain_next();
+    int32_t* const kept = E.kept + pair * E.keep;
+    float* const to = E.tally_out + pair * E.tally_pitch;
+    const bool in_place = E.tally_out == E.tally;
+    constexpr int BATCH = PER < 8 ? PER : 8;
+#pragma unroll
+    for (int i0 = 0; i0 < PER; i0 += BATCH) {
+        float v[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) v[i] = (stays >> (i0 + i)) & 1u ? tally[(i0 + i) * kSelThreads + tid] : 0.f;
+        // (in place a tally moves to where one of this batch or an earlier one was: all of it is read)
+        if (in_place) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const bool stay = (stays >> (i0 + i)) & 1u;
+            const uint32_t votes = __ballot_sync(0xffffffffu, stay);
+            if (stay) {
+                const int at = counts_s[(i0 + i) * kSelWarps + warp] + __popc(votes & ((1u << lane) - 1u));
+                kept[at] = (i0 + i) * kSelThreads + tid;
+                to[at] = v[i];
+            }
+        }
+    }
+    for (int i = n_kept + tid; i < E.keep; i += kSelThreads) kept[i] = -1;
+    if (tid == 0) E.count[pair] = n_kept;
+}
+
+__global__ void __launch_bounds__(kSelThreads) evict_select_long_kernel(const __grid_constant__ EvictView E) {
     __shared__ int hist[256];
     __shared__ uint32_t prefix_s;
     __shared__ int want_s;
@@ -29,11 +189,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long pair = blockIdx.x;
     const int s = (int)(pair / E.n_head);
-    int n = E.len[s];
-    if (n < 0 || n > E.L) {
-        if (tid == 0) report_status(E.dev_status, DSMOE_ERR_INVALID_ARG);
-        n = min(max(n, 0), E.L);
-    }
+    const int n = length_of(E, s);
     const float* const tally = E.tally + pair * E.L;
     const bool all = n <= E.keep;
     const int a = E.sinks, b = n - E.recent;            // candidates: a .. b - 1 (where not all stay)
@@ -126,10 +282,11 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
 
 // A CTA per (sequence, head), keys or values, and stretch of rows.  A row moves towards the front of its cache, to a place that no later row comes
 // from: where source and destination are one buffer, one CTA takes all rows in order, and a batch is read before any of it is written.
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictView E, const int stretches) {
+// Otherwise a CTA takes one batch.
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const __grid_constant__ EvictView E, const int stretches) {
     chain_wait();
     chain_next();
-    const int tid = threadIdx.x, CH = E.d_head / 8;
+    const unsigned tid = threadIdx.x, CH = (unsigned)E.d_head / 8;
     const int stretch = (int)(blockIdx.x % stretches), which = (int)(blockIdx.x / stretches) & 1;
     const long long pair = blockIdx.x / stretches / 2;
     const int s = (int)(pair / E.n_head), j = (int)(pair % E.n_head);
@@ -138,41 +295,44 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
     const __nv_bfloat16* const from = (which ? E.V : E.K) + s * E.kv_s + j * E.kv_h;
     __nv_bfloat16* const to = (which ? E.V_out : E.K_out) + s * E.o_s + j * E.o_h;
     const int32_t* const kept = E.kept + pair * E.keep;
-    const int per = (count + stretches - 1) / stretches, r0 = stretch * per, r1 = min(count, r0 + per);
-    constexpr int PER = 8;
-    const long long pieces = (long long)(r1 - r0) * CH;
-    for (long long p0 = 0; p0 < pieces; p0 += PER * kMoveThreads) {
-        uint4 v[PER];
-        int row[PER];
+    constexpr unsigned BATCH = kMovePieces * kMoveThreads;
+    const unsigned per = E.in_place ? (unsigned)count : BATCH / CH, r0 = stretch * per;
+    if (r0 >= (unsigned)count) return;
+    const unsigned long long pieces = (unsigned long long)(min((unsigned)count, r0 + per) - r0) * CH;
+    for (unsigned long long p0 = 0; p0 < pieces; p0 += BATCH) {
+        uint4 v[kMovePieces];
+        const unsigned n = (unsigned)min((unsigned long long)BATCH, pieces - p0), row0 = (unsigned)(p0 / CH), ch0 = (unsigned)(p0 % CH);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const long long p = p0 + i * kMoveThreads + tid;
-            row[i] = -1;
-            if (p < pieces) {
-                row[i] = r0 + (int)(p / CH);
-                v[i] = *reinterpret_cast<const uint4*>(from + kept[row[i]] * E.kv_p + (p % CH) * 8);
-            }
+        for (int i = 0; i < kMovePieces; ++i) {
+            const unsigned p = i * kMoveThreads + tid, at = ch0 + p;
+            if (p < n) v[i] = *reinterpret_cast<const uint4*>(from + kept[r0 + row0 + at / CH] * E.kv_p + at % CH * 8);
         }
         if (E.in_place) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const long long p = p0 + i * kMoveThreads + tid;
-            if (row[i] >= 0) *reinterpret_cast<uint4*>(to + row[i] * E.o_p + (p % CH) * 8) = v[i];
+        for (int i = 0; i < kMovePieces; ++i) {
+            const unsigned p = i * kMoveThreads + tid, at = ch0 + p;
+            if (p < n) *reinterpret_cast<uint4*>(to + (r0 + row0 + at / CH) * E.o_p + at % CH * 8) = v[i];
         }
     }
+}
+
+template <int PER>
+cudaError_t launch_select(const EvictView& E, unsigned pairs, cudaStream_t s) {
+    return launch_chained(evict_select_kernel<PER>, pairs, kSelThreads, 0, s, E);
 }
 
 }  // namespace
 
 dsmoe_status launch_evict(const EvictView& E, cudaStream_t s) {
     const long long pairs = (long long)E.n_seq * E.n_head;
-    int stretches = 1;
-    if (!E.in_place) {
-        const long long wanted = 4ll * sm_count() / (2 * pairs) + 1, most = (E.keep + kMoveRows - 1) / kMoveRows;
-        stretches = (int)(wanted < most ? wanted : most);
-    }
+    const int rows = kMovePieces * kMoveThreads / (E.d_head / 8), stretches = E.in_place ? 1 : ceil_div(E.keep, rows);
     if (pairs * 2 * stretches > 0x7fffffffll) return DSMOE_ERR_UNSUPPORTED;
-    DSMOE_CUDA_TRY(launch_chained(evict_select_kernel, (unsigned)pairs, kSelThreads, 0, s, E));
+    const unsigned n = (unsigned)pairs;
+    if (E.L <= 2 * kSelThreads) DSMOE_CUDA_TRY(launch_select<2>(E, n, s));
+    else if (E.L <= 8 * kSelThreads) DSMOE_CUDA_TRY(launch_select<8>(E, n, s));
+    else if (E.L <= 16 * kSelThreads) DSMOE_CUDA_TRY(launch_select<16>(E, n, s));
+    else if (E.L <= 32 * kSelThreads) DSMOE_CUDA_TRY(launch_select<32>(E, n, s));
+    else DSMOE_CUDA_TRY(launch_chained(evict_select_long_kernel, n, kSelThreads, 0, s, E));
     DSMOE_CUDA_TRY(launch_chained(evict_move_kernel, (unsigned)(pairs * 2 * stretches), kMoveThreads, 0, s, E, stretches));
     return DSMOE_OK;
 }

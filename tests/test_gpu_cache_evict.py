@@ -71,6 +71,13 @@ def test_what_stays(how, kind, L, keep, sinks, recent):
 
 
 @pytest.mark.parametrize("how", ["apart", "in place"])
+@pytest.mark.parametrize("kind", ["spread", "ties", "equal", "anything"])
+@pytest.mark.parametrize("L", [2048, 2049, 8192, 8193, 16384, 16385, 32768, 32769])
+def test_lengths_at_which_the_kernel_changes(how, kind, L):
+    run(2, 1, L, 32, L // 3, 3, 500, [L, L - 7], kind, how, seed=L)
+
+
+@pytest.mark.parametrize("how", ["apart", "in place"])
 @pytest.mark.parametrize("d", [32, 64, 96, 128, 160, 192, 224, 256])
 def test_head_widths(how, d):
     run(2, 3, 700, d, 345, 2, 40, [700, 513], "spread", how, seed=d)
