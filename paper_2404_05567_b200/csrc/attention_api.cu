@@ -156,7 +156,7 @@ AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, b
     const size_t rows = (size_t)A.T * A.n_head * A.group, blocks = (size_t)tile_blocks(A.T, A.group);
     w.ctas = stream_ctas(A, S, true);
     w.passes = ceil_div(A.T, kListTokens);
-    w.slots = take((size_t)w.passes * 2 * w.ctas * part_bytes(A.d_head));
+    w.slots = take((size_t)w.passes * 2 * w.ctas * stream_heads_at_once(A) * part_bytes(A.d_head));
     w.run_head = take((size_t)w.passes * w.ctas * sizeof(int2));
     w.head = take((size_t)A.n_head * ((size_t)A.T * A.row_tiles + S.row_tiles) * sizeof(int2));
     if (wants_ml) w.ml = take(rows * sizeof(float2));
@@ -185,6 +185,7 @@ dsmoe_status attend(const AttnView& A, const SharedKeys& S, const AttnPlan& w, c
     };
     StreamPlan plan{};
     plan.passes = w.passes;
+    plan.heads_at_once = stream_heads_at_once(A);
     plan.slots = reinterpret_cast<float*>(ws + w.slots);
     plan.own = true;
     int2* const head = reinterpret_cast<int2*>(ws + w.head);

@@ -39,6 +39,10 @@ __device__ __forceinline__ float exp2_fast(float v) {
     return r;
 }
 
+// Where the part of pair p of a group of HB lies that run + i leaves: a run has room for the parts of the pairs that began before it and for those
+// of the pairs that begin in it
+__device__ __forceinline__ long long part_slot(long long run, int i, bool begins, int HB, int p) { return (2 * (run + i) + (begins ? 1 : 0)) * HB + p; }
+
 // Row `at`'s largest logit z (0 if it sees nothing) and sum, for whoever asks
 __device__ __forceinline__ void write_sums(const AttnView& A, size_t at, float z, float den) {
     if (A.lse) A.lse[at] = (z + log2f(den)) * 0.6931471805599453f;
@@ -56,20 +60,25 @@ struct StreamGeo {
     static_assert(BUFS >= 2 && 16 * (DH + 8) * 4 <= UNIT, "accumulators take a unit's place");
 };
 
-template <int DH>
+// HB: heads that a CTA takes at a time.  A unit of the list is 16 keys of HB neighbouring (head, row tile)s; warp w's is the (w % HB)-th, and of the
+// units it takes every (WARPS / HB)-th.  Heads that lie side by side in memory (a cache stored by position) are so read side by side: 62 tokens of
+// 4 heads that see 2052 keys, stored by position, 68 us with one head at a time, 60 with two, 62 with four; by head 53, 53, 60 (cold caches); with fewer
+// keys than warps, a pair's parts are more the more heads share a CTA: 4 tokens behind 1500 keys 15, 23, 34.
+template <int DH, int HB>
 __global__ void __launch_bounds__(32 * StreamGeo<DH>::WARPS, 1)
 attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constant__ StreamPlan P) {
     using G = StreamGeo<DH>;
     constexpr int STRIDE = G::STRIDE, KS = DH / 16, DT = DH / 8, CH = DH / 8, LDO = DH + 8, BUFS = G::BUFS, WARPS = G::WARPS;
-    constexpr int THREADS = 32 * WARPS, QN = (16 * CH + THREADS - 1) / THREADS, PER = kListTokens / THREADS;
+    constexpr int THREADS = 32 * WARPS, PER = kListTokens / THREADS, KW = WARPS / HB, QN = (HB * 16 * CH + THREADS - 1) / THREADS;
     extern __shared__ __align__(16) unsigned char as_smem[];
     __shared__ long long base_s[kListTokens + 2];       // units before entry e's: the shared keys (in the first pass), then tokens
     __shared__ int token_s[kListTokens];                // left tokens: their numbers
     __shared__ long long warp_sum_s[WARPS];
     __shared__ float ms[WARPS][16], ls[WARPS][16];
     __shared__ uint32_t at_s[WARPS];                    // where each warp's accumulators of the pair are
-    __shared__ __align__(16) unsigned char q_s[16 * STRIDE];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
+    const int hb = warp % HB, kw = warp / HB;
+    __shared__ __align__(16) unsigned char q_s[HB * 16 * STRIDE];
     const int own_heads = A.n_head * A.row_tiles, shared_heads = A.n_head * P.shared.row_tiles;
     chain_wait();
     if (P.run_head)
@@ -124,12 +133,12 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
             mine[i] = 0;
             if (e < n) {
                 bool bad = false;
-                mine[i] = (long long)sight_of(A, token_of(e + first), &bad).units() * own_heads;
+                mine[i] = (long long)sight_of(A, token_of(e + first), &bad).units() * (own_heads / HB);
                 if (bad && blockIdx.x == 0) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
             }
             sum += mine[i];
         }
-        const long long shared_units = first ? (long long)((P.shared.P + kUnit - 1) / kUnit) * shared_heads : 0;
+        const long long shared_units = first ? (long long)((P.shared.P + kUnit - 1) / kUnit) * (shared_heads / HB) : 0;
         long long before = scan(sum, &total) + shared_units;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -145,7 +154,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     }
     // Equal runs; no CTA without a unit per warp, as far as there are so many
     const int entries = n + first;
-    const long long total = base_s[entries], wanted = (total + WARPS - 1) / WARPS;
+    const long long total = base_s[entries], wanted = (total + KW - 1) / KW;
     const int n_cta = (int)(wanted < (long long)gridDim.x ? wanted : (long long)gridDim.x);
     if ((int)blockIdx.x >= n_cta) continue;
     const long long share = total / n_cta, extra = total - share * n_cta;
@@ -156,7 +165,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     };
     const long long u0 = run_start(blockIdx.x), u1 = run_start(blockIdx.x + 1);
 
-    // Where a unit lies: entry, its (head, row tile), key block of it
+    // Where a unit lies: entry, its first (head, row tile), key block of it
     struct Cursor {
         int e, h, k, units;
         Sight s;
@@ -172,7 +181,8 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     const auto settle = [&](Cursor& c) {                // k past the pair's units: on to the pair that holds it
         while (c.e < entries && c.k >= c.units) {
             c.k -= c.units;
-            if (++c.h == (is_shared(c.e) ? shared_heads : own_heads)) {
+            c.h += HB;
+            if (c.h == (is_shared(c.e) ? shared_heads : own_heads)) {
                 c.h = 0;
                 ++c.e;
                 look(c);
@@ -190,13 +200,13 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         seg.e = lo;
         look(seg);
         const long long in = u0 - base_s[lo];
-        seg.h = (int)(in / seg.units);
-        seg.k = (int)(in - (long long)seg.h * seg.units);
+        seg.h = (int)(in / seg.units) * HB;
+        seg.k = (int)(in % seg.units);
     }
     Cursor ahead = seg;                                 // the next unit to fetch
-    ahead.k += warp;
+    ahead.k += kw;
     settle(ahead);
-    long long u_ahead = u0 + warp;
+    long long u_ahead = u0 + kw;
     unsigned char* const ring = as_smem + (size_t)warp * BUFS * G::UNIT;
     const uint32_t ring0 = ptx::smem_u32(ring);
     const auto fetch = [&](int buf) {
@@ -207,23 +217,40 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
             const int key0 = ahead.k < su ? ahead.k * kUnit : s.first + (ahead.k - su) * kUnit;
             const int nk = ahead.k < su ? s.sinks - key0 : s.last + 1 - key0;       // keys of the unit, if fewer than kUnit
             const int slot0 = sh ? key0 : slot_of(A, key0);
-            const int j = ahead.h / (sh ? P.shared.row_tiles : A.row_tiles);
+            const int j = (ahead.h + hb) / (sh ? P.shared.row_tiles : A.row_tiles);
             const long long head = sh ? j * P.shared.kv_h : (long long)s.seq * A.kv_s + j * A.kv_h, step = sh ? P.shared.kv_p : A.kv_p;
             const __nv_bfloat16 *const K = (sh ? P.shared.K : A.K) + head, *const V = (sh ? P.shared.V : A.V) + head;
             const uint32_t kd = ring0 + (uint32_t)(buf * G::UNIT), vd = kd + (uint32_t)(kUnit * STRIDE);
+            // a unit of neighbouring slots that is full: no piece needs a look at its row (with that for every piece the kernel issued half as
+            // many instructions again, and they, not the keys, were what it waited for)
+            const bool plain = (CH & (CH - 1)) == 0 && nk >= kUnit && (sh || !A.ring || slot0 + kUnit <= A.L);
+            if (plain) {
+                constexpr int LANES = CH < 32 ? CH : 32, ROWS = 32 / LANES;          // lanes of a row, rows at a time
+                const long long from = (slot0 + lane / LANES) * step + lane % LANES * 8, down = ROWS * step;
+                const __nv_bfloat16 *k = K + from, *v = V + from;
+                const uint32_t to = (uint32_t)(lane / LANES * STRIDE + lane % LANES * 16);
 #pragma unroll
-            for (int i = 0; i < CH * kUnit / 32; ++i) {
-                const int idx = lane + 32 * i, row = idx / CH, ch = idx % CH;
-                int slot = slot0 + (row < nk ? row : 0);
-                if (A.ring && !sh && slot >= A.L) slot -= A.ring;      // in a unit across the end of the ring the slots are not neighbours
-                const long long src = slot * step + ch * 8;
-                const uint32_t nbytes = row < nk ? 16u : 0u, dst = (uint32_t)(row * STRIDE + ch * 16);      // past the last key: zeros
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kd + dst), "l"(K + src), "r"(nbytes) : "memory");
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd + dst), "l"(V + src), "r"(nbytes) : "memory");
+                for (int i = 0; i < kUnit / ROWS; ++i) {
+                    ptx::cp_async16(kd + to + i * ROWS * STRIDE, k);
+                    ptx::cp_async16(vd + to + i * ROWS * STRIDE, v);
+                    k += down;
+                    v += down;
+                }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < CH * kUnit / 32; ++i) {
+                    const int idx = lane + 32 * i, row = idx / CH, ch = idx % CH;
+                    int slot = slot0 + (row < nk ? row : 0);
+                    if (A.ring && !sh && slot >= A.L) slot -= A.ring;  // in a unit across the end of the ring the slots are not neighbours
+                    const long long src = slot * step + ch * 8;
+                    const uint32_t nbytes = row < nk ? 16u : 0u, dst = (uint32_t)(row * STRIDE + ch * 16);      // past the last key: zeros
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kd + dst), "l"(K + src), "r"(nbytes) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd + dst), "l"(V + src), "r"(nbytes) : "memory");
+                }
             }
-            ahead.k += WARPS;
+            ahead.k += KW;
             settle(ahead);
-            u_ahead += WARPS;
+            u_ahead += KW;
         }
         ptx::cp_async_commit();
     };
@@ -232,58 +259,62 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     const uint32_t kfrag = (uint32_t)(((lane >> 4) * 8 + (lane & 7)) * STRIDE + ((lane >> 3) & 1) * 16);
     const uint32_t vfrag = (uint32_t)((((lane >> 3) & 1) * 8 + (lane & 7)) * STRIDE + (lane >> 4) * 16);
     int buf = 0;
-    long long mine = u0 + warp;                         // this warp's next unit
-    uint4 next_q[QN];                                   // a thread's pieces of the next pair's queries; rows that are none are zeros
+    long long mine = u0 + kw;                           // this warp's next unit
+    uint4 next_q[QN];                                   // a thread's pieces of the next pairs' queries; rows that are none are zeros
     const auto ask_queries = [&](const Cursor& c) {
         const bool sh = is_shared(c.e);
         const int tiles = sh ? P.shared.row_tiles : A.row_tiles, t0 = sh ? 0 : token_of(c.e);
         const long long all = sh ? (long long)A.T * A.group : A.group;
 #pragma unroll
         for (int i = 0; i < QN; ++i) {
-            const int idx = tid + i * THREADS, row = (c.h % tiles) * 16 + idx / CH;
+            const int idx = tid + i * THREADS, x = idx / CH, h = c.h + x / 16, row = h % tiles * 16 + x % 16;
             next_q[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (idx < 16 * CH && row < all)
-                next_q[i] = *reinterpret_cast<const uint4*>(A.q + (t0 + row / A.group) * A.q_t + (c.h / tiles) * A.q_h + row % A.group * A.q_g + idx % CH * 8);
+            if (idx < HB * 16 * CH && row < all)
+                next_q[i] = *reinterpret_cast<const uint4*>(A.q + (t0 + row / A.group) * A.q_t + h / tiles * A.q_h + row % A.group * A.q_g + idx % CH * 8);
         }
     };
     ask_queries(seg);
     for (long long at = u0; at < u1;) {
         const bool sh = is_shared(seg.e);
         const int tiles = sh ? P.shared.row_tiles : A.row_tiles, t = sh ? 0 : token_of(seg.e);
-        const int units = seg.units, j = seg.h / tiles, row0 = seg.h % tiles * 16;
-        const long long end = min(u1, at + units - seg.k);
-        const int rows = (int)min(16ll, (sh ? (long long)A.T * A.group : A.group) - row0), first_k = seg.k;
+        const int units = seg.units;
+        const long long end = min(u1, at + units - seg.k), all_rows = sh ? (long long)A.T * A.group : A.group;
+        const int first_k = seg.k;
         const Sight& s = seg.s;
         const int su = s.sink_units();
 #pragma unroll
         for (int i = 0; i < QN; ++i) {
             const int idx = tid + i * THREADS;
-            if (idx < 16 * CH) *reinterpret_cast<uint4*>(q_s + (idx / CH) * STRIDE + idx % CH * 16) = next_q[i];
+            if (idx < HB * 16 * CH) *reinterpret_cast<uint4*>(q_s + (idx / CH) * STRIDE + idx % CH * 16) = next_q[i];
         }
         __syncthreads();
-        const uint32_t qrow = ptx::smem_u32(q_s) + (uint32_t)((lane & 15) * STRIDE + (lane >> 4) * 16);
+        const uint32_t qrow = ptx::smem_u32(q_s) + (uint32_t)((hb * 16 + (lane & 15)) * STRIDE + (lane >> 4) * 16);
         uint32_t qf[KS][4];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) ldsm_x4(qf[ks], qrow + (uint32_t)(ks * 32));
+        // this warp's pair
+        const int j = (seg.h + hb) / tiles, row0 = (seg.h + hb) % tiles * 16, rows = (int)min(16ll, all_rows - row0);
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float o[DT][4];
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-        for (; mine < end; mine += WARPS) {
+        for (; mine < end; mine += KW) {
             __syncwarp();                               // every lane is past its reads of the buffer that is filled again now
             fetch((buf + BUFS - 1) % BUFS);
             ptx::cp_async_wait<BUFS - 1>();
             __syncwarp();
             const uint32_t kb = ring0 + (uint32_t)(buf * G::UNIT) + kfrag, vb = ring0 + (uint32_t)(buf * G::UNIT + kUnit * STRIDE) + vfrag;
-            float sc[2][4];
+            float sc[2][4], sd[2][4];                   // two chains each, even and odd steps of the reduction
 #pragma unroll
-            for (int i = 0; i < 2; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sc[i][c] = sd[i][c] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 uint32_t b[4];
                 ldsm_x4(b, kb + (uint32_t)(ks * 32));
-                mma_16816(sc[0], qf[ks], b[0], b[1]);
-                mma_16816(sc[1], qf[ks], b[2], b[3]);
+                mma_16816(ks & 1 ? sd[0] : sc[0], qf[ks], b[0], b[1]);
+                mma_16816(ks & 1 ? sd[1] : sc[1], qf[ks], b[2], b[3]);
             }
             // to base 2; what is no key is hidden
             const int k = first_k + (int)(mine - at);
@@ -292,18 +323,27 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const bool seen = i * 8 + c < nk;
-                    sc[i][c] = seen ? sc[i][c] * A.scale_log2 : -INFINITY;
-                    sc[i][2 + c] = seen ? sc[i][2 + c] * A.scale_log2 : -INFINITY;
-                    b0 = fmaxf(b0, sc[i][c]);
-                    b1 = fmaxf(b1, sc[i][2 + c]);
+                for (int c = 0; c < 4; ++c) {
+                    const bool seen = i * 8 + (c & 1) < nk;
+                    sc[i][c] = seen ? (sc[i][c] + sd[i][c]) * A.scale_log2 : -INFINITY;
+                    if (c < 2) b0 = fmaxf(b0, sc[i][c]);
+                    else b1 = fmaxf(b1, sc[i][c]);
                 }
-            b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 1));
-            b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 1));
-            b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 2));
-            b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 2));
-            if (__any_sync(0xffffffffu, b0 > m0 || b1 > m1)) {
+            if (P.logits && !sh) {
+                const int col = k * kUnit + q4 * 2;
+                float* const to = P.logits + row_at(A, t, j, row0) * P.logit_pitch + col;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (g < rows) *reinterpret_cast<float2*>(to + g * P.logit_pitch + i * 8) = make_float2(sc[i][0], sc[i][1]);
+                    if (g + 8 < rows) *reinterpret_cast<float2*>(to + (g + 8) * P.logit_pitch + i * 8) = make_float2(sc[i][2], sc[i][3]);
+                }
+            }
+            // the running maximum moves only when a logit passes it by more than 2^8: until then weights are at most 256, and nothing is rescaled
+            if (__any_sync(0xffffffffu, b0 > m0 + 8.f || b1 > m1 + 8.f || (m0 == -INFINITY && b0 > m0) || (m1 == -INFINITY && b1 > m1))) {
+                b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 1));
+                b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 1));
+                b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 2));
+                b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 2));
                 const float n0 = fmaxf(m0, b0), n1 = fmaxf(m1, b1);
                 const float c0 = n0 == -INFINITY ? 1.f : exp2_fast(m0 - n0), c1 = n1 == -INFINITY ? 1.f : exp2_fast(m1 - n1);
                 m0 = n0;
@@ -319,7 +359,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
                 }
             }
             const float z0 = m0 == -INFINITY ? 0.f : m0, z1 = m1 == -INFINITY ? 0.f : m1;
-            // the weights as two bf16 numbers each, the second the first's rounding error: the tensor pipe is idle anyway
+            // the weights as two bf16 numbers each, the second the first's rounding error: the tensor pipe has the time
             uint32_t pf[4], pr[4];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -346,7 +386,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         Cursor next = seg;
         next.k += (int)(end - at);
         settle(next);
-        if (end < u1) ask_queries(next);
+        if (end < u1) ask_queries(next);                // (on their way while the triples meet)
         else if (pass + 1 == P.passes) chain_next();
         // ---- the warps' triples of the pair, through the buffer that each has just finished (the next fetch would fill it)
         l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
@@ -370,34 +410,36 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         }
         __syncthreads();
         const bool whole = end - at == units, begins = first_k == 0;
-        // a pair that begins in this run leaves its first part in the run's second slot, one that began before in the first
-        const long long slot_at = 2ll * ((long long)pass * P.ctas + blockIdx.x) + (begins ? 1 : 0);
-        float* const slot = P.slots + slot_at * 16 * (DH + 2);
-        if (tid == 0 && begins) {
+        const long long run = (long long)pass * P.ctas + blockIdx.x;
+        if (tid < HB && begins) {
             const int parts = whole ? 0 : (int)(run_of(at + units - 1) - blockIdx.x + 1);
-            if (P.keep) P.head[sh ? seg.h : shared_heads + (long long)t * own_heads + seg.h] = make_int2((int)slot_at, parts);
-            else if (!whole) P.run_head[(long long)pass * P.ctas + blockIdx.x] = make_int2(t * own_heads + seg.h, parts);
+            if (P.keep) P.head[sh ? seg.h + tid : shared_heads + (long long)t * own_heads + seg.h + tid] = make_int2((int)run, parts);
+            else if (!whole && tid == 0) P.run_head[run] = make_int2(t * own_heads + seg.h, parts);
         }
         float* const row_o = sh ? P.shared_rows.o : P.own_rows.o;
         float* const row_ml = sh ? P.shared_rows.ml : P.own_rows.ml;
-        for (int idx = tid; idx < rows * (DH / 2); idx += THREADS) {
-            const int row = idx / (DH / 2), col = idx % (DH / 2) * 2;
+        // the group's pairs side by side, 16 rows each
+        for (int idx = tid; idx < HB * 16 * (DH / 2); idx += THREADS) {
+            const int x = idx / (DH / 2), col = idx % (DH / 2) * 2, p = x / 16, row = x % 16;
+            const int head = (seg.h + p) / tiles, first_row = (seg.h + p) % tiles * 16;
+            if (row >= all_rows - first_row) continue;
             float M = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) M = fmaxf(M, ms[w][row]);
+            for (int w = 0; w < KW; ++w) M = fmaxf(M, ms[w * HB + p][row]);
             const float z = M == -INFINITY ? 0.f : M;
             float nx = 0.f, ny = 0.f, den = 0.f;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                const float wgt = exp2_fast(ms[w][row] - z);              // 0 for a warp that saw no key
-                const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(as_smem + at_s[w]) + row * LDO + col);
+            for (int w = 0; w < KW; ++w) {
+                const float wgt = exp2_fast(ms[w * HB + p][row] - z);     // 0 for a warp that saw no key
+                const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(as_smem + at_s[w * HB + p]) + row * LDO + col);
                 nx = fmaf(wgt, v.x, nx);
                 ny = fmaf(wgt, v.y, ny);
-                den = fmaf(wgt, ls[w][row], den);
+                den = fmaf(wgt, ls[w * HB + p][row], den);
             }
-            const int member = (row0 + row) % A.group, tok = t + (row0 + row) / A.group;
-            const long long r = row_at(A, tok, j, member);
+            const int member = (first_row + row) % A.group, tok = t + (first_row + row) / A.group;
+            const long long r = row_at(A, tok, head, member);
             if (!whole) {
+                float* const slot = P.slots + part_slot(run, 0, begins, HB, p) * 16 * (DH + 2);
                 *reinterpret_cast<float2*>(slot + row * DH + col) = make_float2(nx, ny);
                 if (col == 0) *reinterpret_cast<float2*>(slot + 16 * DH + row * 2) = make_float2(M, den);
                 // (the row's whole part: none)
@@ -407,7 +449,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
                 if (col == 0) *reinterpret_cast<float2*>(row_ml + r * 2) = make_float2(M, den);
             } else {
                 const float inv = den == 0.f ? 0.f : 1.f / den;           // no key: zeros
-                *reinterpret_cast<uint32_t*>(A.out + tok * A.o_t + j * A.o_h + member * A.o_g + col) = pack2(nx * inv, ny * inv);
+                *reinterpret_cast<uint32_t*>(A.out + tok * A.o_t + head * A.o_h + member * A.o_g + col) = pack2(nx * inv, ny * inv);
                 if (col == 0) write_sums(A, r, z, den);
             }
         }
@@ -423,76 +465,82 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
 // (no `keep`) per run of the stream kernel's, for the pair that begins there and goes on.  First the weights of all parts, a warp per
 // row, then the sums, a thread per four columns, with sixteen loads under way.
 constexpr int kSumThreads = 256, kSumParts = 448;        // parts at most: whole rows' 2 x 64 + 1, and twice a part per SM
+constexpr int kSumRows = 8;                              // rows at a time
 
 template <int DH>
 __global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid_constant__ AttnView A, const __grid_constant__ StreamPlan P,
                                                                     const __grid_constant__ RowParts M) {
-    __shared__ float wgt_s[16][kSumParts];
-    __shared__ float inv_s[16];
+    __shared__ float wgt_s[kSumRows][kSumParts];
+    __shared__ uint32_t from_s[kSumRows][kSumParts];     // where a part's values begin, in float4s from the slots on (all parts lie behind those)
+    __shared__ float inv_s[kSumRows];
+    __shared__ int n_s[kSumRows];
     chain_wait();
     chain_next();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int heads = A.n_head * A.row_tiles, shared_heads = A.n_head * P.shared.row_tiles;
     long long pair = blockIdx.x;
-    int2 own = make_int2(0, 0);                          // first slot, number of parts
+    int2 own = make_int2(0, 0);                          // first run, number of parts
     if (P.keep) {
-        own = P.own ? P.head[shared_heads + pair] : make_int2(0, 0);
+        if (P.own) own = P.head[shared_heads + pair];
     } else {
-        const int2 h = P.run_head[blockIdx.x];
-        if (h.y == 0) return;
-        pair = h.x;
-        own = make_int2(2 * (int)blockIdx.x + 1, h.y);
+        const int run = (int)blockIdx.x / P.heads_at_once;
+        own = make_int2(run, P.run_head[run].y);
+        if (own.y == 0) return;
+        pair = P.run_head[run].x + (int)blockIdx.x % P.heads_at_once;
     }
     const int t = (int)(pair / heads), h = (int)(pair % heads), j = h / A.row_tiles, row0 = h % A.row_tiles * 16;
-    const int rows = min(16, A.group - row0);
-    // the first part lies in its first run's second slot, the others in their runs' first ones
-    const auto slot = [&](int2 head, int i) { return P.slots + (size_t)(i == 0 ? head.x : (head.x & ~1) + 2 * i) * (16 * (DH + 2)); };
-    const auto shared_head = [&](int row) {
-        if (P.shared.P == 0 || !P.keep) return make_int2(0, 0);
-        return P.head[j * P.shared.row_tiles + ((long long)t * A.group + row0 + row) / 16];
-    };
-    // part i of a row: where its (m, l) and values are
-    struct Where {
-        const float *ml, *o;
-    };
-    const auto where = [&](int i, int row, int2 sh) {
-        const long long r = row_at(A, t, j, row0 + row);
-        if (i < M.n) return Where{M.ml + (i * M.rows + r) * 2, M.o + (i * M.rows + r) * DH};
-        i -= M.n;
-        const bool s = i < sh.y;
-        const int at = s ? (int)(((long long)t * A.group + row0 + row) % 16) : row;
-        const float* const p = s ? slot(sh, i) : slot(own, i - sh.y);
-        return Where{p + 16 * DH + at * 2, p + at * DH};
-    };
+    constexpr long long SLOT = 16 * (DH + 2);
+    for (int c0 = row0; c0 < min(row0 + 16, A.group); c0 += kSumRows) {
+    const int rows = min(min(kSumRows, row0 + 16 - c0), A.group - c0);
+    __syncthreads();
     for (int row = warp; row < rows; row += kSumThreads / 32) {
-        const int2 sh = shared_head(row);
+        const long long r = row_at(A, t, j, c0 + row), folded = (long long)t * A.group + c0 + row;
+        int2 sh = make_int2(0, 0);
+        int sh_pair = 0;
+        if (P.keep && P.shared.P > 0) {
+            sh_pair = j * P.shared.row_tiles + (int)(folded / 16);
+            sh = P.head[sh_pair];
+            sh_pair %= P.heads_at_once;
+        }
         const int n = M.n + sh.y + own.y;
         float top = -INFINITY, den = 0.f;
         for (int i = lane; i < n; i += 32) {
-            const float m = *where(i, row, sh).ml;
-            wgt_s[row][i] = m;
-            top = fmaxf(top, m);
+            const float *o, *ml;
+            if (i < M.n) {
+                o = M.o + (i * M.rows + r) * DH;
+                ml = M.ml + (i * M.rows + r) * 2;
+            } else {
+                const bool s = i < M.n + sh.y;
+                const int k = i - M.n - (s ? 0 : sh.y), at = s ? (int)(folded % 16) : c0 - row0 + row;
+                const float* const slot = P.slots + part_slot(s ? sh.x : own.x, k, k == 0, P.heads_at_once, s ? sh_pair : h % P.heads_at_once) * SLOT;
+                o = slot + at * DH;
+                ml = slot + 16 * DH + at * 2;
+            }
+            const float2 x = *reinterpret_cast<const float2*>(ml);
+            wgt_s[row][i] = x.x;
+            from_s[row][i] = (uint32_t)((o - P.slots) >> 2);
+            const float up = fmaxf(top, x.x);            // (this lane's parts' sum, relative to their maximum)
+            den = den * (up == -INFINITY ? 1.f : exp2_fast(top - up)) + (x.x == -INFINITY ? 0.f : x.y * exp2_fast(x.x - up));
+            top = up;
         }
+        float all = top;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float z = top == -INFINITY ? 0.f : top;
-        for (int i = lane; i < n; i += 32) {
-            const float w = exp2_fast(wgt_s[row][i] - z);
-            wgt_s[row][i] = w;
-            if (w != 0.f) den = fmaf(w, where(i, row, sh).ml[1], den);
-        }
+        for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+        const float z = all == -INFINITY ? 0.f : all;
+        den = top == -INFINITY ? 0.f : den * exp2_fast(top - z);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+        for (int i = lane; i < n; i += 32) wgt_s[row][i] = exp2_fast(wgt_s[row][i] - z);
         if (lane == 0) {
             inv_s[row] = den == 0.f ? 0.f : 1.f / den;
-            write_sums(A, row_at(A, t, j, row0 + row), z, den);
+            n_s[row] = n;
+            write_sums(A, r, z, den);
         }
     }
     __syncthreads();
     for (int idx = tid; idx < rows * (DH / 4); idx += kSumThreads) {
-        const int row = idx / (DH / 4), col = idx % (DH / 4) * 4;
-        const int2 sh = shared_head(row);
-        const int n = M.n + sh.y + own.y;
+        const int row = idx / (DH / 4), col = idx % (DH / 4), n = n_s[row];
+        const float4* const from = reinterpret_cast<const float4*>(P.slots) + col;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int i0 = 0; i0 < n; i0 += 16) {
             float4 v[16];
@@ -501,7 +549,7 @@ __global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid
             for (int k = 0; k < 16; ++k) {
                 w[k] = i0 + k < n ? wgt_s[row][i0 + k] : 0.f;
                 // (a part of no weight is not looked at: it may hold anything)
-                v[k] = w[k] != 0.f ? *reinterpret_cast<const float4*>(where(i0 + k, row, sh).o + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+                v[k] = w[k] != 0.f ? from[from_s[row][i0 + k]] : make_float4(0.f, 0.f, 0.f, 0.f);
             }
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
@@ -512,28 +560,35 @@ __global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid
             }
         }
         const float inv = inv_s[row];
-        *reinterpret_cast<uint2*>(A.out + t * A.o_t + j * A.o_h + (row0 + row) * A.o_g + col) =
+        *reinterpret_cast<uint2*>(A.out + t * A.o_t + j * A.o_h + (c0 + row) * A.o_g + col * 4) =
             make_uint2(pack2(sum.x * inv, sum.y * inv), pack2(sum.z * inv, sum.w * inv));
+    }
     }
 }
 
-template <int DH>
-dsmoe_status launch_stream(const AttnView& A, const StreamPlan& plan, cudaStream_t s) {
+template <int DH, int HB>
+dsmoe_status launch_stream_heads(const AttnView& A, const StreamPlan& plan, cudaStream_t s) {
     static bool attr[kMaxDeviceSlots] = {};
     int dev = 0;
     DeviceState* st = nullptr;
     DSMOE_TRY(device_state(&st, &dev));
     if (!attr[dev]) {
-        DSMOE_CUDA_TRY(cudaFuncSetAttribute(attention_stream_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamGeo<DH>::SMEM));
+        DSMOE_CUDA_TRY(cudaFuncSetAttribute(attention_stream_kernel<DH, HB>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamGeo<DH>::SMEM));
         attr[dev] = true;
     }
-    DSMOE_CUDA_TRY(launch_chained(attention_stream_kernel<DH>, (unsigned)plan.ctas, 32 * StreamGeo<DH>::WARPS, StreamGeo<DH>::SMEM, s, A, plan));
+    DSMOE_CUDA_TRY(launch_chained(attention_stream_kernel<DH, HB>, (unsigned)plan.ctas, 32 * StreamGeo<DH>::WARPS, StreamGeo<DH>::SMEM, s, A, plan));
     return DSMOE_OK;
 }
 
 template <int DH>
+dsmoe_status launch_stream(const AttnView& A, const StreamPlan& plan, cudaStream_t s) {
+    if (plan.heads_at_once == 2) return launch_stream_heads<DH, 2>(A, plan, s);
+    return launch_stream_heads<DH, 1>(A, plan, s);
+}
+
+template <int DH>
 dsmoe_status launch_sum(const AttnView& A, const StreamPlan& plan, const RowParts& rows, cudaStream_t s) {
-    const long long ctas = plan.keep ? (long long)A.T * A.n_head * A.row_tiles : (long long)plan.passes * plan.ctas;
+    const long long ctas = plan.keep ? (long long)A.T * A.n_head * A.row_tiles : (long long)plan.passes * plan.ctas * plan.heads_at_once;
     DSMOE_CUDA_TRY(launch_chained(attention_sum_kernel<DH>, (unsigned)ctas, kSumThreads, 0, s, A, plan, rows));
     return DSMOE_OK;
 }
@@ -552,6 +607,9 @@ dsmoe_status launch_sum(const AttnView& A, const StreamPlan& plan, const RowPart
         case 256: return CALL(256);           \
         default: return DSMOE_ERR_UNSUPPORTED; \
     }
+
+// Two where neighbouring heads are nearer than neighbouring positions (see the kernel)
+int stream_heads_at_once(const AttnView& A) { return A.n_head % 2 == 0 && A.kv_h < A.kv_p ? 2 : 1; }
 
 // One CTA per SM, as far as each has a unit per warp in the longest case
 int stream_ctas(const AttnView& A, const SharedKeys& shared, bool own) {

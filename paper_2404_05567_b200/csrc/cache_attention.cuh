@@ -30,7 +30,7 @@ struct AttnView {
 };
 
 constexpr int kUnit = 16;                 // keys that a warp takes at a time
-constexpr int kListTokens = 1024;         // tokens whose keys are cut into runs at a time
+constexpr int kListTokens = 512;         // tokens whose keys are cut into runs at a time
 
 // The keys that a token sees: 0 .. sinks - 1 and first .. last (nothing: last < first and sinks == 0).
 struct Sight {
@@ -100,10 +100,13 @@ struct StreamPlan {
     // A pair that several CTAs share leaves a part per CTA; one that lies in one CTA's keys is written to out and lse, or (keep) its rows to `own_rows`
     // and `shared_rows`: something else is still to be added
     bool keep;
-    float* slots;                         // [passes][2 * ctas][16][d_head + 2]
-    int2* head;                           // keep: [pairs]: first slot, number of parts
-    int2* run_head;                       // otherwise: [passes][ctas]: the pair that begins in that run and goes on, number of parts; or 0 parts
+    int heads_at_once;                    // neighbouring pairs of a token that a CTA takes together
+    float* slots;                         // [passes][ctas][2][heads_at_once][16][d_head + 2]
+    int2* head;                           // keep: [pairs]: first run, number of parts
+    int2* run_head;                       // otherwise: [passes][ctas]: the first of the pairs that begin in that run and go on, number of parts; or 0 parts
     RowParts own_rows, shared_rows;       // n = 1
+    float* logits;                        // nullable: the tokens' logits in base 2, row r's from r * logit_pitch on (no window, no ring)
+    long long logit_pitch;                // a multiple of 16
 };
 static inline size_t part_bytes(int d_head) { return (size_t)16 * (d_head + 2) * 4; }
 
@@ -119,6 +122,7 @@ struct TilePlan {
 bool tile_supported(const AttnView& A);
 dsmoe_status launch_tile_attention(const AttnView& A, const TilePlan& plan, cudaStream_t s);
 
+int stream_heads_at_once(const AttnView& A);
 int stream_ctas(const AttnView& A, const SharedKeys& shared, bool own);       // CTAs of launch_stream_attention at most
 dsmoe_status launch_stream_attention(const AttnView& A, const StreamPlan& plan, cudaStream_t s);
 // Adds up what launch_stream_attention left in parts, into out and lse: without `keep` the pairs that several CTAs share; with it all rows, whose

@@ -14,7 +14,10 @@ namespace dsmoe {
 
 namespace {
 
-constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32, kMoveThreads = 256, kMovePieces = 8;
+constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32, kMoveThreads = 256;
+// 16-byte pieces that a thread of evict_move_kernel has under way, and CTAs of an SM: 128 caches of 16384 positions, 2000 of which stay, us: 1 and 8
+// 94, 2 and 8 76, 3 and 8 71, 4 and 8 70, 4 and 6 75, 8 and 4 78, 16 and 2 105.  In place a CTA has a whole cache to move, and more under way.
+__host__ __device__ constexpr int move_pieces(bool in_place) { return in_place ? 8 : 4; }
 
 // Tallies in the order of unsigned numbers: -0 and 0 are alike, what is no number comes before all others
 __device__ __forceinline__ uint32_t rank_bits(float v) {
@@ -283,7 +286,9 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_long_kernel(const __
 // A CTA per (sequence, head), keys or values, and stretch of rows.  A row moves towards the front of its cache, to a place that no later row comes
 // from: where source and destination are one buffer, one CTA takes all rows in order, and a batch is read before any of it is written.
 // Otherwise a CTA takes one batch.
-__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const __grid_constant__ EvictView E, const int stretches) {
+template <bool IN_PLACE>
+__global__ void __launch_bounds__(kMoveThreads, IN_PLACE ? 4 : 8) evict_move_kernel(const __grid_constant__ EvictView E, const int stretches) {
+    constexpr int PIECES = move_pieces(IN_PLACE);
     chain_wait();
     chain_next();
     const unsigned tid = threadIdx.x, CH = (unsigned)E.d_head / 8;
@@ -295,21 +300,21 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const __gri
     const __nv_bfloat16* const from = (which ? E.V : E.K) + s * E.kv_s + j * E.kv_h;
     __nv_bfloat16* const to = (which ? E.V_out : E.K_out) + s * E.o_s + j * E.o_h;
     const int32_t* const kept = E.kept + pair * E.keep;
-    constexpr unsigned BATCH = kMovePieces * kMoveThreads;
-    const unsigned per = E.in_place ? (unsigned)count : BATCH / CH, r0 = stretch * per;
+    constexpr unsigned BATCH = PIECES * kMoveThreads;
+    const unsigned per = IN_PLACE ? (unsigned)count : BATCH / CH, r0 = stretch * per;
     if (r0 >= (unsigned)count) return;
     const unsigned long long pieces = (unsigned long long)(min((unsigned)count, r0 + per) - r0) * CH;
     for (unsigned long long p0 = 0; p0 < pieces; p0 += BATCH) {
-        uint4 v[kMovePieces];
+        uint4 v[PIECES];
         const unsigned n = (unsigned)min((unsigned long long)BATCH, pieces - p0), row0 = (unsigned)(p0 / CH), ch0 = (unsigned)(p0 % CH);
 #pragma unroll
-        for (int i = 0; i < kMovePieces; ++i) {
+        for (int i = 0; i < PIECES; ++i) {
             const unsigned p = i * kMoveThreads + tid, at = ch0 + p;
             if (p < n) v[i] = *reinterpret_cast<const uint4*>(from + kept[r0 + row0 + at / CH] * E.kv_p + at % CH * 8);
         }
-        if (E.in_place) __syncthreads();
+        if (IN_PLACE) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kMovePieces; ++i) {
+        for (int i = 0; i < PIECES; ++i) {
             const unsigned p = i * kMoveThreads + tid, at = ch0 + p;
             if (p < n) *reinterpret_cast<uint4*>(to + (r0 + row0 + at / CH) * E.o_p + at % CH * 8) = v[i];
         }
@@ -325,7 +330,7 @@ cudaError_t launch_select(const EvictView& E, unsigned pairs, cudaStream_t s) {
 
 dsmoe_status launch_evict(const EvictView& E, cudaStream_t s) {
     const long long pairs = (long long)E.n_seq * E.n_head;
-    const int rows = kMovePieces * kMoveThreads / (E.d_head / 8), stretches = E.in_place ? 1 : ceil_div(E.keep, rows);
+    const int rows = move_pieces(false) * kMoveThreads / (E.d_head / 8), stretches = E.in_place ? 1 : ceil_div(E.keep, rows);
     if (pairs * 2 * stretches > 0x7fffffffll) return DSMOE_ERR_UNSUPPORTED;
     const unsigned n = (unsigned)pairs;
     if (E.L <= 2 * kSelThreads) DSMOE_CUDA_TRY(launch_select<2>(E, n, s));
@@ -333,7 +338,8 @@ dsmoe_status launch_evict(const EvictView& E, cudaStream_t s) {
     else if (E.L <= 16 * kSelThreads) DSMOE_CUDA_TRY(launch_select<16>(E, n, s));
     else if (E.L <= 32 * kSelThreads) DSMOE_CUDA_TRY(launch_select<32>(E, n, s));
     else DSMOE_CUDA_TRY(launch_chained(evict_select_long_kernel, n, kSelThreads, 0, s, E));
-    DSMOE_CUDA_TRY(launch_chained(evict_move_kernel, (unsigned)(pairs * 2 * stretches), kMoveThreads, 0, s, E, stretches));
+    DSMOE_CUDA_TRY(launch_chained(E.in_place ? evict_move_kernel<true> : evict_move_kernel<false>, (unsigned)(pairs * 2 * stretches), kMoveThreads,
+                                  0, s, E, stretches));
     return DSMOE_OK;
 }
 

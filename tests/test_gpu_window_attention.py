@@ -94,6 +94,14 @@ def test_orders_in_memory(by_token, members_first):
     run(Case(tokens, 4, 5, 128, 2, 64, seed=6, by_token=by_token, members_first=members_first), 25, 2)
 
 
+def test_caches_by_position_with_many_runs():
+    """Two heads at a time: parts of both, groups of more than one tile, a prefix's tests beside it."""
+    tokens = [(0, 1999), (1, 700), (2, -1), (1, 33)]
+    for group in (5, 20):
+        run(Case(tokens, 4, group, 128, 3, 2000, seed=16, by_token=True, hide=unseen(tokens, 1500, 4)), 1500, 4)
+    run(Case([(s, 300 + s) for s in range(50)], 6, 5, 64, 50, 350, seed=17, by_token=True), 2 ** 31 - 1)
+
+
 def test_parts_of_larger_tensors():
     """A slice of a larger cache, queries that are a slice and broadcast over the members, outputs with gaps that are left as they were."""
     c = Case([(0, 20), (1, 44)], 2, 4, 64, 2, 45, seed=7)
