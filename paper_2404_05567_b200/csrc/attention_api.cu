@@ -110,9 +110,11 @@ AttnView view_of(const dsmoe_attention_desc& d, const void* q, const void* K, co
 // where there are more tokens than sequences, on the 128-row kernel, which leaves tokens that have too few neighbours of their sequence; otherwise,
 // and for those, on the stream kernel.
 constexpr int kPrefixStreamRows = 32, kOwnTileRows = 64, kMaxSplits = 64;
+constexpr size_t kMostLogits = (size_t)512 << 20;
 
 struct AttnPlan {
-    size_t slots, head, run_head, count, list, ml, row_o, row_ml, total;
+    size_t slots, head, run_head, count, list, ml, logits, row_o, row_ml, total;
+    long long logit_pitch;                // tally: 0 if the logits are not kept
     int ctas, passes;                     // of the stream kernel, at most
     int prefix_splits;                    // 0: the prefix is not the 128-row kernel's
     int own_splits;                       // ... the own caches
@@ -159,8 +161,17 @@ AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, b
     w.slots = take((size_t)w.passes * 2 * w.ctas * stream_heads_at_once(A) * part_bytes(A.d_head));
     w.run_head = take((size_t)w.passes * w.ctas * sizeof(int2));
     w.head = take((size_t)A.n_head * ((size_t)A.T * A.row_tiles + S.row_tiles) * sizeof(int2));
-    if (wants_ml) w.ml = take(rows * sizeof(float2));
-    if (own_on_tiles(A)) {
+    const bool tiles = own_on_tiles(A);
+    if (wants_ml) {
+        w.ml = take(rows * sizeof(float2));
+        // Decoding: the logits are written and read again (8 bytes a key and row), not the keys read and multiplied again
+        const size_t pitch = align_up(A.L, 16);
+        if (!tiles && A.T <= kListTokens && rows * pitch * 4 <= kMostLogits) {
+            w.logit_pitch = (long long)pitch;
+            w.logits = take(rows * pitch * 4);
+        }
+    }
+    if (tiles) {
         w.own_splits = tile_splits(A, A.L);
         w.count = take(blocks * 4);
         w.list = take(blocks * tile_span(A.group) * 4);
@@ -197,6 +208,10 @@ dsmoe_status attend(const AttnView& A, const SharedKeys& S, const AttnPlan& w, c
         plan.shared_rows = next_parts(1);
     }
     plan.keep = S.P > 0;
+    if (w.logit_pitch) {
+        plan.logits = reinterpret_cast<float*>(ws + w.logits);
+        plan.logit_pitch = w.logit_pitch;
+    }
     if (w.own_splits) {
         // a narrow window needs fewer parts than the workspace has room for
         const long long keys = A.window < A.L ? (long long)A.window + A.sinks + tile_span(A.group) : A.L;
@@ -266,6 +281,11 @@ dsmoe_status dsmoe_attention_workspace_size(const dsmoe_attention_desc* desc, in
         if (kind == DSMOE_ATTENTION_PREFIX) p.P = prefix_len;
         const bool tiles = A.d_head == 64 || A.d_head == 96 || A.d_head == 128;
         *bytes = attention_plan(A, shared_keys(A, p), tiles, kind == DSMOE_ATTENTION_TALLY).total;
+        if (kind == DSMOE_ATTENTION_TALLY) {            // (with sequence numbers, as many as there may be, the logits may be kept)
+            AttnView several = A;
+            several.tok_seq = &desc->n_seq;
+            *bytes = std::max(*bytes, attention_plan(several, SharedKeys{}, false, true).total);
+        }
     }
     return DSMOE_OK;
 }
@@ -323,6 +343,8 @@ dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void*
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
     A.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + w.ml);
     DSMOE_TRY(attend(A, SharedKeys{}, w, static_cast<char*>(workspace), s));
+    if (w.logit_pitch)
+        return launch_tally_add(A, reinterpret_cast<const float*>(static_cast<char*>(workspace) + w.logits), w.logit_pitch, tally_in, tally_out, s);
     return launch_tally(A, tally_in, tally_out, s);
 }
 

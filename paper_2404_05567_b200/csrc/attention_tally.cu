@@ -2,7 +2,8 @@
 //
 //     tally_out[s][j][l] = tally_in[s][j][l] + sum over tokens t of sequence s with pos[t] >= l, members g, of 2^(logit(t,j,g,l) - m) / sum
 //
-// with m and the sum of every row from the attention itself.  A CTA owns 64 keys of a (sequence, head) and walks the rows that see them, in
+// with m and the sum of every row from the attention itself.  Either the attention has left its logits (decoding): tally_add_kernel reads them,
+// a thread per four keys.  Or they are computed again (attention_tally_kernel): a CTA owns 64 keys of a (sequence, head) and walks the rows that see them, in
 // order of the tokens, so that every sum is taken in one order and nothing is added in memory.  The logits are computed again, keys as the
 // rows and queries as the columns of the MMA tile: a thread keeps two keys' sums in registers.
 #include <climits>
@@ -30,6 +31,66 @@ __device__ __forceinline__ float exp2_fast(float v) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+
+constexpr int kAddThreads = 256, kAddKeys = 4 * kAddThreads;
+
+// A CTA per 1024 keys of a (sequence, head); A.T up to kListTokens
+__global__ void __launch_bounds__(kAddThreads) tally_add_kernel(const __grid_constant__ AttnView A, const float* logits, const long long pitch,
+                                                                const float* tally_in, float* tally_out) {
+    __shared__ int list_s[kListTokens], last_s[kListTokens], count_s[kAddThreads / 32];
+    chain_wait();
+    chain_next();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int blocks = (A.L + kAddKeys - 1) / kAddKeys;
+    const int kb = (int)(blockIdx.x % blocks), sj = (int)(blockIdx.x / blocks), s = sj / A.n_head, j = sj % A.n_head;
+    const int key0 = kb * kAddKeys + 4 * tid;
+    int n = 0;                                           // the sequence's tokens that see a key of this block, in order
+    for (int c = 0; c < A.T; c += kAddThreads) {
+        const int t = c + tid;
+        bool bad = false, mine = false;
+        int last = -1;
+        if (t < A.T) {
+            const Sight w = sight_of(A, t, &bad);
+            mine = w.seq == s && w.last >= kb * kAddKeys;
+            last = w.last;
+        }
+        const uint32_t votes = __ballot_sync(0xffffffffu, mine);
+        if (lane == 0) count_s[warp] = __popc(votes);
+        __syncthreads();
+        int at = n;
+        for (int w = 0; w < kAddThreads / 32; ++w) {
+            if (w < warp) at += count_s[w];
+            n += count_s[w];
+        }
+        if (mine) {
+            at += __popc(votes & ((1u << lane) - 1u));
+            list_s[at] = t;
+            last_s[at] = last;
+        }
+        __syncthreads();
+    }
+    if (n == 0 && tally_in == tally_out) return;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; ++i) {
+        const int last = last_s[i];
+        if (key0 > last) continue;
+        const long long r0 = row_at(A, list_s[i], j, 0);
+#pragma unroll 5
+        for (int m = 0; m < A.group; ++m) {
+            const float4 x = *reinterpret_cast<const float4*>(logits + (r0 + m) * pitch + key0);
+            const float2 ml = A.ml[r0 + m];
+            // (chosen, not multiplied by zero: behind the token's last key lies anything)
+            sum[0] += exp2_fast(x.x - ml.x) * ml.y;
+            if (key0 + 1 <= last) sum[1] += exp2_fast(x.y - ml.x) * ml.y;
+            if (key0 + 2 <= last) sum[2] += exp2_fast(x.z - ml.x) * ml.y;
+            if (key0 + 3 <= last) sum[3] += exp2_fast(x.w - ml.x) * ml.y;
+        }
+    }
+    const size_t at = (size_t)sj * A.L + key0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (key0 + k < A.L) tally_out[at + k] = (tally_in ? tally_in[at + k] : 0.f) + sum[k];
 }
 
 template <int DH>
@@ -170,6 +231,13 @@ dsmoe_status launch_tally_dh(const AttnView& A, const float* tally_in, float* ta
 }
 
 }  // namespace
+
+dsmoe_status launch_tally_add(const AttnView& A, const float* logits, long long pitch, const float* tally_in, float* tally_out, cudaStream_t s) {
+    const long long ctas = (long long)A.n_seq * A.n_head * ((A.L + kAddKeys - 1) / kAddKeys);
+    if (A.T > kListTokens || ctas > 0x7fffffffll) return DSMOE_ERR_UNSUPPORTED;
+    DSMOE_CUDA_TRY(launch_chained(tally_add_kernel, (unsigned)ctas, kAddThreads, 0, s, A, logits, pitch, tally_in, tally_out));
+    return DSMOE_OK;
+}
 
 dsmoe_status launch_tally(const AttnView& A, const float* tally_in, float* tally_out, cudaStream_t s) {
     switch (A.d_head) {

@@ -133,6 +133,9 @@ dsmoe_status launch_attention_sum(const AttnView& A, const StreamPlan& plan, con
 // Causal alone: no window, no ring.
 dsmoe_status launch_tally(const AttnView& A, const float* tally_in, float* tally_out, cudaStream_t s);
 
+// The same from the logits that launch_stream_attention left of every token (StreamPlan); up to kListTokens tokens
+dsmoe_status launch_tally_add(const AttnView& A, const float* logits, long long pitch, const float* tally_in, float* tally_out, cudaStream_t s);
+
 struct EvictView {
     int n_seq, n_head, L, d_head;
     int keep, sinks, recent;
