@@ -110,10 +110,12 @@ AttnView view_of(const dsmoe_attention_desc& d, const void* q, const void* K, co
 // where there are more tokens than sequences, on the 128-row kernel, which leaves tokens that have too few neighbours of their sequence; otherwise,
 // and for those, on the stream kernel.
 constexpr int kPrefixStreamRows = 32, kOwnTileRows = 64, kMaxSplits = 64;
+constexpr int kMaxTallyParts = 16;
 constexpr size_t kMostLogits = (size_t)512 << 20;
 
 struct AttnPlan {
-    size_t slots, head, run_head, count, list, ml, logits, row_o, row_ml, total;
+    size_t slots, head, run_head, count, list, ml, logits, sums, row_o, row_ml, total;
+    int tally_parts;                      // tally on the 128-row tiles: parts of the rows; 0: not there
     long long logit_pitch;                // tally: 0 if the logits are not kept
     int ctas, passes;                     // of the stream kernel, at most
     int prefix_splits;                    // 0: the prefix is not the 128-row kernel's
@@ -169,6 +171,13 @@ AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, b
         if (!tiles && A.T <= kListTokens && rows * pitch * 4 <= kMostLogits) {
             w.logit_pitch = (long long)pitch;
             w.logits = take(rows * pitch * 4);
+        }
+        if (tiles) {
+            // parts of the rows until four CTAs come to an SM (two fit; the keys at the end of a sequence are seen by few rows)
+            const size_t cells = (size_t)A.n_seq * A.n_head * A.L;
+            const long long ctas = (long long)A.n_seq * A.n_head * ((A.L + 127) / 128);
+            w.tally_parts = (int)std::max(1ll, std::min(4ll * sm_count() / ctas, (long long)kMaxTallyParts));
+            if (w.tally_parts > 1) w.sums = take(w.tally_parts * cells * 4);
         }
     }
     if (tiles) {
@@ -345,7 +354,7 @@ dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void*
     DSMOE_TRY(attend(A, SharedKeys{}, w, static_cast<char*>(workspace), s));
     if (w.logit_pitch)
         return launch_tally_add(A, reinterpret_cast<const float*>(static_cast<char*>(workspace) + w.logits), w.logit_pitch, tally_in, tally_out, s);
-    return launch_tally(A, tally_in, tally_out, s);
+    return launch_tally(A, w.tally_parts, reinterpret_cast<float*>(static_cast<char*>(workspace) + w.sums), tally_in, tally_out, s);
 }
 
 dsmoe_status dsmoe_evict_workspace_size(const dsmoe_attention_desc* desc, size_t* bytes) {

@@ -3,12 +3,16 @@
 //     tally_out[s][j][l] = tally_in[s][j][l] + sum over tokens t of sequence s with pos[t] >= l, members g, of 2^(logit(t,j,g,l) - m) / sum
 //
 // with m and the sum of every row from the attention itself.  Either the attention has left its logits (decoding): tally_add_kernel reads them,
-// a thread per four keys.  Or they are computed again (attention_tally_kernel): a CTA owns 64 keys of a (sequence, head) and walks the rows that see them, in
+// a thread per four keys.  Or they are computed again.  attention_tally_tile_kernel (prompts): a CTA has 128 keys as the rows of a tcgen05 tile and
+// walks the rows that see them as its columns, 128 at a time; a thread owns a key, takes its line of logits out of tensor memory and adds up the
+// weights: no sum crosses threads.  Four warps fetch the next rows' queries meanwhile, two CTAs fill an SM, and where there are few keys the rows
+// are cut into parts.  attention_tally_kernel (other head widths and strides): a CTA owns 64 keys of a (sequence, head) and walks the rows that see them, in
 // order of the tokens, so that every sum is taken in one order and nothing is added in memory.  The logits are computed again, keys as the
 // rows and queries as the columns of the MMA tile: a thread keeps two keys' sums in registers.
 #include <climits>
 
 #include "cache_attention.cuh"
+#include "tensor_maps.cuh"
 #include "umma.cuh"
 
 namespace dsmoe {
@@ -213,6 +217,244 @@ __global__ void __launch_bounds__(32 * kTallyWarps) attention_tally_kernel(const
     }
 }
 
+// ---------------------------------------------------------------- prompts, on the 5th-generation tensor cores
+
+constexpr int kTtKeys = 128, kTtRows = 128, kTtThreads = 256, kTtList = 1024;
+
+template <int DH>
+struct TallyGeo {
+    static constexpr int HALVES = (DH + 63) / 64;
+    static constexpr uint32_t PIECE = kTtRows * 128, TILE = HALVES * PIECE;
+    static constexpr uint32_t K = 0, Q = TILE, END = 3 * TILE;         // two buffers of queries
+    static constexpr int SMEM = (int)END + 1024;
+};
+
+struct TallyArgs {
+    AttnView A;
+    int at_pos, at_head, at_seq;
+    int key_tiles, parts;
+    const float* in;                      // parts == 1: the tallies
+    float* out;                           // ... or [parts][n_seq * n_head * L]
+};
+
+// Whether all of the four fetching warps' threads say so
+__device__ __forceinline__ bool fetchers_agree(bool x) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"((uint32_t)x) : "memory");
+    return all != 0;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kTtThreads, 2) attention_tally_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ TallyArgs P) {
+    using G = TallyGeo<DH>;
+    constexpr int CH = DH / 8, KS = DH / 16;
+    extern __shared__ unsigned char tt_smem[];
+    __shared__ int list_s[kTtList], last_s[kTtList], count_s[kTtThreads / 32];
+    __shared__ __align__(16) float2 ml_s[2][kTtRows];
+    __shared__ __align__(16) int row_last_s[2][kTtRows];
+    __shared__ int all_see_s[2];
+    __shared__ uint64_t k_full, rows_full[2], s_full[2], s_empty[2];
+    __shared__ uint32_t tmem_s;
+    __shared__ volatile int abort_flag;
+    const AttnView& A = P.A;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t raw = ptx::smem_u32(tt_smem), base = (raw + 1023u) & ~1023u;
+    // (sequence, head) by (sequence, head), the first keys, which most rows see, first
+    const int part = (int)(blockIdx.x % P.parts);
+    const int kt = (int)(blockIdx.x / P.parts / (A.n_seq * A.n_head)), sj = (int)(blockIdx.x / P.parts % (A.n_seq * A.n_head));
+    const int s = sj / A.n_head, j = sj % A.n_head, key0 = kt * kTtKeys, tokens = kTtRows / A.group;
+    if (tid == 0) {
+        ptx::mbar_init(ptx::smem_u32(&k_full), 1);
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(ptx::smem_u32(&rows_full[b]), 128);
+            ptx::mbar_init(ptx::smem_u32(&s_full[b]), 1);
+            ptx::mbar_init(ptx::smem_u32(&s_empty[b]), kTtKeys);
+        }
+        abort_flag = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == 0) {
+        ptx::tmem_alloc(ptx::smem_u32(&tmem_s), 256);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    chain_wait();
+    const uint32_t tmem = tmem_s;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    int done = 0, seen_tiles = 0;         // tiles of rows that this CTA has taken; that there were
+    bool alive = true;
+    for (int t0 = 0; t0 < A.T; t0 += kTtList) {
+        // the tokens of this sequence, among the next 1024, that see a key of this tile: in order
+        int n = 0;
+        __syncthreads();
+        for (int c = 0; c < kTtList && t0 + c < A.T; c += kTtThreads) {
+            const int t = t0 + c + tid;
+            bool bad = false, mine = false;
+            int last = -1;
+            if (t < A.T) {
+                const Sight w = sight_of(A, t, &bad);
+                mine = w.seq == s && w.last >= key0;
+                last = w.last;
+            }
+            const uint32_t votes = __ballot_sync(0xffffffffu, mine);
+            if (lane == 0) count_s[warp] = __popc(votes);
+            __syncthreads();
+            int at = n;
+            for (int w = 0; w < kTtThreads / 32; ++w) {
+                if (w < warp) at += count_s[w];
+                n += count_s[w];
+            }
+            if (mine) {
+                at += __popc(votes & ((1u << lane) - 1u));
+                list_s[at] = t;
+                last_s[at] = last;
+            }
+            __syncthreads();
+        }
+        const int tiles = (n + tokens - 1) / tokens;
+        for (int i = 0; i < tiles; ++i, ++seen_tiles) {
+            if (seen_tiles % P.parts != part || !alive) continue;
+            const int b = done & 1;
+            const uint32_t turn = (uint32_t)(done >> 1) & 1u;
+            if (warp >= 4) {
+                // ---- the rows' queries and sums
+                if (done >= 2) alive = ptx::mbar_wait(ptx::smem_u32(&s_empty[b]), turn ^ 1u, &abort_flag);
+                alive = fetchers_agree(alive);          // (they meet below, or none does)
+                const int at = tid - 128;
+                if (alive) {
+                    const int token = i * tokens + at / A.group;
+                    const bool real = at < tokens * A.group && token < n;
+                    ml_s[b][at] = real ? A.ml[row_at(A, list_s[token], j, at % A.group)] : make_float2(0.f, 0.f);
+                    row_last_s[b][at] = real ? last_s[token] : -1;
+                    if (at == 0) all_see_s[b] = 1;
+                    for (int idx = at; idx < kTtRows * CH; idx += 128) {
+                        const int row = idx / CH, ch = idx % CH, tk = i * tokens + row / A.group;
+                        const bool is = row < tokens * A.group && tk < n;
+                        const __nv_bfloat16* q = A.q + (is ? list_s[tk] : 0) * A.q_t + j * A.q_h + row % A.group * A.q_g + ch * 8;
+                        const uint32_t dst = base + G::Q + b * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(q), "r"(is ? 16u : 0u) : "memory");
+                    }
+                    ptx::cp_async_commit();
+                    ptx::cp_async_wait<0>();
+                    ptx::fence_proxy_async();
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                    if (real && last_s[token] < key0 + kTtKeys - 1) all_see_s[b] = 0;
+                    ptx::mbar_arrive(ptx::smem_u32(&rows_full[b]));
+                }
+                if (warp == 4 && alive) {
+                    if (ptx::elect_one()) {
+                        bool keys = true;
+                        if (done == 0) {
+                            const uint32_t bar = ptx::smem_u32(&k_full);
+                            ptx::mbar_expect_tx(bar, G::TILE);
+                            int c[4];
+                            c[P.at_pos] = key0, c[P.at_head] = j, c[P.at_seq] = s;
+#pragma unroll
+                            for (int h = 0; h < G::HALVES; ++h) ptx::tma_load_4d(base + G::K + h * G::PIECE, &mapK, bar, h * 64, c[1], c[2], c[3]);
+                            keys = ptx::mbar_wait(bar, 0, &abort_flag);
+                        }
+                        ptx::tc_fence_after();
+                        const uint32_t q0 = base + G::Q + b * G::TILE, idesc = ptx::make_idesc_bf16(kTtKeys, kTtRows);
+#pragma unroll
+                        for (int k = 0; k < KS && keys; ++k)
+                            ptx::umma_bf16(tmem + b * 128, ptx::make_desc_k_sw128(base + G::K + (k >> 2) * G::PIECE + (k & 3) * 32),
+                                           ptx::make_desc_k_sw128(q0 + (k >> 2) * G::PIECE + (k & 3) * 32), idesc, (uint32_t)(k != 0));
+                        if (keys) ptx::umma_commit(ptx::smem_u32(&s_full[b]));
+                    }
+                    __syncwarp();
+                }
+            } else {
+                // ---- a key's weights
+                alive = ptx::mbar_wait(ptx::smem_u32(&rows_full[b]), turn, &abort_flag) && ptx::mbar_wait(ptx::smem_u32(&s_full[b]), turn, &abort_flag);
+                alive = __all_sync(0xffffffffu, alive);
+                if (alive) {
+                    ptx::tc_fence_after();
+                    const uint32_t line = tmem + ((uint32_t)(warp * 32) << 16) + b * 128;
+                    const int key = key0 + tid;
+                    const bool all_see = all_see_s[b] != 0;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kTtRows; c0 += 32) {
+                        uint32_t v[32];
+                        ptx::tmem_ld32(line + c0, v);
+                        ptx::tmem_ld_wait();
+                        if (all_see) {
+#pragma unroll
+                            for (int c = 0; c < 32; c += 2) {
+                                const float4 ml = *reinterpret_cast<const float4*>(&ml_s[b][c0 + c]);
+                                sum[c & 3] = fmaf(exp2_fast(fmaf(__uint_as_float(v[c]), A.scale_log2, -ml.x)), ml.y, sum[c & 3]);
+                                sum[(c + 1) & 3] = fmaf(exp2_fast(fmaf(__uint_as_float(v[c + 1]), A.scale_log2, -ml.z)), ml.w, sum[(c + 1) & 3]);
+                            }
+                        } else {
+                            // (chosen, not multiplied by zero: a key that the row does not see may hold anything)
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                const float2 ml = ml_s[b][c0 + c];
+                                if (key <= row_last_s[b][c0 + c])
+                                    sum[c & 3] = fmaf(exp2_fast(fmaf(__uint_as_float(v[c]), A.scale_log2, -ml.x)), ml.y, sum[c & 3]);
+                            }
+                        }
+                    }
+                    ptx::tc_fence_before();
+                    ptx::mbar_arrive(ptx::smem_u32(&s_empty[b]));
+                }
+            }
+            ++done;
+        }
+    }
+    chain_next();
+    if (!alive && lane == 0) report_status(A.dev_status, DSMOE_ERR_TIMEOUT);
+    if (warp < 4 && key0 + tid < A.L) {
+        const size_t cells = (size_t)A.n_seq * A.n_head * A.L, at = (size_t)sj * A.L + key0 + tid;
+        const float x = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (P.parts > 1) P.out[part * cells + at] = x;
+        else P.out[at] = (P.in ? P.in[at] : 0.f) + x;
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, 256);
+    }
+}
+
+// Adds up the parts
+__global__ void __launch_bounds__(256) tally_parts_kernel(const float* sums, const int parts, const size_t cells, const float* tally_in, float* tally_out) {
+    chain_wait();
+    chain_next();
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= cells) return;
+    float x = 0.f;
+    for (int p = 0; p < parts; ++p) x += sums[p * cells + i];
+    tally_out[i] = (tally_in ? tally_in[i] : 0.f) + x;
+}
+
+template <int DH>
+dsmoe_status launch_tally_tile(const AttnView& A, int parts, float* sums, const float* tally_in, float* tally_out, cudaStream_t s) {
+    using G = TallyGeo<DH>;
+    static bool attr[kMaxDeviceSlots] = {};
+    int dev = 0;
+    DeviceState* st = nullptr;
+    DSMOE_TRY(device_state(&st, &dev));
+    if (!attr[dev]) {
+        DSMOE_CUDA_TRY(cudaFuncSetAttribute(attention_tally_tile_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
+        attr[dev] = true;
+    }
+    CUtensorMap mapK;
+    int at[3];
+    DSMOE_TRY(make_cache_map(&mapK, A, A.K, at));
+    const int key_tiles = ceil_div(A.L, kTtKeys);
+    const size_t cells = (size_t)A.n_seq * A.n_head * A.L;
+    const long long ctas = (long long)A.n_seq * A.n_head * key_tiles * parts;
+    if (ctas > 0x7fffffffll || (cells + 255) / 256 > 0x7fffffffull) return DSMOE_ERR_UNSUPPORTED;
+    const TallyArgs P{A, at[0], at[1], at[2], key_tiles, parts, tally_in, parts > 1 ? sums : tally_out};
+    DSMOE_CUDA_TRY(launch_chained(attention_tally_tile_kernel<DH>, (unsigned)ctas, kTtThreads, G::SMEM, s, mapK, P));
+    if (parts > 1) DSMOE_CUDA_TRY(launch_chained(tally_parts_kernel, (unsigned)((cells + 255) / 256), 256, 0, s, sums, parts, cells, tally_in, tally_out));
+    return DSMOE_OK;
+}
+
 template <int DH>
 dsmoe_status launch_tally_dh(const AttnView& A, const float* tally_in, float* tally_out, cudaStream_t s) {
     const long long ctas = (long long)A.n_seq * A.n_head * ((A.L + kTallyKeys - 1) / kTallyKeys);
@@ -239,7 +481,12 @@ dsmoe_status launch_tally_add(const AttnView& A, const float* logits, long long 
     return DSMOE_OK;
 }
 
-dsmoe_status launch_tally(const AttnView& A, const float* tally_in, float* tally_out, cudaStream_t s) {
+dsmoe_status launch_tally(const AttnView& A, int parts, float* sums, const float* tally_in, float* tally_out, cudaStream_t s) {
+    if (parts > 0) {
+        if (A.d_head == 64) return launch_tally_tile<64>(A, parts, sums, tally_in, tally_out, s);
+        if (A.d_head == 96) return launch_tally_tile<96>(A, parts, sums, tally_in, tally_out, s);
+        return launch_tally_tile<128>(A, parts, sums, tally_in, tally_out, s);
+    }
     switch (A.d_head) {
         case 32: return launch_tally_dh<32>(A, tally_in, tally_out, s);
         case 64: return launch_tally_dh<64>(A, tally_in, tally_out, s);

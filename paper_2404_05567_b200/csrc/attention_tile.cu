@@ -99,13 +99,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z, int w) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
-        : "memory");
-}
-
 struct TileArgs {
     AttnView A;
     int tile_tokens;                      // tokens of a 128-row tile
@@ -272,7 +265,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 int c[4];
                 c[P.at_pos] = t.slot, c[P.at_head] = j, c[P.at_seq] = t.seq;
 #pragma unroll
-                for (int h = 0; h < G::HALVES; ++h) tma_load_4d(dst + h * G::PIECE, map, b, h * 64, c[1], c[2], c[3]);
+                for (int h = 0; h < G::HALVES; ++h) ptx::tma_load_4d(dst + h * G::PIECE, map, b, h * 64, c[1], c[2], c[3]);
             };
             for (int i = 0; i < n; ++i) {
                 const int s = i % STAGES;
@@ -595,6 +588,31 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
     }
 }
 
+template <int DH>
+dsmoe_status launch_tile(const AttnView& A, const TilePlan& plan, cudaStream_t s) {
+    using G = TileGeo<DH>;
+    static bool attr[kMaxDeviceSlots] = {};
+    int dev = 0;
+    DeviceState* st = nullptr;
+    DSMOE_TRY(device_state(&st, &dev));
+    if (!attr[dev]) {
+        DSMOE_CUDA_TRY(cudaFuncSetAttribute(attention_tile_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
+        attr[dev] = true;
+    }
+    CUtensorMap mapK, mapV;
+    int at[3];
+    DSMOE_TRY(make_cache_map(&mapK, A, A.K, at));
+    DSMOE_TRY(make_cache_map(&mapV, A, A.V, at));
+    TileArgs P{A, kTileRows / A.group, tile_least_run(A.group), tile_blocks(A.T, A.group), plan.splits, at[0], at[1], at[2], plan.o, plan.ml,
+               plan.count, plan.list, plan.head};
+    const long long ctas = (long long)P.blocks * A.n_head * plan.splits;
+    if (ctas > 0x7fffffffll) return DSMOE_ERR_UNSUPPORTED;
+    DSMOE_CUDA_TRY(launch_chained(attention_tile_kernel<DH>, (unsigned)ctas, kTileThreads, G::SMEM, s, mapK, mapV, P));
+    return DSMOE_OK;
+}
+
+}  // namespace
+
 // K or V as a tensor of four dimensions, d_head and then positions, heads and sequences in the order of their strides
 dsmoe_status make_cache_map(CUtensorMap* m, const AttnView& A, const void* ptr, int (&at)[3]) {
     EncodeTiledFn fn = encode_fn();
@@ -626,31 +644,6 @@ dsmoe_status make_cache_map(CUtensorMap* m, const AttnView& A, const void* ptr, 
                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? DSMOE_OK : DSMOE_ERR_CUDA;
 }
-
-template <int DH>
-dsmoe_status launch_tile(const AttnView& A, const TilePlan& plan, cudaStream_t s) {
-    using G = TileGeo<DH>;
-    static bool attr[kMaxDeviceSlots] = {};
-    int dev = 0;
-    DeviceState* st = nullptr;
-    DSMOE_TRY(device_state(&st, &dev));
-    if (!attr[dev]) {
-        DSMOE_CUDA_TRY(cudaFuncSetAttribute(attention_tile_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
-        attr[dev] = true;
-    }
-    CUtensorMap mapK, mapV;
-    int at[3];
-    DSMOE_TRY(make_cache_map(&mapK, A, A.K, at));
-    DSMOE_TRY(make_cache_map(&mapV, A, A.V, at));
-    TileArgs P{A, kTileRows / A.group, tile_least_run(A.group), tile_blocks(A.T, A.group), plan.splits, at[0], at[1], at[2], plan.o, plan.ml,
-               plan.count, plan.list, plan.head};
-    const long long ctas = (long long)P.blocks * A.n_head * plan.splits;
-    if (ctas > 0x7fffffffll) return DSMOE_ERR_UNSUPPORTED;
-    DSMOE_CUDA_TRY(launch_chained(attention_tile_kernel<DH>, (unsigned)ctas, kTileThreads, G::SMEM, s, mapK, mapV, P));
-    return DSMOE_OK;
-}
-
-}  // namespace
 
 bool tile_supported(const AttnView& A) {
     if (A.d_head != 64 && A.d_head != 96 && A.d_head != 128) return false;

@@ -7,6 +7,8 @@
 // disjoint parts add up after scaling to the larger m, which is how work is split over CTAs, caches and kernels.
 #pragma once
 
+#include <cuda.h>
+
 #include "common.cuh"
 
 namespace dsmoe {
@@ -120,6 +122,8 @@ struct TilePlan {
     int2* head;
 };
 bool tile_supported(const AttnView& A);
+// K or V in boxes of 128 positions and 64 columns, 128-byte swizzle; at[0 .. 2]: the map's dimensions (1 .. 3) of positions, heads, sequences
+dsmoe_status make_cache_map(CUtensorMap* m, const AttnView& A, const void* ptr, int (&at)[3]);
 dsmoe_status launch_tile_attention(const AttnView& A, const TilePlan& plan, cudaStream_t s);
 
 int stream_heads_at_once(const AttnView& A);
@@ -130,8 +134,9 @@ dsmoe_status launch_stream_attention(const AttnView& A, const StreamPlan& plan, 
 dsmoe_status launch_attention_sum(const AttnView& A, const StreamPlan& plan, const RowParts& rows, cudaStream_t s);
 
 // tally_out[s][j][l] = tally_in[s][j][l] (nullptr: 0) + the sum of the softmax weights that the tokens of sequence s gave key l, from A.ml.
-// Causal alone: no window, no ring.
-dsmoe_status launch_tally(const AttnView& A, const float* tally_in, float* tally_out, cudaStream_t s);
+// Causal alone: no window, no ring.  parts > 0 (tile_supported): on the 5th-generation tensor cores, the rows cut into so many parts, whose sums go to
+// `sums`, [parts][n_seq * n_head * L], with more than one.
+dsmoe_status launch_tally(const AttnView& A, int parts, float* sums, const float* tally_in, float* tally_out, cudaStream_t s);
 
 // The same from the logits that launch_stream_attention left of every token (StreamPlan); up to kListTokens tokens
 dsmoe_status launch_tally_add(const AttnView& A, const float* logits, long long pitch, const float* tally_in, float* tally_out, cudaStream_t s);

@@ -70,6 +70,17 @@ def test_tokens_in_no_order():
     run(Case(tokens, 1, 2, 32, 5, 70, seed=2))
 
 
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_long_prompts_and_several_sequences(d):
+    """Parts of the rows, more tokens than are listed at a time, keys that the last tile's rows see in part."""
+    run(Case([(0, p) for p in range(5, 305)], 1, 5, d, 1, 310, seed=d, hide=lambda s, l: l > 304))
+    rng = np.random.default_rng(d)
+    tokens = [(int(s), int(p)) for s, p in zip(rng.integers(0, 3, 1300), rng.integers(-1, 200, 1300))]
+    run(Case(tokens, 2, 2, d, 4, 200, seed=d), "same")
+    run(Case([(2, p) for p in range(1100)], 1, 1, d, 3, 1100, seed=d))
+    run(Case([(s, p) for s in (1, 0) for p in range(100)], 2, 33, d, 2, 129, seed=d), "none")
+
+
 def test_every_weight_is_counted_once():
     """Each row's weights add up to 1."""
     tokens = [(s, 1000 + 37 * s) for s in range(6)]
