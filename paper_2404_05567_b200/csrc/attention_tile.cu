@@ -4,9 +4,9 @@
 // tiles of 128 keys, which both tiles use.  Per tile of rows and keys: S = Q.K^T into tensor memory; a thread per row takes the row's logits
 // from there, its weights 2^(logit - m) go back as bf16 where the logits lay, and O += P.V with P as the operand in tensor memory and V as it
 // lies in memory (N-major).  The running maximum moves only when a logit passes it by more than 2^8: until then the weights are at most 256, the
-// sums lose nothing, and O needs no rescaling; then the row's threads rescale it in tensor memory.  Roles: warp 0 copies (TMA, a ring of
-// tiles), warp 1 issues the MMAs, warp 2 clears the values behind a stretch's last key (0 times what is no number is no number), warps 4-7
-// and 8-11 are the two tiles' rows.  While one tile's threads are at their weights the tensor pipe works for the other one.
+// sums lose nothing, and O needs no rescaling; then the row's threads rescale it in tensor memory.  Roles: warps 0-7 and 8-15 are the two tiles' rows, two
+// threads a row; warp 16 copies (TMA, a ring of tiles), warp 17 issues the MMAs, warp 18 clears the values behind a stretch's last key (0
+// times what is no number is no number).  While one tile's threads are at their weights the tensor pipe works for the other one.
 //
 // What a CTA's tokens see: tokens of one sequence that follow one another are a run; a run's keys are at most three stretches of slots (sinks, and
 // the window, cut in two where a ring ends).  In blocks of many runs, those too short to be worth a
@@ -21,7 +21,7 @@ namespace dsmoe {
 namespace {
 
 // A block of up to kFewRuns runs (prompts' ends and beginnings) is taken as it is: each costs a pass over its keys
-constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 384, kFewRuns = 4, kMaxRuns = 16, kMaxStretches = 3 * kMaxRuns;
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 608, kLoadWarp = 16, kMmaWarp = 17, kClearWarp = 18, kFewRuns = 4, kMaxRuns = 16, kMaxStretches = 3 * kMaxRuns;
 
 template <int DH>
 struct TileGeo {
@@ -42,10 +42,10 @@ struct TileShared {
     volatile int abort_flag;
     int n_tiles, n_stretches, n_runs;
     int begin, end;                       // this CTA's tiles
-    int redo_n;
     int seq[2 * kTileRows], first[2 * kTileRows], last[2 * kTileRows], run[2 * kTileRows];
     int run_len[2 * kTileRows], run_lo[2 * kTileRows], run_hi[2 * kTileRows];
-    int redo[2 * kTileRows];
+    int redo[2 * kTileRows];              // rows that came out as no numbers
+    float swap[2][2][kTileRows];          // the halves of a row's threads tell each other
     Stretch st[kMaxStretches];
 };
 
@@ -99,6 +99,21 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// The two warps that share rows (64 threads) at their barrier: whether any of them, or all, say so
+__device__ __forceinline__ bool pair_any(int id, bool x) {
+    uint32_t y;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(y) : "r"(id), "r"((uint32_t)x) : "memory");
+    return y != 0;
+}
+__device__ __forceinline__ bool pair_all(int id, bool x) {
+    uint32_t y;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(y) : "r"(id), "r"((uint32_t)x) : "memory");
+    return y != 0;
+}
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+
 struct TileArgs {
     AttnView A;
     int tile_tokens;                      // tokens of a 128-row tile
@@ -147,34 +162,46 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         }
         for (int r = 0; r < 2; ++r) {
             ptx::mbar_init(ptx::smem_u32(&S.s_full[r]), 1);
-            ptx::mbar_init(ptx::smem_u32(&S.p_full[r]), kTileRows);
+            ptx::mbar_init(ptx::smem_u32(&S.p_full[r]), 2 * kTileRows);
             ptx::mbar_init(ptx::smem_u32(&S.o_done[r]), 1);
         }
         S.abort_flag = 0;
-        S.redo_n = 0;
         ptx::fence_barrier_init();
     }
-    if (warp == 1) {
+    if (warp == kMmaWarp) {
         ptx::tmem_alloc(ptx::smem_u32(&S.tmem), 512);
         ptx::tmem_relinquish();
     }
     chain_wait();
+    // ---- queries, in the swizzle's order; rows that are none are zeros
+    for (int idx = tid; idx < tiles_of_rows * kTileRows * CH; idx += kTileThreads) {
+        const int row = idx / CH, ch = idx % CH, r = row >> 7, at = row & 127;
+        const int tl = r * P.tile_tokens + at / A.group, m = at % A.group;
+        const bool real = at < P.tile_tokens * A.group && tl < ng;
+        const __nv_bfloat16* q = A.q + (tg0 + (real ? tl : 0)) * A.q_t + j * A.q_h + m * A.q_g + ch * 8;
+        const uint32_t dst = base + G::Q + r * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + at * 128 + (((ch & 7) ^ (at & 7)) << 4));
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(q), "r"(real ? 16u : 0u) : "memory");
+    }
+    ptx::cp_async_commit();
     // ---- what the tokens see, and the runs
     bool bad = false;
     if (tid < ng) {
         const Sight s = sight_of(A, tg0 + tid, &bad);
         S.seq[tid] = s.seq;
         S.last[tid] = s.last;
-        S.first[tid] = max(0, s.last >= A.window ? s.last - A.window + 1 : 0);
+        S.first[tid] = s.last >= A.window ? s.last - A.window + 1 : 0;
+        S.run[tid] = 0;
         S.run_len[tid] = 0;
         S.run_lo[tid] = 0x7fffffff;
         S.run_hi[tid] = -1;
     }
+    if (tid < 2 * kTileRows) S.redo[tid] = 0;
     if (bad) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
     __syncthreads();
+    const bool alike = __syncthreads_and(tid >= ng || S.seq[tid] == S.seq[0]) != 0;
     if (warp == 0) {                      // a token's run: how many runs begin at or before it, less one
         int before = 0;
-        for (int c = 0; c < ng; c += 32) {
+        for (int c = 0; c < ng && !alike; c += 32) {
             const int t = c + lane;
             const bool begins = t < ng && t > 0 && S.seq[t] != S.seq[t - 1];
             const uint32_t votes = __ballot_sync(0xffffffffu, begins);
@@ -183,13 +210,23 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         }
         if (lane == 0) S.n_runs = before + 1;
     }
-    __syncthreads();
-    if (tid < ng) {
-        const int r = S.run[tid];
-        atomicAdd(&S.run_len[r], 1);
-        if (S.last[tid] >= 0) {
-            atomicMin(&S.run_lo[r], S.first[tid]);
-            atomicMax(&S.run_hi[r], S.last[tid]);
+    if (!alike) __syncthreads();
+    if (warp * 32 < ng) {
+        const int t = min(tid, ng - 1), r = S.run[t];
+        const bool sees = S.last[t] >= 0;
+        if (alike) {                      // one run: a warp's tokens at once
+            const int lo = __reduce_min_sync(0xffffffffu, sees ? S.first[t] : 0x7fffffff), hi = __reduce_max_sync(0xffffffffu, sees ? S.last[t] : -1);
+            if (lane == 0) {
+                atomicMin(&S.run_lo[0], lo);
+                atomicMax(&S.run_hi[0], hi);
+                if (warp == 0) S.run_len[0] = ng;
+            }
+        } else if (tid < ng) {
+            atomicAdd(&S.run_len[r], 1);
+            if (sees) {
+                atomicMin(&S.run_lo[r], S.first[t]);
+                atomicMax(&S.run_hi[r], S.last[t]);
+            }
         }
     }
     __syncthreads();
@@ -237,16 +274,6 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         S.begin = (int)((long long)tiles * split / P.splits);
         S.end = (int)((long long)tiles * (split + 1) / P.splits);
     }
-    // ---- queries, in the swizzle's order; rows that are none are zeros
-    for (int idx = tid; idx < tiles_of_rows * kTileRows * CH; idx += kTileThreads) {
-        const int row = idx / CH, ch = idx % CH, r = row >> 7, at = row & 127;
-        const int tl = r * P.tile_tokens + at / A.group, m = at % A.group;
-        const bool real = at < P.tile_tokens * A.group && tl < ng;
-        const __nv_bfloat16* q = A.q + (tg0 + (real ? tl : 0)) * A.q_t + j * A.q_h + m * A.q_g + ch * 8;
-        const uint32_t dst = base + G::Q + r * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + at * 128 + (((ch & 7) ^ (at & 7)) << 4));
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(q), "r"(real ? 16u : 0u) : "memory");
-    }
-    ptx::cp_async_commit();
     ptx::cp_async_wait<0>();
     ptx::fence_proxy_async();
     ptx::tc_fence_before();
@@ -255,7 +282,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
     const uint32_t tmem = S.tmem;
     const int begin = S.begin, n = S.end - S.begin;
 
-    if (warp == 0) {
+    if (warp == kLoadWarp) {
         // ---- copies
         if (ptx::elect_one()) {
             int at = 0, issued = 0;
@@ -271,9 +298,9 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 const int s = i % STAGES;
                 const uint32_t parity = (uint32_t)((i / STAGES) & 1) ^ 1u;
                 const Tile t = tile_at(S, begin + i, at);
-                if (i >= STAGES && !ptx::mbar_wait(ptx::smem_u32(&S.k_empty[s]), parity, &S.abort_flag)) break;
+                if (i >= STAGES && !ptx::mbar_sleep(ptx::smem_u32(&S.k_empty[s]), parity, &S.abort_flag)) break;
                 load(&mapK, base + G::K + s * G::TILE, &S.k_full[s], t);
-                if (i >= STAGES && !ptx::mbar_wait(ptx::smem_u32(&S.v_empty[s]), parity, &S.abort_flag)) break;
+                if (i >= STAGES && !ptx::mbar_sleep(ptx::smem_u32(&S.v_empty[s]), parity, &S.abort_flag)) break;
                 load(&mapV, base + G::V + s * G::TILE, &S.v_full[s], t);
                 issued = i + 1;
             }
@@ -287,7 +314,25 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             }
         }
         __syncwarp();
-    } else if (warp == 1) {
+    } else if (warp == kClearWarp) {
+        // ---- values that are no keys': zeros
+        int at = 0;
+        for (int i = 0; i < n; ++i) {
+            const Tile t = tile_at(S, begin + i, at);
+            const int s = i % STAGES;
+            if (!__all_sync(0xffffffffu, ptx::mbar_sleep(ptx::smem_u32(&S.v_full[s]), (uint32_t)((i / STAGES) & 1), &S.abort_flag))) break;
+            if (t.n < kTileKeys) {
+                unsigned char* const v = smem + G::V + s * G::TILE;
+                for (int idx = lane; idx < (kTileKeys - t.n) * 8 * G::HALVES; idx += 32) {
+                    const int piece = idx % (8 * G::HALVES), row = t.n + idx / (8 * G::HALVES);
+                    *reinterpret_cast<uint4*>(v + (piece >> 3) * G::PIECE + row * 128 + (piece & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                ptx::fence_proxy_async();
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&S.v_clear[s]));         // (of every tile: the MMAs wait for it alone)
+        }
+    } else if (warp == kMmaWarp) {
         // ---- MMAs
         if (ptx::elect_one()) {
             const uint32_t idesc_s = ptx::make_idesc_bf16(kTileRows, kTileKeys), idesc_o = ptx::make_idesc_bf16(kTileRows, DH) | (1u << 16);
@@ -301,7 +346,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             };
             bool ok = true;
             if (n > 0) {
-                ok = ptx::mbar_wait(ptx::smem_u32(&S.k_full[0]), 0, &S.abort_flag);
+                ok = ptx::mbar_sleep(ptx::smem_u32(&S.k_full[0]), 0, &S.abort_flag);
                 if (ok) {
                     for (int r = 0; r < tiles_of_rows; ++r) logits(0, r);
                     ptx::umma_commit(ptx::smem_u32(&S.k_empty[0]));
@@ -309,11 +354,11 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             }
             for (int i = 0; ok && i < n; ++i) {
                 const int s = i % STAGES;
-                ok = ptx::mbar_wait(ptx::smem_u32(&S.v_clear[s]), (uint32_t)((i / STAGES) & 1), &S.abort_flag);
+                ok = ptx::mbar_sleep(ptx::smem_u32(&S.v_clear[s]), (uint32_t)((i / STAGES) & 1), &S.abort_flag);
                 if (ok && i + 1 < n)
-                    ok = ptx::mbar_wait(ptx::smem_u32(&S.k_full[(i + 1) % STAGES]), (uint32_t)(((i + 1) / STAGES) & 1), &S.abort_flag);
+                    ok = ptx::mbar_sleep(ptx::smem_u32(&S.k_full[(i + 1) % STAGES]), (uint32_t)(((i + 1) / STAGES) & 1), &S.abort_flag);
                 for (int r = 0; ok && r < tiles_of_rows; ++r) {
-                    ok = ptx::mbar_wait(ptx::smem_u32(&S.p_full[r]), (uint32_t)(i & 1), &S.abort_flag);
+                    ok = ptx::mbar_sleep(ptx::smem_u32(&S.p_full[r]), (uint32_t)(i & 1), &S.abort_flag);
                     if (!ok) break;
                     ptx::tc_fence_after();
                     const uint32_t v0 = base + G::V + s * G::TILE;
@@ -330,30 +375,14 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             }
         }
         __syncwarp();
-    } else if (warp == 2) {
-        // ---- values that are no keys': zeros
-        int at = 0;
-        for (int i = 0; i < n; ++i) {
-            const Tile t = tile_at(S, begin + i, at);
-            if (!__all_sync(0xffffffffu, ptx::mbar_wait(ptx::smem_u32(&S.v_full[i % STAGES]), (uint32_t)((i / STAGES) & 1), &S.abort_flag))) break;
-            unsigned char* const v = smem + G::V + (i % STAGES) * G::TILE;
-            for (int idx = lane; idx < (kTileKeys - t.n) * 8 * G::HALVES; idx += 32) {
-                const int piece = idx % (8 * G::HALVES), row = t.n + idx / (8 * G::HALVES);
-                *reinterpret_cast<uint4*>(v + (piece >> 3) * G::PIECE + row * 128 + (piece & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            ptx::fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&S.v_clear[i % STAGES]));        // (of every tile: the MMAs wait for it alone)
-        }
-        __syncwarp();
-    }
-    if (warp >= 4) {
-        // ---- rows
-        const int r = (warp - 4) >> 2, at = tid - 128 - r * 128;          // row tile, row of it = lane of tensor memory
+    } else {
+        // ---- rows: two threads each, with 64 of the 128 logits of a tile and half of O's columns
+        const int r = warp >> 3, half = (warp >> 2) & 1, at = (warp & 3) * 32 + lane;      // row tile, half, row of the tile = lane of tensor memory
         const int tl = r * P.tile_tokens + at / A.group, m_of = at % A.group;
         const bool real = at < P.tile_tokens * A.group && tl < ng;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + lanes + r * 128, tO = tmem + lanes + 256 + r * 128;
+        const uint32_t tS = tmem + lanes + r * 128, tO = tmem + lanes + 256 + r * 128 + half * (DH / 2);
+        const int pair = 1 + r * 4 + (warp & 3);                          // the barrier of the two warps that share rows
         const bool taken = real && (!P.count || S.n_runs <= kFewRuns || S.run_len[S.run[tl]] >= P.least_run);
         const int run = taken ? S.run[tl] : -1, last = taken ? S.last[tl] : -1, first = taken ? S.first[tl] : 0;
         const float sl2 = A.scale_log2;
@@ -363,30 +392,33 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         if (r < tiles_of_rows) {
             for (int i = 0; i < n; ++i) {
                 const Tile t = tile_at(S, begin + i, stretch);
-                // keys a .. b of the tile are this row's, and those before c
+                // keys a .. b of this half of the tile are this row's, and those before c
                 const bool in = t.run == run;               // (the same sequence may have two runs in this block)
-                const int b = in ? min(last - t.pos, t.n - 1) : -1, a = first - t.pos, c = A.sinks - t.pos;
-                const bool full = __all_sync(0xffffffffu, b == kTileKeys - 1 && (a <= 0 || c >= kTileKeys)) && sl2 > 0.f;
-                alive = ptx::mbar_wait(ptx::smem_u32(&S.s_full[r]), (uint32_t)(i & 1), &S.abort_flag);
-                alive = __all_sync(0xffffffffu, alive);
+                const int pos = t.pos + half * 64;
+                const int b = in ? min(last - pos, t.n - 1 - half * 64) : -1, a = first - pos, c = A.sinks - pos;
+                // (rows that are nobody's see anything)
+                const bool full = __all_sync(0xffffffffu, !taken || (b >= 63 && (a <= 0 || c >= 64))) && sl2 > 0.f;
+                alive = ptx::mbar_sleep(ptx::smem_u32(&S.s_full[r]), (uint32_t)(i & 1), &S.abort_flag);
+                // (both warps of a pair go on, or neither: they meet below)
+                alive = pair_all(pair, alive);
                 if (!alive) break;
                 ptx::tc_fence_after();
-                uint32_t v[4][32];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) ptx::tmem_ld32(tS + q * 32, v[q]);
+                uint32_t v[2][32];
+                ptx::tmem_ld32(tS + half * 64, v[0]);
+                ptx::tmem_ld32(tS + half * 64 + 32, v[1]);
                 ptx::tmem_ld_wait();
                 float top = -INFINITY, scale = sl2;
                 if (full) {
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < 2; ++q)
 #pragma unroll
                         for (int k = 0; k < 32; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(v[q][k]));
                     top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
                 } else {
                     scale = 1.f;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < 2; ++q)
 #pragma unroll
                         for (int k = 0; k < 32; ++k) {
                             const int x = q * 32 + k;
@@ -395,31 +427,34 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                             top = fmaxf(top, y);
                         }
                 }
-                // the maximum moves if it has to
-                const bool moves = top > m + 8.f || m == -INFINITY;
-                const float was = m;
-                if (moves) m = fmaxf(m, top);
-                if (__any_sync(0xffffffffu, moves && was != -INFINITY)) {
-                    const float f = moves && was != -INFINITY ? exp2_fast(was - m) : 1.f;
-                    l *= f;
-                    alive = i == 0 || ptx::mbar_wait(ptx::smem_u32(&S.o_done[r]), (uint32_t)((i - 1) & 1), &S.abort_flag);
-                    alive = __all_sync(0xffffffffu, alive);
-                    if (!alive) break;
-                    ptx::tc_fence_after();
+                // the maximum moves if it has to: the row's, over both halves.  (This barrier also lets the other half read its logits before the
+                // weights go where they lay.)
+                if (pair_any(pair, top > m + 8.f || (m == -INFINITY && top != -INFINITY))) {
+                    S.swap[r][half][at] = top;
+                    pair_sync(pair);
+                    top = fmaxf(top, S.swap[r][half ^ 1][at]);
+                    const bool moves = top > m + 8.f || m == -INFINITY;
+                    const float was = m;
+                    if (moves) m = fmaxf(m, top);
+                    if (__any_sync(0xffffffffu, moves && was != -INFINITY)) {
+                        // (S of this tile follows the tile before's P.V in the tensor pipe: O is all there)
+                        const float f = moves && was != -INFINITY ? exp2_fast(was - m) : 1.f;
+                        l *= f;
 #pragma unroll 1
-                    for (int q = 0; q < DH / 16; ++q) {
-                        uint32_t o[16];
-                        ptx::tmem_ld16(tO + q * 16, o);
-                        ptx::tmem_ld_wait();
+                        for (int q = 0; q < DH / 32; ++q) {
+                            uint32_t o[16];
+                            ptx::tmem_ld16(tO + q * 16, o);
+                            ptx::tmem_ld_wait();
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                        tmem_st16(tO + q * 16, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st16(tO + q * 16, o);
+                        }
                     }
                 }
                 const float z = m == -INFINITY ? 0.f : m;
                 float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < 2; ++q) {
                     uint32_t pk[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
@@ -429,118 +464,98 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                         s4[(2 * k + 1) & 3] += p1;
                         pk[k] = pack2(p0, p1);
                     }
-                    tmem_st16(tS + q * 16, pk);
+                    tmem_st16(tS + half * 32 + q * 16, pk);
                 }
                 l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
                 tmem_st_wait();
                 ptx::tc_fence_before();
                 ptx::mbar_arrive(ptx::smem_u32(&S.p_full[r]));
             }
-            if (alive && n > 0) {
-                alive = ptx::mbar_wait(ptx::smem_u32(&S.o_done[r]), (uint32_t)((n - 1) & 1), &S.abort_flag);
-                alive = __all_sync(0xffffffffu, alive);
-            }
+            if (alive && n > 0) alive = ptx::mbar_sleep(ptx::smem_u32(&S.o_done[r]), (uint32_t)((n - 1) & 1), &S.abort_flag);
+            alive = pair_all(pair, alive);
             ptx::tc_fence_after();
             if (!alive && lane == 0) report_status(A.dev_status, DSMOE_ERR_TIMEOUT);
         }
-        const long long row = ((long long)(tg0 + tl) * A.n_head + j) * A.group + m_of;
         if (alive && r < tiles_of_rows) {
+            S.swap[r][half][at] = l;
+            pair_sync(pair);
+            l = S.swap[r][0][at] + S.swap[r][1][at];
+            const long long row = row_at(A, tg0 + tl, j, m_of);
             const float inv = P.o ? 1.f : l == 0.f ? 0.f : 1.f / l;
             float check = l * 0.f;
-            // through shared memory (the queries' place: every S is done), so that a store writes whole rows
-            unsigned char* const stage = smem + G::Q + r * G::TILE + (warp & 3) * 32 * (G::TILE / kTileRows);
-            constexpr int LINE = (int)(G::TILE / kTileRows);              // bytes of staging a row: 128 or 256
-            constexpr int COLS = LINE / 4;                                // fp32 columns at a time
-            if (P.o) {
+            // through shared memory (the queries' place: every S is done), so that a store writes whole sectors; 16 columns of a row at a time
+            constexpr int LINE = (int)(G::TILE / kTileRows);              // bytes of staging a row: 128 or 256, half of them a thread's
+            unsigned char* const stage = smem + G::Q + r * G::TILE + (warp & 3) * 32 * LINE + half * (LINE / 2);
+            const long long dst = P.o ? (real ? ((long long)split * A.T * A.n_head * A.group + row) * DH : -1)
+                                      : (taken ? (tg0 + tl) * A.o_t + j * A.o_h + m_of * A.o_g : -1);
 #pragma unroll 1
-                for (int c0 = 0; c0 < DH; c0 += COLS) {
-                    __syncwarp();
+            for (int q = 0; q < DH / 32; ++q) {
+                uint32_t o[16];
+                if (n > 0) {
+                    ptx::tmem_ld16(tO + q * 16, o);
+                    ptx::tmem_ld_wait();
+                } else {
 #pragma unroll
-                    for (int q = 0; q < COLS / 32; ++q) {
-                        uint32_t o[32];
-                        if (c0 + q * 32 < DH) {
-                            if (n > 0) {
-                                ptx::tmem_ld32(tO + c0 + q * 32, o);
-                                ptx::tmem_ld_wait();
-                            } else {
-#pragma unroll
-                                for (int k = 0; k < 32; ++k) o[k] = 0u;
-                            }
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                check = fmaf(__uint_as_float(o[4 * k]) + __uint_as_float(o[4 * k + 1]) + __uint_as_float(o[4 * k + 2]) +
-                                                 __uint_as_float(o[4 * k + 3]), 0.f, check);
-                                const int ch = q * 8 + k;
-                                *reinterpret_cast<uint4*>(stage + lane * LINE + ((ch ^ (lane & 7)) << 4)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-                            }
-                        }
-                    }
-                    __syncwarp();
-                    const int chunks = min(COLS, DH - c0) / 4;
-                    for (int idx = lane; idx < 32 * chunks; idx += 32) {
-                        const int rw = idx / chunks, ch = idx % chunks;
-                        const long long to = __shfl_sync(0xffffffffu, real ? row : -1ll, rw);
-                        if (to >= 0)
-                            *reinterpret_cast<uint4*>(P.o + ((size_t)split * A.T * A.n_head * A.group + to) * DH + c0 + ch * 4) =
-                                *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw & 7)) << 4));
-                    }
+                    for (int k = 0; k < 16; ++k) o[k] = 0u;
                 }
-            } else {
-#pragma unroll 1
-                for (int q = 0; q < DH / 32; ++q) {
-                    uint32_t o[32];
-                    if (n > 0) {
-                        ptx::tmem_ld32(tO + q * 32, o);
-                        ptx::tmem_ld_wait();
-                    } else {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = 0u;
+                for (int k = 0; k < 16; ++k) check = fmaf(__uint_as_float(o[k]), 0.f, check);
+                const int col = half * (DH / 2) + q * 16;
+                __syncwarp();
+                if (P.o) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<uint4*>(stage + lane * LINE + ((k ^ (lane & 3)) << 4)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int rw = x * 8 + lane / 4, ch = lane % 4;
+                        const long long to = __shfl_sync(0xffffffffu, dst, rw);
+                        if (to >= 0) *reinterpret_cast<uint4*>(P.o + to + col + ch * 4) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw & 3)) << 4));
                     }
+                } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k = 0; k < 2; ++k) {
                         uint32_t w[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float x = __uint_as_float(o[8 * k + 2 * e]), y = __uint_as_float(o[8 * k + 2 * e + 1]);
-                            check = fmaf(x + y, 0.f, check);
-                            w[e] = pack2(x * inv, y * inv);
-                        }
-                        const int ch = q * 4 + k;
-                        *reinterpret_cast<uint4*>(stage + lane * LINE + ((ch ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int e = 0; e < 4; ++e) w[e] = pack2(__uint_as_float(o[8 * k + 2 * e]) * inv, __uint_as_float(o[8 * k + 2 * e + 1]) * inv);
+                        *reinterpret_cast<uint4*>(stage + lane * LINE + ((k ^ (lane & 1)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int rw = x * 16 + lane / 2, ch = lane % 2;
+                        const long long to = __shfl_sync(0xffffffffu, dst, rw);
+                        if (to >= 0) *reinterpret_cast<uint4*>(A.out + to + col + ch * 8) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw & 1)) << 4));
                     }
                 }
-                __syncwarp();
-                const bool good = taken && check == 0.f;
-                const long long dst = good ? (tg0 + tl) * A.o_t + j * A.o_h + m_of * A.o_g : -1ll;
-                for (int idx = lane; idx < 32 * CH; idx += 32) {
-                    const int rw = idx / CH, ch = idx % CH;
-                    const long long to = __shfl_sync(0xffffffffu, dst, rw);
-                    if (to >= 0)
-                        *reinterpret_cast<uint4*>(A.out + to + ch * 8) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw & 7)) << 4));
-                }
             }
-            if (taken && check != 0.f) {
-                S.redo[atomicAdd(&S.redo_n, 1)] = r * kTileRows + at;
-            } else if (P.o) {
-                if (real) *reinterpret_cast<float2*>(P.ml + ((size_t)split * A.T * A.n_head * A.group + row) * 2) = make_float2(l == 0.f ? -INFINITY : m, l);
-            } else if (taken) {
-                const float z = m == -INFINITY ? 0.f : m;
-                if (A.lse) A.lse[row] = (z + log2f(l)) * 0.6931471805599453f;
-                if (A.ml) A.ml[row] = make_float2(z, l == 0.f ? 0.f : 1.f / l);
+            if (taken && check != 0.f) S.redo[r * kTileRows + at] = 1;
+            if (half == 0) {
+                if (P.o) {
+                    if (real)
+                        *reinterpret_cast<float2*>(P.ml + ((size_t)split * A.T * A.n_head * A.group + row) * 2) =
+                            taken && l != 0.f ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+                } else if (taken) {
+                    const float z = m == -INFINITY ? 0.f : m;
+                    if (A.lse) A.lse[row] = (z + log2f(l)) * 0.6931471805599453f;
+                    if (A.ml) A.ml[row] = make_float2(z, inv);
+                }
             }
         }
     }
     chain_next();
     ptx::tc_fence_before();
     __syncthreads();
-    if (warp == 1) {
+    if (warp == kMmaWarp) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, 512);
     }
     // ---- rows that came out as no numbers: a warp per row, a key at a time, over this CTA's tiles
-    for (int x = warp; x < S.redo_n; x += kTileThreads / 32) {
+    for (int rr = warp; rr < 2 * kTileRows; rr += kTileThreads / 32) {
+        if (!S.redo[rr]) continue;
         constexpr int PER = DH / 32;
-        const int rr = S.redo[x], r = rr / kTileRows, at = rr % kTileRows, tl = r * P.tile_tokens + at / A.group, m_of = at % A.group;
+        const int r = rr / kTileRows, at = rr % kTileRows, tl = r * P.tile_tokens + at / A.group, m_of = at % A.group;
         const __nv_bfloat16* const q = A.q + (tg0 + tl) * A.q_t + j * A.q_h + m_of * A.q_g;
         float qv[PER], o[PER], m = -INFINITY, l = 0.f;
 #pragma unroll
