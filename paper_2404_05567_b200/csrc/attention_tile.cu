@@ -1,10 +1,9 @@
 // Attention of many rows that share their keys (prompts; a batch's shared prefix) on the 5th-generation tensor cores.
 //
 // A CTA owns up to 256 rows (neighbouring tokens' query heads of one key/value head) as two tiles of 128, and walks the keys that any of them sees in
-// tiles of 128 keys, which both tiles use.  Per tile of rows and keys: S = Q.K^T into tensor memory; a thread per row takes the row's logits
-// from there, its weights 2^(logit - m) go back as bf16 where the logits lay, and O += P.V with P as the operand in tensor memory and V as it
-// lies in memory (N-major).  The running maximum moves only when a logit passes it by more than 2^8: until then the weights are at most 256, the
-// sums lose nothing, and O needs no rescaling; then the row's threads rescale it in tensor memory.  Roles: warps 0-7 and 8-15 are the two tiles' rows, two
+// tiles of 128 keys, which both tiles use.  Per tile of rows and keys: S = Q.K^T into tensor memory; a row's two threads take its logits from there, its weights 2^(logit - m) go back as bf16 where the logits lay, and O += P.V with P as the operand in tensor
+// memory and V as it lies in memory (N-major).  The running maximum hardly ever moves (kMoves); if it does, the row's threads rescale O in
+// tensor memory.  Roles: warps 0-7 and 8-15 are the two tiles' rows, two
 // threads a row; warp 16 copies (TMA, a ring of tiles), warp 17 issues the MMAs, warp 18 clears the values behind a stretch's last key (0
 // times what is no number is no number).  While one tile's threads are at their weights the tensor pipe works for the other one.
 //
@@ -37,7 +36,7 @@ struct Stretch {
 };
 
 struct TileShared {
-    uint64_t k_full[4], k_empty[4], v_full[4], v_clear[4], v_empty[4], s_full[2], p_full[2], o_done[2];
+    uint64_t k_full[4], k_empty[4], v_full[4], v_clear[4], v_empty[4], s_full[2], p_full[2], o_done[2], stagger;
     uint32_t tmem;
     volatile int abort_flag;
     int n_tiles, n_stretches, n_runs;
@@ -57,6 +56,29 @@ __device__ __forceinline__ float exp2_fast(float v) {
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&v);
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// Two fp32 numbers at a time
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void halves_of(uint64_t p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 
 // Operand B = V as it lies in memory, [128 keys][64 columns] in the 128-byte swizzle: N-major.  Eight keys are 1024 bytes, the next 64 columns
@@ -79,18 +101,7 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
         "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -102,17 +113,22 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // The two warps that share rows (64 threads) at their barrier: whether any of them, or all, say so
 __device__ __forceinline__ bool pair_any(int id, bool x) {
     uint32_t y;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbar.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "=r"(y) : "r"(id), "r"((uint32_t)x) : "memory");
     return y != 0;
 }
 __device__ __forceinline__ bool pair_all(int id, bool x) {
     uint32_t y;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbar.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "=r"(y) : "r"(id), "r"((uint32_t)x) : "memory");
     return y != 0;
 }
-__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void pair_sync(int id) {
+    __syncwarp();
+    asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
+}
 
 struct TileArgs {
     AttnView A;
@@ -165,6 +181,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             ptx::mbar_init(ptx::smem_u32(&S.p_full[r]), 2 * kTileRows);
             ptx::mbar_init(ptx::smem_u32(&S.o_done[r]), 1);
         }
+        ptx::mbar_init(ptx::smem_u32(&S.stagger), 1);
         S.abort_flag = 0;
         ptx::fence_barrier_init();
     }
@@ -348,7 +365,13 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             if (n > 0) {
                 ok = ptx::mbar_sleep(ptx::smem_u32(&S.k_full[0]), 0, &S.abort_flag);
                 if (ok) {
-                    for (int r = 0; r < tiles_of_rows; ++r) logits(0, r);
+                    logits(0, 0);
+                    if (tiles_of_rows > 1) {
+                        // The second tile begins half a turn behind the first, and stays there: side by side, both would be at their exponentials, and
+                        // then both would wait for the tensor pipe
+                        ok = ptx::mbar_sleep(ptx::smem_u32(&S.stagger), 0, &S.abort_flag);
+                        logits(0, 1);
+                    }
                     ptx::umma_commit(ptx::smem_u32(&S.k_empty[0]));
                 }
             }
@@ -362,9 +385,10 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                     if (!ok) break;
                     ptx::tc_fence_after();
                     const uint32_t v0 = base + G::V + s * G::TILE;
+                    // (the weights of keys 0 .. 63 lie in the first 32 columns of those keys' logits, and the others' in the first of theirs)
 #pragma unroll
                     for (int k = 0; k < kTileKeys / 16; ++k)
-                        umma_bf16_ts(tmem + 256 + r * 128, tmem + r * 128 + k * 8, make_desc_values(v0 + k * 2048), idesc_o,
+                        umma_bf16_ts(tmem + 256 + r * 128, tmem + r * 128 + (k >> 2) * 64 + (k & 3) * 8, make_desc_values(v0 + k * 2048), idesc_o,
                                      (uint32_t)(i != 0 || k != 0));
                     ptx::umma_commit(ptx::smem_u32(&S.o_done[r]));
                     if (i + 1 < n) logits(i + 1, r);
@@ -376,7 +400,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         }
         __syncwarp();
     } else {
-        // ---- rows: two threads each, with 64 of the 128 logits of a tile and half of O's columns
+        // ---- rows: two threads each, with 64 of a tile's 128 logits and half of O's columns
         const int r = warp >> 3, half = (warp >> 2) & 1, at = (warp & 3) * 32 + lane;      // row tile, half, row of the tile = lane of tensor memory
         const int tl = r * P.tile_tokens + at / A.group, m_of = at % A.group;
         const bool real = at < P.tile_tokens * A.group && tl < ng;
@@ -387,53 +411,69 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         const int run = taken ? S.run[tl] : -1, last = taken ? S.last[tl] : -1, first = taken ? S.first[tl] : 0;
         const float sl2 = A.scale_log2;
         float m = -INFINITY, l = 0.f;
-        bool alive = true;
+        bool alive = true;                // (no tile is left out when a wait runs out, so that the warps of a pair keep meeting)
         int stretch = 0;
         if (r < tiles_of_rows) {
+            const uint32_t place = tS + half * 64;
+            bool told = false;
             for (int i = 0; i < n; ++i) {
                 const Tile t = tile_at(S, begin + i, stretch);
-                // keys a .. b of this half of the tile are this row's, and those before c
-                const bool in = t.run == run;               // (the same sequence may have two runs in this block)
-                const int pos = t.pos + half * 64;
-                const int b = in ? min(last - pos, t.n - 1 - half * 64) : -1, a = first - pos, c = A.sinks - pos;
-                // (rows that are nobody's see anything)
-                const bool full = __all_sync(0xffffffffu, !taken || (b >= 63 && (a <= 0 || c >= 64))) && sl2 > 0.f;
-                alive = ptx::mbar_sleep(ptx::smem_u32(&S.s_full[r]), (uint32_t)(i & 1), &S.abort_flag);
-                // (both warps of a pair go on, or neither: they meet below)
-                alive = pair_all(pair, alive);
-                if (!alive) break;
-                ptx::tc_fence_after();
-                uint32_t v[2][32];
-                ptx::tmem_ld32(tS + half * 64, v[0]);
-                ptx::tmem_ld32(tS + half * 64 + 32, v[1]);
-                ptx::tmem_ld_wait();
-                float top = -INFINITY, scale = sl2;
-                if (full) {
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(v[q][k]));
-                    top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
-                } else {
-                    scale = 1.f;
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) {
-                            const int x = q * 32 + k;
-                            const float y = x <= b && (x >= a || x < c) ? __uint_as_float(v[q][k]) * sl2 : -INFINITY;
-                            v[q][k] = __float_as_uint(y);
-                            top = fmaxf(top, y);
-                        }
+                // keys a .. b of this half of the tile are the row's, and those before c
+                const int off = half * 64, pos = t.pos + off;
+                const int b = t.run == run ? min(last - pos, t.n - 1 - off) : -1, a = first - pos, c = A.sinks - pos;
+                // (rows that are nobody's see anything; the same sequence may have two runs in this block)
+                const bool full = __all_sync(0xffffffffu, !taken || (b >= 63 && (a <= 0 || c >= 64)));
+                uint64_t seen = ~0ull;
+                if (!full) {
+                    const uint64_t upto = b < 0 ? 0ull : b >= 63 ? ~0ull : (2ull << b) - 1ull;
+                    const uint64_t from = a <= 0 ? ~0ull : a >= 64 ? 0ull : ~0ull << a;
+                    const uint64_t sinks = c <= 0 ? 0ull : c >= 64 ? ~0ull : (1ull << c) - 1ull;
+                    seen = upto & (from | sinks);
                 }
-                // the maximum moves if it has to: the row's, over both halves.  (This barrier also lets the other half read its logits before the
-                // weights go where they lay.)
-                if (pair_any(pair, top > m + 8.f || (m == -INFINITY && top != -INFINITY))) {
+                alive = ptx::mbar_sleep(ptx::smem_u32(&S.s_full[r]), (uint32_t)(i & 1), &S.abort_flag) && alive;
+                __syncwarp();
+                ptx::tc_fence_after();
+                uint32_t v[64];                   // logits, then (0 .. 31) the weights in pairs
+                float sum;
+                // Weights relative to the maximum as it is; once more if that has to move: the row's, over both halves
+                while (true) {
+                    ptx::tmem_ld32(place, *reinterpret_cast<uint32_t(*)[32]>(v));
+                    ptx::tmem_ld32(place + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
+                    ptx::tmem_ld_wait();
+                    if (!full) {
+#pragma unroll
+                        for (int k = 0; k < 64; ++k)
+                            v[k] = (k < 32 ? (uint32_t)seen & (1u << (k & 31)) : (uint32_t)(seen >> 32) & (1u << (k & 31))) ? v[k] : 0xff800000u;   // -inf
+                    }
+                    float top = -INFINITY, other = -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < 64; k += 4) {
+                        top = max3(top, __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+                        other = max3(other, __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
+                    }
+                    top = fmaxf(top, other) * sl2;
+                    const float z = m == -INFINITY ? 0.f : -m;
+                    const uint64_t scale2 = pair_of(sl2, sl2), z2 = pair_of(z, z);
+                    uint64_t s2[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        float x, y;
+                        halves_of(fma2(pair_of(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), scale2, z2), x, y);
+                        x = exp2_fast(x);
+                        y = exp2_fast(y);
+                        s2[k & 1] = add2(s2[k & 1], pair_of(x, y));
+                        v[k] = pack2(x, y);
+                    }
+                    float x, y;
+                    halves_of(add2(s2[0], s2[1]), x, y);
+                    sum = x + y;
+                    if (i == 0 && tid == 0 && !told) ptx::mbar_arrive(ptx::smem_u32(&S.stagger));
+                    told = true;
+                    if (!pair_any(pair, top > m + kMoves || (m == -INFINITY && top != -INFINITY))) break;
                     S.swap[r][half][at] = top;
                     pair_sync(pair);
                     top = fmaxf(top, S.swap[r][half ^ 1][at]);
-                    const bool moves = top > m + 8.f || m == -INFINITY;
+                    const bool moves = top > m + kMoves || m == -INFINITY;
                     const float was = m;
                     if (moves) m = fmaxf(m, top);
                     if (__any_sync(0xffffffffu, moves && was != -INFINITY)) {
@@ -451,28 +491,17 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                         }
                     }
                 }
-                const float z = m == -INFINITY ? 0.f : m;
-                float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const float p0 = exp2_fast(fmaf(__uint_as_float(v[q][2 * k]), scale, -z));
-                        const float p1 = exp2_fast(fmaf(__uint_as_float(v[q][2 * k + 1]), scale, -z));
-                        s4[(2 * k) & 3] += p0;
-                        s4[(2 * k + 1) & 3] += p1;
-                        pk[k] = pack2(p0, p1);
-                    }
-                    tmem_st16(tS + half * 32 + q * 16, pk);
-                }
-                l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                l += sum;
+                tmem_st16(place, v);
+                tmem_st16(place + 16, v + 16);
                 tmem_st_wait();
                 ptx::tc_fence_before();
                 ptx::mbar_arrive(ptx::smem_u32(&S.p_full[r]));
             }
-            if (alive && n > 0) alive = ptx::mbar_sleep(ptx::smem_u32(&S.o_done[r]), (uint32_t)((n - 1) & 1), &S.abort_flag);
-            alive = pair_all(pair, alive);
+            // (one phase to wait for: the last logits came behind the last but one tile's P.V)
+            if (n > 0) alive = ptx::mbar_sleep(ptx::smem_u32(&S.o_done[r]), (uint32_t)((n - 1) & 1), &S.abort_flag) && alive;
+            __syncwarp();
+            alive = pair_all(pair, alive && !S.abort_flag);
             ptx::tc_fence_after();
             if (!alive && lane == 0) report_status(A.dev_status, DSMOE_ERR_TIMEOUT);
         }
@@ -662,6 +691,7 @@ dsmoe_status make_cache_map(CUtensorMap* m, const AttnView& A, const void* ptr, 
 
 bool tile_supported(const AttnView& A) {
     if (A.d_head != 64 && A.d_head != 96 && A.d_head != 128) return false;
+    if (!(A.scale_log2 > 0.f)) return false;          // (what is hidden is -inf before it is scaled)
     const long long stride[3] = {A.kv_p, A.kv_h, A.kv_s};
     const int size[3] = {A.L, A.n_head, A.n_seq};
     for (int d = 0; d < 3; ++d)

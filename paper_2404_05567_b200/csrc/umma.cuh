@@ -71,11 +71,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
-// mbar_wait for threads that wait long beside others at work: the hardware puts the warp aside until the phase is over or about 20 us have passed,
-// instead of having it ask again and again
+// mbar_wait for threads that wait long beside others at work: the hardware puts the warp aside until the phase is over or some time has passed.
+// Its limit is in cycles (2 s at 2 GHz): the wall clock takes longer to read than most waits last.
+constexpr long long kWaitLimitCycles = 4000000000ll;
 __device__ __forceinline__ bool mbar_sleep(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    uint64_t t0 = 0;
-    while (true) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t tries = 1;; ++tries) {
         uint32_t ok;
         asm volatile(
             "{\n\t.reg .pred p;\n\t"
@@ -85,12 +87,12 @@ __device__ __forceinline__ bool mbar_sleep(uint32_t bar, uint32_t parity, volati
             : "r"(bar), "r"(parity), "r"(20000u)
             : "memory");
         if (ok) return true;
-        if (*abort_flag) return false;
-        const uint64_t now = globaltimer_ns();
-        if (t0 == 0) t0 = now;
-        if (now - t0 > kWaitLimitNs) {
-            *abort_flag = 1;
-            return false;
+        if ((tries & 15) == 0) {
+            if (*abort_flag) return false;
+            if (clock64() - t0 > kWaitLimitCycles) {
+                *abort_flag = 1;
+                return false;
+            }
         }
     }
 }
