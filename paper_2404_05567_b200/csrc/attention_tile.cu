@@ -11,6 +11,8 @@
 // the window, cut in two where a ring ends).  In blocks of many runs, those too short to be worth a
 // pass of a tile's over their keys are left to attention_stream_kernel.
 // A value that is not finite reaches all rows of a tile, also those that do not see it: rows that come out as no numbers are done again, one by one.
+#include <stddef.h>
+
 #include "cache_attention.cuh"
 #include "tensor_maps.cuh"
 #include "umma.cuh"
@@ -36,17 +38,22 @@ struct Stretch {
 };
 
 struct TileShared {
+    // (in one row: a thread each sets them up)
     uint64_t k_full[4], k_empty[4], v_full[4], v_clear[4], v_empty[4], s_full[2], p_full[2], o_done[2], stagger;
     uint32_t tmem;
     volatile int abort_flag;
-    int n_tiles, n_stretches, n_runs;
+    int n_stretches, n_runs;
     int begin, end;                       // this CTA's tiles
+    long long q_at[2 * kTileRows];        // where a row's queries are; -1: no row
     int seq[2 * kTileRows], first[2 * kTileRows], last[2 * kTileRows], run[2 * kTileRows];
     int run_len[2 * kTileRows], run_lo[2 * kTileRows], run_hi[2 * kTileRows];
     int redo[2 * kTileRows];              // rows that came out as no numbers
+    float tops[2][2][2][kTileRows];       // the largest logit of each half of a tile's, by turn
     float swap[2][2][kTileRows];          // the halves of a row's threads tell each other
     Stretch st[kMaxStretches];
 };
+constexpr int kTileBars = 27, kFirstPFull = 22;
+static_assert(offsetof(TileShared, tmem) == kTileBars * 8 && offsetof(TileShared, p_full) == kFirstPFull * 8, "the barriers in a row");
 
 __device__ __forceinline__ float exp2_fast(float v) {
     float r;
@@ -168,128 +175,151 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
     const int block = P.blocks - 1 - (int)(blockIdx.x / A.n_head / P.splits);
     const int span = 2 * P.tile_tokens, tg0 = block * span, ng = min(A.T - tg0, span);
     const int tiles_of_rows = ng > P.tile_tokens ? 2 : 1;
-    if (tid == 0) {
-        for (int i = 0; i < STAGES; ++i) {
-            ptx::mbar_init(ptx::smem_u32(&S.k_full[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&S.k_empty[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&S.v_full[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&S.v_clear[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&S.v_empty[i]), 1);
-        }
-        for (int r = 0; r < 2; ++r) {
-            ptx::mbar_init(ptx::smem_u32(&S.s_full[r]), 1);
-            ptx::mbar_init(ptx::smem_u32(&S.p_full[r]), 2 * kTileRows);
-            ptx::mbar_init(ptx::smem_u32(&S.o_done[r]), 1);
-        }
-        ptx::mbar_init(ptx::smem_u32(&S.stagger), 1);
-        S.abort_flag = 0;
+    if (tid < kTileBars) {
+        ptx::mbar_init(ptx::smem_u32(&S.k_full[0]) + 8u * tid, tid == kFirstPFull || tid == kFirstPFull + 1 ? 2 * kTileRows : 1);
         ptx::fence_barrier_init();
     }
     if (warp == kMmaWarp) {
         ptx::tmem_alloc(ptx::smem_u32(&S.tmem), 512);
         ptx::tmem_relinquish();
     }
+    if (tid < 2 * kTileRows) {
+        const int r = tid >> 7, at = tid & 127, tl = r * P.tile_tokens + at / A.group;
+        S.q_at[tid] = at < P.tile_tokens * A.group && tl < ng ? (tg0 + tl) * A.q_t + j * A.q_h + at % A.group * A.q_g : -1;
+        S.redo[tid] = 0;
+    }
+    if (tid == 0) {
+        S.abort_flag = 0;
+        S.n_runs = 1;
+        S.run_lo[0] = 0x7fffffff;
+        S.run_hi[0] = -1;
+    }
+    __syncthreads();
     chain_wait();
-    // ---- queries, in the swizzle's order; rows that are none are zeros
-    for (int idx = tid; idx < tiles_of_rows * kTileRows * CH; idx += kTileThreads) {
-        const int row = idx / CH, ch = idx % CH, r = row >> 7, at = row & 127;
-        const int tl = r * P.tile_tokens + at / A.group, m = at % A.group;
-        const bool real = at < P.tile_tokens * A.group && tl < ng;
-        const __nv_bfloat16* q = A.q + (tg0 + (real ? tl : 0)) * A.q_t + j * A.q_h + m * A.q_g + ch * 8;
-        const uint32_t dst = base + G::Q + r * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + at * 128 + (((ch & 7) ^ (at & 7)) << 4));
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(q), "r"(real ? 16u : 0u) : "memory");
-    }
-    ptx::cp_async_commit();
     // ---- what the tokens see, and the runs
-    bool bad = false;
-    if (tid < ng) {
-        const Sight s = sight_of(A, tg0 + tid, &bad);
-        S.seq[tid] = s.seq;
-        S.last[tid] = s.last;
-        S.first[tid] = s.last >= A.window ? s.last - A.window + 1 : 0;
-        S.run[tid] = 0;
-        S.run_len[tid] = 0;
-        S.run_lo[tid] = 0x7fffffff;
-        S.run_hi[tid] = -1;
-    }
-    if (tid < 2 * kTileRows) S.redo[tid] = 0;
-    if (bad) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
-    __syncthreads();
-    const bool alike = __syncthreads_and(tid >= ng || S.seq[tid] == S.seq[0]) != 0;
-    if (warp == 0) {                      // a token's run: how many runs begin at or before it, less one
-        int before = 0;
-        for (int c = 0; c < ng && !alike; c += 32) {
-            const int t = c + lane;
-            const bool begins = t < ng && t > 0 && S.seq[t] != S.seq[t - 1];
-            const uint32_t votes = __ballot_sync(0xffffffffu, begins);
-            if (t < ng) S.run[t] = before + __popc(votes & (0xffffffffu >> (31 - lane)));
-            before += __popc(votes);
-        }
-        if (lane == 0) S.n_runs = before + 1;
-    }
-    if (!alike) __syncthreads();
+    bool bad = false, like = true;
     if (warp * 32 < ng) {
-        const int t = min(tid, ng - 1), r = S.run[t];
-        const bool sees = S.last[t] >= 0;
-        if (alike) {                      // one run: a warp's tokens at once
-            const int lo = __reduce_min_sync(0xffffffffu, sees ? S.first[t] : 0x7fffffff), hi = __reduce_max_sync(0xffffffffu, sees ? S.last[t] : -1);
-            if (lane == 0) {
-                atomicMin(&S.run_lo[0], lo);
-                atomicMax(&S.run_hi[0], hi);
-                if (warp == 0) S.run_len[0] = ng;
+        int lo = 0x7fffffff, hi = -1;
+        if (tid < ng) {
+            const Sight s = sight_of(A, tg0 + tid, &bad);
+            like = s.seq == (A.tok_seq ? min(max(A.tok_seq[tg0], 0), A.n_seq - 1) : 0);
+            hi = s.last;
+            const int first = hi >= A.window ? hi - A.window + 1 : 0;
+            if (hi >= 0) lo = first;
+            S.seq[tid] = s.seq;
+            S.last[tid] = hi;
+            S.first[tid] = first;
+        }
+        // (of one run: of all tokens)
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        if (lane == 0) {
+            atomicMin(&S.run_lo[0], lo);
+            atomicMax(&S.run_hi[0], hi);
+        }
+        if (bad) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
+    }
+    const bool alike = __syncthreads_and(like) != 0;
+    if (!alike) {
+        if (tid < ng) {
+            S.run_len[tid] = 0;
+            S.run_lo[tid] = 0x7fffffff;
+            S.run_hi[tid] = -1;
+        }
+        if (warp == 0) {                  // a token's run: how many runs begin at or before it, less one
+            int before = 0;
+            for (int c = 0; c < ng; c += 32) {
+                const int t = c + lane;
+                const bool begins = t < ng && t > 0 && S.seq[t] != S.seq[t - 1];
+                const uint32_t votes = __ballot_sync(0xffffffffu, begins);
+                if (t < ng) S.run[t] = before + __popc(votes & (0xffffffffu >> (31 - lane)));
+                before += __popc(votes);
             }
-        } else if (tid < ng) {
+            if (lane == 0) S.n_runs = before + 1;
+        }
+        __syncthreads();
+        if (tid < ng) {
+            const int r = S.run[tid];
             atomicAdd(&S.run_len[r], 1);
-            if (sees) {
-                atomicMin(&S.run_lo[r], S.first[t]);
-                atomicMax(&S.run_hi[r], S.last[t]);
+            if (S.last[tid] >= 0) {
+                atomicMin(&S.run_lo[r], S.first[tid]);
+                atomicMax(&S.run_hi[r], S.last[tid]);
             }
         }
+        __syncthreads();
     }
-    __syncthreads();
+    const bool takes_all = alike || !P.count || S.n_runs <= kFewRuns;
     if (split == 0 && P.head && tid < ng)
         for (int i = 0; i < A.row_tiles; ++i) P.head[((long long)(tg0 + tid) * A.n_head + j) * A.row_tiles + i] = make_int2(0, 0);
     if (warp == 1 && split == 0 && j == 0 && P.count) {        // the tokens that are left, in order
         int n = 0;
-        for (int c = 0; c < ng; c += 32) {
+        for (int c = 0; c < ng && !takes_all; c += 32) {
             const int t = c + lane;
-            const bool left = t < ng && S.n_runs > kFewRuns && S.run_len[S.run[t]] < P.least_run;
+            const bool left = t < ng && S.run_len[S.run[t]] < P.least_run;
             const uint32_t votes = __ballot_sync(0xffffffffu, left);
             if (left) P.list[(long long)block * span + n + __popc(votes & ((1u << lane) - 1u))] = tg0 + t;
             n += __popc(votes);
         }
         if (lane == 0) P.count[block] = n;
     }
-    if (tid == 0) {
-        int n = 0, tiles = 0, t = 0;
-        const auto put = [&](int run, int seq, int pos0, int count) {
-            while (count > 0) {           // (in a ring, up to its end and then from its beginning)
-                const int slot = slot_of(A, pos0), m = A.ring && pos0 >= A.sinks ? min(count, A.L - slot) : count;
-                S.st[n++] = Stretch{run, seq, slot, pos0, m, tiles};
-                tiles += (m + kTileKeys - 1) / kTileKeys;
-                pos0 += m;
-                count -= m;
-                if (n == kMaxStretches) return;
-            }
-        };
-        for (int r = 0; r < S.n_runs; ++r) {
-            const int len = S.run_len[r], lo = S.run_lo[r], hi = S.run_hi[r];
-            const bool mine = !P.count || S.n_runs <= kFewRuns || len >= P.least_run;
-            if (mine && hi >= 0 && n + 3 <= kMaxStretches) {
-                const int sinks = min(A.sinks, hi + 1);
-                if (lo <= sinks) {
-                    put(r, S.seq[t], 0, hi + 1);
-                } else {
-                    put(r, S.seq[t], 0, sinks);
-                    put(r, S.seq[t], lo, hi + 1 - lo);
+    int load_at = 0;                      // the stretch of the load warp's next tile
+    const auto load = [&](const CUtensorMap* map, uint32_t dst, uint64_t* bar, const Tile& t) {
+        const uint32_t b = ptx::smem_u32(bar);
+        ptx::mbar_expect_tx(b, G::TILE);
+        int c[4];
+        c[P.at_pos] = t.slot, c[P.at_head] = j, c[P.at_seq] = t.seq;
+#pragma unroll
+        for (int h = 0; h < G::HALVES; ++h) ptx::tma_load_4d(dst + h * G::PIECE, map, b, h * 64, c[1], c[2], c[3]);
+    };
+    if (warp == kLoadWarp) {
+        // ---- the stretches, and the first tiles' copies
+        if (ptx::elect_one()) {
+            int n = 0, tiles = 0, t = 0;
+            const auto put = [&](int run, int seq, int pos0, int count) {
+                while (count > 0) {       // (in a ring, up to its end and then from its beginning)
+                    const int slot = slot_of(A, pos0), m = A.ring && pos0 >= A.sinks ? min(count, A.L - slot) : count;
+                    S.st[n++] = Stretch{run, seq, slot, pos0, m, tiles};
+                    tiles += (m + kTileKeys - 1) / kTileKeys;
+                    pos0 += m;
+                    count -= m;
+                    if (n == kMaxStretches) return;
                 }
+            };
+            const int n_runs = alike ? 1 : S.n_runs;
+            for (int r = 0; r < n_runs; ++r) {
+                const int len = alike ? ng : S.run_len[r], lo = S.run_lo[r], hi = S.run_hi[r];
+                if ((takes_all || len >= P.least_run) && hi >= 0 && n + 3 <= kMaxStretches) {
+                    const int sinks = min(A.sinks, hi + 1);
+                    if (lo <= sinks) {
+                        put(r, S.seq[t], 0, hi + 1);
+                    } else {
+                        put(r, S.seq[t], 0, sinks);
+                        put(r, S.seq[t], lo, hi + 1 - lo);
+                    }
+                }
+                t += len;
             }
-            t += len;
+            S.n_stretches = n;
+            const int begin = P.splits == 1 ? 0 : (int)((long long)tiles * split / P.splits);
+            const int end = P.splits == 1 ? tiles : (int)((long long)tiles * (split + 1) / P.splits);
+            S.begin = begin;
+            S.end = end;
+            for (int i = 0; i < min(STAGES, end - begin); ++i) {
+                const Tile x = tile_at(S, begin + i, load_at);
+                load(&mapK, base + G::K + i * G::TILE, &S.k_full[i], x);
+                load(&mapV, base + G::V + i * G::TILE, &S.v_full[i], x);
+            }
         }
-        S.n_stretches = n;
-        S.n_tiles = tiles;
-        S.begin = (int)((long long)tiles * split / P.splits);
-        S.end = (int)((long long)tiles * (split + 1) / P.splits);
+        __syncwarp();
+    } else {
+        // ---- queries, in the swizzle's order; rows that are none are zeros
+        for (int idx = warp < kLoadWarp ? tid : tid - 32; idx < tiles_of_rows * kTileRows * CH; idx += kTileThreads - 32) {
+            const int row = idx / CH, ch = idx % CH, r = row >> 7, at = row & 127;
+            const long long from = S.q_at[row];
+            const uint32_t dst = base + G::Q + r * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + at * 128 + (((ch & 7) ^ (at & 7)) << 4));
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(A.q + (from < 0 ? 0 : from) + ch * 8), "r"(from < 0 ? 0u : 16u) : "memory");
+        }
+        ptx::cp_async_commit();
     }
     ptx::cp_async_wait<0>();
     ptx::fence_proxy_async();
@@ -302,22 +332,14 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
     if (warp == kLoadWarp) {
         // ---- copies
         if (ptx::elect_one()) {
-            int at = 0, issued = 0;
-            const auto load = [&](const CUtensorMap* map, uint32_t dst, uint64_t* bar, const Tile& t) {
-                const uint32_t b = ptx::smem_u32(bar);
-                ptx::mbar_expect_tx(b, G::TILE);
-                int c[4];
-                c[P.at_pos] = t.slot, c[P.at_head] = j, c[P.at_seq] = t.seq;
-#pragma unroll
-                for (int h = 0; h < G::HALVES; ++h) ptx::tma_load_4d(dst + h * G::PIECE, map, b, h * 64, c[1], c[2], c[3]);
-            };
-            for (int i = 0; i < n; ++i) {
+            int issued = min(STAGES, n);
+            for (int i = issued; i < n; ++i) {
                 const int s = i % STAGES;
                 const uint32_t parity = (uint32_t)((i / STAGES) & 1) ^ 1u;
-                const Tile t = tile_at(S, begin + i, at);
-                if (i >= STAGES && !ptx::mbar_sleep(ptx::smem_u32(&S.k_empty[s]), parity, &S.abort_flag)) break;
+                const Tile t = tile_at(S, begin + i, load_at);
+                if (!ptx::mbar_sleep(ptx::smem_u32(&S.k_empty[s]), parity, &S.abort_flag)) break;
                 load(&mapK, base + G::K + s * G::TILE, &S.k_full[s], t);
-                if (i >= STAGES && !ptx::mbar_sleep(ptx::smem_u32(&S.v_empty[s]), parity, &S.abort_flag)) break;
+                if (!ptx::mbar_sleep(ptx::smem_u32(&S.v_empty[s]), parity, &S.abort_flag)) break;
                 load(&mapV, base + G::V + s * G::TILE, &S.v_full[s], t);
                 issued = i + 1;
             }
@@ -407,14 +429,15 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + r * 128, tO = tmem + lanes + 256 + r * 128 + half * (DH / 2);
         const int pair = 1 + r * 4 + (warp & 3);                          // the barrier of the two warps that share rows
-        const bool taken = real && (!P.count || S.n_runs <= kFewRuns || S.run_len[S.run[tl]] >= P.least_run);
-        const int run = taken ? S.run[tl] : -1, last = taken ? S.last[tl] : -1, first = taken ? S.first[tl] : 0;
+        const bool taken = real && (takes_all || S.run_len[S.run[tl]] >= P.least_run);
+        const int run = !taken ? -1 : alike ? 0 : S.run[tl], last = taken ? S.last[tl] : -1, first = taken ? S.first[tl] : 0;
         const float sl2 = A.scale_log2;
-        float m = -INFINITY, l = 0.f;
+        float m = taken ? -INFINITY : 0.f, l = 0.f, top = -INFINITY;
         bool alive = true;                // (no tile is left out when a wait runs out, so that the warps of a pair keep meeting)
         int stretch = 0;
         if (r < tiles_of_rows) {
             const uint32_t place = tS + half * 64;
+            const uint64_t scale2 = pair_of(sl2, sl2);
             bool told = false;
             for (int i = 0; i < n; ++i) {
                 const Tile t = tile_at(S, begin + i, stretch);
@@ -433,52 +456,14 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 alive = ptx::mbar_sleep(ptx::smem_u32(&S.s_full[r]), (uint32_t)(i & 1), &S.abort_flag) && alive;
                 __syncwarp();
                 ptx::tc_fence_after();
-                uint32_t v[64];                   // logits, then (0 .. 31) the weights in pairs
-                float sum;
-                // Weights relative to the maximum as it is; once more if that has to move: the row's, over both halves
-                while (true) {
-                    ptx::tmem_ld32(place, *reinterpret_cast<uint32_t(*)[32]>(v));
-                    ptx::tmem_ld32(place + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
-                    ptx::tmem_ld_wait();
-                    if (!full) {
-#pragma unroll
-                        for (int k = 0; k < 64; ++k)
-                            v[k] = (k < 32 ? (uint32_t)seen & (1u << (k & 31)) : (uint32_t)(seen >> 32) & (1u << (k & 31))) ? v[k] : 0xff800000u;   // -inf
-                    }
-                    float top = -INFINITY, other = -INFINITY;
-#pragma unroll
-                    for (int k = 0; k < 64; k += 4) {
-                        top = max3(top, __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
-                        other = max3(other, __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
-                    }
-                    top = fmaxf(top, other) * sl2;
-                    const float z = m == -INFINITY ? 0.f : -m;
-                    const uint64_t scale2 = pair_of(sl2, sl2), z2 = pair_of(z, z);
-                    uint64_t s2[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        float x, y;
-                        halves_of(fma2(pair_of(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), scale2, z2), x, y);
-                        x = exp2_fast(x);
-                        y = exp2_fast(y);
-                        s2[k & 1] = add2(s2[k & 1], pair_of(x, y));
-                        v[k] = pack2(x, y);
-                    }
-                    float x, y;
-                    halves_of(add2(s2[0], s2[1]), x, y);
-                    sum = x + y;
-                    if (i == 0 && tid == 0 && !told) ptx::mbar_arrive(ptx::smem_u32(&S.stagger));
-                    told = true;
-                    if (!pair_any(pair, top > m + kMoves || (m == -INFINITY && top != -INFINITY))) break;
-                    S.swap[r][half][at] = top;
-                    pair_sync(pair);
-                    top = fmaxf(top, S.swap[r][half ^ 1][at]);
-                    const bool moves = top > m + kMoves || m == -INFINITY;
-                    const float was = m;
-                    if (moves) m = fmaxf(m, top);
-                    if (__any_sync(0xffffffffu, moves && was != -INFINITY)) {
-                        // (S of this tile follows the tile before's P.V in the tensor pipe: O is all there)
-                        const float f = moves && was != -INFINITY ? exp2_fast(was - m) : 1.f;
+                // The maximum moves if the tile before asks for it.  (What the other half found there lies ready: these logits come behind both
+                // halves' weights.  O is all there too: S of this tile follows the tile before's P.V in the tensor pipe.)
+                if (i > 0) {
+                    top = fmaxf(top, S.tops[(i - 1) & 1][r][half ^ 1][at]);
+                    const bool moves = m != -INFINITY && top > m + kMoves;
+                    if (__any_sync(0xffffffffu, moves)) {
+                        const float f = moves ? exp2_fast(m - top) : 1.f;
+                        if (moves) m = top;
                         l *= f;
 #pragma unroll 1
                         for (int q = 0; q < DH / 32; ++q) {
@@ -491,6 +476,55 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                         }
                     }
                 }
+                // whether some row has no maximum yet: the same for both halves, which then find one together
+                const bool none = __any_sync(0xffffffffu, m == -INFINITY);
+                uint32_t v[64];                   // logits, then (0 .. 31) the weights in pairs
+                float sum;
+                while (true) {
+                    const float z = m == -INFINITY ? 0.f : -m;
+                    const uint64_t z2 = pair_of(z, z);
+                    uint64_t s2[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+                    float top2 = -INFINITY;
+                    top = -INFINITY;
+                    ptx::tmem_ld32(place, *reinterpret_cast<uint32_t(*)[32]>(v));
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {        // (the second 32 are on their way while the first are worked on)
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) asm volatile("" : "+r"(v[part * 32 + k]));
+                        if (part == 0) ptx::tmem_ld32(place + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
+                        const uint32_t bits = (uint32_t)(seen >> (32 * part));
+                        if (!full) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) v[part * 32 + k] = bits & (1u << k) ? v[part * 32 + k] : 0xff800000u;   // -inf
+                        }
+#pragma unroll
+                        for (int k = part * 32; k < part * 32 + 32; k += 4) {
+                            top = max3(top, __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+                            top2 = max3(top2, __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
+                        }
+#pragma unroll
+                        for (int k = part * 16; k < part * 16 + 16; ++k) {
+                            float x, y;
+                            halves_of(fma2(pair_of(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), scale2, z2), x, y);
+                            x = exp2_fast(x);
+                            y = exp2_fast(y);
+                            s2[k & 1] = add2(s2[k & 1], pair_of(x, y));
+                            v[k] = pack2(x, y);
+                        }
+                    }
+                    float x, y;
+                    halves_of(add2(s2[0], s2[1]), x, y);
+                    sum = x + y;
+                    top = fmaxf(top, top2) * sl2;
+                    if (i == 0 && tid == 0 && !told) ptx::mbar_arrive(ptx::smem_u32(&S.stagger));
+                    told = true;
+                    if (!none || !pair_any(pair, m == -INFINITY && top != -INFINITY)) break;
+                    S.swap[r][half][at] = top;
+                    pair_sync(pair);
+                    if (m == -INFINITY) m = fmaxf(top, S.swap[r][half ^ 1][at]);
+                }
+                S.tops[i & 1][r][half][at] = top;
                 l += sum;
                 tmem_st16(place, v);
                 tmem_st16(place + 16, v + 16);
@@ -511,52 +545,61 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             l = S.swap[r][0][at] + S.swap[r][1][at];
             const long long row = row_at(A, tg0 + tl, j, m_of);
             const float inv = P.o ? 1.f : l == 0.f ? 0.f : 1.f / l;
+            constexpr int HC = DH / 2;                                    // a thread's columns
+            constexpr int LINE = (int)(G::TILE / kTileRows) / 2;          // its staging: 64 or 128 bytes, through the queries' place (every S is done)
+            uint32_t o[HC];
+            if (n > 0) {
+                ptx::tmem_ld32(tO, *reinterpret_cast<uint32_t(*)[32]>(o));
+                if (HC == 64) ptx::tmem_ld32(tO + 32, *reinterpret_cast<uint32_t(*)[32]>(o + HC - 32));
+                if (HC == 48) ptx::tmem_ld16(tO + 32, *reinterpret_cast<uint32_t(*)[16]>(o + HC - 16));
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < HC; ++k) asm volatile("" : "+r"(o[k]));
+            } else {
+#pragma unroll
+                for (int k = 0; k < HC; ++k) o[k] = 0u;
+            }
             float check = l * 0.f;
-            // through shared memory (the queries' place: every S is done), so that a store writes whole sectors; 16 columns of a row at a time
-            constexpr int LINE = (int)(G::TILE / kTileRows);              // bytes of staging a row: 128 or 256, half of them a thread's
-            unsigned char* const stage = smem + G::Q + r * G::TILE + (warp & 3) * 32 * LINE + half * (LINE / 2);
-            const long long dst = P.o ? (real ? ((long long)split * A.T * A.n_head * A.group + row) * DH : -1)
-                                      : (taken ? (tg0 + tl) * A.o_t + j * A.o_h + m_of * A.o_g : -1);
-#pragma unroll 1
-            for (int q = 0; q < DH / 32; ++q) {
-                uint32_t o[16];
-                if (n > 0) {
-                    ptx::tmem_ld16(tO + q * 16, o);
-                    ptx::tmem_ld_wait();
-                } else {
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) o[k] = 0u;
+            for (int k = 0; k < HC; ++k) check = fmaf(__uint_as_float(o[k]), 0.f, check);
+            unsigned char* const stage = smem + G::Q + r * G::TILE + ((warp & 3) * 2 + half) * 32 * LINE;
+            const long long dst = (P.o ? (real ? ((long long)split * A.T * A.n_head * A.group + row) * DH : -1)
+                                       : (taken ? (tg0 + tl) * A.o_t + j * A.o_h + m_of * A.o_g : -1));
+            if (P.o) {
+                constexpr int AT_ONCE = LINE / 4;                         // columns
+#pragma unroll
+                for (int c0 = 0; c0 < HC; c0 += AT_ONCE) {
+                    constexpr int SLOTS = LINE / 16;
+                    const int chunks = min(AT_ONCE, HC - c0) / 4;
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < SLOTS; ++k)
+                        if (c0 + 4 * k < HC)
+                            *reinterpret_cast<uint4*>(stage + lane * LINE + ((k ^ (lane % SLOTS)) << 4)) =
+                                make_uint4(o[(c0 + 4 * k) % HC], o[(c0 + 4 * k + 1) % HC], o[(c0 + 4 * k + 2) % HC], o[(c0 + 4 * k + 3) % HC]);
+                    __syncwarp();
+                    for (int idx = lane; idx < 32 * chunks; idx += 32) {
+                        const int rw = idx / chunks, ch = idx % chunks;
+                        const long long to = __shfl_sync(0xffffffffu, dst, rw);
+                        if (to >= 0)
+                            *reinterpret_cast<uint4*>(P.o + to + half * HC + c0 + ch * 4) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw % SLOTS)) << 4));
+                    }
                 }
+            } else {
+                constexpr int CHUNKS = HC / 8, SLOTS = LINE / 16;
 #pragma unroll
-                for (int k = 0; k < 16; ++k) check = fmaf(__uint_as_float(o[k]), 0.f, check);
-                const int col = half * (DH / 2) + q * 16;
+                for (int k = 0; k < CHUNKS; ++k) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = pack2(__uint_as_float(o[8 * k + 2 * e]) * inv, __uint_as_float(o[8 * k + 2 * e + 1]) * inv);
+                    *reinterpret_cast<uint4*>(stage + lane * LINE + ((k ^ (lane % SLOTS)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
                 __syncwarp();
-                if (P.o) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        *reinterpret_cast<uint4*>(stage + lane * LINE + ((k ^ (lane & 3)) << 4)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-                    __syncwarp();
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int rw = x * 8 + lane / 4, ch = lane % 4;
-                        const long long to = __shfl_sync(0xffffffffu, dst, rw);
-                        if (to >= 0) *reinterpret_cast<uint4*>(P.o + to + col + ch * 4) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw & 3)) << 4));
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = pack2(__uint_as_float(o[8 * k + 2 * e]) * inv, __uint_as_float(o[8 * k + 2 * e + 1]) * inv);
-                        *reinterpret_cast<uint4*>(stage + lane * LINE + ((k ^ (lane & 1)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                    __syncwarp();
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int rw = x * 16 + lane / 2, ch = lane % 2;
-                        const long long to = __shfl_sync(0xffffffffu, dst, rw);
-                        if (to >= 0) *reinterpret_cast<uint4*>(A.out + to + col + ch * 8) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw & 1)) << 4));
-                    }
+                for (int x = 0; x < CHUNKS; ++x) {
+                    const int idx = lane + 32 * x, rw = idx / CHUNKS, ch = idx % CHUNKS;
+                    const long long to = __shfl_sync(0xffffffffu, dst, rw);
+                    if (to >= 0) *reinterpret_cast<uint4*>(A.out + to + half * HC + ch * 8) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw % SLOTS)) << 4));
                 }
             }
             if (taken && check != 0.f) S.redo[r * kTileRows + at] = 1;
@@ -595,7 +638,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         int stretch = 0;
         for (int i = 0; i < n; ++i) {
             const Tile t = tile_at(S, begin + i, stretch);
-            if (t.run != S.run[tl]) continue;
+            if (!alike && t.run != S.run[tl]) continue;
             for (int k = 0; k < t.n; ++k) {
                 const int pos = t.pos + k;
                 if (pos > S.last[tl] || (pos < S.first[tl] && pos >= A.sinks)) continue;
