@@ -160,8 +160,9 @@ AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, b
     const size_t rows = (size_t)A.T * A.n_head * A.group, blocks = (size_t)tile_blocks(A.T, A.group);
     w.ctas = stream_ctas(A, S, true);
     w.passes = ceil_div(A.T, kListTokens);
-    w.slots = take((size_t)w.passes * 2 * w.ctas * stream_heads_at_once(A) * part_bytes(A.d_head));
-    w.run_head = take((size_t)w.passes * w.ctas * sizeof(int2));
+    const size_t warps = (size_t)w.passes * w.ctas * 8;
+    w.slots = take(2 * warps * part_bytes(A.d_head));
+    w.run_head = take(warps * sizeof(int2));
     w.head = take((size_t)A.n_head * ((size_t)A.T * A.row_tiles + S.row_tiles) * sizeof(int2));
     const bool tiles = own_on_tiles(A);
     if (wants_ml) {
@@ -245,6 +246,7 @@ dsmoe_status attend(const AttnView& A, const SharedKeys& S, const AttnPlan& w, c
         plan.own_rows = next_parts(1);
     }
     plan.ctas = std::min(w.ctas, stream_ctas(A, plan.shared, plan.own));
+    plan.by_warp = stream_by_warp(A, plan);
     if (plan.keep) plan.head = head;
     else plan.run_head = reinterpret_cast<int2*>(ws + w.run_head);
     if (plan.own || plan.shared.P > 0) DSMOE_TRY(launch_stream_attention(A, plan, s));

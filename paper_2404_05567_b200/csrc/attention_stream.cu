@@ -39,15 +39,19 @@ __device__ __forceinline__ float exp2_fast(float v) {
     return r;
 }
 
-// Where the part of pair p of a group of HB lies that run + i leaves: a run has room for the parts of the pairs that began before it and for those
+// Where the part of pair p of a group of HB lies that a run leaves: a run has room for the parts of the pairs that began before it and for those
 // of the pairs that begin in it
-__device__ __forceinline__ long long part_slot(long long run, int i, bool begins, int HB, int p) { return (2 * (run + i) + (begins ? 1 : 0)) * HB + p; }
+__device__ __forceinline__ long long part_slot(long long run, bool begins, int HB, int p) { return (2 * run + (begins ? 1 : 0)) * HB + p; }
+// What is said of a pair's parts beside its first run: their number, and how many runs there are from one to the next
+__device__ __forceinline__ int parts_word(int parts, int stride) { return parts == 0 ? 0 : parts | stride << 16; }
 
 // Row `at`'s largest logit z (0 if it sees nothing) and sum, for whoever asks
 __device__ __forceinline__ void write_sums(const AttnView& A, size_t at, float z, float den) {
     if (A.lse) A.lse[at] = (z + log2f(den)) * 0.6931471805599453f;
     if (A.ml) A.ml[at] = make_float2(z, den == 0.f ? 0.f : 1.f / den);
 }
+
+constexpr int kPartsAtMost = 200;         // BY_WARP: parts that the longest pair leaves (with more there are fewer runs)
 
 template <int DH>
 struct StreamGeo {
@@ -64,7 +68,11 @@ struct StreamGeo {
 // units it takes every (WARPS / HB)-th.  Heads that lie side by side in memory (a cache stored by position) are so read side by side: 62 tokens of
 // 4 heads that see 2052 keys, stored by position, 68 us with one head at a time, 60 with two, 62 with four; by head 53, 53, 60 (cold caches); with fewer
 // keys than warps, a pair's parts are more the more heads share a CTA: 4 tokens behind 1500 keys 15, 23, 34.
-template <int DH, int HB>
+//
+// A run is a CTA's, whose warps share its units and meet at the end of each pair; or, where there are as many pairs as warps, BY_WARP, a warp's (of each of
+// the HB heads), which takes its units one after the other and owes the others nothing.  256 tokens of 8 heads with 384 keys each, behind a
+// prefix, us: a CTA's 275, a warp's 260; 32 tokens of 4 heads with 3000 keys, with sums and tallies, 56, 61.
+template <int DH, int HB, bool BY_WARP>
 __global__ void __launch_bounds__(32 * StreamGeo<DH>::WARPS, 1)
 attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constant__ StreamPlan P) {
     using G = StreamGeo<DH>;
@@ -74,15 +82,16 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     __shared__ long long base_s[kListTokens + 2];       // units before entry e's: the shared keys (in the first pass), then tokens
     __shared__ int token_s[kListTokens];                // left tokens: their numbers
     __shared__ long long warp_sum_s[WARPS];
+    __shared__ int longest_s[WARPS];
     __shared__ float ms[WARPS][16], ls[WARPS][16];
     __shared__ uint32_t at_s[WARPS];                    // where each warp's accumulators of the pair are
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q4 = lane & 3;
     const int hb = warp % HB, kw = warp / HB;
-    __shared__ __align__(16) unsigned char q_s[HB * 16 * STRIDE];
+    __shared__ __align__(16) unsigned char q_s[BY_WARP ? 16 : HB * 16 * STRIDE];
     const int own_heads = A.n_head * A.row_tiles, shared_heads = A.n_head * P.shared.row_tiles;
     chain_wait();
     if (P.run_head)
-        for (int i = tid; i < P.passes; i += THREADS) P.run_head[(long long)i * P.ctas + blockIdx.x] = make_int2(0, 0);
+        for (int i = tid; i < P.passes * KW; i += THREADS) P.run_head[(long long)(i / KW) * P.ctas * KW + blockIdx.x * KW + i % KW] = make_int2(0, 0);
 
     // Sum over the CTA's threads of what lies before this one's x; *all: of all
     const auto scan = [&](long long x, long long* all) {
@@ -127,18 +136,23 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     if (n + first == 0) break;
     {
         long long mine[PER], sum = 0, total;
+        int longest = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = tid * PER + i;
             mine[i] = 0;
             if (e < n) {
                 bool bad = false;
-                mine[i] = (long long)sight_of(A, token_of(e + first), &bad).units() * (own_heads / HB);
+                const int units = sight_of(A, token_of(e + first), &bad).units();
+                longest = max(longest, units);
+                mine[i] = (long long)units * (own_heads / HB);
                 if (bad && blockIdx.x == 0) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
             }
             sum += mine[i];
         }
         const long long shared_units = first ? (long long)((P.shared.P + kUnit - 1) / kUnit) * (shared_heads / HB) : 0;
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        if (lane == 0) longest_s[warp] = longest;
         long long before = scan(sum, &total) + shared_units;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -152,18 +166,30 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         }
         __syncthreads();
     }
-    // Equal runs; no CTA without a unit per warp, as far as there are so many
+    // Equal runs, of at least a unit for each warp
     const int entries = n + first;
-    const long long total = base_s[entries], wanted = (total + KW - 1) / KW;
-    const int n_cta = (int)(wanted < (long long)gridDim.x ? wanted : (long long)gridDim.x);
-    if ((int)blockIdx.x >= n_cta) continue;
-    const long long share = total / n_cta, extra = total - share * n_cta;
+    const long long total = base_s[entries];
+    long long wanted = min((long long)gridDim.x, (total + KW - 1) / KW);
+    if (BY_WARP) {
+        int longest = first ? (P.shared.P + kUnit - 1) / kUnit : 1;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) longest = max(longest, longest_s[w]);
+        wanted = max(1ll, min(min((long long)gridDim.x * KW, total), kPartsAtMost * total / longest));
+    }
+    const int n_runs = (int)wanted, stride = BY_WARP ? 1 : KW, run_no = BY_WARP ? (int)blockIdx.x * KW + kw : (int)blockIdx.x;
+    if (run_no >= n_runs) {
+        __syncwarp();
+        continue;
+    }
+    const long long share = total / n_runs, extra = total - share * n_runs;
     const auto run_start = [&](long long c) { return c * share + (c < extra ? c : extra); };
-    const auto run_of = [&](long long u) {              // the CTA whose run holds unit u
+    const auto run_of = [&](long long u) {              // the run that holds unit u
         const long long cut = extra * (share + 1);
         return u < cut ? u / (share + 1) : extra + (u - cut) / share;
     };
-    const long long u0 = run_start(blockIdx.x), u1 = run_start(blockIdx.x + 1);
+    const long long u0 = run_start(run_no), u1 = run_start(run_no + 1);
+    // where a run's parts lie, and the next run's after it
+    const long long run = (long long)pass * P.ctas * KW + (long long)run_no * stride;
 
     // Where a unit lies: entry, its first (head, row tile), key block of it
     struct Cursor {
@@ -204,9 +230,10 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         seg.k = (int)(in % seg.units);
     }
     Cursor ahead = seg;                                 // the next unit to fetch
-    ahead.k += kw;
+    const int hop = BY_WARP ? 1 : KW, begin = BY_WARP ? 0 : kw;
+    ahead.k += begin;
     settle(ahead);
-    long long u_ahead = u0 + kw;
+    long long u_ahead = u0 + begin;
     unsigned char* const ring = as_smem + (size_t)warp * BUFS * G::UNIT;
     const uint32_t ring0 = ptx::smem_u32(ring);
     const auto fetch = [&](int buf) {
@@ -248,9 +275,9 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd + dst), "l"(V + src), "r"(nbytes) : "memory");
                 }
             }
-            ahead.k += KW;
+            ahead.k += hop;
             settle(ahead);
-            u_ahead += KW;
+            u_ahead += hop;
         }
         ptx::cp_async_commit();
     };
@@ -259,7 +286,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     const uint32_t kfrag = (uint32_t)(((lane >> 4) * 8 + (lane & 7)) * STRIDE + ((lane >> 3) & 1) * 16);
     const uint32_t vfrag = (uint32_t)((((lane >> 3) & 1) * 8 + (lane & 7)) * STRIDE + (lane >> 4) * 16);
     int buf = 0;
-    long long mine = u0 + kw;                           // this warp's next unit
+    long long mine = u0 + begin;                        // this warp's next unit
     uint4 next_q[QN];                                   // a thread's pieces of the next pairs' queries; rows that are none are zeros
     const auto ask_queries = [&](const Cursor& c) {
         const bool sh = is_shared(c.e);
@@ -273,7 +300,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
                 next_q[i] = *reinterpret_cast<const uint4*>(A.q + (t0 + row / A.group) * A.q_t + h / tiles * A.q_h + row % A.group * A.q_g + idx % CH * 8);
         }
     };
-    ask_queries(seg);
+    if (!BY_WARP) ask_queries(seg);
     for (long long at = u0; at < u1;) {
         const bool sh = is_shared(seg.e);
         const int tiles = sh ? P.shared.row_tiles : A.row_tiles, t = sh ? 0 : token_of(seg.e);
@@ -282,23 +309,37 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         const int first_k = seg.k;
         const Sight& s = seg.s;
         const int su = s.sink_units();
-#pragma unroll
-        for (int i = 0; i < QN; ++i) {
-            const int idx = tid + i * THREADS;
-            if (idx < HB * 16 * CH) *reinterpret_cast<uint4*>(q_s + (idx / CH) * STRIDE + idx % CH * 16) = next_q[i];
-        }
-        __syncthreads();
-        const uint32_t qrow = ptx::smem_u32(q_s) + (uint32_t)((hb * 16 + (lane & 15)) * STRIDE + (lane >> 4) * 16);
-        uint32_t qf[KS][4];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) ldsm_x4(qf[ks], qrow + (uint32_t)(ks * 32));
         // this warp's pair
         const int j = (seg.h + hb) / tiles, row0 = (seg.h + hb) % tiles * 16, rows = (int)min(16ll, all_rows - row0);
+        uint32_t qf[KS][4];                             // its queries (the MMAs' A operand); rows that are none are zeros
+        if (BY_WARP) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int row = row0 + g + 8 * half;
+                const bool real = row < all_rows;
+                const __nv_bfloat16* const q = A.q + (t + (real ? row / A.group : 0)) * A.q_t + j * A.q_h + (real ? row % A.group : 0) * A.q_g + q4 * 2;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    qf[ks][half] = real ? *reinterpret_cast<const uint32_t*>(q + ks * 16) : 0u;
+                    qf[ks][2 + half] = real ? *reinterpret_cast<const uint32_t*>(q + ks * 16 + 8) : 0u;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < QN; ++i) {
+                const int idx = tid + i * THREADS;
+                if (idx < HB * 16 * CH) *reinterpret_cast<uint4*>(q_s + (idx / CH) * STRIDE + idx % CH * 16) = next_q[i];
+            }
+            __syncthreads();
+            const uint32_t qrow = ptx::smem_u32(q_s) + (uint32_t)((hb * 16 + (lane & 15)) * STRIDE + (lane >> 4) * 16);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) ldsm_x4(qf[ks], qrow + (uint32_t)(ks * 32));
+        }
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float o[DT][4];
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-        for (; mine < end; mine += KW) {
+        for (; mine < end; mine += hop) {
             __syncwarp();                               // every lane is past its reads of the buffer that is filled again now
             fetch((buf + BUFS - 1) % BUFS);
             ptx::cp_async_wait<BUFS - 1>();
@@ -386,8 +427,17 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         Cursor next = seg;
         next.k += (int)(end - at);
         settle(next);
-        if (end < u1) ask_queries(next);                // (on their way while the triples meet)
-        else if (pass + 1 == P.passes) chain_next();
+        if (end < u1) {
+            if (!BY_WARP) ask_queries(next);            // (on their way while the triples meet)
+        } else if (pass + 1 == P.passes) {
+            chain_next();
+        }
+        const bool whole = end - at == units, begins = first_k == 0;
+        if (begins && (BY_WARP ? lane == 0 : tid < HB)) {
+            const int p = BY_WARP ? hb : tid, parts = whole ? 0 : parts_word((int)(run_of(at + units - 1) - run_no + 1), stride);
+            if (P.keep) P.head[sh ? seg.h + p : shared_heads + (long long)t * own_heads + seg.h + p] = make_int2((int)run, parts);
+            else if (!whole && p == 0) P.run_head[run] = make_int2(t * own_heads + seg.h, parts);
+        }
         // ---- the warps' triples of the pair, through the buffer that each has just finished (the next fetch would fill it)
         l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
         l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
@@ -408,21 +458,45 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
             *reinterpret_cast<float2*>(acc + g * LDO + dt * 8 + q4 * 2) = make_float2(o[dt][0], o[dt][1]);
             if (rows > 8) *reinterpret_cast<float2*>(acc + (g + 8) * LDO + dt * 8 + q4 * 2) = make_float2(o[dt][2], o[dt][3]);
         }
-        __syncthreads();
-        const bool whole = end - at == units, begins = first_k == 0;
-        const long long run = (long long)pass * P.ctas + blockIdx.x;
-        if (tid < HB && begins) {
-            const int parts = whole ? 0 : (int)(run_of(at + units - 1) - blockIdx.x + 1);
-            if (P.keep) P.head[sh ? seg.h + tid : shared_heads + (long long)t * own_heads + seg.h + tid] = make_int2((int)run, parts);
-            else if (!whole && tid == 0) P.run_head[run] = make_int2(t * own_heads + seg.h, parts);
-        }
+        if (BY_WARP) __syncwarp();
+        else __syncthreads();
         float* const row_o = sh ? P.shared_rows.o : P.own_rows.o;
         float* const row_ml = sh ? P.shared_rows.ml : P.own_rows.ml;
+        // where two columns of a row go, and beside the first ones the row's sums
+        const auto put = [&](int p, int row, int col, float nx, float ny, float M, float den) {
+            const int head = (seg.h + p) / tiles, first_row = (seg.h + p) % tiles * 16;
+            const int member = (first_row + row) % A.group, tok = t + (first_row + row) / A.group;
+            const long long r = row_at(A, tok, head, member);
+            if (!whole) {
+                float* const slot = P.slots + part_slot(run, begins, HB, p) * 16 * (DH + 2);
+                *reinterpret_cast<float2*>(slot + row * DH + col) = make_float2(nx, ny);
+                if (col == 0) *reinterpret_cast<float2*>(slot + 16 * DH + row * 2) = make_float2(M, den);
+                // (the row's whole part: none)
+                if (col == 0 && P.keep && begins) *reinterpret_cast<float2*>(row_ml + r * 2) = make_float2(-INFINITY, 0.f);
+            } else if (P.keep) {
+                *reinterpret_cast<float2*>(row_o + r * DH + col) = make_float2(nx, ny);
+                if (col == 0) *reinterpret_cast<float2*>(row_ml + r * 2) = make_float2(M, den);
+            } else {
+                const float inv = den == 0.f ? 0.f : 1.f / den;           // no key: zeros
+                *reinterpret_cast<uint32_t*>(A.out + tok * A.o_t + head * A.o_h + member * A.o_g + col) = pack2(nx * inv, ny * inv);
+                if (col == 0) write_sums(A, r, M == -INFINITY ? 0.f : M, den);
+            }
+        };
+        if (BY_WARP) {
+            for (int idx = lane; idx < rows * (DH / 2); idx += 32) {
+                const int row = idx / (DH / 2), col = idx % (DH / 2) * 2;
+                const float2 v = *reinterpret_cast<const float2*>(acc + row * LDO + col);
+                put(hb, row, col, v.x, v.y, ms[warp][row], ls[warp][row]);
+            }
+            __syncwarp();                               // ... read before the next fetch overwrites them
+            seg = next;
+            at = end;
+            continue;
+        }
         // the group's pairs side by side, 16 rows each
         for (int idx = tid; idx < HB * 16 * (DH / 2); idx += THREADS) {
             const int x = idx / (DH / 2), col = idx % (DH / 2) * 2, p = x / 16, row = x % 16;
-            const int head = (seg.h + p) / tiles, first_row = (seg.h + p) % tiles * 16;
-            if (row >= all_rows - first_row) continue;
+            if (row >= all_rows - (seg.h + p) % tiles * 16) continue;
             float M = -INFINITY;
 #pragma unroll
             for (int w = 0; w < KW; ++w) M = fmaxf(M, ms[w * HB + p][row]);
@@ -436,22 +510,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
                 ny = fmaf(wgt, v.y, ny);
                 den = fmaf(wgt, ls[w * HB + p][row], den);
             }
-            const int member = (first_row + row) % A.group, tok = t + (first_row + row) / A.group;
-            const long long r = row_at(A, tok, head, member);
-            if (!whole) {
-                float* const slot = P.slots + part_slot(run, 0, begins, HB, p) * 16 * (DH + 2);
-                *reinterpret_cast<float2*>(slot + row * DH + col) = make_float2(nx, ny);
-                if (col == 0) *reinterpret_cast<float2*>(slot + 16 * DH + row * 2) = make_float2(M, den);
-                // (the row's whole part: none)
-                if (col == 0 && P.keep && begins) *reinterpret_cast<float2*>(row_ml + r * 2) = make_float2(-INFINITY, 0.f);
-            } else if (P.keep) {
-                *reinterpret_cast<float2*>(row_o + r * DH + col) = make_float2(nx, ny);
-                if (col == 0) *reinterpret_cast<float2*>(row_ml + r * 2) = make_float2(M, den);
-            } else {
-                const float inv = den == 0.f ? 0.f : 1.f / den;           // no key: zeros
-                *reinterpret_cast<uint32_t*>(A.out + tok * A.o_t + head * A.o_h + member * A.o_g + col) = pack2(nx * inv, ny * inv);
-                if (col == 0) write_sums(A, r, z, den);
-            }
+            put(p, row, col, nx, ny, M, den);
         }
         __syncthreads();                                // the warps' triples are read before the next fetch overwrites them
         seg = next;
@@ -464,8 +523,10 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
 // Adds up the parts of a pair's rows, in order: parts of whole rows, those of the shared keys, then those of the token's own.  A CTA per pair, or
 // (no `keep`) per run of the stream kernel's, for the pair that begins there and goes on.  First the weights of all parts, a warp per
 // row, then the sums, a thread per four columns, with sixteen loads under way.
-constexpr int kSumThreads = 256, kSumParts = 448;        // parts at most: whole rows' 2 x 64 + 1, and twice a part per SM
+constexpr int kSumThreads = 256, kSumParts = 544;        // parts at most: whole rows' 2 x 64, and twice a part per SM or kPartsAtMost + 2
 constexpr int kSumRows = 8;                              // rows at a time
+
+__host__ __device__ static inline int stream_warps(int d_head) { return d_head <= 128 ? 8 : 4; }
 
 template <int DH>
 __global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid_constant__ AttnView A, const __grid_constant__ StreamPlan P,
@@ -483,7 +544,7 @@ __global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid
     if (P.keep) {
         if (P.own) own = P.head[shared_heads + pair];
     } else {
-        const int run = (int)blockIdx.x / P.heads_at_once;
+        const int run = (int)blockIdx.x / P.heads_at_once * (P.by_warp ? 1 : stream_warps(DH) / P.heads_at_once);
         own = make_int2(run, P.run_head[run].y);
         if (own.y == 0) return;
         pair = P.run_head[run].x + (int)blockIdx.x % P.heads_at_once;
@@ -502,7 +563,7 @@ __global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid
             sh = P.head[sh_pair];
             sh_pair %= P.heads_at_once;
         }
-        const int n = M.n + sh.y + own.y;
+        const int sh_n = sh.y & 0xffff, n = M.n + sh_n + (own.y & 0xffff);
         float top = -INFINITY, den = 0.f;
         for (int i = lane; i < n; i += 32) {
             const float *o, *ml;
@@ -510,9 +571,10 @@ __global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid
                 o = M.o + (i * M.rows + r) * DH;
                 ml = M.ml + (i * M.rows + r) * 2;
             } else {
-                const bool s = i < M.n + sh.y;
-                const int k = i - M.n - (s ? 0 : sh.y), at = s ? (int)(folded % 16) : c0 - row0 + row;
-                const float* const slot = P.slots + part_slot(s ? sh.x : own.x, k, k == 0, P.heads_at_once, s ? sh_pair : h % P.heads_at_once) * SLOT;
+                const bool s = i < M.n + sh_n;
+                const int k = i - M.n - (s ? 0 : sh_n), at = s ? (int)(folded % 16) : c0 - row0 + row;
+                const int2 head = s ? sh : own;
+                const float* const slot = P.slots + part_slot(head.x + (long long)k * (head.y >> 16), k == 0, P.heads_at_once, s ? sh_pair : h % P.heads_at_once) * SLOT;
                 o = slot + at * DH;
                 ml = slot + 16 * DH + at * 2;
             }
@@ -566,29 +628,31 @@ __global__ void __launch_bounds__(kSumThreads) attention_sum_kernel(const __grid
     }
 }
 
-template <int DH, int HB>
+template <int DH, int HB, bool BY_WARP>
 dsmoe_status launch_stream_heads(const AttnView& A, const StreamPlan& plan, cudaStream_t s) {
+    auto* kernel = attention_stream_kernel<DH, HB, BY_WARP>;
     static bool attr[kMaxDeviceSlots] = {};
     int dev = 0;
     DeviceState* st = nullptr;
     DSMOE_TRY(device_state(&st, &dev));
     if (!attr[dev]) {
-        DSMOE_CUDA_TRY(cudaFuncSetAttribute(attention_stream_kernel<DH, HB>, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamGeo<DH>::SMEM));
+        DSMOE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, StreamGeo<DH>::SMEM));
         attr[dev] = true;
     }
-    DSMOE_CUDA_TRY(launch_chained(attention_stream_kernel<DH, HB>, (unsigned)plan.ctas, 32 * StreamGeo<DH>::WARPS, StreamGeo<DH>::SMEM, s, A, plan));
+    DSMOE_CUDA_TRY(launch_chained(kernel, (unsigned)plan.ctas, 32 * StreamGeo<DH>::WARPS, StreamGeo<DH>::SMEM, s, A, plan));
     return DSMOE_OK;
 }
 
 template <int DH>
 dsmoe_status launch_stream(const AttnView& A, const StreamPlan& plan, cudaStream_t s) {
-    if (plan.heads_at_once == 2) return launch_stream_heads<DH, 2>(A, plan, s);
-    return launch_stream_heads<DH, 1>(A, plan, s);
+    const bool by_warp = plan.by_warp;
+    if (plan.heads_at_once == 2) return by_warp ? launch_stream_heads<DH, 2, true>(A, plan, s) : launch_stream_heads<DH, 2, false>(A, plan, s);
+    return by_warp ? launch_stream_heads<DH, 1, true>(A, plan, s) : launch_stream_heads<DH, 1, false>(A, plan, s);
 }
 
 template <int DH>
 dsmoe_status launch_sum(const AttnView& A, const StreamPlan& plan, const RowParts& rows, cudaStream_t s) {
-    const long long ctas = plan.keep ? (long long)A.T * A.n_head * A.row_tiles : (long long)plan.passes * plan.ctas * plan.heads_at_once;
+    const long long ctas = plan.keep ? (long long)A.T * A.n_head * A.row_tiles : (long long)plan.passes * plan.ctas * (plan.by_warp ? stream_warps(A.d_head) : plan.heads_at_once);
     DSMOE_CUDA_TRY(launch_chained(attention_sum_kernel<DH>, (unsigned)ctas, kSumThreads, 0, s, A, plan, rows));
     return DSMOE_OK;
 }
@@ -611,9 +675,15 @@ dsmoe_status launch_sum(const AttnView& A, const StreamPlan& plan, const RowPart
 // Two where neighbouring heads are nearer than neighbouring positions (see the kernel)
 int stream_heads_at_once(const AttnView& A) { return A.n_head % 2 == 0 && A.kv_h < A.kv_p ? 2 : 1; }
 
+// As many pairs as warps (those of a list of tokens are not known here: few)
+bool stream_by_warp(const AttnView& A, const StreamPlan& plan) {
+    const long long pairs = plan.list ? 0 : (plan.own ? (long long)A.T * A.n_head * A.row_tiles : 0) + (long long)A.n_head * plan.shared.row_tiles;
+    return pairs >= (long long)plan.ctas * stream_warps(A.d_head);
+}
+
 // One CTA per SM, as far as each has a unit per warp in the longest case
 int stream_ctas(const AttnView& A, const SharedKeys& shared, bool own) {
-    const long long seen = A.window < A.L ? (long long)A.window + A.sinks : A.L, warps = A.d_head <= 128 ? 8 : 4;
+    const long long seen = A.window < A.L ? (long long)A.window + A.sinks : A.L, warps = stream_warps(A.d_head);
     long long units = own ? ((seen + kUnit - 1) / kUnit + 1) * ((long long)A.T * A.n_head * A.row_tiles) : 0;
     units += (long long)((shared.P + kUnit - 1) / kUnit) * A.n_head * shared.row_tiles;
     const long long wanted = (units + warps - 1) / warps, most = sm_count() < 160 ? sm_count() : 160;      // (kSumParts)

@@ -107,10 +107,11 @@ struct StreamPlan {
     // A pair that several CTAs share leaves a part per CTA; one that lies in one CTA's keys is written to out and lse, or (keep) its rows to `own_rows`
     // and `shared_rows`: something else is still to be added
     bool keep;
+    bool by_warp;                         // runs are warps', not CTAs'
     int heads_at_once;                    // neighbouring pairs of a token that a CTA takes together
-    float* slots;                         // [passes][ctas][2][heads_at_once][16][d_head + 2]
-    int2* head;                           // keep: [pairs]: first run, number of parts
-    int2* run_head;                       // otherwise: [passes][ctas]: the first of the pairs that begin in that run and go on, number of parts; or 0 parts
+    float* slots;                         // [passes][runs][2][heads_at_once][16][d_head + 2], runs = ctas * (8 or 4 warps) / heads_at_once
+    int2* head;                           // keep: [pairs]: first run, parts_word
+    int2* run_head;                       // otherwise: [passes][runs]: the first of the pairs that begin in that run and go on, parts_word; or 0 parts
     RowParts own_rows, shared_rows;       // n = 1
     float* logits;                        // nullable: the tokens' logits in base 2, row r's from r * logit_pitch on (no window, no ring)
     long long logit_pitch;                // a multiple of 16
@@ -132,6 +133,7 @@ dsmoe_status make_cache_map(CUtensorMap* m, const AttnView& A, const void* ptr, 
 dsmoe_status launch_tile_attention(const AttnView& A, const TilePlan& plan, cudaStream_t s);
 
 int stream_heads_at_once(const AttnView& A);
+bool stream_by_warp(const AttnView& A, const StreamPlan& plan);
 int stream_ctas(const AttnView& A, const SharedKeys& shared, bool own);       // CTAs of launch_stream_attention at most
 dsmoe_status launch_stream_attention(const AttnView& A, const StreamPlan& plan, cudaStream_t s);
 // Adds up what launch_stream_attention left in parts, into out and lse: without `keep` the pairs that several CTAs share; with it all rows, whose

@@ -57,6 +57,14 @@ def test_many_rows():
     run(Case([(i % 7, i % 40) for i in range(1200)], 1, 2, 64, 7, 40, P=100, seed=3))
 
 
+def test_many_short_caches():
+    """Runs of single warps that leave parts and whole rows, and the prefix's parts."""
+    rng = np.random.default_rng(8)
+    for n_head, P in ((8, 777), (16, 20)):
+        tokens = [(s, int(p)) for s, p in enumerate(rng.integers(-1, 300, 160))]
+        run(Case(tokens, n_head, 4, 64, 160, 300, P=P, seed=P))
+
+
 def test_prompts_behind_a_prefix():
     tokens = [(0, p) for p in range(120)] + [(1, p) for p in range(40, 90)]
     run(Case(tokens, 2, 5, 128, 2, 128, P=200, seed=4, hide=beyond(tokens)))

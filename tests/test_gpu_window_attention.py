@@ -102,6 +102,16 @@ def test_caches_by_position_with_many_runs():
     run(Case([(s, 300 + s) for s in range(50)], 6, 5, 64, 50, 350, seed=17, by_token=True), 2 ** 31 - 1)
 
 
+@pytest.mark.parametrize("by_token", [False, True])
+def test_many_short_pairs(by_token):
+    """As many pairs as warps and more: runs of single warps, some of which cut pairs in two; whole ones beside them; padding."""
+    rng = np.random.default_rng(18)
+    tokens = [(s, int(p)) for s, p in enumerate(rng.integers(-1, 400, 320))]
+    run(Case(tokens, 4, 3, 64, 320, 400, seed=18, by_token=by_token), 2 ** 31 - 1)
+    tokens = [(s % 40, 3000 - 7 * (s % 40)) for s in range(200)]
+    run(Case(tokens, 8, 17, 32, 40, 3001, seed=19, by_token=by_token), 100, 4)
+
+
 def test_parts_of_larger_tensors():
     """A slice of a larger cache, queries that are a slice and broadcast over the members, outputs with gaps that are left as they were."""
     c = Case([(0, 20), (1, 44)], 2, 4, 64, 2, 45, seed=7)
