@@ -114,7 +114,7 @@ constexpr int kMaxTallyParts = 16;
 constexpr size_t kMostLogits = (size_t)512 << 20;
 
 struct AttnPlan {
-    size_t slots, head, run_head, count, list, ml, logits, sums, row_o, row_ml, total;
+    size_t slots, head, run_head, count, list, ml, logits, sums, tokens, row_o, row_ml, total;
     int tally_parts;                      // tally on the 128-row tiles: parts of the rows; 0: not there
     long long logit_pitch;                // tally: 0 if the logits are not kept
     int ctas, passes;                     // of the stream kernel, at most
@@ -178,6 +178,7 @@ AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, b
             const size_t cells = (size_t)A.n_seq * A.n_head * A.L;
             const long long ctas = (long long)A.n_seq * A.n_head * ((A.L + 127) / 128);
             w.tally_parts = (int)std::max(1ll, std::min(4ll * sm_count() / ctas, (long long)kMaxTallyParts));
+            w.tokens = take(((size_t)A.T + A.n_seq) * sizeof(int2));
             if (w.tally_parts > 1) w.sums = take(w.tally_parts * cells * 4);
         }
     }
@@ -356,7 +357,8 @@ dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void*
     DSMOE_TRY(attend(A, SharedKeys{}, w, static_cast<char*>(workspace), s));
     if (w.logit_pitch)
         return launch_tally_add(A, reinterpret_cast<const float*>(static_cast<char*>(workspace) + w.logits), w.logit_pitch, tally_in, tally_out, s);
-    return launch_tally(A, w.tally_parts, reinterpret_cast<float*>(static_cast<char*>(workspace) + w.sums), tally_in, tally_out, s);
+    int2* const tokens = reinterpret_cast<int2*>(static_cast<char*>(workspace) + w.tokens);
+    return launch_tally(A, w.tally_parts, reinterpret_cast<float*>(static_cast<char*>(workspace) + w.sums), tokens, tokens + A.T, tally_in, tally_out, s);
 }
 
 dsmoe_status dsmoe_evict_workspace_size(const dsmoe_attention_desc* desc, size_t* bytes) {

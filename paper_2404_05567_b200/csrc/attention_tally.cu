@@ -219,7 +219,61 @@ __global__ void __launch_bounds__(32 * kTallyWarps) attention_tally_kernel(const
 
 // ---------------------------------------------------------------- prompts, on the 5th-generation tensor cores
 
-constexpr int kTtKeys = 128, kTtRows = 128, kTtThreads = 256, kTtList = 1024;
+constexpr int kTtKeys = 128, kTtRows = 128, kTtThreads = 256, kTtAhead = 4;
+
+// The tokens of every sequence, in order, with their last visible keys: sequence s's are list[from[s].x .. + from[s].y - 1].  A CTA per sequence.
+// (Each CTA of the next launch looked through all tokens itself at first: 16 rounds of 256 for 4000 tokens, 20 of its 60 us.)
+__global__ void __launch_bounds__(1024) tally_list_kernel(const __grid_constant__ AttnView A, int2* list, int2* from) {
+    __shared__ int warp_s[2][32];
+    chain_wait();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, s = (int)blockIdx.x;
+    int before = 0, n = 0;                // tokens of earlier sequences; of this one, so far
+    for (int turn = 0; turn < 2; ++turn) {
+        n = 0;
+        for (int t0 = 0; t0 < A.T; t0 += 1024 * kTtAhead) {
+            int last[kTtAhead], less = 0, mine = 0;
+#pragma unroll
+            for (int i = 0; i < kTtAhead; ++i) {
+                const int t = t0 + tid * kTtAhead + i;
+                last[i] = -1;
+                if (t < A.T) {
+                    bool bad = false;
+                    const Sight w = sight_of(A, t, &bad);
+                    less += w.last >= 0 && w.seq < s;
+                    if (w.seq == s) last[i] = w.last;
+                    mine += last[i] >= 0;
+                }
+            }
+            if (turn == 0) {
+                before += less;           // (this thread's)
+                continue;
+            }
+            int incl = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += up;
+            }
+            __syncthreads();
+            if (lane == 31) warp_s[0][warp] = incl;
+            __syncthreads();
+            const int w = warp_s[0][lane];
+            int at = n + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + incl - mine;
+            n += __reduce_add_sync(0xffffffffu, w);
+#pragma unroll
+            for (int i = 0; i < kTtAhead; ++i)
+                if (last[i] >= 0) list[before + at++] = make_int2(t0 + tid * kTtAhead + i, last[i]);
+        }
+        if (turn == 0) {
+            before = __reduce_add_sync(0xffffffffu, before);
+            if (lane == 0) warp_s[1][warp] = before;
+            __syncthreads();
+            before = __reduce_add_sync(0xffffffffu, warp_s[1][lane]);
+        }
+    }
+    if (tid == 0) from[s] = make_int2(before, n);
+    chain_next();
+}
 
 template <int DH>
 struct TallyGeo {
@@ -232,7 +286,8 @@ struct TallyGeo {
 struct TallyArgs {
     AttnView A;
     int at_pos, at_head, at_seq;
-    int key_tiles, parts;
+    int parts;
+    const int2 *list, *from;              // the sequences' tokens
     const float* in;                      // parts == 1: the tallies
     float* out;                           // ... or [parts][n_seq * n_head * L]
 };
@@ -240,7 +295,8 @@ struct TallyArgs {
 // Whether all of the four fetching warps' threads say so
 __device__ __forceinline__ bool fetchers_agree(bool x) {
     uint32_t all;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "=r"(all) : "r"((uint32_t)x) : "memory");
     return all != 0;
 }
@@ -250,7 +306,8 @@ __global__ void __launch_bounds__(kTtThreads, 2) attention_tally_tile_kernel(con
     using G = TallyGeo<DH>;
     constexpr int CH = DH / 8, KS = DH / 16;
     extern __shared__ unsigned char tt_smem[];
-    __shared__ int list_s[kTtList], last_s[kTtList], count_s[kTtThreads / 32];
+    __shared__ int first_s, last_s;       // the first and the last of the sequence's tokens that see a key of this tile
+    __shared__ long long q_s[kTtRows];    // where the rows' queries are; -1: no row
     __shared__ __align__(16) float2 ml_s[2][kTtRows];
     __shared__ __align__(16) int row_last_s[2][kTtRows];
     __shared__ int all_see_s[2];
@@ -284,64 +341,71 @@ __global__ void __launch_bounds__(kTtThreads, 2) attention_tally_tile_kernel(con
     chain_wait();
     const uint32_t tmem = tmem_s;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    int done = 0, seen_tiles = 0;         // tiles of rows that this CTA has taken; that there were
+    int done = 0;                         // tiles of rows that this CTA has taken
     bool alive = true;
-    for (int t0 = 0; t0 < A.T; t0 += kTtList) {
-        // the tokens of this sequence, among the next 1024, that see a key of this tile: in order
-        int n = 0;
-        __syncthreads();
-        for (int c = 0; c < kTtList && t0 + c < A.T; c += kTtThreads) {
-            const int t = t0 + c + tid;
-            bool bad = false, mine = false;
-            int last = -1;
-            if (t < A.T) {
-                const Sight w = sight_of(A, t, &bad);
-                mine = w.seq == s && w.last >= key0;
-                last = w.last;
+    const int2 from = P.from[s];
+    const int2* const list = P.list + from.x;
+    if (tid == 0) {
+        first_s = 0x7fffffff;
+        last_s = -1;
+    }
+    __syncthreads();
+    {
+        int first = 0x7fffffff, last = -1;
+        for (int i = tid; i < from.y; i += kTtThreads)
+            if (list[i].y >= key0) {
+                first = min(first, i);
+                last = i;
             }
-            const uint32_t votes = __ballot_sync(0xffffffffu, mine);
-            if (lane == 0) count_s[warp] = __popc(votes);
-            __syncthreads();
-            int at = n;
-            for (int w = 0; w < kTtThreads / 32; ++w) {
-                if (w < warp) at += count_s[w];
-                n += count_s[w];
-            }
-            if (mine) {
-                at += __popc(votes & ((1u << lane) - 1u));
-                list_s[at] = t;
-                last_s[at] = last;
-            }
-            __syncthreads();
+        first = __reduce_min_sync(0xffffffffu, first);
+        last = __reduce_max_sync(0xffffffffu, last);
+        if (lane == 0 && last >= 0) {
+            atomicMin(&first_s, first);
+            atomicMax(&last_s, last);
         }
-        const int tiles = (n + tokens - 1) / tokens;
-        for (int i = 0; i < tiles; ++i, ++seen_tiles) {
-            if (seen_tiles % P.parts != part || !alive) continue;
+    }
+    __syncthreads();
+    {
+        const int i0 = first_s, n = last_s < 0 ? 0 : last_s + 1 - i0, tiles = (n + tokens - 1) / tokens;
+        // a fetching thread's row: its token and sums, asked for a tile ahead
+        const int at = tid - 128;
+        const bool row = warp >= 4 && at < tokens * A.group;
+        const int of = row ? at / A.group : 0, member = row ? at % A.group : 0;
+        int2 token = make_int2(0, -1);
+        float2 ml = make_float2(0.f, 0.f);
+        const auto ask = [&](int i) {
+            const int k = i * tokens + of;
+            token = row && k < n ? list[i0 + k] : make_int2(0, -1);
+            ml = token.y >= 0 ? A.ml[row_at(A, token.x, j, member)] : make_float2(0.f, 0.f);
+        };
+        ask(part);
+        for (int i = part; i < tiles; i += P.parts) {
+            if (!alive) break;
             const int b = done & 1;
             const uint32_t turn = (uint32_t)(done >> 1) & 1u;
             if (warp >= 4) {
                 // ---- the rows' queries and sums
-                if (done >= 2) alive = ptx::mbar_wait(ptx::smem_u32(&s_empty[b]), turn ^ 1u, &abort_flag);
+                if (done >= 2) alive = ptx::mbar_sleep(ptx::smem_u32(&s_empty[b]), turn ^ 1u, &abort_flag);
                 alive = fetchers_agree(alive);          // (they meet below, or none does)
-                const int at = tid - 128;
                 if (alive) {
-                    const int token = i * tokens + at / A.group;
-                    const bool real = at < tokens * A.group && token < n;
-                    ml_s[b][at] = real ? A.ml[row_at(A, list_s[token], j, at % A.group)] : make_float2(0.f, 0.f);
-                    row_last_s[b][at] = real ? last_s[token] : -1;
-                    if (at == 0) all_see_s[b] = 1;
+                    const bool partial = token.y >= 0 && token.y < key0 + kTtKeys - 1;
+                    q_s[at] = token.y >= 0 ? token.x * A.q_t + j * A.q_h + member * A.q_g : -1;
+                    ml_s[b][at] = ml;
+                    row_last_s[b][at] = token.y;
+                    const bool all = fetchers_agree(!partial);         // (and the rows' places are there)
+                    if (at == 0) all_see_s[b] = all;
                     for (int idx = at; idx < kTtRows * CH; idx += 128) {
-                        const int row = idx / CH, ch = idx % CH, tk = i * tokens + row / A.group;
-                        const bool is = row < tokens * A.group && tk < n;
-                        const __nv_bfloat16* q = A.q + (is ? list_s[tk] : 0) * A.q_t + j * A.q_h + row % A.group * A.q_g + ch * 8;
-                        const uint32_t dst = base + G::Q + b * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(q), "r"(is ? 16u : 0u) : "memory");
+                        const int rw = idx / CH, ch = idx % CH;
+                        const long long q = q_s[rw];
+                        const uint32_t dst = base + G::Q + b * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + rw * 128 + (((ch & 7) ^ (rw & 7)) << 4));
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(A.q + (q < 0 ? 0 : q) + ch * 8), "r"(q < 0 ? 0u : 16u) : "memory");
                     }
+                    if (i + P.parts < tiles) ask(i + P.parts);
                     ptx::cp_async_commit();
                     ptx::cp_async_wait<0>();
                     ptx::fence_proxy_async();
+                    __syncwarp();
                     asm volatile("bar.sync 1, 128;" ::: "memory");
-                    if (real && last_s[token] < key0 + kTtKeys - 1) all_see_s[b] = 0;
                     ptx::mbar_arrive(ptx::smem_u32(&rows_full[b]));
                 }
                 if (warp == 4 && alive) {
@@ -354,7 +418,7 @@ __global__ void __launch_bounds__(kTtThreads, 2) attention_tally_tile_kernel(con
                             c[P.at_pos] = key0, c[P.at_head] = j, c[P.at_seq] = s;
 #pragma unroll
                             for (int h = 0; h < G::HALVES; ++h) ptx::tma_load_4d(base + G::K + h * G::PIECE, &mapK, bar, h * 64, c[1], c[2], c[3]);
-                            keys = ptx::mbar_wait(bar, 0, &abort_flag);
+                            keys = ptx::mbar_sleep(bar, 0, &abort_flag);
                         }
                         ptx::tc_fence_after();
                         const uint32_t q0 = base + G::Q + b * G::TILE, idesc = ptx::make_idesc_bf16(kTtKeys, kTtRows);
@@ -368,7 +432,7 @@ __global__ void __launch_bounds__(kTtThreads, 2) attention_tally_tile_kernel(con
                 }
             } else {
                 // ---- a key's weights
-                alive = ptx::mbar_wait(ptx::smem_u32(&rows_full[b]), turn, &abort_flag) && ptx::mbar_wait(ptx::smem_u32(&s_full[b]), turn, &abort_flag);
+                alive = ptx::mbar_sleep(ptx::smem_u32(&rows_full[b]), turn, &abort_flag) && ptx::mbar_sleep(ptx::smem_u32(&s_full[b]), turn, &abort_flag);
                 alive = __all_sync(0xffffffffu, alive);
                 if (alive) {
                     ptx::tc_fence_after();
@@ -432,7 +496,7 @@ __global__ void __launch_bounds__(256) tally_parts_kernel(const float* sums, con
 }
 
 template <int DH>
-dsmoe_status launch_tally_tile(const AttnView& A, int parts, float* sums, const float* tally_in, float* tally_out, cudaStream_t s) {
+dsmoe_status launch_tally_tile(const AttnView& A, int parts, float* sums, int2* list, int2* from, const float* tally_in, float* tally_out, cudaStream_t s) {
     using G = TallyGeo<DH>;
     static bool attr[kMaxDeviceSlots] = {};
     int dev = 0;
@@ -446,10 +510,11 @@ dsmoe_status launch_tally_tile(const AttnView& A, int parts, float* sums, const 
     int at[3];
     DSMOE_TRY(make_cache_map(&mapK, A, A.K, at));
     const int key_tiles = ceil_div(A.L, kTtKeys);
+    DSMOE_CUDA_TRY(launch_chained(tally_list_kernel, (unsigned)A.n_seq, 1024, 0, s, A, list, from));
     const size_t cells = (size_t)A.n_seq * A.n_head * A.L;
     const long long ctas = (long long)A.n_seq * A.n_head * key_tiles * parts;
     if (ctas > 0x7fffffffll || (cells + 255) / 256 > 0x7fffffffull) return DSMOE_ERR_UNSUPPORTED;
-    const TallyArgs P{A, at[0], at[1], at[2], key_tiles, parts, tally_in, parts > 1 ? sums : tally_out};
+    const TallyArgs P{A, at[0], at[1], at[2], parts, list, from, tally_in, parts > 1 ? sums : tally_out};
     DSMOE_CUDA_TRY(launch_chained(attention_tally_tile_kernel<DH>, (unsigned)ctas, kTtThreads, G::SMEM, s, mapK, P));
     if (parts > 1) DSMOE_CUDA_TRY(launch_chained(tally_parts_kernel, (unsigned)((cells + 255) / 256), 256, 0, s, sums, parts, cells, tally_in, tally_out));
     return DSMOE_OK;
@@ -481,11 +546,11 @@ dsmoe_status launch_tally_add(const AttnView& A, const float* logits, long long 
     return DSMOE_OK;
 }
 
-dsmoe_status launch_tally(const AttnView& A, int parts, float* sums, const float* tally_in, float* tally_out, cudaStream_t s) {
+dsmoe_status launch_tally(const AttnView& A, int parts, float* sums, int2* list, int2* from, const float* tally_in, float* tally_out, cudaStream_t s) {
     if (parts > 0) {
-        if (A.d_head == 64) return launch_tally_tile<64>(A, parts, sums, tally_in, tally_out, s);
-        if (A.d_head == 96) return launch_tally_tile<96>(A, parts, sums, tally_in, tally_out, s);
-        return launch_tally_tile<128>(A, parts, sums, tally_in, tally_out, s);
+        if (A.d_head == 64) return launch_tally_tile<64>(A, parts, sums, list, from, tally_in, tally_out, s);
+        if (A.d_head == 96) return launch_tally_tile<96>(A, parts, sums, list, from, tally_in, tally_out, s);
+        return launch_tally_tile<128>(A, parts, sums, list, from, tally_in, tally_out, s);
     }
     switch (A.d_head) {
         case 32: return launch_tally_dh<32>(A, tally_in, tally_out, s);

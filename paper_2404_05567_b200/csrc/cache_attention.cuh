@@ -142,8 +142,8 @@ dsmoe_status launch_attention_sum(const AttnView& A, const StreamPlan& plan, con
 
 // tally_out[s][j][l] = tally_in[s][j][l] (nullptr: 0) + the sum of the softmax weights that the tokens of sequence s gave key l, from A.ml.
 // Causal alone: no window, no ring.  parts > 0 (tile_supported): on the 5th-generation tensor cores, the rows cut into so many parts, whose sums go to
-// `sums`, [parts][n_seq * n_head * L], with more than one.
-dsmoe_status launch_tally(const AttnView& A, int parts, float* sums, const float* tally_in, float* tally_out, cudaStream_t s);
+// `sums`, [parts][n_seq * n_head * L], with more than one; list [T] and from [n_seq]: scratch.
+dsmoe_status launch_tally(const AttnView& A, int parts, float* sums, int2* list, int2* from, const float* tally_in, float* tally_out, cudaStream_t s);
 
 // The same from the logits that launch_stream_attention left of every token (StreamPlan); up to kListTokens tokens
 dsmoe_status launch_tally_add(const AttnView& A, const float* logits, long long pitch, const float* tally_in, float* tally_out, cudaStream_t s);
