@@ -39,7 +39,7 @@ struct Stretch {
 
 struct TileShared {
     // (in one row: a thread each sets them up)
-    uint64_t k_full[4], k_empty[4], v_full[4], v_clear[4], v_empty[4], s_full[2], p_full[2], o_done[2], stagger;
+    uint64_t k_full[4], k_empty[4], v_full[4], v_clear[4], v_empty[4], s_full[2], p_full[2][2], o_done[2];
     uint32_t tmem;
     volatile int abort_flag;
     int n_stretches, n_runs;
@@ -52,7 +52,7 @@ struct TileShared {
     float swap[2][2][kTileRows];          // the halves of a row's threads tell each other
     Stretch st[kMaxStretches];
 };
-constexpr int kTileBars = 27, kFirstPFull = 22;
+constexpr int kTileBars = 28, kFirstPFull = 22;
 static_assert(offsetof(TileShared, tmem) == kTileBars * 8 && offsetof(TileShared, p_full) == kFirstPFull * 8, "the barriers in a row");
 
 __device__ __forceinline__ float exp2_fast(float v) {
@@ -176,7 +176,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
     const int span = 2 * P.tile_tokens, tg0 = block * span, ng = min(A.T - tg0, span);
     const int tiles_of_rows = ng > P.tile_tokens ? 2 : 1;
     if (tid < kTileBars) {
-        ptx::mbar_init(ptx::smem_u32(&S.k_full[0]) + 8u * tid, tid == kFirstPFull || tid == kFirstPFull + 1 ? 2 * kTileRows : 1);
+        ptx::mbar_init(ptx::smem_u32(&S.k_full[0]) + 8u * tid, tid >= kFirstPFull && tid < kFirstPFull + 4 ? 2 * kTileRows : 1);
         ptx::fence_barrier_init();
     }
     if (warp == kMmaWarp) {
@@ -387,13 +387,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             if (n > 0) {
                 ok = ptx::mbar_sleep(ptx::smem_u32(&S.k_full[0]), 0, &S.abort_flag);
                 if (ok) {
-                    logits(0, 0);
-                    if (tiles_of_rows > 1) {
-                        // The second tile begins half a turn behind the first, and stays there: side by side, both would be at their exponentials, and
-                        // then both would wait for the tensor pipe
-                        ok = ptx::mbar_sleep(ptx::smem_u32(&S.stagger), 0, &S.abort_flag);
-                        logits(0, 1);
-                    }
+                    for (int r = 0; r < tiles_of_rows; ++r) logits(0, r);
                     ptx::umma_commit(ptx::smem_u32(&S.k_empty[0]));
                 }
             }
@@ -403,15 +397,22 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 if (ok && i + 1 < n)
                     ok = ptx::mbar_sleep(ptx::smem_u32(&S.k_full[(i + 1) % STAGES]), (uint32_t)(((i + 1) / STAGES) & 1), &S.abort_flag);
                 for (int r = 0; ok && r < tiles_of_rows; ++r) {
-                    ok = ptx::mbar_sleep(ptx::smem_u32(&S.p_full[r]), (uint32_t)(i & 1), &S.abort_flag);
-                    if (!ok) break;
-                    ptx::tc_fence_after();
                     const uint32_t v0 = base + G::V + s * G::TILE;
-                    // (the weights of keys 0 .. 63 lie in the first 32 columns of those keys' logits, and the others' in the first of theirs)
+                    // The weights of keys 0 .. 63 lie in the first 32 columns of those keys' logits, and the others' in the first of theirs; each 64
+                    // come in two parts, and the first ones' products run while the rows' threads are at the second
 #pragma unroll
-                    for (int k = 0; k < kTileKeys / 16; ++k)
-                        umma_bf16_ts(tmem + 256 + r * 128, tmem + r * 128 + (k >> 2) * 64 + (k & 3) * 8, make_desc_values(v0 + k * 2048), idesc_o,
-                                     (uint32_t)(i != 0 || k != 0));
+                    for (int part = 0; part < 2; ++part) {
+                        ok = ok && ptx::mbar_sleep(ptx::smem_u32(&S.p_full[r][part]), (uint32_t)(i & 1), &S.abort_flag);
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int k = (q >> 1) * 4 + part * 2 + (q & 1);
+                            umma_bf16_ts(tmem + 256 + r * 128, tmem + r * 128 + (k >> 2) * 64 + (k & 3) * 8, make_desc_values(v0 + k * 2048), idesc_o,
+                                         (uint32_t)(i != 0 || k != 0));
+                        }
+                    }
+                    if (!ok) break;
                     ptx::umma_commit(ptx::smem_u32(&S.o_done[r]));
                     if (i + 1 < n) logits(i + 1, r);
                 }
@@ -438,7 +439,6 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         if (r < tiles_of_rows) {
             const uint32_t place = tS + half * 64;
             const uint64_t scale2 = pair_of(sl2, sl2);
-            bool told = false;
             for (int i = 0; i < n; ++i) {
                 const Tile t = tile_at(S, begin + i, stretch);
                 // keys a .. b of this half of the tile are the row's, and those before c
@@ -480,6 +480,12 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 const bool none = __any_sync(0xffffffffu, m == -INFINITY);
                 uint32_t v[64];                   // logits, then (0 .. 31) the weights in pairs
                 float sum;
+                const auto tell = [&](int part) {
+                    tmem_st16(place + part * 16, *reinterpret_cast<uint32_t(*)[16]>(v + part * 16));
+                    tmem_st_wait();
+                    ptx::tc_fence_before();
+                    ptx::mbar_arrive(ptx::smem_u32(&S.p_full[r][part]));
+                };
                 while (true) {
                     const float z = m == -INFINITY ? 0.f : -m;
                     const uint64_t z2 = pair_of(z, z);
@@ -512,13 +518,12 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                             s2[k & 1] = add2(s2[k & 1], pair_of(x, y));
                             v[k] = pack2(x, y);
                         }
+                        if (part == 0 && !none) tell(0);
                     }
                     float x, y;
                     halves_of(add2(s2[0], s2[1]), x, y);
                     sum = x + y;
                     top = fmaxf(top, top2) * sl2;
-                    if (i == 0 && tid == 0 && !told) ptx::mbar_arrive(ptx::smem_u32(&S.stagger));
-                    told = true;
                     if (!none || !pair_any(pair, m == -INFINITY && top != -INFINITY)) break;
                     S.swap[r][half][at] = top;
                     pair_sync(pair);
@@ -526,11 +531,8 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 }
                 S.tops[i & 1][r][half][at] = top;
                 l += sum;
-                tmem_st16(place, v);
-                tmem_st16(place + 16, v + 16);
-                tmem_st_wait();
-                ptx::tc_fence_before();
-                ptx::mbar_arrive(ptx::smem_u32(&S.p_full[r]));
+                if (none) tell(0);
+                tell(1);
             }
             // (one phase to wait for: the last logits came behind the last but one tile's P.V)
             if (n > 0) alive = ptx::mbar_sleep(ptx::smem_u32(&S.o_done[r]), (uint32_t)((n - 1) & 1), &S.abort_flag) && alive;
