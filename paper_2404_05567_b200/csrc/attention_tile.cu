@@ -108,6 +108,20 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// 32 columns, waited for.  (A wait of its own needs a fence for each of the 32 registers, and those cost moves.)
+__device__ __forceinline__ void tmem_ld32_now(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -328,6 +342,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
     ptx::tc_fence_after();
     const uint32_t tmem = S.tmem;
     const int begin = S.begin, n = S.end - S.begin;
+    bool not_finite = false;              // this thread's row
 
     if (warp == kLoadWarp) {
         // ---- copies
@@ -476,63 +491,63 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                         }
                     }
                 }
-                // whether some row has no maximum yet: the same for both halves, which then find one together
-                const bool none = __any_sync(0xffffffffu, m == -INFINITY);
-                uint32_t v[64];                   // logits, then (0 .. 31) the weights in pairs
-                float sum;
-                const auto tell = [&](int part) {
-                    tmem_st16(place + part * 16, *reinterpret_cast<uint32_t(*)[16]>(v + part * 16));
+                const auto logits_of = [&](int part, uint32_t (&x)[32]) {
+                    tmem_ld32_now(place + part * 32, x);
+                    if (!full) {
+                        const uint32_t bits = (uint32_t)(seen >> (32 * part));
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] = bits & (1u << k) ? x[k] : 0xff800000u;   // -inf
+                    }
+                };
+                // Rows that have no maximum yet (m is the same in both halves) find one first
+                if (__any_sync(0xffffffffu, m == -INFINITY)) {
+                    top = -INFINITY;
+#pragma unroll 1
+                    for (int part = 0; part < 2; ++part) {
+                        uint32_t x[32];
+                        logits_of(part, x);
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2) top = max3(top, __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+                    }
+                    S.swap[r][half][at] = top * sl2;
+                    pair_sync(pair);
+                    if (m == -INFINITY) m = fmaxf(top * sl2, S.swap[r][half ^ 1][at]);
+                }
+                const float z = m == -INFINITY ? 0.f : -m;
+                const uint64_t z2 = pair_of(z, z);
+                uint64_t s2[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+                float top2 = -INFINITY;
+                top = -INFINITY;
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    uint32_t x[32], w[16];
+                    logits_of(part, x);
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) {
+                        top = max3(top, __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+                        top2 = max3(top2, __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float a, b;
+                        halves_of(fma2(pair_of(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), scale2, z2), a, b);
+                        a = exp2_fast(a);
+                        b = exp2_fast(b);
+                        s2[k & 1] = add2(s2[k & 1], pair_of(a, b));
+                        w[k] = pack2(a, b);
+                    }
+                    tmem_st16(place + part * 16, w);
+                    if (part == 1) {
+                        top = fmaxf(top, top2) * sl2;
+                        S.tops[i & 1][r][half][at] = top;
+                    }
                     tmem_st_wait();
                     ptx::tc_fence_before();
                     ptx::mbar_arrive(ptx::smem_u32(&S.p_full[r][part]));
-                };
-                while (true) {
-                    const float z = m == -INFINITY ? 0.f : -m;
-                    const uint64_t z2 = pair_of(z, z);
-                    uint64_t s2[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
-                    float top2 = -INFINITY;
-                    top = -INFINITY;
-                    ptx::tmem_ld32(place, *reinterpret_cast<uint32_t(*)[32]>(v));
-#pragma unroll
-                    for (int part = 0; part < 2; ++part) {        // (the second 32 are on their way while the first are worked on)
-                        ptx::tmem_ld_wait();
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) asm volatile("" : "+r"(v[part * 32 + k]));
-                        if (part == 0) ptx::tmem_ld32(place + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
-                        const uint32_t bits = (uint32_t)(seen >> (32 * part));
-                        if (!full) {
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) v[part * 32 + k] = bits & (1u << k) ? v[part * 32 + k] : 0xff800000u;   // -inf
-                        }
-#pragma unroll
-                        for (int k = part * 32; k < part * 32 + 32; k += 4) {
-                            top = max3(top, __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
-                            top2 = max3(top2, __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
-                        }
-#pragma unroll
-                        for (int k = part * 16; k < part * 16 + 16; ++k) {
-                            float x, y;
-                            halves_of(fma2(pair_of(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), scale2, z2), x, y);
-                            x = exp2_fast(x);
-                            y = exp2_fast(y);
-                            s2[k & 1] = add2(s2[k & 1], pair_of(x, y));
-                            v[k] = pack2(x, y);
-                        }
-                        if (part == 0 && !none) tell(0);
-                    }
-                    float x, y;
-                    halves_of(add2(s2[0], s2[1]), x, y);
-                    sum = x + y;
-                    top = fmaxf(top, top2) * sl2;
-                    if (!none || !pair_any(pair, m == -INFINITY && top != -INFINITY)) break;
-                    S.swap[r][half][at] = top;
-                    pair_sync(pair);
-                    if (m == -INFINITY) m = fmaxf(top, S.swap[r][half ^ 1][at]);
                 }
-                S.tops[i & 1][r][half][at] = top;
-                l += sum;
-                if (none) tell(0);
-                tell(1);
+                float s_a, s_b;
+                halves_of(add2(s2[0], s2[1]), s_a, s_b);
+                l += s_a + s_b;
             }
             // (one phase to wait for: the last logits came behind the last but one tile's P.V)
             if (n > 0) alive = ptx::mbar_sleep(ptx::smem_u32(&S.o_done[r]), (uint32_t)((n - 1) & 1), &S.abort_flag) && alive;
@@ -604,7 +619,8 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                     if (to >= 0) *reinterpret_cast<uint4*>(A.out + to + half * HC + ch * 8) = *reinterpret_cast<const uint4*>(stage + rw * LINE + ((ch ^ (rw % SLOTS)) << 4));
                 }
             }
-            if (taken && check != 0.f) S.redo[r * kTileRows + at] = 1;
+            not_finite = taken && check != 0.f;
+            if (not_finite) S.redo[r * kTileRows + at] = 1;
             if (half == 0) {
                 if (P.o) {
                     if (real)
@@ -620,11 +636,12 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
     }
     chain_next();
     ptx::tc_fence_before();
-    __syncthreads();
+    const bool again = __syncthreads_or(not_finite) != 0;
     if (warp == kMmaWarp) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, 512);
     }
+    if (!again) return;
     // ---- rows that came out as no numbers: a warp per row, a key at a time, over this CTA's tiles
     for (int rr = warp; rr < 2 * kTileRows; rr += kTileThreads / 32) {
         if (!S.redo[rr]) continue;
