@@ -22,7 +22,7 @@ namespace dsmoe {
 namespace {
 
 // A block of up to kFewRuns runs (prompts' ends and beginnings) is taken as it is: each costs a pass over its keys
-constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 608, kLoadWarp = 16, kMmaWarp = 17, kClearWarp = 18, kFewRuns = 4, kMaxRuns = 16, kMaxStretches = 3 * kMaxRuns;
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 608, kLoadWarp = 16, kMmaWarp = 17, kClearWarp = 18, kFewRuns = 4, kMaxRuns = 16, kMaxStretches = 3 * kMaxRuns, kSightWarps = 8;
 
 template <int DH>
 struct TileGeo {
@@ -42,7 +42,7 @@ struct TileShared {
     uint64_t k_full[4], k_empty[4], v_full[4], v_clear[4], v_empty[4], s_full[2], p_full[2][2], o_done[2];
     uint32_t tmem;
     volatile int abort_flag;
-    int n_stretches, n_runs;
+    int n_stretches, n_runs, alike;      // (alike: of one sequence)
     int begin, end;                       // this CTA's tiles
     long long q_at[2 * kTileRows];        // where a row's queries are; -1: no row
     int seq[2 * kTileRows], first[2 * kTileRows], last[2 * kTileRows], run[2 * kTileRows];
@@ -151,6 +151,11 @@ __device__ __forceinline__ void pair_sync(int id) {
     asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
 }
 
+__device__ __forceinline__ void sight_sync() {
+    __syncwarp();
+    asm volatile("bar.sync 9, %0;" ::"n"(32 * (kSightWarps + 1)) : "memory");
+}
+
 struct TileArgs {
     AttnView A;
     int tile_tokens;                      // tokens of a 128-row tile
@@ -205,77 +210,12 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
     if (tid == 0) {
         S.abort_flag = 0;
         S.n_runs = 1;
+        S.alike = 1;
         S.run_lo[0] = 0x7fffffff;
         S.run_hi[0] = -1;
     }
     __syncthreads();
     chain_wait();
-    // ---- what the tokens see, and the runs
-    bool bad = false, like = true;
-    if (warp * 32 < ng) {
-        int lo = 0x7fffffff, hi = -1;
-        if (tid < ng) {
-            const Sight s = sight_of(A, tg0 + tid, &bad);
-            like = s.seq == (A.tok_seq ? min(max(A.tok_seq[tg0], 0), A.n_seq - 1) : 0);
-            hi = s.last;
-            const int first = hi >= A.window ? hi - A.window + 1 : 0;
-            if (hi >= 0) lo = first;
-            S.seq[tid] = s.seq;
-            S.last[tid] = hi;
-            S.first[tid] = first;
-        }
-        // (of one run: of all tokens)
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        if (lane == 0) {
-            atomicMin(&S.run_lo[0], lo);
-            atomicMax(&S.run_hi[0], hi);
-        }
-        if (bad) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
-    }
-    const bool alike = __syncthreads_and(like) != 0;
-    if (!alike) {
-        if (tid < ng) {
-            S.run_len[tid] = 0;
-            S.run_lo[tid] = 0x7fffffff;
-            S.run_hi[tid] = -1;
-        }
-        if (warp == 0) {                  // a token's run: how many runs begin at or before it, less one
-            int before = 0;
-            for (int c = 0; c < ng; c += 32) {
-                const int t = c + lane;
-                const bool begins = t < ng && t > 0 && S.seq[t] != S.seq[t - 1];
-                const uint32_t votes = __ballot_sync(0xffffffffu, begins);
-                if (t < ng) S.run[t] = before + __popc(votes & (0xffffffffu >> (31 - lane)));
-                before += __popc(votes);
-            }
-            if (lane == 0) S.n_runs = before + 1;
-        }
-        __syncthreads();
-        if (tid < ng) {
-            const int r = S.run[tid];
-            atomicAdd(&S.run_len[r], 1);
-            if (S.last[tid] >= 0) {
-                atomicMin(&S.run_lo[r], S.first[tid]);
-                atomicMax(&S.run_hi[r], S.last[tid]);
-            }
-        }
-        __syncthreads();
-    }
-    const bool takes_all = alike || !P.count || S.n_runs <= kFewRuns;
-    if (split == 0 && P.head && tid < ng)
-        for (int i = 0; i < A.row_tiles; ++i) P.head[((long long)(tg0 + tid) * A.n_head + j) * A.row_tiles + i] = make_int2(0, 0);
-    if (warp == 1 && split == 0 && j == 0 && P.count) {        // the tokens that are left, in order
-        int n = 0;
-        for (int c = 0; c < ng && !takes_all; c += 32) {
-            const int t = c + lane;
-            const bool left = t < ng && S.run_len[S.run[t]] < P.least_run;
-            const uint32_t votes = __ballot_sync(0xffffffffu, left);
-            if (left) P.list[(long long)block * span + n + __popc(votes & ((1u << lane) - 1u))] = tg0 + t;
-            n += __popc(votes);
-        }
-        if (lane == 0) P.count[block] = n;
-    }
     int load_at = 0;                      // the stretch of the load warp's next tile
     const auto load = [&](const CUtensorMap* map, uint32_t dst, uint64_t* bar, const Tile& t) {
         const uint32_t b = ptx::smem_u32(bar);
@@ -285,49 +225,120 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
 #pragma unroll
         for (int h = 0; h < G::HALVES; ++h) ptx::tma_load_4d(dst + h * G::PIECE, map, b, h * 64, c[1], c[2], c[3]);
     };
-    if (warp == kLoadWarp) {
-        // ---- the stretches, and the first tiles' copies
-        if (ptx::elect_one()) {
-            int n = 0, tiles = 0, t = 0;
-            const auto put = [&](int run, int seq, int pos0, int count) {
-                while (count > 0) {       // (in a ring, up to its end and then from its beginning)
-                    const int slot = slot_of(A, pos0), m = A.ring && pos0 >= A.sinks ? min(count, A.L - slot) : count;
-                    S.st[n++] = Stretch{run, seq, slot, pos0, m, tiles};
-                    tiles += (m + kTileKeys - 1) / kTileKeys;
-                    pos0 += m;
-                    count -= m;
-                    if (n == kMaxStretches) return;
-                }
-            };
-            const int n_runs = alike ? 1 : S.n_runs;
-            for (int r = 0; r < n_runs; ++r) {
-                const int len = alike ? ng : S.run_len[r], lo = S.run_lo[r], hi = S.run_hi[r];
-                if ((takes_all || len >= P.least_run) && hi >= 0 && n + 3 <= kMaxStretches) {
-                    const int sinks = min(A.sinks, hi + 1);
-                    if (lo <= sinks) {
-                        put(r, S.seq[t], 0, hi + 1);
-                    } else {
-                        put(r, S.seq[t], 0, sinks);
-                        put(r, S.seq[t], lo, hi + 1 - lo);
-                    }
-                }
-                t += len;
+    if (warp < kSightWarps || warp == kLoadWarp) {
+        // ---- what the tokens see, and the runs
+        bool bad = false, like = true;
+        if (warp * 32 < ng) {
+            int lo = 0x7fffffff, hi = -1;
+            if (tid < ng) {
+                const Sight s = sight_of(A, tg0 + tid, &bad);
+                like = s.seq == (A.tok_seq ? min(max(A.tok_seq[tg0], 0), A.n_seq - 1) : 0);
+                hi = s.last;
+                const int first = hi >= A.window ? hi - A.window + 1 : 0;
+                if (hi >= 0) lo = first;
+                S.seq[tid] = s.seq;
+                S.last[tid] = hi;
+                S.first[tid] = first;
             }
-            S.n_stretches = n;
-            const int begin = P.splits == 1 ? 0 : (int)((long long)tiles * split / P.splits);
-            const int end = P.splits == 1 ? tiles : (int)((long long)tiles * (split + 1) / P.splits);
-            S.begin = begin;
-            S.end = end;
-            for (int i = 0; i < min(STAGES, end - begin); ++i) {
-                const Tile x = tile_at(S, begin + i, load_at);
-                load(&mapK, base + G::K + i * G::TILE, &S.k_full[i], x);
-                load(&mapV, base + G::V + i * G::TILE, &S.v_full[i], x);
+            // (of one run: of all tokens)
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            hi = __reduce_max_sync(0xffffffffu, hi);
+            if (lane == 0) {
+                atomicMin(&S.run_lo[0], lo);
+                atomicMax(&S.run_hi[0], hi);
             }
+            if (bad) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
         }
-        __syncwarp();
+        if (__any_sync(0xffffffffu, !like) && lane == 0) S.alike = 0;
+        sight_sync();
+        const bool alike = S.alike != 0;
+        if (!alike) {
+            if (tid < ng) {
+                S.run_len[tid] = 0;
+                S.run_lo[tid] = 0x7fffffff;
+                S.run_hi[tid] = -1;
+            }
+            if (warp == 0) {                  // a token's run: how many runs begin at or before it, less one
+                int before = 0;
+                for (int c = 0; c < ng; c += 32) {
+                    const int t = c + lane;
+                    const bool begins = t < ng && t > 0 && S.seq[t] != S.seq[t - 1];
+                    const uint32_t votes = __ballot_sync(0xffffffffu, begins);
+                    if (t < ng) S.run[t] = before + __popc(votes & (0xffffffffu >> (31 - lane)));
+                    before += __popc(votes);
+                }
+                if (lane == 0) S.n_runs = before + 1;
+            }
+            sight_sync();
+            if (tid < ng) {
+                const int r = S.run[tid];
+                atomicAdd(&S.run_len[r], 1);
+                if (S.last[tid] >= 0) {
+                    atomicMin(&S.run_lo[r], S.first[tid]);
+                    atomicMax(&S.run_hi[r], S.last[tid]);
+                }
+            }
+            sight_sync();
+        }
+        const bool takes_all = alike || !P.count || S.n_runs <= kFewRuns;
+        if (split == 0 && P.head && tid < ng)
+            for (int i = 0; i < A.row_tiles; ++i) P.head[((long long)(tg0 + tid) * A.n_head + j) * A.row_tiles + i] = make_int2(0, 0);
+        if (warp == 1 && split == 0 && j == 0 && P.count) {        // the tokens that are left, in order
+            int n = 0;
+            for (int c = 0; c < ng && !takes_all; c += 32) {
+                const int t = c + lane;
+                const bool left = t < ng && S.run_len[S.run[t]] < P.least_run;
+                const uint32_t votes = __ballot_sync(0xffffffffu, left);
+                if (left) P.list[(long long)block * span + n + __popc(votes & ((1u << lane) - 1u))] = tg0 + t;
+                n += __popc(votes);
+            }
+            if (lane == 0) P.count[block] = n;
+        }
+        if (warp == kLoadWarp) {
+            // ---- the stretches, and the first tiles' copies
+            if (ptx::elect_one()) {
+                int n = 0, tiles = 0, t = 0;
+                const auto put = [&](int run, int seq, int pos0, int count) {
+                    while (count > 0) {       // (in a ring, up to its end and then from its beginning)
+                        const int slot = slot_of(A, pos0), m = A.ring && pos0 >= A.sinks ? min(count, A.L - slot) : count;
+                        S.st[n++] = Stretch{run, seq, slot, pos0, m, tiles};
+                        tiles += (m + kTileKeys - 1) / kTileKeys;
+                        pos0 += m;
+                        count -= m;
+                        if (n == kMaxStretches) return;
+                    }
+                };
+                const int n_runs = alike ? 1 : S.n_runs;
+                for (int r = 0; r < n_runs; ++r) {
+                    const int len = alike ? ng : S.run_len[r], lo = S.run_lo[r], hi = S.run_hi[r];
+                    if ((takes_all || len >= P.least_run) && hi >= 0 && n + 3 <= kMaxStretches) {
+                        const int sinks = min(A.sinks, hi + 1);
+                        if (lo <= sinks) {
+                            put(r, S.seq[t], 0, hi + 1);
+                        } else {
+                            put(r, S.seq[t], 0, sinks);
+                            put(r, S.seq[t], lo, hi + 1 - lo);
+                        }
+                    }
+                    t += len;
+                }
+                S.n_stretches = n;
+                const int begin = P.splits == 1 ? 0 : (int)((long long)tiles * split / P.splits);
+                const int end = P.splits == 1 ? tiles : (int)((long long)tiles * (split + 1) / P.splits);
+                S.begin = begin;
+                S.end = end;
+                for (int i = 0; i < min(STAGES, end - begin); ++i) {
+                    const Tile x = tile_at(S, begin + i, load_at);
+                    load(&mapK, base + G::K + i * G::TILE, &S.k_full[i], x);
+                    load(&mapV, base + G::V + i * G::TILE, &S.v_full[i], x);
+                }
+            }
+            __syncwarp();
+        }
     } else {
         // ---- queries, in the swizzle's order; rows that are none are zeros
-        for (int idx = warp < kLoadWarp ? tid : tid - 32; idx < tiles_of_rows * kTileRows * CH; idx += kTileThreads - 32) {
+        constexpr int QUERY_THREADS = kTileThreads - 32 * (kSightWarps + 1);
+        for (int idx = tid - 32 * (warp < kLoadWarp ? kSightWarps : kSightWarps + 1); idx < tiles_of_rows * kTileRows * CH; idx += QUERY_THREADS) {
             const int row = idx / CH, ch = idx % CH, r = row >> 7, at = row & 127;
             const long long from = S.q_at[row];
             const uint32_t dst = base + G::Q + r * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + at * 128 + (((ch & 7) ^ (at & 7)) << 4));
@@ -335,11 +346,16 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         }
         ptx::cp_async_commit();
     }
+    // the rows' threads: two each, with 64 of a tile's 128 logits and half of O's columns
+    const int r = warp >> 3, half = (warp >> 2) & 1, at = (warp & 3) * 32 + lane;      // row tile, half, row of the tile = lane of tensor memory
+    const int tl = r * P.tile_tokens + at / A.group, m_of = at % A.group;
+    const bool real = at < P.tile_tokens * A.group && tl < ng;
     ptx::cp_async_wait<0>();
     ptx::fence_proxy_async();
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
+    const bool alike = S.alike != 0, takes_all = alike || !P.count || S.n_runs <= kFewRuns;
     const uint32_t tmem = S.tmem;
     const int begin = S.begin, n = S.end - S.begin;
     bool not_finite = false;              // this thread's row
@@ -438,10 +454,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
         }
         __syncwarp();
     } else {
-        // ---- rows: two threads each, with 64 of a tile's 128 logits and half of O's columns
-        const int r = warp >> 3, half = (warp >> 2) & 1, at = (warp & 3) * 32 + lane;      // row tile, half, row of the tile = lane of tensor memory
-        const int tl = r * P.tile_tokens + at / A.group, m_of = at % A.group;
-        const bool real = at < P.tile_tokens * A.group && tl < ng;
+        // ---- rows
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + r * 128, tO = tmem + lanes + 256 + r * 128 + half * (DH / 2);
         const int pair = 1 + r * 4 + (warp & 3);                          // the barrier of the two warps that share rows
