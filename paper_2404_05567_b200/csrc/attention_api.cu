@@ -246,6 +246,12 @@ dsmoe_status attend(const AttnView& A, const SharedKeys& S, const AttnPlan& w, c
     } else if (plan.keep) {
         plan.own_rows = next_parts(1);
     }
+    if (plan.own && stream_whole(A, plan)) {
+        plan.whole = true;
+        plan.heads_at_once = 1;
+        plan.ctas = A.T * A.n_head * A.row_tiles;
+        return launch_stream_attention(A, plan, s);
+    }
     plan.ctas = std::min(w.ctas, stream_ctas(A, plan.shared, plan.own));
     plan.by_warp = stream_by_warp(A, plan);
     if (plan.keep) plan.head = head;

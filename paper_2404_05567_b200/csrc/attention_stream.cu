@@ -176,6 +176,8 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         for (int w = 0; w < WARPS; ++w) longest = max(longest, longest_s[w]);
         wanted = max(1ll, min(min((long long)gridDim.x * KW, total), kPartsAtMost * total / longest));
     }
+    const int pairs_each = own_heads / HB;              // pairs (of HB heads) of a token
+    if (P.whole) wanted = (long long)n * pairs_each;
     const int n_runs = (int)wanted, stride = BY_WARP ? 1 : KW, run_no = BY_WARP ? (int)blockIdx.x * KW + kw : (int)blockIdx.x;
     if (run_no >= n_runs) {
         __syncwarp();
@@ -187,7 +189,16 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         const long long cut = extra * (share + 1);
         return u < cut ? u / (share + 1) : extra + (u - cut) / share;
     };
-    const long long u0 = run_start(run_no), u1 = run_start(run_no + 1);
+    long long u0, u1;
+    if (P.whole) {
+        const int e = run_no / pairs_each;
+        const long long units = (base_s[e + 1] - base_s[e]) / pairs_each;
+        u0 = base_s[e] + run_no % pairs_each * units;
+        u1 = u0 + units;
+    } else {
+        u0 = run_start(run_no);
+        u1 = run_start(run_no + 1);
+    }
     // where a run's parts lie, and the next run's after it
     const long long run = (long long)pass * P.ctas * KW + (long long)run_no * stride;
 
@@ -231,9 +242,11 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
     }
     Cursor ahead = seg;                                 // the next unit to fetch
     const int hop = BY_WARP ? 1 : KW, begin = BY_WARP ? 0 : kw;
-    ahead.k += begin;
-    settle(ahead);
     long long u_ahead = u0 + begin;
+    if (u_ahead < u1) {
+        ahead.k += begin;
+        settle(ahead);
+    }
     unsigned char* const ring = as_smem + (size_t)warp * BUFS * G::UNIT;
     const uint32_t ring0 = ptx::smem_u32(ring);
     const auto fetch = [&](int buf) {
@@ -275,9 +288,11 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd + dst), "l"(V + src), "r"(nbytes) : "memory");
                 }
             }
-            ahead.k += hop;
-            settle(ahead);
             u_ahead += hop;
+            if (u_ahead < u1) {                         // (settling may wait for a token's sequence and position)
+                ahead.k += hop;
+                settle(ahead);
+            }
         }
         ptx::cp_async_commit();
     };
@@ -425,9 +440,9 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
             buf = buf + 1 == BUFS ? 0 : buf + 1;
         }
         Cursor next = seg;
-        next.k += (int)(end - at);
-        settle(next);
         if (end < u1) {
+            next.k += (int)(end - at);
+            settle(next);
             if (!BY_WARP) ask_queries(next);            // (on their way while the triples meet)
         } else if (pass + 1 == P.passes) {
             chain_next();
@@ -674,6 +689,14 @@ dsmoe_status launch_sum(const AttnView& A, const StreamPlan& plan, const RowPart
 
 // Two where neighbouring heads are nearer than neighbouring positions (see the kernel)
 int stream_heads_at_once(const AttnView& A) { return A.n_head % 2 == 0 && A.kv_h < A.kv_p ? 2 : 1; }
+
+// Whether a CTA takes all of a pair's keys, so that no part is left to add up: the second launch and the parts' way through memory cost as much as three
+// rounds of a unit a warp, so where the CTAs that stay idle would save fewer.  One launch, and two, us: a token of 4 heads and 256 keys 7.5,
+// 9.4, 384 8.8, 9.4, 512 10.3, 9.6; 16 such tokens with 512 keys 11.0, 13.9, 1024 16.0, 16.4; 32 with 2048 28.7, 33.2.
+bool stream_whole(const AttnView& A, const StreamPlan& plan) {
+    const long long seen = A.window < A.L ? (long long)A.window + A.sinks : A.L, pairs = (long long)A.T * A.n_head * A.row_tiles;
+    return !plan.keep && !plan.list && pairs <= sm_count() && seen * (sm_count() - pairs) <= 3ll * kUnit * stream_warps(A.d_head) * sm_count();
+}
 
 // As many pairs as warps (those of a list of tokens are not known here: few)
 bool stream_by_warp(const AttnView& A, const StreamPlan& plan) {

@@ -108,6 +108,7 @@ struct StreamPlan {
     // and `shared_rows`: something else is still to be added
     bool keep;
     bool by_warp;                         // runs are warps', not CTAs'
+    bool whole;                           // each CTA's run is a pair's units: no parts (not with shared keys, a list or more than a pass)
     int heads_at_once;                    // neighbouring pairs of a token that a CTA takes together
     float* slots;                         // [passes][runs][2][heads_at_once][16][d_head + 2], runs = ctas * (8 or 4 warps) / heads_at_once
     int2* head;                           // keep: [pairs]: first run, parts_word
@@ -133,6 +134,7 @@ dsmoe_status make_cache_map(CUtensorMap* m, const AttnView& A, const void* ptr, 
 dsmoe_status launch_tile_attention(const AttnView& A, const TilePlan& plan, cudaStream_t s);
 
 int stream_heads_at_once(const AttnView& A);
+bool stream_whole(const AttnView& A, const StreamPlan& plan);
 bool stream_by_warp(const AttnView& A, const StreamPlan& plan);
 int stream_ctas(const AttnView& A, const SharedKeys& shared, bool own);       // CTAs of launch_stream_attention at most
 dsmoe_status launch_stream_attention(const AttnView& A, const StreamPlan& plan, cudaStream_t s);

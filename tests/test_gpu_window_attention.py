@@ -206,3 +206,13 @@ def test_the_same_bits_every_time_on_any_stream_and_in_a_graph():
     once(c.out, c.lse, flipped)
     torch.cuda.synchronize()
     assert torch.equal(outs[1], c.out)
+
+
+@pytest.mark.parametrize("d", [64, 128, 160])
+@pytest.mark.parametrize("T,keys", [(1, 1), (1, 192), (1, 193), (1, 210), (1, 384), (1, 394), (1, 410), (1, 2500), (7, 420), (7, 460), (20, 500),
+                                    (20, 560), (40, 700), (73, 900), (75, 230), (80, 1000)])
+def test_pairs_of_one_cta_and_pairs_cut_into_parts(T, keys, d):
+    """Few pairs of few keys are a CTA's each; with more keys, or more pairs than SMs, they leave parts.  Tokens of one key and of none among them."""
+    tokens = [(t, keys - 1 - 3 * t if t % 5 != 3 else [0, -1][t % 2]) for t in range(T)]
+    run(Case(tokens, 2, 5, d, T, keys + 3, seed=T + keys, hide=unseen(tokens, 2 ** 31 - 1, 0)), 2 ** 31 - 1)
+    run(Case(tokens, 2, 5, d, T, keys + 3, seed=T + keys, hide=unseen(tokens, keys // 2 + 1, 4), by_token=True), keys // 2 + 1, 4)
