@@ -1,11 +1,17 @@
 // Attention of many rows that share their keys (prompts; a batch's shared prefix) on the 5th-generation tensor cores.
 //
 // A CTA owns up to 256 rows (neighbouring tokens' query heads of one key/value head) as two tiles of 128, and walks the keys that any of them sees in
-// tiles of 128 keys, which both tiles use.  Per tile of rows and keys: S = Q.K^T into tensor memory; a row's two threads take its logits from there, its weights 2^(logit - m) go back as bf16 where the logits lay, and O += P.V with P as the operand in tensor
-// memory and V as it lies in memory (N-major).  The running maximum hardly ever moves (kMoves); if it does, the row's threads rescale O in
-// tensor memory.  Roles: warps 0-7 and 8-15 are the two tiles' rows, two
-// threads a row; warp 16 copies (TMA, a ring of tiles), warp 17 issues the MMAs, warp 18 clears the values behind a stretch's last key (0
-// times what is no number is no number).  While one tile's threads are at their weights the tensor pipe works for the other one.
+// tiles of 128 keys, which both tiles use.  Per tile of rows and keys: S = Q.K^T into tensor memory; a row's two threads take its logits from
+// there, its weights 2^(logit - m) go back as bf16 where the logits lay, and O += P.V with P as the operand in tensor memory and V as it lies in
+// memory (N-major).  The weights are rounded to bf16 (by 2^-8 of each at most): the tensor pipe takes no wider ones at this rate.  Sums and O are
+// fp32.  The running maximum hardly ever moves (kMoves); if it does, the row's threads rescale O in tensor memory.
+// Roles: warps 0-7 and 8-15 are the two tiles' rows, two threads a row; warp 16 copies (TMA, a ring of tiles), warp 17 issues the MMAs, warp 18 clears
+// the values behind a stretch's last key (0 times what is no number is no number).  While one tile's threads are at their weights the tensor
+// pipe works for the other one.
+// Bound by the threads' way from logits to weights: a step of 256 rows and 128 keys of 128 numbers takes 3400 cycles, of which the exponentials
+// alone take the special-function units 2048 and the MMAs the tensor pipe 2100; with an eighth of the MMAs a call still took four fifths of its time.
+// 8192 tokens of 4 x 5 heads with a window of 4096: 271 us, 0.57 of the tensor rate.  Tried there, us: a quarter of the
+// exponentials by polynomial 289 (276 without), the two row tiles taking turns at their exponentials 312 (311 without).
 //
 // What a CTA's tokens see: tokens of one sequence that follow one another are a run; a run's keys are at most three stretches of slots (sinks, and
 // the window, cut in two where a ring ends).  In blocks of many runs, those too short to be worth a
