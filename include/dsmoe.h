@@ -358,7 +358,7 @@ dsmoe_status dsmoe_moa_forward(const dsmoe_layer_desc* desc, const dsmoe_moa_arg
  *            sequence's cache; -1: none (a padded entry of the batch: zeros in out, -inf in lse).
  *   lse      fp32 [T][n_head][group] or NULL: the natural logarithm of the sum of the exponentials of a row's logits.
  *
- * All strides are multiples of 8 elements, addresses of 16 bytes.  d_head a multiple of 32 up to 256, group up to 64, otherwise
+ * All strides are multiples of 8 elements, addresses of 16 bytes.  d_head a multiple of 32 up to 256, group up to 64, L up to 2^30, otherwise
  * DSMOE_ERR_UNSUPPORTED.  The memory from out's first element to its last must not overlap q's or the caches'.  Products of bf16 are added
  * in fp32, softmax statistics are fp32, and out is rounded once; the weights that multiply the values are two bf16 numbers each (as good as
  * 16 bits), on the 128-row tiles of prompts and long prefixes one.  Keys that a token does not see may hold anything, numbers or not.  A tok_seq or pos entry out of range is clamped and reported
@@ -383,9 +383,9 @@ dsmoe_status dsmoe_attention_workspace_size(const dsmoe_attention_desc* desc, in
  * Attention with a sliding window and sinks: token t at position p = pos[t] sees key l iff 0 <= l <= p and (p - l < window or l < sinks).
  *   window >= 1, sinks >= 0.
  *   rolling 0: position l lies in slot l of the cache, pos[t] < L.  rolling 1: the cache keeps the first `sinks` positions and the latest
- *   others: position l lies in slot l (l < sinks) or sinks + (l - sinks) % (L - sinks); pos[t] has no bound, window <= L - sinks.  The caller
+ *   others: position l lies in slot l (l < sinks) or sinks + (l - sinks) % (L - sinks); pos[t] < 2^31 - 1, window <= L - sinks.  The caller
  *   sees to it that the keys that the call's tokens see are all there: with n neighbouring tokens of a sequence in one call, window + n - 1
- *   <= L - sinks.
+ *   <= L - sinks.  (Where that is not so, tokens get what lies in the slots, or less; a call that notices reports DSMOE_ERR_INVALID_ARG.)
  */
 dsmoe_status dsmoe_window_attention(const dsmoe_attention_desc* desc, int window, int sinks, int rolling, const void* q, const void* K,
                                     const void* V, const int32_t* tok_seq, const int32_t* pos, void* out, float* lse, void* workspace,

@@ -47,7 +47,7 @@ dsmoe_status check_cache(const dsmoe_attention_desc* d) {
     if (d->n_head <= 0 || d->d_head <= 0 || d->n_seq <= 0 || d->L <= 0) return DSMOE_ERR_INVALID_ARG;
     if (!strides_ok(d->kv_stride, 3)) return DSMOE_ERR_INVALID_ARG;
     if (d->d_head % 32 || d->d_head > 256) return DSMOE_ERR_UNSUPPORTED;
-    if ((long long)d->n_seq * d->n_head > INT_MAX / 4) return DSMOE_ERR_UNSUPPORTED;
+    if (d->L > 1 << 30 || (long long)d->n_seq * d->n_head > INT_MAX / 4) return DSMOE_ERR_UNSUPPORTED;
     for (int i = 0; i < 3; ++i)
         if (d->kv_stride[i] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
     return DSMOE_OK;
@@ -271,7 +271,7 @@ dsmoe_status check_prefix(const dsmoe_attention_desc* d, const dsmoe_prefix* p, 
     if (!p || p->P < 0) return DSMOE_ERR_INVALID_ARG;
     if (p->P == 0) return DSMOE_OK;
     if (!p->Kp || !p->Vp || !aligned16(p->Kp) || !aligned16(p->Vp) || !strides_ok(p->stride, 2)) return DSMOE_ERR_INVALID_ARG;
-    if (p->stride[0] > (1ll << 40) || p->stride[1] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
+    if (p->P > 1 << 30 || p->stride[0] > (1ll << 40) || p->stride[1] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
     const int64_t n[3] = {d->T, d->n_head, d->group}, c[3] = {1, d->n_head, p->P}, st[3] = {0, p->stride[0], p->stride[1]};
     const Extent o = extent(out, d->o_stride, n, d->d_head, 2);
     if (o.meets(extent(p->Kp, st, c, d->d_head, 2)) || o.meets(extent(p->Vp, st, c, d->d_head, 2))) return DSMOE_ERR_INVALID_ARG;
@@ -290,6 +290,7 @@ dsmoe_status dsmoe_attention_workspace_size(const dsmoe_attention_desc* desc, in
     DSMOE_TRY(check_attention(desc));
     if (!bytes || kind < DSMOE_ATTENTION_WINDOW || kind > DSMOE_ATTENTION_TALLY) return DSMOE_ERR_INVALID_ARG;
     if (kind == DSMOE_ATTENTION_PREFIX && prefix_len < 0) return DSMOE_ERR_INVALID_ARG;
+    if (kind == DSMOE_ATTENTION_PREFIX && prefix_len > 1 << 30) return DSMOE_ERR_UNSUPPORTED;
     const AttnView A = view_of(*desc, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
     if (desc->T == 0) {
         *bytes = 0;

@@ -316,7 +316,12 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 };
                 const int n_runs = alike ? 1 : S.n_runs;
                 for (int r = 0; r < n_runs; ++r) {
-                    const int len = alike ? ng : S.run_len[r], lo = S.run_lo[r], hi = S.run_hi[r];
+                    const int len = alike ? ng : S.run_len[r], hi = S.run_hi[r];
+                    int lo = S.run_lo[r];
+                    if (A.ring && hi - max(lo, A.sinks) >= A.ring) {      // more positions than a ring holds: the latest of them, and no more
+                        lo = hi - A.ring + 1;
+                        report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
+                    }
                     if ((takes_all || len >= P.least_run) && hi >= 0 && n + 3 <= kMaxStretches) {
                         const int sinks = min(A.sinks, hi + 1);
                         if (lo <= sinks) {
@@ -476,8 +481,9 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             for (int i = 0; i < n; ++i) {
                 const Tile t = tile_at(S, begin + i, stretch);
                 // keys a .. b of this half of the tile are the row's, and those before c
-                const int off = half * 64, pos = t.pos + off;
-                const int b = t.run == run ? min(last - pos, t.n - 1 - off) : -1, a = first - pos, c = A.sinks - pos;
+                // (positions reach 2^31 - 2, so they are compared before anything is added)
+                const int off = half * 64;
+                const int b = t.run == run ? min(max(last - t.pos, -1), t.n - 1) - off : -1, a = max(first - t.pos, 0) - off, c = max(A.sinks - t.pos, 0) - off;
                 // (rows that are nobody's see anything; the same sequence may have two runs in this block)
                 const bool full = __all_sync(0xffffffffu, !taken || (b >= 63 && (a <= 0 || c >= 64)));
                 uint64_t seen = ~0ull;

@@ -8,6 +8,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <limits.h>
 
 #include "common.cuh"
 
@@ -53,11 +54,11 @@ struct Sight {
 // A token's sequence and position, clamped into the cache; *bad: they were not in it
 __device__ __forceinline__ Sight sight_of(const AttnView& A, int t, bool* bad) {
     int sq = A.tok_seq ? A.tok_seq[t] : 0, p = A.pos ? A.pos[t] : A.L - 1;
-    if (sq < 0 || sq >= A.n_seq || p < -1 || (!A.ring && p >= A.L)) {
+    const int most = A.ring ? INT_MAX - 1 : A.L - 1;      // (one more than a position is still a number)
+    if (sq < 0 || sq >= A.n_seq || p < -1 || p > most) {
         *bad = true;
         sq = min(max(sq, 0), A.n_seq - 1);
-        p = max(p, -1);
-        if (!A.ring) p = min(p, A.L - 1);
+        p = min(max(p, -1), most);
     }
     Sight s;
     s.seq = sq;

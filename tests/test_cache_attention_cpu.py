@@ -99,6 +99,11 @@ def test_calls_that_are_refused(name, more, tail):
         assert _call(name, d, more, tail=tail, **kw) == 3, kw
 
 
+def test_caches_of_more_positions_than_are_counted():
+    assert _size(_desc(L=2 ** 30, kv_stride=(0, 0, 0)))[0] == 0 and _size(_desc(L=2 ** 30 + 1, kv_stride=(0, 0, 0)))[0] == 2
+    assert _size(_desc(), dm.ATTENTION_PREFIX, 2 ** 30)[0] == 0 and _size(_desc(), dm.ATTENTION_PREFIX, 2 ** 30 + 1)[0] == 2
+
+
 def test_windows_that_are_refused():
     for window, sinks, rolling in ((0, 0, 0), (-1, 0, 0), (4, -1, 0), (4, 0, 2), (4, 0, -1), (31, 2, 1), (1, 32, 1), (33, 0, 1)):
         assert _call("dsmoe_window_attention", _desc(), (window, sinks, rolling)) == 1, (window, sinks, rolling)

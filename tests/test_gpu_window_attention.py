@@ -216,3 +216,47 @@ def test_pairs_of_one_cta_and_pairs_cut_into_parts(T, keys, d):
     tokens = [(t, keys - 1 - 3 * t if t % 5 != 3 else [0, -1][t % 2]) for t in range(T)]
     run(Case(tokens, 2, 5, d, T, keys + 3, seed=T + keys, hide=unseen(tokens, 2 ** 31 - 1, 0)), 2 ** 31 - 1)
     run(Case(tokens, 2, 5, d, T, keys + 3, seed=T + keys, hide=unseen(tokens, keys // 2 + 1, 4), by_token=True), keys // 2 + 1, 4)
+
+
+@pytest.mark.parametrize("d,group", [(64, 5), (128, 2), (32, 5)])
+def test_the_last_positions_of_a_rolling_cache(d, group, monkeypatch):
+    """A prompt that ends at the last position there is, on the 128-row tiles and on the streaming kernel; padding and a young token beside it."""
+    import cache_attention_reference as ref
+    monkeypatch.setattr(ref, "visible", lambda p, w, k: sorted(set(range(max(0, p - w + 1), p + 1)) | set(range(min(k, p + 1)))))
+    last, window, sinks = 2 ** 31 - 2, 200, 3
+    tokens = [(0, p) for p in range(last - 79, last + 1)] + [(0, -1), (1, -1), (1, 5), (2, last)]
+    run(Case(tokens, 1, group, d, 3, window + 79 + sinks, seed=d), window, sinks, True)
+
+
+def test_tokens_too_far_apart_for_a_rolling_cache(monkeypatch):
+    """A young and an old token of one sequence, whose keys cannot all be in its ring: the call ends, reports it, and others have their results."""
+    import cache_attention_reference as ref
+    monkeypatch.setattr(ref, "visible", lambda p, w, k: sorted(set(range(max(0, p - w + 1), p + 1)) | set(range(min(k, p + 1)))))
+    last, window, sinks = 2 ** 31 - 2, 60, 3
+    tokens = [(0, p) for p in range(200, 240)] + [(1, 5), (1, last)] + [(2, p) for p in range(40)]
+    c = Case(tokens, 1, 3, 64, 3, 110, seed=1)
+    call(c, window, sinks, True)
+    assert c.status.item() == 1
+    want = c.expected(window, sinks, True)
+    out, lse = torch.from_numpy(want[0]).bfloat16(), torch.from_numpy(want[1]).float()
+    c.out[40:42], c.lse[40:42] = out[40:42].cuda(), lse[40:42].cuda()
+    c.check(want)
+
+
+def test_positions_that_are_none_are_reported():
+    """Beyond the last one, and of a sequence that there is not: taken as the nearest, and reported."""
+    c = Case([(0, 2 ** 31 - 1), (1, -2), (1, 7)], 2, 5, 64, 2, 40, seed=1)
+    c.tok_seq[2] = 2
+    call(c, 20, 3, True)
+    assert c.status.item() == 1
+    c.check(nearest(c))
+
+
+def nearest(c):
+    import cache_attention_reference as ref
+    c.tokens = [(0, 2 ** 31 - 2), (1, -1), (1, 7)]
+    plain, ref.visible = ref.visible, lambda p, w, k: sorted(set(range(max(0, p - w + 1), p + 1)) | set(range(min(k, p + 1))))
+    try:
+        return c.expected(20, 3, True)
+    finally:
+        ref.visible = plain
