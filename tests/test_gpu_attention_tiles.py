@@ -171,3 +171,16 @@ def test_the_same_bits_every_time_and_in_a_graph():
     torch.cuda.synchronize()
     assert torch.equal(c.out, first) and torch.equal(outs[0], outs[1])
     assert c.status.item() == 0
+
+
+def test_offsets_beyond_32_bits():
+    """Prompts at the end of a cache of more than 2^32 elements."""
+    L, d = 17_000_000, 128
+    K, V = (torch.empty((2, 1, L, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    c = Case(prompt(1, 199, 60) + prompt(0, 150, 50), 1, 5, d, 2, 200, seed=16)
+    K[:, :, -200:], V[:, :, -200:] = c.K, c.V
+    want = c.expected(90, 0)
+    c.K, c.V, c.pos = K, V, (c.pos + (L - 200)).to(torch.int32)
+    call(c, 90, 0)
+    c.check(want)
+    assert c.status.item() == 0

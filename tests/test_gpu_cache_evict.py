@@ -126,3 +126,27 @@ def test_in_a_graph_and_again():
     first = kept[0][0, 0].long()
     for m in (0, 50, 99):
         assert torch.equal(K[0, 0, m], saved[1][0, 0, first[kept[1][0, 0, m]]])
+
+
+@pytest.mark.parametrize("how", ["apart", "in place"])
+def test_offsets_beyond_32_bits(how):
+    """A cache of more than 2^32 elements: what stays lies at its end and at its beginning."""
+    L, d, keep, recent = 17_000_000, 128, 40, 25
+    K, V = (torch.zeros((2, 1, L, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    tally = torch.zeros((2, 1, L), device="cuda")
+    stay = [0, 5, 4000, 8_400_000, 8_500_000, 12_000_000, L - 40_000, L - 300] + list(range(L - 32, L))
+    at = torch.tensor(stay, device="cuda")
+    K[:, 0, at], V[:, 0, at] = (torch.randn((2, keep, d), device="cuda").bfloat16() for _ in range(2))
+    want_K, want_V = K[:, 0, at].clone(), V[:, 0, at].clone()
+    tally[:, :, at] = torch.rand((2, 1, keep), device="cuda") + 1
+    want_tally = tally[:, :, at].clone()
+    length = torch.tensor([L, L], dtype=torch.int32, device="cuda")
+    kept = torch.zeros((2, 1, keep), dtype=torch.int32, device="cuda")
+    K_out, V_out, tally_out = (K, V, tally) if how == "in place" else (torch.zeros_like(K[:, :, :keep]), torch.zeros_like(V[:, :, :keep]),
+                                                                       torch.zeros((2, 1, keep), device="cuda"))
+    desc = dm.make_attention_desc(None, K)
+    ws = torch.empty(dm.dsmoe_evict_workspace_size(desc), dtype=torch.uint8, device="cuda")
+    dm.dsmoe_cache_evict(desc, keep, 0, recent, length, tally, K, V, kept, length, tally_out, K_out, V_out, ws)
+    torch.cuda.synchronize()
+    assert kept[0, 0].tolist() == stay == kept[1, 0].tolist() and length.tolist() == [keep, keep]
+    assert torch.equal(K_out[:, 0, :keep], want_K) and torch.equal(V_out[:, 0, :keep], want_V) and torch.equal(tally_out[..., :keep], want_tally)
