@@ -334,7 +334,8 @@ def dsmoe_prefix_attention(desc, Kp, Vp, q, K, V, tok_seq, pos, out, lse, worksp
 
 def dsmoe_tally_attention(desc, q, K, V, tok_seq, pos, out, lse, tally_in, tally_out, workspace, dev_status=None, stream=None):
     """Attention that adds the keys' weights to tallies [n_seq, n_head, L] fp32."""
-    if tally_out.shape != desc.cache_layout[0][:3]:
+    shape = tally_out.shape
+    if shape != desc.cache_layout[0][:3] or not (tally_in is None or tally_in is tally_out or tally_in.shape == shape):
         raise ValueError("tallies are [n_seq, n_head, L]")
     _check(lib().dsmoe_tally_attention(ctypes.byref(desc), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse), _ptr(tally_in),
                                        _ptr(tally_out), _ptr(workspace), workspace.numel() if workspace is not None else 0,
@@ -351,15 +352,19 @@ def dsmoe_cache_evict(desc, keep, sinks, recent, length, tally, K, V, kept, len_
                       stream=None):
     """Thins a cache out to ``keep`` keys a sequence and head.  K_out, V_out: [n_seq, n_head, at least keep, d_head], or K and V themselves;
     tally_out: [n_seq, n_head, at least keep], or tally."""
-    if not (K_out.dtype == V_out.dtype == torch.bfloat16 and K_out.stride() == V_out.stride() and K_out.stride(3) == 1
-            and K_out.shape == V_out.shape and K_out.shape[2] >= keep and K_out.shape[:2] == tally_out.shape[:2] == desc.cache_layout[0][:2]
-            and K_out.shape[3] == desc.d_head):
+    # (each look at a tensor's shape or strides makes an object, and small calls are as long as the host takes)
+    n_seq, n_head, L, d_head = desc.cache_layout[0]
+    in_place = K_out is K and V_out is V                 # (checked with them)
+    shape, stride = desc.cache_layout if in_place else (K_out.shape, K_out.stride())
+    room = tally_out.shape
+    if not ((in_place or (K_out.dtype == V_out.dtype == torch.bfloat16 and V_out.shape == shape and V_out.stride() == stride and stride[3] == 1))
+            and shape[2] >= keep and shape == (n_seq, n_head, shape[2], d_head) and len(room) == 3 and room[0] == n_seq and room[1] == n_head):
         raise ValueError("K_out, V_out and tally_out have room for `keep` keys of every sequence and head, K_out and V_out one layout")
-    if tally.shape != desc.cache_layout[0][:3] or kept.shape != (desc.n_seq, desc.n_head, keep):
+    if (room if tally is tally_out else tally.shape) != (n_seq, n_head, L) or kept.shape != (n_seq, n_head, keep):
         raise ValueError("tally is [n_seq, n_head, L], kept is [n_seq, n_head, keep]")
     args = EvictArgs(int(keep), int(sinks), int(recent))
-    args.out_stride[:] = K_out.stride()[:3]
-    args.tally_pitch = tally_out.shape[2]
+    args.out_stride[:] = stride[:3]
+    args.tally_pitch = room[2]
     _check(lib().dsmoe_cache_evict(ctypes.byref(desc), ctypes.byref(args), _ptr(length), _ptr(tally), *_cache_ptrs(desc, K, V), _ptr(kept),
                                    _ptr(len_out), _ptr(tally_out), K_out.data_ptr(), V_out.data_ptr(), _ptr(workspace),
                                    workspace.numel() if workspace is not None else 0, _ptr(dev_status), _stream(stream)),

@@ -171,3 +171,26 @@ def test_the_binding_checks_shapes_and_types():
     with pytest.raises(ValueError):
         dm.dsmoe_cache_evict(desc, 8, 0, 0, None, torch.zeros((2, 2, 32)), K, K.clone(), torch.zeros((2, 2, 7), dtype=torch.int32), None,
                              torch.zeros((2, 2, 8)), K[:, :, :8].clone(), K[:, :, :8].clone(), None)
+
+
+def test_the_binding_checks_tallies_and_places_for_what_stays():
+    q = torch.zeros((4, 2, 3, 64), dtype=torch.bfloat16)
+    K, V = (torch.zeros((2, 2, 32, 64), dtype=torch.bfloat16) for _ in range(2))
+    desc, tally, pos = dm.make_attention_desc(q, K, 0.125), torch.zeros((2, 2, 32)), torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        dm.dsmoe_tally_attention(desc, q, K, V, None, pos, torch.zeros_like(q), None, torch.zeros((1, 2, 32)), tally, None)
+    out, room, kept, length = torch.zeros((2, 2, 8, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 8)), torch.zeros((2, 2, 8), dtype=torch.int32), pos[:2]
+    for a, b, c in ((out, out[:, :, :7], room), (out.float(), out.float(), room), (out[..., :32], out[..., :32], room), (out[:1], out[:1], room),
+                    (out, out, room[:1]), (out, out, room[:, :1]), (out, out, room[0]), (out.transpose(2, 3), out.transpose(2, 3), room)):
+        with pytest.raises(ValueError):
+            dm.dsmoe_cache_evict(desc, 8, 0, 0, length, tally, K, V, kept, length, c, a, b, None)
+    for a, t in ((kept[..., :7], tally), (kept, tally[:, :, :31]), (kept, tally[:1])):
+        with pytest.raises(ValueError):
+            dm.dsmoe_cache_evict(desc, 8, 0, 0, length, t, K, V, a, length, room, out, out.clone(), None)
+    with pytest.raises(ValueError):                      # in place: the whole cache's tallies are kept
+        dm.dsmoe_cache_evict(desc, 8, 0, 0, length, tally[:, :, :8], K, V, kept, length, tally[:, :, :8], K, V, None)
+    # nothing wrong with the shapes: what is missing is the workspace
+    for place in ((tally, K, V), (room, out, out.clone())):
+        with pytest.raises(dm.DsmoeError) as e:
+            dm.dsmoe_cache_evict(desc, 8, 0, 0, length, tally, K, V, kept, length, *place, None, stream=type("S", (), {"cuda_stream": 0}))
+        assert e.value.code == 3
