@@ -172,3 +172,27 @@ def test_a_prompt_and_the_tokens_after_it(n_seq, n_head, group, d, L, prompt, P)
     torch.cuda.synchronize()
     for x, y in zip(s.state(), want):
         assert torch.equal(x, y)
+
+
+def test_two_servers_at_once():
+    """Two streams, each with its own caches and workspace and no wait between them, do what they do one after the other."""
+    sizes = ((2, 2, 3, 64, 300, 280, 500), (5, 2, 8, 128, 420, 401, 900))
+    states = []
+    for at_once in (False, True):
+        servers = [Server(*x, seed=i) for i, x in enumerate(sizes)]
+        streams = [torch.cuda.Stream() if at_once else torch.cuda.current_stream() for _ in servers]
+        torch.cuda.synchronize()
+        for turn in range(12):
+            for s, stream in zip(servers, streams):
+                with torch.cuda.stream(stream):
+                    if turn == 0:
+                        s.take_prompt()
+                        s.thin_out()
+                    s.step()
+                    if turn % 5 == 4:
+                        s.thin_out()
+        torch.cuda.synchronize()
+        assert all(s.status.item() == 0 for s in servers)
+        states.append([x for s in servers for x in s.state() + [s.prompt_out, s.prompt_lse]])
+    for x, y in zip(*states):
+        assert torch.equal(x, y)
