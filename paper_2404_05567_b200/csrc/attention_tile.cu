@@ -10,7 +10,7 @@
 // pipe works for the other one.
 // Bound by the threads' way from logits to weights: a step of 256 rows and 128 keys of 128 numbers takes 3400 cycles, of which the exponentials
 // alone take the special-function units 2048 and the MMAs the tensor pipe 2100; with an eighth of the MMAs a call still took four fifths of its time.
-// 8192 tokens of 4 x 5 heads with a window of 4096: 271 us, 0.57 of the tensor rate.  Tried there, us: a quarter of the
+// 8192 tokens of 4 x 5 heads with a window of 4096: 274 us, 0.57 of the tensor rate, at the power limit (1.7 GHz).  Tried there, us: a quarter of the
 // exponentials by polynomial 289 (276 without), the two row tiles taking turns at their exponentials 312 (311 without).
 //
 // What a CTA's tokens see: tokens of one sequence that follow one another are a run; a run's keys are at most three stretches of slots (sinks, and
