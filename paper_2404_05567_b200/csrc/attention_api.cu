@@ -121,6 +121,7 @@ struct AttnPlan {
     int prefix_splits;                    // 0: the prefix is not the 128-row kernel's
     int own_splits;                       // ... the own caches
     int row_parts;                        // parts of whole rows
+    bool fits;                            // a workspace of that size is supported
 };
 
 // Parts into which the 128-row kernel's keys are cut: as many as fill the SMs, two tiles of keys or more in each
@@ -192,6 +193,7 @@ AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, b
     w.row_ml = take((size_t)w.row_parts * rows * 2 * 4);
     w.row_o = take((size_t)w.row_parts * rows * A.d_head * 4);
     w.total = off;
+    w.fits = off < (size_t)1 << 36;       // (attention_sum_kernel finds parts by their number of 16 bytes, in 32 bits)
     return w;
 }
 
@@ -299,7 +301,9 @@ dsmoe_status dsmoe_attention_workspace_size(const dsmoe_attention_desc* desc, in
         dsmoe_prefix p{};
         if (kind == DSMOE_ATTENTION_PREFIX) p.P = prefix_len;
         const bool tiles = A.d_head == 64 || A.d_head == 96 || A.d_head == 128;
-        *bytes = attention_plan(A, shared_keys(A, p), tiles, kind == DSMOE_ATTENTION_TALLY).total;
+        const AttnPlan w = attention_plan(A, shared_keys(A, p), tiles, kind == DSMOE_ATTENTION_TALLY);
+        if (!w.fits) return DSMOE_ERR_UNSUPPORTED;
+        *bytes = w.total;
         if (kind == DSMOE_ATTENTION_TALLY) {            // (with sequence numbers, as many as there may be, the logits may be kept)
             AttnView several = A;
             several.tok_seq = &desc->n_seq;
@@ -319,6 +323,7 @@ dsmoe_status dsmoe_window_attention(const dsmoe_attention_desc* desc, int window
     AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
     // (the workspace is that of a window as wide as the cache: the most CTAs that any window can have)
     const AttnPlan w = attention_plan(A, SharedKeys{}, false, false);
+    if (!w.fits) return DSMOE_ERR_UNSUPPORTED;
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
     A.window = window;
     A.sinks = sinks;
@@ -337,6 +342,7 @@ dsmoe_status dsmoe_prefix_attention(const dsmoe_attention_desc* desc, const dsmo
     const AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
     const SharedKeys S = prefix->P > 0 ? shared_keys(A, *prefix) : SharedKeys{};
     const AttnPlan w = attention_plan(A, S, S.P > 0 && tile_supported(shared_view(A, S)), false);
+    if (!w.fits) return DSMOE_ERR_UNSUPPORTED;
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
     return attend(A, S, w, static_cast<char*>(workspace), (cudaStream_t)stream);
 }
@@ -359,6 +365,7 @@ dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void*
     }
     AttnView A = view_of(*desc, q, K, V, tok_seq, pos, out, lse, dev_status);
     const AttnPlan w = attention_plan(A, SharedKeys{}, false, true);
+    if (!w.fits) return DSMOE_ERR_UNSUPPORTED;
     if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
     A.ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + w.ml);
     DSMOE_TRY(attend(A, SharedKeys{}, w, static_cast<char*>(workspace), s));

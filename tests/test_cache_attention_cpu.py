@@ -102,6 +102,9 @@ def test_calls_that_are_refused(name, more, tail):
 def test_caches_of_more_positions_than_are_counted():
     assert _size(_desc(L=2 ** 30, kv_stride=(0, 0, 0)))[0] == 0 and _size(_desc(L=2 ** 30 + 1, kv_stride=(0, 0, 0)))[0] == 2
     assert _size(_desc(), dm.ATTENTION_PREFIX, 2 ** 30)[0] == 0 and _size(_desc(), dm.ATTENTION_PREFIX, 2 ** 30 + 1)[0] == 2
+    # parts of 2^36 bytes and more
+    big = dict(n_head=16, group=8, d_head=128, o_stride=(16384, 1024, 128))
+    assert _size(_desc(T=2 ** 18, **big), dm.ATTENTION_PREFIX, 4096)[0] == 0 and _size(_desc(T=2 ** 22, **big), dm.ATTENTION_PREFIX, 4096)[0] == 2
 
 
 def test_windows_that_are_refused():
