@@ -76,10 +76,20 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
         for (int i = 0; i < PER; ++i) stays |= (uint32_t)(i * kSelThreads + tid < n) << i;
     } else {
         uint32_t u[PER];                                // 0: no candidate (or a tally that is no number)
+        {
+            // (every thread asks for PER numbers at once, for the first one where it has no candidate: behind branches they came one by one, 14 of
+            // the 35 thousand cycles with 16)
+            float v[PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int k = i * kSelThreads + tid;
-            u[i] = k >= a && k < b ? rank_bits(tally[k]) : 0u;
+            for (int i = 0; i < PER; ++i) {
+                const int k = i * kSelThreads + tid;
+                v[i] = tally[k >= a && k < b ? k : 0];
+            }
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int k = i * kSelThreads + tid;
+                u[i] = k >= a && k < b ? rank_bits(v[i]) : 0u;
+            }
         }
         bool tied = true;                               // more have exactly the bound than stay
         if (want > 0) {
@@ -165,7 +175,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
     for (int i0 = 0; i0 < PER; i0 += BATCH) {
         float v[BATCH];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) v[i] = (stays >> (i0 + i)) & 1u ? tally[(i0 + i) * kSelThreads + tid] : 0.f;
+        for (int i = 0; i < BATCH; ++i) v[i] = tally[(stays >> (i0 + i)) & 1u ? (i0 + i) * kSelThreads + tid : 0];
         // (in place a tally moves to where one of this batch or an earlier one was: all of it is read)
         if (in_place) __syncthreads();
 #pragma unroll
