@@ -259,34 +259,48 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_long_kernel(const __
     int32_t* const kept = E.kept + pair * E.keep;
     float* const to = E.tally_out + pair * E.tally_pitch;
     int n_ties = 0, n_kept = 0;
-    for (int i0 = 0; i0 < n; i0 += kSelThreads) {
-        const int i = i0 + tid;
-        const float v = i < n ? tally[i] : 0.f;
-        const uint32_t u = rank_bits(v);
-        const bool middle = !all && i >= a && i < b, tie = i < n && middle && u == bound;
-        const uint32_t tie_votes = __ballot_sync(0xffffffffu, tie);
-        if (lane == 0) ties_s[warp] = __popc(tie_votes);
+    // four neighbours a thread: a call on 32 caches of 131072 positions 141 us, with one 422
+    constexpr int NEXT = 4;
+    // x of this thread's and what the threads before it have, on top of *so_far, which grows by all of it
+    const auto place = [&](int x, int* warps, int* so_far) {
+        int incl = x;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 31) warps[warp] = incl;
         __syncthreads();
-        int rank = n_ties + __popc(tie_votes & ((1u << lane) - 1u));
-        for (int w = 0; w < kSelThreads / 32; ++w) {
-            const int c = ties_s[w];
-            if (w < warp) rank += c;
-            n_ties += c;
+        const int w = warps[lane];
+        const int at = *so_far + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + incl - x;
+        *so_far += __reduce_add_sync(0xffffffffu, w);
+        return at;
+    };
+    for (int i0 = 0; i0 < n; i0 += NEXT * kSelThreads) {
+        const int first = i0 + NEXT * tid;
+        float v[NEXT];
+#pragma unroll
+        for (int k = 0; k < NEXT; ++k) v[k] = tally[first + k < n ? first + k : 0];
+        uint32_t ties_here = 0u, stays = 0u;
+#pragma unroll
+        for (int k = 0; k < NEXT; ++k) {
+            const int i = first + k;
+            const uint32_t u = rank_bits(v[k]);
+            const bool middle = !all && i >= a && i < b;
+            ties_here |= (uint32_t)(i < n && middle && u == bound) << k;
+            stays |= (uint32_t)(i < n && (!middle || u > bound)) << k;
         }
-        const bool stays = i < n && (!middle || u > bound || (tie && rank < ties));
-        const uint32_t votes = __ballot_sync(0xffffffffu, stays);
-        if (lane == 0) kept_s[warp] = __popc(votes);
-        __syncthreads();                                // (and every thread has read its tally: it may be written over now)
-        int at = n_kept + __popc(votes & ((1u << lane) - 1u));
-        for (int w = 0; w < kSelThreads / 32; ++w) {
-            const int c = kept_s[w];
-            if (w < warp) at += c;
-            n_kept += c;
-        }
-        if (stays) {
-            kept[at] = i;
-            to[at] = v;
-        }
+        int rank = place(__popc(ties_here), ties_s, &n_ties);
+#pragma unroll
+        for (int k = 0; k < NEXT; ++k)
+            if ((ties_here >> k) & 1u) stays |= (uint32_t)(rank++ < ties) << k;
+        int at = place(__popc(stays), kept_s, &n_kept);        // (its wait: every thread has read its tallies, so they may be written over)
+#pragma unroll
+        for (int k = 0; k < NEXT; ++k)
+            if ((stays >> k) & 1u) {
+                kept[at] = first + k;
+                to[at++] = v[k];
+            }
     }
     for (int i = n_kept + tid; i < E.keep; i += kSelThreads) kept[i] = -1;
     if (tid == 0) E.count[pair] = n_kept;
