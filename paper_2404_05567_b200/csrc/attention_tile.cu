@@ -498,12 +498,14 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 ptx::tc_fence_after();
                 // The maximum moves if the tile before asks for it.  (What the other half found there lies ready: these logits come behind both
                 // halves' weights.  O is all there too: S of this tile follows the tile before's P.V in the tensor pipe.)
+                // So that tile's weights were relative to the maximum before it: up to 2^128, beyond which the row is no number and is done again.
+                // The smallest factor is 2^-126 (a smaller one would be flushed, and the tile's sums with it): the rest is within kMoves.
                 if (i > 0) {
                     top = fmaxf(top, S.tops[(i - 1) & 1][r][half ^ 1][at]);
                     const bool moves = m != -INFINITY && top > m + kMoves;
                     if (__any_sync(0xffffffffu, moves)) {
-                        const float f = moves ? exp2_fast(m - top) : 1.f;
-                        if (moves) m = top;
+                        const float by = moves ? fminf(top - m, 126.f) : 0.f, f = exp2_fast(-by);
+                        m += by;
                         l *= f;
 #pragma unroll 1
                         for (int q = 0; q < DH / 32; ++q) {
@@ -585,6 +587,12 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             S.swap[r][half][at] = l;
             pair_sync(pair);
             l = S.swap[r][0][at] + S.swap[r][1][at];
+            // Where the last tile's weights were far above 1, the maximum follows them by a power of two: 1 / l and other parts' factors keep their bits
+            const bool high = l >= 0x1p64f;                               // (infinite sums are found below)
+            const int up = high ? min((int)(__float_as_uint(l) >> 23) - 127, 126) : 0;
+            const float down = __uint_as_float((uint32_t)(127 - up) << 23);
+            l *= down;
+            m += (float)up;
             const long long row = row_at(A, tg0 + tl, j, m_of);
             const float inv = P.o ? 1.f : l == 0.f ? 0.f : 1.f / l;
             constexpr int HC = DH / 2;                                    // a thread's columns
@@ -597,6 +605,10 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int k = 0; k < HC; ++k) asm volatile("" : "+r"(o[k]));
+                if (__any_sync(0xffffffffu, high)) {
+#pragma unroll
+                    for (int k = 0; k < HC; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * down);
+                }
             } else {
 #pragma unroll
                 for (int k = 0; k < HC; ++k) o[k] = 0u;

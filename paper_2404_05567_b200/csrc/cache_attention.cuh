@@ -32,9 +32,10 @@ struct AttnView {
     int32_t* dev_status;
 };
 
-// The maximum that weights are relative to moves only when a logit passes it by more than 2^kMoves: until then the weights are at most that, fp32 sums
-// and bf16 weights (which have fp32's exponents) lose nothing, and nothing is rescaled.  With 2^8, a row whose first keys happened to have small
-// logits (four sinks) moved now and then, and one such row held up its tile: a prompt of 8192 tokens 359 us, 311 with 2^32.
+// The maximum that weights are relative to moves only when a logit passes it by more than kMoves: until then the weights are at most 2^kMoves, fp32 sums
+// and bf16 weights (which have fp32's exponents) lose nothing, and nothing is rescaled.  The 128-row kernel moves it behind the tile that asks for it,
+// so a single tile's weights may be larger there.  With 8, a row whose first keys happened to have small
+// logits (four sinks) moved now and then, and one such row held up its tile: a prompt of 8192 tokens 359 us, 311 with 32.
 constexpr float kMoves = 32.f;
 
 constexpr int kUnit = 16;                 // keys that a warp takes at a time
