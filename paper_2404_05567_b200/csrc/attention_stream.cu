@@ -598,14 +598,15 @@ __global__ void __launch_bounds__(32 * ROWS) attention_sum_kernel(const __grid_c
             wgt_s[row][i] = x.x;
             from_s[row][i] = (uint32_t)((o - P.slots) >> 2);
             const float up = fmaxf(top, x.x);            // (this lane's parts' sum, relative to their maximum)
-            den = den * (up == -INFINITY ? 1.f : exp2_fast(top - up)) + (x.x == -INFINITY ? 0.f : x.y * exp2_fast(x.x - up));
+            // (a part without a maximum has seen no key, or none whose logit is a number: then its sum is none either, and the row's is none)
+            den = den * (up == -INFINITY ? 1.f : exp2_fast(top - up)) + (x.x == -INFINITY ? x.y : x.y * exp2_fast(x.x - up));
             top = up;
         }
         float all = top;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
         const float z = all == -INFINITY ? 0.f : all;
-        den = top == -INFINITY ? 0.f : den * exp2_fast(top - z);
+        den = top == -INFINITY ? den : den * exp2_fast(top - z);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
         for (int i = lane; i < n; i += 32) wgt_s[row][i] = exp2_fast(wgt_s[row][i] - z);

@@ -4,10 +4,10 @@ import numpy as np
 import pytest
 import torch
 
-import cache_attention_reference as ref
 from cache_attention_reference import Case
 from test_gpu_attention_tiles import prompt
-from test_gpu_window_attention import run
+from test_gpu_prefix_attention import call as call_prefix
+from test_gpu_window_attention import call as call_window, run
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +40,47 @@ def test_logits_that_jump_within_a_part(jump, at):
     """Keys in four parts, and another part whose largest logit was there from its first tile on."""
     c = Case(prompt(0, 1023, 60), 1, 5, 128, 1, 1024, seed=at, scale=LN2)
     run(with_logits(c, -100.0, {at: jump - 100, 600: jump - 97}), 2 ** 31 - 1)
+
+
+def rows_of(c, call, want, bad):
+    """Runs the call: rows that `bad` [T, n_head, group] marks are no numbers, and neither is their lse; the others are what is wanted."""
+    call(c)
+    got, lse = c.out.float().cpu().numpy(), c.lse.cpu().numpy()
+    assert np.isnan(got[bad]).all() and np.isnan(lse[bad]).all()
+    c.out[torch.from_numpy(bad).cuda()] = torch.from_numpy(want[0][bad]).bfloat16().cuda()
+    c.lse[torch.from_numpy(bad).cuda()] = torch.from_numpy(want[1][bad]).float().cuda()
+    c.check(want)
+    assert c.status.item() == 0
+
+
+# (a CTA's keys; a pair cut into parts; keys of a prompt in parts; beside a prefix on either kernel)
+@pytest.mark.parametrize("tokens,L,P", [([(0, 150)], 160, 0), ([(0, 4000), (1, 300)], 4001, 0), (prompt(0, 1099, 60), 1100, 0),
+                                        ([(0, 40), (1, 20)], 50, 300), ([(s, 40) for s in range(20)], 50, 1000)])
+def test_queries_that_are_no_numbers(tokens, L, P):
+    c = Case(tokens, 2, 5, 64, max(s for s, _ in tokens) + 1, L, P=P, seed=L + P)
+    want = c.expected()
+    bad = np.zeros((len(tokens), 2, 5), dtype=bool)
+    bad[0, 1, 3] = bad[-1, 0, 0] = True
+    for t, j, g in np.argwhere(bad):
+        c.q[t, j, g, 7] = float("nan")
+    rows_of(c, call_prefix if P else lambda c: call_window(c, 2 ** 31 - 1), want, bad)
+
+
+@pytest.mark.parametrize("n,L", [(1, 6), (60, 6), (1, 700)])
+def test_keys_that_are_no_numbers_beside_a_prefix(n, L):
+    """All that a token sees of its own cache: its result is no number, although the prefix alone has one."""
+    c = Case([(s, L - 1) for s in range(n)] + [(n, 2)], 1, 5, 64, n + 1, L, P=300, seed=n + L)
+    want = c.expected()
+    c.K[0, 0] = float("nan")
+    bad = np.zeros((n + 1, 1, 5), dtype=bool)
+    bad[0] = True
+    rows_of(c, call_prefix, want, bad)
+
+
+def test_keys_of_a_part_that_are_no_numbers():
+    """A prompt whose keys lie in parts, all of one part's no numbers."""
+    tokens = prompt(0, 1099, 60)
+    c = Case(tokens, 1, 5, 64, 1, 1100, seed=3)
+    want = c.expected()
+    c.K[0, 0, :512] = float("nan")
+    rows_of(c, lambda c: call_window(c, 2 ** 31 - 1), want, np.ones((60, 1, 5), dtype=bool))
