@@ -705,7 +705,7 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
 #pragma unroll
                 for (int w = 16; w > 0; w >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, w);
                 dot *= A.scale_log2;
-                const float top = fmaxf(m, dot), f = m == -INFINITY ? 0.f : exp2_fast(m - top), p = exp2_fast(dot - top);
+                const float top = fmaxf(m, dot), f = m == -INFINITY ? 0.f : exp2_fast(m - top), p = dot == -INFINITY ? 0.f : exp2_fast(dot - top);
                 m = top;
                 l = fmaf(l, f, p);
 #pragma unroll

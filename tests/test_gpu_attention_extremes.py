@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import cache_attention_reference as ref
 from cache_attention_reference import Case
 from test_gpu_attention_tiles import prompt
 from test_gpu_prefix_attention import call as call_prefix
@@ -84,3 +85,22 @@ def test_keys_of_a_part_that_are_no_numbers():
     want = c.expected()
     c.K[0, 0, :512] = float("nan")
     rows_of(c, lambda c: call_window(c, 2 ** 31 - 1), want, np.ones((60, 1, 5), dtype=bool))
+
+
+@pytest.mark.parametrize("L", [384, 1024])
+def test_keys_of_no_weight_before_values_that_are_no_numbers(L, monkeypatch):
+    """Rows that are done again for a value that they do not see: their first keys have logits of -inf."""
+    monkeypatch.setattr(ref, "visible", lambda p, w, k: [l for l in range(p + 1) if l % 128])
+    tokens = prompt(0, L - 1, 50)
+    c = Case(tokens, 1, 5, 64, 1, L, seed=L)
+    c.q[..., 0] = c.q[..., 0].abs() + 1
+    c.q_np = c.q.float().cpu().numpy()
+    want = c.expected()
+    c.K[0, 0, ::128, 0] = -float("inf")
+    c.V[0, 0, L - 20, 5] = float("inf")
+    call_window(c, 2 ** 31 - 1)
+    sees = np.array([p >= L - 20 for _, p in tokens])
+    assert (~np.isfinite(c.out.float().cpu().numpy()[sees][..., 5])).all()
+    c.out[torch.from_numpy(sees).cuda(), :, :, 5] = torch.from_numpy(want[0][sees][..., 5]).bfloat16().cuda()
+    c.check(want)
+    assert c.status.item() == 0
