@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kTtThreads, 2) attention_tally_tile_kernel(con
     constexpr int CH = DH / 8, KS = DH / 16;
     extern __shared__ unsigned char tt_smem[];
     __shared__ int first_s, last_s;       // the first and the last of the sequence's tokens that see a key of this tile
-    __shared__ long long q_s[kTtRows];    // where the rows' queries are; -1: no row
+    __shared__ long long q_s[kTtRows];    // where the rows' queries are
     __shared__ __align__(16) float2 ml_s[2][kTtRows];
     __shared__ __align__(16) int row_last_s[2][kTtRows];
     __shared__ int all_see_s[2];
@@ -367,18 +367,23 @@ __global__ void __launch_bounds__(kTtThreads, 2) attention_tally_tile_kernel(con
     __syncthreads();
     {
         const int i0 = first_s, n = last_s < 0 ? 0 : last_s + 1 - i0, tiles = (n + tokens - 1) / tokens;
-        // a fetching thread's row: its token and sums, asked for a tile ahead
+        // a fetching thread's row: its token and sums, asked for a tile ahead.  Places without a row have the tile's first row once more, by a factor of
+        // 0: with zeros for a query, a key that holds an infinity would have a logit that is no number, and so would its sum.
         const int at = tid - 128;
-        const bool row = warp >= 4 && at < tokens * A.group;
-        const int of = row ? at / A.group : 0, member = row ? at % A.group : 0;
+        const int of = at / A.group;
+        int member = 0;
+        bool real = false;
         int2 token = make_int2(0, -1);
         float2 ml = make_float2(0.f, 0.f);
         const auto ask = [&](int i) {
             const int k = i * tokens + of;
-            token = row && k < n ? list[i0 + k] : make_int2(0, -1);
-            ml = token.y >= 0 ? A.ml[row_at(A, token.x, j, member)] : make_float2(0.f, 0.f);
+            real = of < tokens && k < n;
+            member = real ? at % A.group : 0;
+            token = list[i0 + (real ? k : i * tokens)];
+            ml = A.ml[row_at(A, token.x, j, member)];
+            if (!real) ml.y = 0.f;
         };
-        ask(part);
+        if (warp >= 4 && part < tiles) ask(part);
         for (int i = part; i < tiles; i += P.parts) {
             if (!alive) break;
             const int b = done & 1;
@@ -388,17 +393,16 @@ __global__ void __launch_bounds__(kTtThreads, 2) attention_tally_tile_kernel(con
                 if (done >= 2) alive = ptx::mbar_sleep(ptx::smem_u32(&s_empty[b]), turn ^ 1u, &abort_flag);
                 alive = fetchers_agree(alive);          // (they meet below, or none does)
                 if (alive) {
-                    const bool partial = token.y >= 0 && token.y < key0 + kTtKeys - 1;
-                    q_s[at] = token.y >= 0 ? token.x * A.q_t + j * A.q_h + member * A.q_g : -1;
+                    const bool partial = real && token.y < key0 + kTtKeys - 1;
+                    q_s[at] = token.x * A.q_t + j * A.q_h + member * A.q_g;
                     ml_s[b][at] = ml;
-                    row_last_s[b][at] = token.y;
+                    row_last_s[b][at] = real ? token.y : -1;
                     const bool all = fetchers_agree(!partial);         // (and the rows' places are there)
                     if (at == 0) all_see_s[b] = all;
                     for (int idx = at; idx < kTtRows * CH; idx += 128) {
                         const int rw = idx / CH, ch = idx % CH;
-                        const long long q = q_s[rw];
                         const uint32_t dst = base + G::Q + b * G::TILE + (uint32_t)((ch >> 3) * G::PIECE + rw * 128 + (((ch & 7) ^ (rw & 7)) << 4));
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(A.q + (q < 0 ? 0 : q) + ch * 8), "r"(q < 0 ? 0u : 16u) : "memory");
+                        ptx::cp_async16(dst, A.q + q_s[rw] + ch * 8);
                     }
                     if (i + P.parts < tiles) ask(i + P.parts);
                     ptx::cp_async_commit();

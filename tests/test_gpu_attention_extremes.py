@@ -8,6 +8,7 @@ import cache_attention_reference as ref
 from cache_attention_reference import Case
 from test_gpu_attention_tiles import prompt
 from test_gpu_prefix_attention import call as call_prefix
+from test_gpu_tally_attention import run as run_tally
 from test_gpu_window_attention import call as call_window, run
 
 pytestmark = pytest.mark.gpu
@@ -104,3 +105,16 @@ def test_keys_of_no_weight_before_values_that_are_no_numbers(L, monkeypatch):
     c.out[torch.from_numpy(sees).cuda(), :, :, 5] = torch.from_numpy(want[0][sees][..., 5]).bfloat16().cuda()
     c.check(want)
     assert c.status.item() == 0
+
+
+@pytest.mark.parametrize("group", [1, 5, 33])
+def test_tallies_of_keys_of_no_weight(group, monkeypatch):
+    """Keys whose logits are -inf for all rows get nothing, in tiles that the rows do not fill too."""
+    monkeypatch.setattr(ref, "visible", lambda p, w=None, k=0: [l for l in range(p + 1) if l not in (7, 130)])
+    c = Case(prompt(0, 399, 100), 1, group, 64, 1, 400, seed=group)
+    c.q[..., 0] = c.q[..., 0].abs() + 1
+    c.q_np = c.q.float().cpu().numpy()
+    c.K[0, 0, [7, 130], 0] = -float("inf")
+    run_tally(c)
+    want = c.expected()[4]
+    assert (want[0, 0, [7, 130]] == 0).all()
