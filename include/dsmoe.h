@@ -358,7 +358,8 @@ dsmoe_status dsmoe_moa_forward(const dsmoe_layer_desc* desc, const dsmoe_moa_arg
  *            sequence's cache; -1: none (a padded entry of the batch: zeros in out, -inf in lse).
  *   lse      fp32 [T][n_head][group] or NULL: the natural logarithm of the sum of the exponentials of a row's logits.
  *
- * All strides are multiples of 8 elements, addresses of 16 bytes.  d_head a multiple of 32 up to 256, group up to 64, L up to 2^30, otherwise
+ * All strides are multiples of 8 elements, addresses of 16 bytes.  d_head a multiple of 32 up to 256, group up to 64, L up to 2^30, strides up to 2^40
+ * and a tensor's last row less than 2^50 elements behind its first, otherwise
  * DSMOE_ERR_UNSUPPORTED.  The memory from out's first element to its last must not overlap q's or the caches'.  Products of bf16 are added
  * in fp32, softmax statistics are fp32, and out is rounded once; the weights that multiply the values are two bf16 numbers each (as good as
  * 16 bits), on the 128-row tiles of prompts and long prefixes one.  Keys that a token does not see may hold anything, numbers or not.  A tok_seq or pos entry out of range is clamped and reported

@@ -16,7 +16,19 @@ bool strides_ok(const int64_t* s, int n) {
     return true;
 }
 
-// Whether rows of `row` elements at these strides are apart from one another: each stride, in their order, spans what lies within it
+// Whether the last of rows at these strides begins within 2^50 elements of the first, further than addresses go.  (Beyond it are strides and sizes that
+// are allowed one by one, and offsets that no longer fit 64 bits.)
+bool within_reach(const int64_t* stride, const int64_t* n, int count) {
+    int64_t left = 1ll << 50;
+    for (int i = 0; i < count; ++i) {
+        if (n[i] <= 1) continue;
+        if (stride[i] > left / (n[i] - 1)) return false;
+        left -= stride[i] * (n[i] - 1);
+    }
+    return true;
+}
+
+// Whether rows of `row` elements at these strides (within_reach) are apart from one another: each stride, in their order, spans what lies within it
 bool rows_apart(const int64_t* stride, const int64_t* n, int64_t row) {
     int order[3] = {0, 1, 2};
     std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
@@ -24,13 +36,12 @@ bool rows_apart(const int64_t* stride, const int64_t* n, int64_t row) {
     for (int i : order) {
         if (n[i] <= 1) continue;
         if (stride[i] < span) return false;
-        if (stride[i] > (INT64_MAX / 4) / n[i]) return false;
         span += stride[i] * (n[i] - 1);
     }
     return true;
 }
 
-// The bytes that rows at these strides lie in
+// The bytes that rows at these strides (within_reach) lie in
 struct Extent {
     uintptr_t begin, end;
     bool meets(const Extent& o) const { return begin < o.end && o.begin < end; }
@@ -50,7 +61,8 @@ dsmoe_status check_cache(const dsmoe_attention_desc* d) {
     if (d->L > 1 << 30 || (long long)d->n_seq * d->n_head > INT_MAX / 4) return DSMOE_ERR_UNSUPPORTED;
     for (int i = 0; i < 3; ++i)
         if (d->kv_stride[i] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
-    return DSMOE_OK;
+    const int64_t n[3] = {d->n_seq, d->n_head, d->L};
+    return within_reach(d->kv_stride, n, 3) ? DSMOE_OK : DSMOE_ERR_UNSUPPORTED;
 }
 
 dsmoe_status check_attention(const dsmoe_attention_desc* d) {
@@ -62,6 +74,7 @@ dsmoe_status check_attention(const dsmoe_attention_desc* d) {
     for (int i = 0; i < 3; ++i)
         if (d->q_stride[i] > (1ll << 40) || d->o_stride[i] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
     const int64_t n[3] = {d->T, d->n_head, d->group};
+    if (!within_reach(d->q_stride, n, 3) || !within_reach(d->o_stride, n, 3)) return DSMOE_ERR_UNSUPPORTED;
     if (!rows_apart(d->o_stride, n, d->d_head)) return DSMOE_ERR_INVALID_ARG;
     return DSMOE_OK;
 }
@@ -275,6 +288,7 @@ dsmoe_status check_prefix(const dsmoe_attention_desc* d, const dsmoe_prefix* p, 
     if (!p->Kp || !p->Vp || !aligned16(p->Kp) || !aligned16(p->Vp) || !strides_ok(p->stride, 2)) return DSMOE_ERR_INVALID_ARG;
     if (p->P > 1 << 30 || p->stride[0] > (1ll << 40) || p->stride[1] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
     const int64_t n[3] = {d->T, d->n_head, d->group}, c[3] = {1, d->n_head, p->P}, st[3] = {0, p->stride[0], p->stride[1]};
+    if (!within_reach(st, c, 3)) return DSMOE_ERR_UNSUPPORTED;
     const Extent o = extent(out, d->o_stride, n, d->d_head, 2);
     if (o.meets(extent(p->Kp, st, c, d->d_head, 2)) || o.meets(extent(p->Vp, st, c, d->d_head, 2))) return DSMOE_ERR_INVALID_ARG;
     return DSMOE_OK;
@@ -395,6 +409,8 @@ dsmoe_status dsmoe_cache_evict(const dsmoe_attention_desc* desc, const dsmoe_evi
         if (a.out_stride[i] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
     if (a.tally_pitch > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
     const int64_t n[3] = {desc->n_seq, desc->n_head, desc->L}, m[3] = {desc->n_seq, desc->n_head, a.keep};
+    const int64_t pairs = (int64_t)desc->n_seq * desc->n_head;
+    if (!within_reach(a.out_stride, m, 3) || !within_reach(&a.tally_pitch, &pairs, 1)) return DSMOE_ERR_UNSUPPORTED;
     const bool in_place = K_out == K;
     if (in_place != (V_out == V) || K_out == V_out) return DSMOE_ERR_INVALID_ARG;
     if (!rows_apart(a.out_stride, m, desc->d_head)) return DSMOE_ERR_INVALID_ARG;
@@ -407,7 +423,6 @@ dsmoe_status dsmoe_cache_evict(const dsmoe_attention_desc* desc, const dsmoe_evi
     } else if (ok.meets(ek) || ok.meets(ev) || ov.meets(ek) || ov.meets(ev)) {
         return DSMOE_ERR_INVALID_ARG;
     }
-    const int64_t pairs = (int64_t)desc->n_seq * desc->n_head;
     if (tally_out == tally) {
         if (a.tally_pitch != desc->L) return DSMOE_ERR_INVALID_ARG;
     } else if (tally < tally_out + (pairs - 1) * a.tally_pitch + a.keep && tally_out < tally + pairs * desc->L) {

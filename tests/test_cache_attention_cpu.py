@@ -197,3 +197,21 @@ def test_the_binding_checks_tallies_and_places_for_what_stays():
         with pytest.raises(dm.DsmoeError) as e:
             dm.dsmoe_cache_evict(desc, 8, 0, 0, length, tally, K, V, kept, length, *place, None, stream=type("S", (), {"cuda_stream": 0}))
         assert e.value.code == 3
+
+
+def test_extents_beyond_64_bits_are_refused():
+    """Strides and sizes that are allowed one by one, but lie further apart than addresses go."""
+    far, ok = 2 ** 40, (384, 192, 64)
+    for kw in (dict(L=2 ** 30, kv_stride=(0, 0, far)), dict(n_seq=2 ** 27, n_head=1, kv_stride=(far, 2048, 64)),
+               dict(T=2 ** 26, group=1, o_stride=(128, 64, 64), q_stride=(far, 64, 64))):
+        assert _call("dsmoe_window_attention", _desc(**kw), (4, 0, 0)) == 2, kw
+        assert _call("dsmoe_tally_attention", _desc(**kw), tail=(None, 1 << 50)) == 2, kw
+    p = dm.Prefix(10 * A, 11 * A, 2 ** 30)
+    p.stride[:] = (512, far)
+    assert _call("dsmoe_prefix_attention", _desc(o_stride=ok), (ctypes.byref(p),)) == 2
+    for L, kv, out in ((2 ** 30, (0, 0, far), (2048, 1024, 64)), (2 ** 30, (64, 64, 128), (64, 128, far))):
+        a = dm.EvictArgs(2 ** 28, 0, 0)
+        a.out_stride[:], a.tally_pitch = out, 2 ** 30
+        d = _desc(L=L, kv_stride=kv)
+        assert dm.lib().dsmoe_cache_evict(ctypes.byref(d), ctypes.byref(a), A, 2 * A, 3 * A, 4 * A, 5 * A, 6 * A, 1 << 45, 1 << 50, 1 << 51, 10 * A, 1 << 20,
+                                          None, None) == 2, kv
