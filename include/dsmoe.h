@@ -425,6 +425,7 @@ dsmoe_status dsmoe_tally_attention(const dsmoe_attention_desc* desc, const void*
  *   K_out, V_out: bf16, room for keep positions by out_stride (sequence, head, position); tally_out: fp32, heads tally_pitch (>= keep) apart.
  *   Rows behind the last one that stays are left as they were.  K_out = K and V_out = V with the same strides: in place; likewise tally_out =
  *   tally with tally_pitch = L.  Otherwise the memory from their first elements to their last must not overlap that of K, V and tally.
+ *   No row of K_out may overlap one of V_out (in place: of K and V); rows may lie between one another.
  *   workspace: dsmoe_evict_workspace_size bytes.
  */
 typedef struct dsmoe_evict_args {

@@ -41,6 +41,26 @@ bool rows_apart(const int64_t* stride, const int64_t* n, int64_t row) {
     return true;
 }
 
+// Whether any two rows at these strides (rows_apart), one behind the first address and one behind the second, `apart` elements further on, share an element.
+// What lies within a stride spans no more than it, so of each dimension only the two steps on either side of the distance come near enough.
+bool rows_meet(int64_t apart, const int64_t* stride, const int64_t* n, int64_t row) {
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return stride[a] > stride[b]; });
+    for (int ways = 0; ways < 8; ++ways) {
+        int64_t left = apart;
+        bool there = true;
+        for (int k = 0; k < 3; ++k) {
+            const int i = order[k];
+            if (n[i] <= 1) continue;
+            const int64_t steps = left / stride[i] - (left % stride[i] < 0) + (ways >> k & 1);
+            there = there && steps < n[i] && steps > -n[i];
+            left -= steps * stride[i];
+        }
+        if (there && left < row && left > -row) return true;
+    }
+    return false;
+}
+
 // The bytes that rows at these strides (within_reach) lie in
 struct Extent {
     uintptr_t begin, end;
@@ -412,15 +432,17 @@ dsmoe_status dsmoe_cache_evict(const dsmoe_attention_desc* desc, const dsmoe_evi
     const int64_t pairs = (int64_t)desc->n_seq * desc->n_head;
     if (!within_reach(a.out_stride, m, 3) || !within_reach(&a.tally_pitch, &pairs, 1)) return DSMOE_ERR_UNSUPPORTED;
     const bool in_place = K_out == K;
-    if (in_place != (V_out == V) || K_out == V_out) return DSMOE_ERR_INVALID_ARG;
+    if (in_place != (V_out == V)) return DSMOE_ERR_INVALID_ARG;
     if (!rows_apart(a.out_stride, m, desc->d_head)) return DSMOE_ERR_INVALID_ARG;
+    // (in place the whole caches move, not the first `keep` positions alone)
+    const int64_t between = ((intptr_t)V_out - (intptr_t)K_out) / 2;
     const Extent ek = extent(K, desc->kv_stride, n, desc->d_head, 2), ev = extent(V, desc->kv_stride, n, desc->d_head, 2);
     const Extent ok = extent(K_out, a.out_stride, m, desc->d_head, 2), ov = extent(V_out, a.out_stride, m, desc->d_head, 2);
     if (in_place) {
         for (int i = 0; i < 3; ++i)
             if (a.out_stride[i] != desc->kv_stride[i]) return DSMOE_ERR_INVALID_ARG;
-        if (!rows_apart(desc->kv_stride, n, desc->d_head)) return DSMOE_ERR_INVALID_ARG;
-    } else if (ok.meets(ek) || ok.meets(ev) || ov.meets(ek) || ov.meets(ev)) {
+        if (!rows_apart(desc->kv_stride, n, desc->d_head) || rows_meet(between, desc->kv_stride, n, desc->d_head)) return DSMOE_ERR_INVALID_ARG;
+    } else if (ok.meets(ek) || ok.meets(ev) || ov.meets(ek) || ov.meets(ev) || rows_meet(between, a.out_stride, m, desc->d_head)) {
         return DSMOE_ERR_INVALID_ARG;
     }
     if (tally_out == tally) {

@@ -215,3 +215,46 @@ def test_extents_beyond_64_bits_are_refused():
         d = _desc(L=L, kv_stride=kv)
         assert dm.lib().dsmoe_cache_evict(ctypes.byref(d), ctypes.byref(a), A, 2 * A, 3 * A, 4 * A, 5 * A, 6 * A, 1 << 45, 1 << 50, 1 << 51, 10 * A, 1 << 20,
                                           None, None) == 2, kv
+
+
+def test_places_for_what_stays_that_overlap():
+    """Keys' and values' rows in part the same memory are refused, in place or not; rows that lie between one another are not."""
+    def go(kv_stride, out_stride, K, V, K_out, V_out, keep=16, d=None):
+        a = dm.EvictArgs(keep, 2, 4)
+        a.out_stride[:], a.tally_pitch = out_stride, 32
+        # (what is not refused lacks its workspace: 3)
+        return dm.lib().dsmoe_cache_evict(ctypes.byref(d or _desc(kv_stride=kv_stride)), ctypes.byref(a), A, 2 * A, K, V, 5 * A, 6 * A, 7 * A, K_out, V_out, None, 0,
+                                          None, None)
+    whole, room, at = (4096, 2048, 64), (2048, 1024, 64), 8 * A
+    for off, want in ((0, 1), (16, 1), (128, 1), (1024 * 2, 1), (2048 * 2 - 16, 1), (4096 * 2 - 16, 1), (4096 * 2, 3), (-16, 1), (-4096 * 2 + 16, 1), (-4096 * 2, 3)):
+        assert go(whole, room, 3 * A, 4 * A, at, at + off) == want, off
+    # keys and values side by side in each position, head or sequence: [n_seq][n_head][16][2][64] and so on
+    for stride, step in (((4096, 2048, 128), 64), ((4096, 2048, 64), 1024), ((4096, 1024, 64), 2048)):
+        for off, want in ((step * 2, 3), (step * 2 - 16, 1), (step * 2 + 16, 1), (-step * 2, 3), (step * 2 + stride[0] * 2, 3)):
+            assert go(whole, stride, 3 * A, 4 * A, at, at + off) == want, (stride, off)
+    # in place: [n_seq][n_head][32][2][64]
+    both = (8192, 4096, 128)
+    for off, want in ((128, 3), (-128, 3), (64, 1), (256, 1), (16, 1), (4096 * 2, 1), (4096 * 2 + 128, 3), (8192 * 2, 1), (2 * 8192 * 2, 3)):
+        assert go(both, both, at, at + off, at, at + off) == want, off
+    # rows of less than a stride: a place between them, and one that is too small
+    for off, want in ((64 * 2, 3), (96 * 2, 3), (112 * 2, 1), (48 * 2, 1)):
+        assert go(whole, (8192, 4096, 160), 3 * A, 4 * A, at, at + off) == want, off
+    # any order of dimensions with any gaps, against the addresses themselves
+    rng = np.random.default_rng(0)
+    seen = set()
+    for _ in range(1500):
+        n = rng.integers(1, 4, 3)
+        stride, span = np.zeros(3, dtype=np.int64), 32
+        for i in rng.permutation(3):
+            stride[i] = span + 8 * rng.integers(0, 12)
+            span += stride[i] * (n[i] - 1)
+        off = 8 * int(rng.integers(-span // 8 - 4, span // 8 + 5))
+        d = _desc(d_head=32, n_seq=n[0], n_head=n[1], L=n[2], kv_stride=(0, 0, 32))
+        a = dm.EvictArgs(n[2], 0, 0)
+        a.out_stride[:], a.tally_pitch = stride.tolist(), 32
+        got = dm.lib().dsmoe_cache_evict(ctypes.byref(d), ctypes.byref(a), A, 2 * A, 3 * A, 4 * A, 5 * A, 6 * A, 7 * A, at, at + 2 * off, None, 0, None, None)
+        rows = [s * stride[0] + h * stride[1] + p * stride[2] for s in range(n[0]) for h in range(n[1]) for p in range(n[2])]
+        meet = any(abs(x - y - off) < 32 for x in rows for y in rows)
+        assert got == (1 if meet else 3), (n, stride, off)
+        seen.add((meet, abs(off) < span))
+    assert seen == {(True, True), (False, True), (False, False)}
