@@ -284,25 +284,69 @@ def make_attention_desc(q, K, scale=1.0, out=None) -> AttentionDesc:
         desc.q_stride[:] = q.stride()[:3]
         if out is not None:
             o_stride = out.stride()[:3]
-        desc.layout = q.shape, q.stride(), o_stride + (1,)
+        desc.layout = q.shape, q.stride(), o_stride + (1,), T, T * n_head * group
     desc.o_stride[:] = o_stride
     desc.cache_layout = K.shape, K.stride()
+    desc.ref = ctypes.byref(desc)
+    desc.evict = None, None              # the last eviction's sizes, and the arguments they make
     return desc
 
 
-def _cache_ptrs(desc, K, V):
+def _entries(t, dtype, n, device):
+    """Address of a tensor of ``n`` entries or more, of this type, on the caches' device (-1: the host); ``None`` and addresses are passed on."""
+    if t is None:
+        return None
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.numel() >= n and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        if isinstance(t, int):
+            return t
+        raise
+    raise ValueError(f"expected a contiguous tensor of {n} {dtype} or more on the caches' device, got {t.dtype}, {tuple(t.shape)}, {t.device}")
+    return t.data_ptr()
+
+
+def _room(workspace, device):
+    """Address and bytes of a workspace (of a tensor of wider elements as many as it has elements)."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("a workspace is a contiguous tensor on the caches' device")
+    return workspace.data_ptr(), workspace.numel()
+
+
+# (torch.cuda.current_device() looks first whether there is a context; where there is a tensor there is one)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_of(device, stream):
+    """``stream``, or the current one, which has to be of the tensors' device (-1: the host)."""
+    if stream is not None:
+        return stream.cuda_stream
+    if device < 0 or _raw_stream is None:
+        return _stream()
+    current = _current_device()
+    if device != current:
+        raise ValueError(f"the tensors are on device {device}, the current one is {current}")
+    return _raw_stream(current)
+
+
+def _cache_ptrs(desc, K, V, device):
     shape, stride = desc.cache_layout
-    if not (K.dtype == V.dtype == torch.bfloat16 and K.shape == V.shape == shape and K.stride() == V.stride() == stride and stride[3] == 1):
-        raise ValueError("caches are bf16 tensors of the descriptor's shape and strides, d_head contiguous")
+    if not (K.dtype == V.dtype == torch.bfloat16 and K.shape == V.shape == shape and K.stride() == V.stride() == stride and stride[3] == 1
+            and V.get_device() == device):
+        raise ValueError("caches are bf16 tensors of the descriptor's shape and strides, d_head contiguous, on one device")
     return K.data_ptr(), V.data_ptr()
 
 
-def _attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse):
-    shape, q_stride, o_stride = desc.layout
+def _attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device):
+    shape, q_stride, o_stride, T, rows = desc.layout
     if not (q.dtype == out.dtype == torch.bfloat16 and q.shape == out.shape == shape and q.stride() == q_stride and out.stride() == o_stride
-            and q_stride[3] == 1):
-        raise ValueError("queries and outputs are bf16 tensors of the descriptor's shape and strides, d_head contiguous")
-    return (q.data_ptr(), *_cache_ptrs(desc, K, V), _ptr(tok_seq), _ptr(pos), out.data_ptr(), _ptr(lse))
+            and q_stride[3] == 1 and q.get_device() == out.get_device() == device):
+        raise ValueError("queries and outputs are bf16 tensors of the descriptor's shape and strides, d_head contiguous, on the caches' device")
+    return (q.data_ptr(), *_cache_ptrs(desc, K, V, device), _entries(tok_seq, torch.int32, T, device), _entries(pos, torch.int32, T, device),
+            out.data_ptr(), _entries(lse, torch.float32, rows, device))
 
 
 def dsmoe_attention_workspace_size(desc: AttentionDesc, kind: int, prefix_len: int = 0) -> int:
@@ -315,21 +359,23 @@ def dsmoe_attention_workspace_size(desc: AttentionDesc, kind: int, prefix_len: i
 def dsmoe_window_attention(desc, window, sinks, rolling, q, K, V, tok_seq, pos, out, lse, workspace, dev_status=None, stream=None):
     """Attention with a sliding window and sinks.  q, out: [T, n_head, group, d_head]; K, V: [n_seq, n_head, L, d_head]; lse: [T, n_head,
     group] fp32 or ``None``."""
-    _check(lib().dsmoe_window_attention(ctypes.byref(desc), window, sinks, rolling, *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse),
-                                        _ptr(workspace), workspace.numel() if workspace is not None else 0, _ptr(dev_status),
-                                        _stream(stream)), "dsmoe_window_attention")
+    device = K.get_device()
+    _check(lib().dsmoe_window_attention(desc.ref, window, sinks, rolling, *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
+                                        *_room(workspace, device), _entries(dev_status, torch.int32, 1, device), _stream_of(device, stream)),
+           "dsmoe_window_attention")
 
 
 def dsmoe_prefix_attention(desc, Kp, Vp, q, K, V, tok_seq, pos, out, lse, workspace, dev_status=None, stream=None):
     """Attention behind a prefix Kp, Vp [n_head, P, d_head] that all tokens share."""
     if not (Kp.dtype == Vp.dtype == torch.bfloat16 and Kp.shape == Vp.shape == (desc.n_head, Kp.shape[1], desc.d_head)
-            and Kp.stride() == Vp.stride() and Kp.stride(2) == 1):
-        raise ValueError("prefixes are bf16 tensors [n_head, P, d_head] of one layout, d_head contiguous")
+            and Kp.stride() == Vp.stride() and Kp.stride(2) == 1 and Kp.get_device() == Vp.get_device() == K.get_device()):
+        raise ValueError("prefixes are bf16 tensors [n_head, P, d_head] of one layout, d_head contiguous, on the caches' device")
     prefix = Prefix(Kp.data_ptr(), Vp.data_ptr(), Kp.shape[1])
     prefix.stride[:] = Kp.stride()[:2]
-    _check(lib().dsmoe_prefix_attention(ctypes.byref(desc), ctypes.byref(prefix), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse),
-                                        _ptr(workspace), workspace.numel() if workspace is not None else 0, _ptr(dev_status),
-                                        _stream(stream)), "dsmoe_prefix_attention")
+    device = K.get_device()
+    _check(lib().dsmoe_prefix_attention(desc.ref, ctypes.byref(prefix), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
+                                        *_room(workspace, device), _entries(dev_status, torch.int32, 1, device), _stream_of(device, stream)),
+           "dsmoe_prefix_attention")
 
 
 def dsmoe_tally_attention(desc, q, K, V, tok_seq, pos, out, lse, tally_in, tally_out, workspace, dev_status=None, stream=None):
@@ -337,9 +383,12 @@ def dsmoe_tally_attention(desc, q, K, V, tok_seq, pos, out, lse, tally_in, tally
     shape = tally_out.shape
     if shape != desc.cache_layout[0][:3] or not (tally_in is None or tally_in is tally_out or tally_in.shape == shape):
         raise ValueError("tallies are [n_seq, n_head, L]")
-    _check(lib().dsmoe_tally_attention(ctypes.byref(desc), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse), _ptr(tally_in),
-                                       _ptr(tally_out), _ptr(workspace), workspace.numel() if workspace is not None else 0,
-                                       _ptr(dev_status), _stream(stream)), "dsmoe_tally_attention")
+    device = K.get_device()
+    # (their entries are counted above)
+    _check(lib().dsmoe_tally_attention(desc.ref, *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
+                                       _entries(tally_in, torch.float32, 0, device), _entries(tally_out, torch.float32, 0, device),
+                                       *_room(workspace, device), _entries(dev_status, torch.int32, 1, device), _stream_of(device, stream)),
+           "dsmoe_tally_attention")
 
 
 def dsmoe_evict_workspace_size(desc: AttentionDesc) -> int:
@@ -348,26 +397,40 @@ def dsmoe_evict_workspace_size(desc: AttentionDesc) -> int:
     return n.value
 
 
+def _evict_args(desc, keep, sinks, recent, shape, stride, room, tally, kept):
+    n_seq, n_head, L, d_head = desc.cache_layout[0]
+    if not (len(shape) == 4 and shape[2] >= keep and shape == (n_seq, n_head, shape[2], d_head) and len(room) == 3 and room[0] == n_seq
+            and room[1] == n_head):
+        raise ValueError("K_out, V_out and tally_out have room for `keep` keys of every sequence and head")
+    if tally != (n_seq, n_head, L) or kept != (n_seq, n_head, keep):
+        raise ValueError("tally is [n_seq, n_head, L], kept is [n_seq, n_head, keep]")
+    args = EvictArgs(int(keep), int(sinks), int(recent))
+    args.out_stride[:], args.tally_pitch = stride[:3], room[2]
+    return ctypes.byref(args)
+
+
 def dsmoe_cache_evict(desc, keep, sinks, recent, length, tally, K, V, kept, len_out, tally_out, K_out, V_out, workspace, dev_status=None,
                       stream=None):
     """Thins a cache out to ``keep`` keys a sequence and head.  K_out, V_out: [n_seq, n_head, at least keep, d_head], or K and V themselves;
     tally_out: [n_seq, n_head, at least keep], or tally."""
-    # (each look at a tensor's shape or strides makes an object, and small calls are as long as the host takes)
-    n_seq, n_head, L, d_head = desc.cache_layout[0]
+    # (each look at a tensor's shape or strides makes an object, and small calls are as long as the host takes: sizes like the last call's are not
+    # compared with one another, nor laid out for the library, again)
+    device, n_seq = K.get_device(), desc.n_seq
     in_place = K_out is K and V_out is V                 # (checked with them)
     shape, stride = desc.cache_layout if in_place else (K_out.shape, K_out.stride())
-    room = tally_out.shape
-    if not ((in_place or (K_out.dtype == V_out.dtype == torch.bfloat16 and V_out.shape == shape and V_out.stride() == stride and stride[3] == 1))
-            and shape[2] >= keep and shape == (n_seq, n_head, shape[2], d_head) and len(room) == 3 and room[0] == n_seq and room[1] == n_head):
-        raise ValueError("K_out, V_out and tally_out have room for `keep` keys of every sequence and head, K_out and V_out one layout")
-    if (room if tally is tally_out else tally.shape) != (n_seq, n_head, L) or kept.shape != (n_seq, n_head, keep):
-        raise ValueError("tally is [n_seq, n_head, L], kept is [n_seq, n_head, keep]")
-    args = EvictArgs(int(keep), int(sinks), int(recent))
-    args.out_stride[:] = stride[:3]
-    args.tally_pitch = room[2]
-    _check(lib().dsmoe_cache_evict(ctypes.byref(desc), ctypes.byref(args), _ptr(length), _ptr(tally), *_cache_ptrs(desc, K, V), _ptr(kept),
-                                   _ptr(len_out), _ptr(tally_out), K_out.data_ptr(), V_out.data_ptr(), _ptr(workspace),
-                                   workspace.numel() if workspace is not None else 0, _ptr(dev_status), _stream(stream)),
+    sizes = keep, sinks, recent, shape, stride, tally_out.shape, tally.shape, kept.shape
+    last, args = desc.evict
+    if last != sizes:
+        args = _evict_args(desc, *sizes)
+        desc.evict = sizes, args
+    if not (in_place or (K_out.dtype == V_out.dtype == torch.bfloat16 and V_out.shape == shape and V_out.stride() == stride and stride[3] == 1
+                         and K_out.get_device() == V_out.get_device() == device)):
+        raise ValueError("K_out and V_out are bf16 tensors of one shape and layout, d_head contiguous, on the caches' device")
+    _check(lib().dsmoe_cache_evict(desc.ref, args, _entries(length, torch.int32, n_seq, device),
+                                   _entries(tally, torch.float32, 0, device), *_cache_ptrs(desc, K, V, device), _entries(kept, torch.int32, 0, device),
+                                   _entries(len_out, torch.int32, n_seq, device), _entries(tally_out, torch.float32, 0, device), K_out.data_ptr(),
+                                   V_out.data_ptr(), *_room(workspace, device), _entries(dev_status, torch.int32, 1, device),
+                                   _stream_of(device, stream)),
            "dsmoe_cache_evict")
 
 

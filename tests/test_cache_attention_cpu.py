@@ -258,3 +258,68 @@ def test_places_for_what_stays_that_overlap():
         assert got == (1 if meet else 3), (n, stride, off)
         seen.add((meet, abs(off) < span))
     assert seen == {(True, True), (False, True), (False, False)}
+
+
+def test_the_binding_checks_numbers_and_lengths():
+    """What the kernels read as int32 and fp32 is that, and is long enough."""
+    q, K = torch.zeros((4, 2, 3, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 32, 64), dtype=torch.bfloat16)
+    desc, pos, tally = dm.make_attention_desc(q, K, 0.125), torch.zeros(4, dtype=torch.int32), torch.zeros((2, 2, 32))
+    stream = type("S", (), {"cuda_stream": 0})
+    Kp = torch.zeros((2, 8, 64), dtype=torch.bfloat16)
+
+    def calls(**kw):
+        a = dict(q=q, K=K, V=K.clone(), tok_seq=pos, pos=pos, out=torch.zeros_like(q), lse=torch.zeros(4, 2, 3))
+        a.update({k: v for k, v in kw.items() if k in a})
+        dev_status, tally_in, prefix = kw.get("dev_status"), kw.get("tally_in", tally), kw.get("Kp", Kp)
+        yield lambda: dm.dsmoe_window_attention(desc, 4, 0, False, *a.values(), None, dev_status, stream)
+        yield lambda: dm.dsmoe_prefix_attention(desc, prefix, prefix, *a.values(), None, dev_status, stream)
+        yield lambda: dm.dsmoe_tally_attention(desc, *a.values(), tally_in, kw.get("tally_out", tally), None, dev_status, stream)
+
+    for call in calls():                                  # nothing wrong but the missing workspace
+        with pytest.raises(dm.DsmoeError):
+            call()
+    for kw in (dict(pos=pos.long()), dict(tok_seq=pos.long()), dict(pos=pos[:3]), dict(tok_seq=pos[:3]), dict(pos=torch.zeros((4, 2), dtype=torch.int32)[:, 0]),
+               dict(lse=torch.zeros(4, 2, 3).double()), dict(lse=torch.zeros(4, 2, 2)), dict(lse=torch.zeros(4, 3, 2).transpose(1, 2)),
+               dict(dev_status=torch.zeros(1, dtype=torch.int64)), dict(dev_status=pos[:0])):
+        for call in calls(**kw):
+            with pytest.raises(ValueError):
+                call()
+    for kw in (dict(tally_in=tally.double()), dict(tally_out=tally.bfloat16()), dict(tally_in=tally.half(), tally_out=tally.clone())):
+        with pytest.raises(ValueError):
+            list(calls(**kw))[2]()
+    out, room, kept, length = torch.zeros((2, 2, 8, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 8)), torch.zeros((2, 2, 8), dtype=torch.int32), pos[:2]
+    good = dict(length=length, tally=tally, K=K, V=K.clone(), kept=kept, len_out=length, tally_out=room, K_out=out, V_out=out.clone(), workspace=None, dev_status=None)
+    for kw in (dict(length=length.long()), dict(length=pos[:1]), dict(len_out=length.long()), dict(len_out=pos[:1]), dict(kept=kept.long()),
+               dict(kept=kept.float()), dict(tally=tally.double()), dict(tally_out=room.double()), dict(tally=tally.transpose(0, 1)),
+               dict(dev_status=length.long())):
+        with pytest.raises(ValueError):
+            dm.dsmoe_cache_evict(desc, 8, 0, 0, *{**good, **kw}.values(), stream)
+    with pytest.raises(dm.DsmoeError):
+        dm.dsmoe_cache_evict(desc, 8, 0, 0, *good.values(), stream)
+
+
+def test_the_binding_checks_devices(monkeypatch):
+    """Tensors on several devices, and on another than the current one.  (There is one device here: some say that they are elsewhere.)"""
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 1
+    away = lambda x: x.as_subclass(Elsewhere)
+    q, K = torch.zeros((4, 2, 3, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 32, 64), dtype=torch.bfloat16)
+    desc, pos, tally = dm.make_attention_desc(q, K, 0.125), torch.zeros(4, dtype=torch.int32), torch.zeros((2, 2, 32))
+    good = dict(q=q, K=K, V=K.clone(), tok_seq=pos, pos=pos, out=torch.zeros_like(q), lse=torch.zeros(4, 2, 3), workspace=torch.zeros(8, dtype=torch.uint8),
+                dev_status=pos, stream=type("S", (), {"cuda_stream": 0}))
+    for name in list(good)[:-1]:
+        with pytest.raises(ValueError):
+            dm.dsmoe_window_attention(desc, 4, 0, False, *{**good, name: away(good[name])}.values())
+    Kp = torch.zeros((2, 8, 64), dtype=torch.bfloat16)
+    for a, b in ((away(Kp), Kp), (Kp, away(Kp))):
+        with pytest.raises(ValueError):
+            dm.dsmoe_prefix_attention(desc, a, b, *good.values())
+    with pytest.raises(ValueError):
+        dm.dsmoe_tally_attention(desc, *list(good.values())[:7], tally, away(tally.clone()), *list(good.values())[7:])
+    monkeypatch.setattr(dm.binding, "_current_device", lambda: 0)
+    here = {k: away(v) if isinstance(v, torch.Tensor) else v for k, v in good.items()}
+    with pytest.raises(ValueError, match="current"):
+        dm.dsmoe_window_attention(desc, 4, 0, False, *{**here, "stream": None}.values())
+    with pytest.raises(dm.DsmoeError):                    # one device, and a stream that the caller has chosen: what is missing is workspace
+        dm.dsmoe_window_attention(desc, 4, 0, False, *here.values())
