@@ -192,13 +192,14 @@ AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, b
         return at;
     };
     const size_t rows = (size_t)A.T * A.n_head * A.group, blocks = (size_t)tile_blocks(A.T, A.group);
-    w.ctas = stream_ctas(A, S, true);
-    w.passes = ceil_div(A.T, kListTokens);
-    const size_t warps = (size_t)w.passes * w.ctas * 8;
+    // The stream kernel has no token to attend where the 128-row kernel takes all: then it has the shared keys, or is not launched
+    const bool tiles = own_on_tiles(A), streams_own = !tiles || A.n_seq > 1;
+    w.ctas = stream_ctas(A, S, streams_own);
+    w.passes = streams_own ? ceil_div(A.T, kListTokens) : S.P > 0 ? 1 : 0;
+    const size_t warps = (size_t)w.passes * w.ctas * stream_warps(A.d_head);
     w.slots = take(2 * warps * part_bytes(A.d_head));
     w.run_head = take(warps * sizeof(int2));
-    w.head = take((size_t)A.n_head * ((size_t)A.T * A.row_tiles + S.row_tiles) * sizeof(int2));
-    const bool tiles = own_on_tiles(A);
+    w.head = take((size_t)A.n_head * ((streams_own ? (size_t)A.T * A.row_tiles : 0) + (S.P > 0 ? S.row_tiles : 0)) * sizeof(int2));
     if (wants_ml) {
         w.ml = take(rows * sizeof(float2));
         // Decoding: the logits are written and read again (8 bytes a key and row), not the keys read and multiplied again
@@ -218,14 +219,16 @@ AttnPlan attention_plan(const AttnView& A, const SharedKeys& S, bool may_tile, b
     }
     if (tiles) {
         w.own_splits = tile_splits(A, A.L);
-        w.count = take(blocks * 4);
-        w.list = take(blocks * tile_span(A.group) * 4);
+        if (streams_own) {
+            w.count = take(blocks * 4);
+            w.list = take(blocks * tile_span(A.group) * 4);
+        }
     }
     if (S.P > 0 && may_tile && (long long)A.T * A.group > kPrefixStreamRows) w.prefix_splits = tile_splits(A, S.P);
     if (S.P > 0 || w.own_splits > 1) w.row_parts = (S.P > 0 ? std::max(1, w.prefix_splits) : 0) + std::max(1, w.own_splits);
     w.row_ml = take((size_t)w.row_parts * rows * 2 * 4);
     w.row_o = take((size_t)w.row_parts * rows * A.d_head * 4);
-    w.total = off;
+    w.total = std::max(off, (size_t)256); // (so that there is an address to pass)
     w.fits = off < (size_t)1 << 36;       // (attention_sum_kernel finds parts by their number of 16 bytes, in 32 bits)
     return w;
 }
@@ -267,9 +270,9 @@ dsmoe_status attend(const AttnView& A, const SharedKeys& S, const AttnPlan& w, c
         if (plan.keep) {
             plan.own_rows = next_parts(splits);
             tile.o = plan.own_rows.o, tile.ml = plan.own_rows.ml;
-            tile.head = head + (size_t)A.n_head * plan.shared.row_tiles;
         }
         if (!one_sequence) {
+            if (plan.keep) tile.head = head + (size_t)A.n_head * plan.shared.row_tiles;
             plan.count = tile.count = reinterpret_cast<int32_t*>(ws + w.count);
             plan.list = tile.list = reinterpret_cast<int32_t*>(ws + w.list);
             plan.blocks = tile_blocks(A.T, A.group);

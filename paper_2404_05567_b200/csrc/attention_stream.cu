@@ -55,7 +55,7 @@ constexpr int kPartsAtMost = 200;         // BY_WARP: parts that the longest pai
 
 template <int DH>
 struct StreamGeo {
-    static constexpr int WARPS = DH <= 128 ? 8 : 4;
+    static constexpr int WARPS = stream_warps(DH);
     static constexpr int STRIDE = DH * 2 + 16;                     // bytes per key row in shared memory: 16 of padding, no bank conflicts
     static constexpr int UNIT = 2 * kUnit * STRIDE;                // K and V; also holds a warp's 16 x (DH + 8) accumulators
     static constexpr int FIT = 208 * 1024 / (WARPS * UNIT);
@@ -539,8 +539,6 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
 // (no `keep`) per run of the stream kernel's, for the pair that begins there and goes on.  First the weights of all parts, a warp per
 // row, then the sums, a thread per four columns, with sixteen loads under way.
 constexpr int kSumParts = 544;                           // parts at most: whole rows' 2 x 64, and twice a part per SM or kPartsAtMost + 2
-
-__host__ __device__ static inline int stream_warps(int d_head) { return d_head <= 128 ? 8 : 4; }
 
 // ROWS: rows at a time, a warp each: four for groups of up to four, so that twice as many CTAs fit an SM: 2048 pairs of 4 rows and 5 parts, 11.6 us, with
 // eight 19.7.

@@ -104,7 +104,7 @@ struct StreamPlan {
     SharedKeys shared;
     const int32_t *count, *list;
     int blocks, span;
-    int ctas, passes;                     // passes of kListTokens tokens at most
+    int ctas, passes;                     // passes of kListTokens tokens at most; the shared keys are the first one's
     bool own;                             // attends tokens at all
     // A pair that several CTAs share leaves a part per CTA; one that lies in one CTA's keys is written to out and lse, or (keep) its rows to `own_rows`
     // and `shared_rows`: something else is still to be added
@@ -112,13 +112,14 @@ struct StreamPlan {
     bool by_warp;                         // runs are warps', not CTAs'
     bool whole;                           // each CTA's run is a pair's units: no parts (not with shared keys, a list or more than a pass)
     int heads_at_once;                    // neighbouring pairs of a token that a CTA takes together
-    float* slots;                         // [passes][runs][2][heads_at_once][16][d_head + 2], runs = ctas * (8 or 4 warps) / heads_at_once
+    float* slots;                         // [passes][runs][2][heads_at_once][16][d_head + 2], runs = ctas * stream_warps / heads_at_once
     int2* head;                           // keep: [pairs]: first run, parts_word
     int2* run_head;                       // otherwise: [passes][runs]: the first of the pairs that begin in that run and go on, parts_word; or 0 parts
     RowParts own_rows, shared_rows;       // n = 1
     float* logits;                        // nullable: the tokens' logits in base 2, row r's from r * logit_pitch on (no window, no ring)
     long long logit_pitch;                // a multiple of 16
 };
+__host__ __device__ static constexpr int stream_warps(int d_head) { return d_head <= 128 ? 8 : 4; }       // of a CTA
 static inline size_t part_bytes(int d_head) { return (size_t)16 * (d_head + 2) * 4; }
 
 // The 128-row kernel: heads of 64, 96 and 128, caches that a tensor map describes.  Its rows' keys are cut into `splits`; o, ml: where their parts

@@ -323,3 +323,20 @@ def test_the_binding_checks_devices(monkeypatch):
         dm.dsmoe_window_attention(desc, 4, 0, False, *{**here, "stream": None}.values())
     with pytest.raises(dm.DsmoeError):                    # one device, and a stream that the caller has chosen: what is missing is workspace
         dm.dsmoe_window_attention(desc, 4, 0, False, *here.values())
+
+
+def test_workspaces_hold_what_the_calls_use():
+    """Prompts of one sequence and heads of more than 128 have no room for parts that nobody leaves."""
+    def one(T, d=128, n_seq=1, kind=0, P=0):
+        row = 4 * 5 * d
+        return _size(_desc(T=T, n_head=4, group=5, d_head=d, n_seq=n_seq, L=T, o_stride=(row, 5 * d, d), q_stride=(row, 5 * d, d),
+                           kv_stride=(4 * T * d, T * d, d)), kind, P)[1]
+    # (one part of the rows at most where there are enough tokens to fill the GPU)
+    for T in (8192, 32768, 131072):
+        rows = T * 20
+        assert one(T) < 1 << 20
+        assert one(T, kind=dm.ATTENTION_TALLY) < rows * 8 + T * 8 + 4 * T * 4 * 16 + (1 << 20)
+        assert one(T, kind=dm.ATTENTION_PREFIX, P=1000) < 2 * rows * (128 + 2) * 4 + (64 << 20)
+        assert one(T, n_seq=2) > 100 << 20               # tokens of short runs may be left to the other kernel
+    # a pass of 512 tokens: for each warp of 148 CTAs two tiles of 16 rows
+    assert one(512, 160, 512) < 2.1 * 148 * 4 * 16 * 162 * 4 + (1 << 20) < one(512, 128, 512)
