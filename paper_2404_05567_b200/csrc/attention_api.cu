@@ -142,7 +142,7 @@ AttnView view_of(const dsmoe_attention_desc& d, const void* q, const void* K, co
 // its MMAs), its keys cut so that all SMs have some; with fewer rows on the stream kernel, in one launch with the own caches.  The own caches:
 // where there are more tokens than sequences, on the 128-row kernel, which leaves tokens that have too few neighbours of their sequence; otherwise,
 // and for those, on the stream kernel.
-constexpr int kPrefixStreamRows = 32, kOwnTileRows = 64, kMaxSplits = 64;
+constexpr int kPrefixStreamRows = 32, kOwnTileRows = 64;
 constexpr int kMaxTallyParts = 16;
 constexpr size_t kMostLogits = (size_t)512 << 20;
 

@@ -51,7 +51,16 @@ __device__ __forceinline__ void write_sums(const AttnView& A, size_t at, float z
     if (A.ml) A.ml[at] = make_float2(z, den == 0.f ? 0.f : 1.f / den);
 }
 
-constexpr int kPartsAtMost = 200;         // BY_WARP: parts that the longest pair leaves (with more there are fewer runs)
+// BY_WARP: runs that `total` units are cut into, `most` at most.  None is shorter than a kPartsAtMost-th of the longest pair's units, so that no pair lies in
+// more than kPartsAtMost + 1 runs.
+constexpr int kPartsAtMost = 200;
+__host__ __device__ constexpr long long warp_runs(long long total, long long longest, long long most) {
+    const long long least = (longest + kPartsAtMost - 1) / kPartsAtMost, runs = total / least;
+    return runs < 1 ? 1 : runs < most ? runs : most;
+}
+// (runs are of total / runs units and more: 250 units beside 159 and 1183 pairs of one)
+static_assert(250 <= (kPartsAtMost - 1) * (409 / warp_runs(409, 250, 1184)) + 1 && 250 <= (kPartsAtMost - 1) * (1433 / warp_runs(1433, 250, 1184)) + 1);
+static_assert(warp_runs(1, 1, 1184) == 1 && warp_runs(100000, 400, 1184) == 1184 && warp_runs(800, 800, 1184) == 200);
 
 template <int DH>
 struct StreamGeo {
@@ -174,7 +183,7 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
         int longest = first ? (P.shared.P + kUnit - 1) / kUnit : 1;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) longest = max(longest, longest_s[w]);
-        wanted = max(1ll, min(min((long long)gridDim.x * KW, total), kPartsAtMost * total / longest));
+        wanted = warp_runs(total, longest, (long long)gridDim.x * KW);
     }
     const int pairs_each = own_heads / HB;              // pairs (of HB heads) of a token
     if (P.whole) wanted = (long long)n * pairs_each;
@@ -538,7 +547,9 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
 // Adds up the parts of a pair's rows, in order: parts of whole rows, those of the shared keys, then those of the token's own.  A CTA per pair, or
 // (no `keep`) per run of the stream kernel's, for the pair that begins there and goes on.  First the weights of all parts, a warp per
 // row, then the sums, a thread per four columns, with sixteen loads under way.
-constexpr int kSumParts = 544;                           // parts at most: whole rows' 2 x 64, and twice a part per SM or kPartsAtMost + 2
+// Parts at most: the prefix's and the own caches' parts of whole rows, and of the shared keys' pair and the own one a part a CTA, or a run of warp_runs
+constexpr int kSumParts = 544;
+static_assert(kSumParts >= 2 * kMaxSplits + 2 * (kMostStreamCtas > kPartsAtMost + 1 ? kMostStreamCtas : kPartsAtMost + 1), "a place for each part");
 
 // ROWS: rows at a time, a warp each: four for groups of up to four, so that twice as many CTAs fit an SM: 2048 pairs of 4 rows and 5 parts, 11.6 us, with
 // eight 19.7.
@@ -710,7 +721,7 @@ int stream_ctas(const AttnView& A, const SharedKeys& shared, bool own) {
     const long long seen = A.window < A.L ? (long long)A.window + A.sinks : A.L, warps = stream_warps(A.d_head);
     long long units = own ? ((seen + kUnit - 1) / kUnit + 1) * ((long long)A.T * A.n_head * A.row_tiles) : 0;
     units += (long long)((shared.P + kUnit - 1) / kUnit) * A.n_head * shared.row_tiles;
-    const long long wanted = (units + warps - 1) / warps, most = sm_count() < 160 ? sm_count() : 160;      // (kSumParts)
+    const long long wanted = (units + warps - 1) / warps, most = sm_count() < kMostStreamCtas ? sm_count() : kMostStreamCtas;
     return (int)(wanted < most ? wanted : most);
 }
 

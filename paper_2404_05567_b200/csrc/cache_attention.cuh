@@ -39,6 +39,8 @@ struct AttnView {
 constexpr float kMoves = 32.f;
 
 constexpr int kUnit = 16;                 // keys that a warp takes at a time
+constexpr int kMaxSplits = 64;            // parts that the 128-row kernel's keys are cut into
+constexpr int kMostStreamCtas = 160;      // CTAs of the streaming kernel, one an SM
 constexpr int kListTokens = 512;         // tokens whose keys are cut into runs at a time
 
 // The keys that a token sees: 0 .. sinks - 1 and first .. last (nothing: last < first and sinks == 0).

@@ -5,6 +5,8 @@ import torch
 import paper_2404_05567_b200 as dm
 from cache_attention_reference import Case
 from test_gpu_attention_tiles import prompt
+from test_gpu_prefix_attention import run as run_prefix
+from test_gpu_window_attention import run as run_window
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +73,10 @@ def test_workspaces(name, plain_heads):
             for a, b in zip(results[0], other):
                 assert torch.equal(a, b)
         assert torch.isfinite(results[0][0].float()).all()
+
+
+def test_a_long_pair_among_many_short_ones():
+    """Runs of single warps, the last pair as long as 250 units and the others one: its parts are no more than the sum has places for."""
+    run_window(Case([(0, 0)] * 1183 + [(1, 3999)], 1, 1, 32, 2, 4000, seed=1), 2 ** 31 - 1)
+    tokens = [(0, 0)] * 31 + [(1, 3999)]
+    run_prefix(Case(tokens, 40, 1, 32, 2, 4000, P=500, seed=2))
