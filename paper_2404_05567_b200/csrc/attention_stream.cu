@@ -403,8 +403,8 @@ attention_stream_kernel(const __grid_constant__ AttnView A, const __grid_constan
                     if (g + 8 < rows) *reinterpret_cast<float2*>(to + (g + 8) * P.logit_pitch + i * 8) = make_float2(sc[i][2], sc[i][3]);
                 }
             }
-            // (see kMoves)
-            if (__any_sync(0xffffffffu, b0 > m0 + kMoves || b1 > m1 + kMoves || (m0 == -INFINITY && b0 > m0) || (m1 == -INFINITY && b1 > m1))) {
+            // (see kStreamMoves)
+            if (__any_sync(0xffffffffu, b0 > m0 + kStreamMoves || b1 > m1 + kStreamMoves || (m0 == -INFINITY && b0 > m0) || (m1 == -INFINITY && b1 > m1))) {
                 b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 1));
                 b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 1));
                 b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 2));

@@ -587,8 +587,9 @@ attention_tile_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_con
             S.swap[r][half][at] = l;
             pair_sync(pair);
             l = S.swap[r][0][at] + S.swap[r][1][at];
-            // Where the last tile's weights were far above 1, the maximum follows them by a power of two: 1 / l and other parts' factors keep their bits
-            const bool high = l >= 0x1p64f;                               // (infinite sums are found below)
+            // Where weights were far above 1, the maximum follows them by a power of two: 1 / l and other parts' factors keep their bits, and parts of
+            // large values have a sum
+            const bool high = l >= 0x1p16f;                               // (infinite sums are found below)
             const int up = high ? min((int)(__float_as_uint(l) >> 23) - 127, 126) : 0;
             const float down = __uint_as_float((uint32_t)(127 - up) << 23);
             l *= down;

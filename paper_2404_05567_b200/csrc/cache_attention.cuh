@@ -37,6 +37,8 @@ struct AttnView {
 // so a single tile's weights may be larger there.  With 8, a row whose first keys happened to have small
 // logits (four sinks) moved now and then, and one such row held up its tile: a prompt of 8192 tokens 359 us, 311 with 32.
 constexpr float kMoves = 32.f;
+// In the streaming kernel, which has no second way for rows whose sums overflow: with large values (2^96) 2^32 of them do, where 2^8 do not.  Its times are the same.
+constexpr float kStreamMoves = 8.f;
 
 constexpr int kUnit = 16;                 // keys that a warp takes at a time
 constexpr int kMaxSplits = 64;            // parts that the 128-row kernel's keys are cut into

@@ -7,7 +7,7 @@ import torch
 import cache_attention_reference as ref
 from cache_attention_reference import Case
 from test_gpu_attention_tiles import prompt
-from test_gpu_prefix_attention import call as call_prefix
+from test_gpu_prefix_attention import call as call_prefix, run as run_prefix
 from test_gpu_tally_attention import run as run_tally
 from test_gpu_window_attention import call as call_window, run
 
@@ -118,3 +118,21 @@ def test_tallies_of_keys_of_no_weight(group, monkeypatch):
     run_tally(c)
     want = c.expected()[4]
     assert (want[0, 0, [7, 130]] == 0).all()
+
+
+# (a CTA's keys; a pair cut into parts; runs of warps; a prompt; keys of a prompt in parts; prefixes on either kernel)
+@pytest.mark.parametrize("tokens,n_seq,L,P", [([(0, 150)], 1, 160, 0), ([(0, 4000), (1, 300)], 2, 4001, 0), ([(s % 2, 200) for s in range(1300)], 1300, 201, 0),
+                                              (prompt(0, 383, 60), 1, 384, 0), (prompt(0, 1099, 60), 1, 1100, 0), ([(0, 40), (1, 20)], 2, 50, 700),
+                                              ([(s, 40) for s in range(20)], 20, 50, 1000)])
+@pytest.mark.parametrize("jump", [7.0, 31.0, 60.0, 120.0])
+def test_values_far_above_1(tokens, n_seq, L, P, jump):
+    """Values of about 2^100, whose weighted mean is a number of 32 bits, behind logits that grow by `jump`."""
+    n_head = 1 if len(tokens) > 1000 else 2
+    c = with_logits(Case(tokens, n_head, 2, 64, n_seq, L, P=P, seed=L, scale=LN2), 0.0, {l: jump * l / (L - 1) for l in range(0, L, 3)})
+    c.V = (c.V.float() * 2.0 ** 110).to(torch.bfloat16)
+    c.V_np = c.V.float().cpu().numpy()
+    if P:
+        c.Kp[..., 0] = torch.linspace(0, jump, P, device="cuda").bfloat16()
+        c.Vp = (c.Vp.float() * 2.0 ** 100).to(torch.bfloat16)
+        c.Kp_np, c.Vp_np = (x.float().cpu().numpy() for x in (c.Kp, c.Vp))
+    run_prefix(c) if P else run(c, 2 ** 31 - 1)
