@@ -359,13 +359,19 @@ dsmoe_status dsmoe_moa_forward(const dsmoe_layer_desc* desc, const dsmoe_moa_arg
  *   lse      fp32 [T][n_head][group] or NULL: the natural logarithm of the sum of the exponentials of a row's logits.
  *
  * All strides are multiples of 8 elements, addresses of 16 bytes.  d_head a multiple of 32 up to 256, group up to 64, L up to 2^30, strides up to 2^40
- * and a tensor's last row less than 2^50 elements behind its first, otherwise
- * DSMOE_ERR_UNSUPPORTED.  The memory from out's first element to its last must not overlap q's or the caches'.  Products of bf16 are added
- * in fp32, softmax statistics are fp32, and out is rounded once; the weights that multiply the values are two bf16 numbers each (as good as
- * 16 bits), on the 128-row tiles of prompts and long prefixes one.  Keys that a token does not see may hold anything, numbers or not.  A tok_seq or pos entry out of range is clamped and reported
- * as DSMOE_ERR_INVALID_ARG in *dev_status.  workspace: dsmoe_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one
- * call to the next.  Results do not change from run to run.  A call with no more tokens than sequences (and tok_seq) is taken for decoding;
- * a prompt in a cache of more slots than it has tokens is faster with K and V of its own sequence, n_seq 1 and no tok_seq.
+ * and a tensor's last row less than 2^50 elements behind its first, otherwise DSMOE_ERR_UNSUPPORTED.  The memory from out's first element to
+ * its last must not overlap q's or the caches'.
+ * Products of bf16 are added in fp32, softmax statistics are fp32, and out is rounded once.  The weights that multiply the values are two bf16
+ * numbers each (as good as 16 bits); or one (8 bits) where 128 rows are taken at a time, which is so with d_head 64, 96 or 128, scale > 0 and keys
+ * whose strides are not 0,
+ *   for the tokens' own caches in calls of more tokens than sequences (without tok_seq: of more than one token) and T * group >= 64 rows; of several
+ *   sequences, tokens whose neighbours of the same sequence have fewer than 32 rows with them may still get 16 bits;
+ *   for the keys of a prefix in calls of T * group > 32 rows, however long the prefix is.
+ * Keys that a token does not see may hold anything, numbers or not; a row with a query, or a key that it sees, that is no number is none.
+ * A tok_seq or pos entry out of range is clamped and reported as DSMOE_ERR_INVALID_ARG in *dev_status.  workspace:
+ * dsmoe_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one call to the next.  Results do not change from run to
+ * run.  A call with no more tokens than sequences (and tok_seq) is taken for decoding; a prompt in a cache of more slots than it has tokens is
+ * faster with K and V of its own sequence, n_seq 1 and no tok_seq.
  */
 typedef struct dsmoe_attention_desc {
     int32_t T, n_head, group, d_head, n_seq, L;
