@@ -287,7 +287,6 @@ def make_attention_desc(q, K, scale=1.0, out=None) -> AttentionDesc:
         desc.layout = q.shape, q.stride(), o_stride + (1,), T, T * n_head * group
     desc.o_stride[:] = o_stride
     desc.cache_layout = K.shape, K.stride()
-    desc.ref = ctypes.byref(desc)
     desc.evict = None, None              # the last eviction's sizes, and the arguments they make
     return desc
 
@@ -360,7 +359,7 @@ def dsmoe_window_attention(desc, window, sinks, rolling, q, K, V, tok_seq, pos, 
     """Attention with a sliding window and sinks.  q, out: [T, n_head, group, d_head]; K, V: [n_seq, n_head, L, d_head]; lse: [T, n_head,
     group] fp32 or ``None``."""
     device = K.get_device()
-    _check(lib().dsmoe_window_attention(desc.ref, window, sinks, rolling, *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
+    _check(lib().dsmoe_window_attention(ctypes.byref(desc), window, sinks, rolling, *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
                                         *_room(workspace, device), _entries(dev_status, torch.int32, 1, device), _stream_of(device, stream)),
            "dsmoe_window_attention")
 
@@ -373,7 +372,7 @@ def dsmoe_prefix_attention(desc, Kp, Vp, q, K, V, tok_seq, pos, out, lse, worksp
     prefix = Prefix(Kp.data_ptr(), Vp.data_ptr(), Kp.shape[1])
     prefix.stride[:] = Kp.stride()[:2]
     device = K.get_device()
-    _check(lib().dsmoe_prefix_attention(desc.ref, ctypes.byref(prefix), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
+    _check(lib().dsmoe_prefix_attention(ctypes.byref(desc), ctypes.byref(prefix), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
                                         *_room(workspace, device), _entries(dev_status, torch.int32, 1, device), _stream_of(device, stream)),
            "dsmoe_prefix_attention")
 
@@ -385,7 +384,7 @@ def dsmoe_tally_attention(desc, q, K, V, tok_seq, pos, out, lse, tally_in, tally
         raise ValueError("tallies are [n_seq, n_head, L]")
     device = K.get_device()
     # (their entries are counted above)
-    _check(lib().dsmoe_tally_attention(desc.ref, *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
+    _check(lib().dsmoe_tally_attention(ctypes.byref(desc), *_attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device),
                                        _entries(tally_in, torch.float32, 0, device), _entries(tally_out, torch.float32, 0, device),
                                        *_room(workspace, device), _entries(dev_status, torch.int32, 1, device), _stream_of(device, stream)),
            "dsmoe_tally_attention")
@@ -406,7 +405,7 @@ def _evict_args(desc, keep, sinks, recent, shape, stride, room, tally, kept):
         raise ValueError("tally is [n_seq, n_head, L], kept is [n_seq, n_head, keep]")
     args = EvictArgs(int(keep), int(sinks), int(recent))
     args.out_stride[:], args.tally_pitch = stride[:3], room[2]
-    return ctypes.byref(args)
+    return args
 
 
 def dsmoe_cache_evict(desc, keep, sinks, recent, length, tally, K, V, kept, len_out, tally_out, K_out, V_out, workspace, dev_status=None,
@@ -426,7 +425,7 @@ def dsmoe_cache_evict(desc, keep, sinks, recent, length, tally, K, V, kept, len_
     if not (in_place or (K_out.dtype == V_out.dtype == torch.bfloat16 and V_out.shape == shape and V_out.stride() == stride and stride[3] == 1
                          and K_out.get_device() == V_out.get_device() == device)):
         raise ValueError("K_out and V_out are bf16 tensors of one shape and layout, d_head contiguous, on the caches' device")
-    _check(lib().dsmoe_cache_evict(desc.ref, args, _entries(length, torch.int32, n_seq, device),
+    _check(lib().dsmoe_cache_evict(ctypes.byref(desc), ctypes.byref(args), _entries(length, torch.int32, n_seq, device),
                                    _entries(tally, torch.float32, 0, device), *_cache_ptrs(desc, K, V, device), _entries(kept, torch.int32, 0, device),
                                    _entries(len_out, torch.int32, n_seq, device), _entries(tally_out, torch.float32, 0, device), K_out.data_ptr(),
                                    V_out.data_ptr(), *_room(workspace, device), _entries(dev_status, torch.int32, 1, device),

@@ -1,4 +1,5 @@
 """The attention steps on a key/value cache: the plain forms that the GPU tests compare with, and what the calls refuse (no GPU needed)."""
+import copy
 import ctypes
 
 import numpy as np
@@ -340,3 +341,23 @@ def test_workspaces_hold_what_the_calls_use():
         assert one(T, n_seq=2) > 100 << 20               # tokens of short runs may be left to the other kernel
     # a pass of 512 tokens: for each warp of 148 CTAs two tiles of 16 rows
     assert one(512, 160, 512) < 2.1 * 148 * 4 * 16 * 162 * 4 + (1 << 20) < one(512, 128, 512)
+
+
+def test_descriptors_can_be_copied():
+    """A copy is a descriptor of its own, also behind a call."""
+    q, K = torch.zeros((4, 2, 3, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 32, 64), dtype=torch.bfloat16)
+    desc, pos, tally, stream = dm.make_attention_desc(q, K, 0.125), torch.zeros(4, dtype=torch.int32), torch.zeros((2, 2, 32)), type("S", (), {"cuda_stream": 0})
+    kept = torch.zeros((2, 2, 8), dtype=torch.int32)
+
+    def code(d, **kw):
+        with pytest.raises(dm.DsmoeError) as e:
+            if kw:
+                dm.dsmoe_cache_evict(d, 8, kw["sinks"], 0, pos[:2], tally, K, V, kept, pos[:2], tally, K, V, None, None, stream)
+            else:
+                dm.dsmoe_window_attention(d, 4, 0, False, q, K, V, None, pos, torch.zeros_like(q), None, None, None, stream)
+        return e.value.code
+    V = K.clone()
+    assert code(desc) == 3 and code(desc, sinks=2) == 3 and code(desc, sinks=9) == 1 and code(desc, sinks=2) == 3
+    for other in (copy.copy(desc), copy.deepcopy(desc)):
+        other.scale, other.kv_stride[1] = float("nan"), 4
+        assert code(other) == 1 and code(other, sinks=2) == 1 and code(desc) == 3 and code(desc, sinks=2) == 3
