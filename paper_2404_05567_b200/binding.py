@@ -303,7 +303,6 @@ def _entries(t, dtype, n, device):
             return t
         raise
     raise ValueError(f"expected a contiguous tensor of {n} {dtype} or more on the caches' device, got {t.dtype}, {tuple(t.shape)}, {t.device}")
-    return t.data_ptr()
 
 
 def _room(workspace, device):
