@@ -445,6 +445,79 @@ dsmoe_status dsmoe_cache_evict(const dsmoe_attention_desc* desc, const dsmoe_evi
                                void* workspace, size_t ws_bytes, int32_t* dev_status, dsmoe_stream stream);
 
 /*
+ * A key/value cache in 4 bits, written as tokens come and attended to as it is: 4.5 bits a value instead of 16 (the paper has no counterpart).
+ *
+ * A row (sequence, head, position) of K or V is d_head values in groups of 32 neighbours.  A group has a scale s (bf16): its largest magnitude / 7, rounded up to
+ * four significant bits (and to a multiple of 2^-129); its values are s * c, c = x / s rounded to an integer, halves to the even one, -7 .. 7.  Where
+ * s would pass 2^122 it is that (values beyond 7.5 * 2^122 become 7 * 2^122).  A group with a value that is no finite number reads as NaN.  s * c is exactly
+ * a bf16, so that whatever reads the cache sees the same numbers; the largest value of a group is off by s / 2 at most, as all others are.
+ *   codes    K, V: bytes [n_seq][n_head][L][d_head / 2] by code_stride (sequence, head, position; in bytes, multiples of 16).  With G = d_head / 32, 32-bit
+ *            word t * G + g of a row (t < 4) holds c + 8 of values 32 g + 8 t .. 32 g + 8 t + 7, the first in the lowest 4 bits.
+ *   scales   K_scale, V_scale: bf16 [n_seq][n_head][L][2, 4 or 8: G rounded up] by scale_stride (elements, multiples of that), the g-th group's g-th.
+ *            Places behind the G-th are not written.
+ * Addresses of codes are multiples of 16, those of scales of a row's bytes (4, 8, 16).  d_head a multiple of 32 up to 256, L up to 2^30, strides up to 2^40 and the last row less than 2^50 elements
+ * behind the first, otherwise DSMOE_ERR_UNSUPPORTED.  A cache of zero bytes, scales too, is valid and reads as zeros.  The struct is on the host, read during
+ * the call.
+ */
+typedef struct dsmoe_quant_cache {
+    int32_t n_seq, n_head, L, d_head;
+    void* K;
+    void* V;
+    void* K_scale;
+    void* V_scale;
+    int64_t code_stride[3];      /* bytes: sequence, head, position */
+    int64_t scale_stride[3];     /* elements: sequence, head, position */
+} dsmoe_quant_cache;
+
+/*
+ * Writes tokens' keys and values into the cache.  k, v: bf16 [T][n_head][d_head] by in_stride (token, head; multiples of 8 elements, 0 allowed).
+ *   tok_seq, pos: as for dsmoe_window_attention; pos -1: a padded entry, of which nothing is written.  Position l goes to slot l, or, rolling, to slot l
+ *   (l < sinks) or sinks + (l - sinks) % (L - sinks).  A tok_seq or pos entry out of range is reported as DSMOE_ERR_INVALID_ARG in *dev_status, and nothing is
+ *   written of that token.
+ *   The tokens of a call go to different slots.  One exception: rolling, token t is passed over if token t + (L - sinks) is of the same sequence and that
+ *   many positions further on, so that a prompt longer than the ring leaves its latest keys.  (Otherwise a slot's row may hold pieces of several tokens.)
+ *   k_back, v_back: NULL, or bf16 [T][n_head][d_head] by back_stride: the tokens' rows as the cache holds them (also of tokens passed over), for callers
+ *   that go on with those, as a prompt's own attention does.
+ * Rows of the cache must not overlap; the memory of k, v, k_back and v_back must not overlap the cache's, nor k's and v's that of k_back and v_back; no row of
+ * k_back may overlap one of v_back.
+ */
+typedef struct dsmoe_quant_write_args {
+    int32_t T, sinks, rolling;
+    int64_t in_stride[2];        /* token, head */
+    int64_t back_stride[2];      /* token, head; not looked at without k_back and v_back */
+} dsmoe_quant_write_args;
+dsmoe_status dsmoe_quant_cache_write(const dsmoe_quant_cache* cache, const dsmoe_quant_write_args* args, const void* k, const void* v,
+                                     const int32_t* tok_seq, const int32_t* pos, void* k_back, void* v_back, int32_t* dev_status, dsmoe_stream stream);
+
+/*
+ * Reads slots first .. first + rows - 1 of all sequences back: K_out, V_out bf16 [n_seq][n_head][rows][d_head] by out_stride (sequence, head, position;
+ * multiples of 8).  len: int32 [n_seq] device, slots from len[s] on are left as they were in K_out and V_out; or NULL.  first + rows <= L.
+ * K_out and V_out must not overlap the cache, nor any of their rows one another.
+ */
+typedef struct dsmoe_quant_read_args {
+    int32_t first, rows;
+    int64_t out_stride[3];
+} dsmoe_quant_read_args;
+dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_quant_read_args* args, const int32_t* len, void* K_out, void* V_out,
+                                    dsmoe_stream stream);
+
+/*
+ * dsmoe_window_attention over a cache in 4 bits: the same queries, windows, sinks, rolling caches, outputs, limits, and clamping and reporting of
+ * tok_seq and pos (desc->kv_stride is not looked at; its other sizes must be the cache's).  window 2^31 - 1: all keys.  The weights that multiply the
+ * values are two bf16 numbers each, or one in calls of prompts.
+ *   A call of eight tokens or more a sequence of the cache (T >= 8 * n_seq), T * group >= 64, d_head 64, 96 or 128 and scale > 0 is taken as one of prompts:
+ *   what its tokens see is read back into the workspace, 4 * d_head bytes a slot and head of the cache, and attended to as by
+ *   dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences alone.  Other calls read the 4 bits once per token.
+ *   Magnitudes of queries up to 2^114 (other calls; a group's queries times 136 are added in fp32).
+ * workspace: dsmoe_quant_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one call to the next.  Results do not change from
+ * run to run.
+ */
+dsmoe_status dsmoe_quant_attention_workspace_size(const dsmoe_attention_desc* desc, size_t* bytes);
+dsmoe_status dsmoe_quant_attention(const dsmoe_attention_desc* desc, const dsmoe_quant_cache* cache, int window, int sinks, int rolling, const void* q,
+                                   const int32_t* tok_seq, const int32_t* pos, void* out, float* lse, void* workspace, size_t ws_bytes,
+                                   int32_t* dev_status, dsmoe_stream stream);
+
+/*
  * Measurement aid (no counterpart in the paper): a ring of CUDA event pairs on the caller's stream.
  * After dsmoe_timing_enable(n_pairs) (n_pairs > 0; events are created here, so call it outside any
  * timed region), every launch of an expert-MLP tensor-core kernel is bracketed by the next pair until

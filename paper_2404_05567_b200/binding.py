@@ -28,6 +28,7 @@ EXPORTS = (
     "dsmoe_mi_loss", "dsmoe_dense_backward", "dsmoe_moa_forward",
     "dsmoe_attention_workspace_size", "dsmoe_window_attention", "dsmoe_prefix_attention", "dsmoe_tally_attention",
     "dsmoe_evict_workspace_size", "dsmoe_cache_evict",
+    "dsmoe_quant_cache_write", "dsmoe_quant_cache_read", "dsmoe_quant_attention_workspace_size", "dsmoe_quant_attention",
 )
 
 
@@ -58,15 +59,30 @@ class EvictArgs(ctypes.Structure):
                 ("out_stride", ctypes.c_int64 * 3), ("tally_pitch", ctypes.c_int64)]
 
 
+class QuantCache(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("n_head", ctypes.c_int32), ("L", ctypes.c_int32), ("d_head", ctypes.c_int32),
+                ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
+                ("code_stride", ctypes.c_int64 * 3), ("scale_stride", ctypes.c_int64 * 3)]
+
+
+class QuantWriteArgs(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("sinks", ctypes.c_int32), ("rolling", ctypes.c_int32),
+                ("in_stride", ctypes.c_int64 * 2), ("back_stride", ctypes.c_int64 * 2)]
+
+
+class QuantReadArgs(ctypes.Structure):
+    _fields_ = [("first", ctypes.c_int32), ("rows", ctypes.c_int32), ("out_stride", ctypes.c_int64 * 3)]
+
+
 class DsmoeError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
         super().__init__(f"{where}: {status_string(code)} (status {code})")
 
 
-# Arguments of the entry points by letter: d(escriptor), a(ttention descriptor), p(ointer), n (size_t), i(nt).  Declared once, so that a call passes plain numbers:
+# Arguments of the entry points by letter: d(escriptor), a(ttention descriptor), q(uantised cache), p(ointer), n (size_t), i(nt).  Declared once, so that a call passes plain numbers:
 # building a ctypes object for each of a call's dozen arguments cost as much host time as the call's launches.
-_ARGTYPES = {"d": ctypes.POINTER(LayerDesc), "a": ctypes.POINTER(AttentionDesc), "p": ctypes.c_void_p, "n": ctypes.c_size_t, "i": ctypes.c_int}
+_ARGTYPES = {"d": ctypes.POINTER(LayerDesc), "a": ctypes.POINTER(AttentionDesc), "q": ctypes.POINTER(QuantCache), "p": ctypes.c_void_p, "n": ctypes.c_size_t, "i": ctypes.c_int}
 _SIGNATURES = {
     "dsmoe_workspace_size": "dp", "dsmoe_workspace_size_packed": "dp", "dsmoe_workspace_size_stages": "dp", "dsmoe_packed_size": "dp",
     "dsmoe_router": "dppppp", "dsmoe_select": "dppppppnp", "dsmoe_select_static": "dpppppp", "dsmoe_permute": "dpppppppppnp",
@@ -76,6 +92,8 @@ _SIGNATURES = {
     "dsmoe_dense_backward": "dppppppppppnpp", "dsmoe_moa_forward": "dpppppppppnpp",
     "dsmoe_attention_workspace_size": "aiip", "dsmoe_window_attention": "aiii" + "p" * 8 + "npp", "dsmoe_prefix_attention": "ap" + "p" * 8 + "npp",
     "dsmoe_tally_attention": "a" + "p" * 10 + "npp", "dsmoe_evict_workspace_size": "ap", "dsmoe_cache_evict": "ap" + "p" * 10 + "npp",
+    "dsmoe_quant_cache_write": "qp" + "p" * 8, "dsmoe_quant_cache_read": "qp" + "p" * 4, "dsmoe_quant_attention_workspace_size": "ap",
+    "dsmoe_quant_attention": "aqiii" + "p" * 6 + "npp",
     "dsmoe_timing_enable": "i", "dsmoe_timing_read": "pip",
 }
 
@@ -347,6 +365,15 @@ def _attention_ptrs(desc, q, K, V, tok_seq, pos, out, lse, device):
             out.data_ptr(), _entries(lse, torch.float32, rows, device))
 
 
+def _query_ptrs(desc, q, tok_seq, pos, out, lse, device):
+    shape, q_stride, o_stride, T, rows = desc.layout
+    if not (q.dtype == out.dtype == torch.bfloat16 and q.shape == out.shape == shape and q.stride() == q_stride and out.stride() == o_stride
+            and q_stride[3] == 1 and q.get_device() == out.get_device() == device):
+        raise ValueError("queries and outputs are bf16 tensors of the descriptor's shape and strides, d_head contiguous, on the caches' device")
+    return (q.data_ptr(), _entries(tok_seq, torch.int32, T, device), _entries(pos, torch.int32, T, device), out.data_ptr(),
+            _entries(lse, torch.float32, rows, device))
+
+
 def dsmoe_attention_workspace_size(desc: AttentionDesc, kind: int, prefix_len: int = 0) -> int:
     n = ctypes.c_size_t(0)
     _check(lib().dsmoe_attention_workspace_size(ctypes.byref(desc), int(kind), int(prefix_len), ctypes.byref(n)),
@@ -430,6 +457,101 @@ def dsmoe_cache_evict(desc, keep, sinks, recent, length, tally, K, V, kept, len_
                                    V_out.data_ptr(), *_room(workspace, device), _entries(dev_status, torch.int32, 1, device),
                                    _stream_of(device, stream)),
            "dsmoe_cache_evict")
+
+
+def quant_scales(d_head: int) -> int:
+    """Places for scales in a row of a cache in 4 bits."""
+    return 2 if d_head <= 64 else 4 if d_head <= 128 else 8
+
+
+def make_quant_cache(K, V, K_scale, V_scale) -> QuantCache:
+    """A key/value cache in 4 bits: codes K, V uint8 [n_seq, n_head, L, d_head / 2] and scales bf16 [n_seq, n_head, L, quant_scales(d_head)], or
+    views in another order whose last dimension is contiguous.  Codes share a layout, and scales do.  Keeps the tensors."""
+    n_seq, n_head, L, row = K.shape
+    scales = (n_seq, n_head, L, quant_scales(2 * row))
+    device = K.get_device()
+    if not (K.dtype == V.dtype == torch.uint8 and V.shape == K.shape and V.stride() == K.stride() and K.stride(3) == 1):
+        raise ValueError("codes are uint8 tensors of one shape and layout, the last dimension contiguous")
+    if not (K_scale.dtype == V_scale.dtype == torch.bfloat16 and K_scale.shape == V_scale.shape == scales and K_scale.stride() == V_scale.stride()
+            and K_scale.stride(3) == 1):
+        raise ValueError(f"scales are bf16 tensors {scales} of one layout, the last dimension contiguous")
+    if not (V.get_device() == K_scale.get_device() == V_scale.get_device() == device):
+        raise ValueError("codes and scales are on one device")
+    cache = QuantCache(n_seq, n_head, L, 2 * row, K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr())
+    cache.code_stride[:], cache.scale_stride[:] = K.stride()[:3], K_scale.stride()[:3]
+    cache.tensors, cache.device = (K, V, K_scale, V_scale), device
+    cache.write = None, None             # the last write's shapes, and the arguments they make
+    return cache
+
+
+def make_quant_attention_desc(q, cache: QuantCache, scale=1.0, out=None) -> AttentionDesc:
+    """As ``make_attention_desc``, for queries [T, n_head, group, d_head] on a cache in 4 bits."""
+    T, n_head, group, d_head = q.shape
+    if (n_head, d_head) != (cache.n_head, cache.d_head) or not (out is None or out.shape == q.shape):
+        raise ValueError("queries and outputs are [T, n_head, group, d_head] with the cache's heads")
+    desc = AttentionDesc(T, n_head, group, d_head, cache.n_seq, cache.L, float(scale))
+    o_stride = (n_head * group * d_head, group * d_head, d_head) if out is None else out.stride()[:3]
+    desc.q_stride[:], desc.o_stride[:] = q.stride()[:3], o_stride
+    desc.layout = q.shape, q.stride(), o_stride + (1,), T, T * n_head * group
+    return desc
+
+
+def _write_args(cache, shape, stride, sinks, rolling, back):
+    T = shape[0]
+    if shape != (T, cache.n_head, cache.d_head) or stride[2] != 1 or not (back is None or back[2] == 1):
+        raise ValueError("k, v, k_back and v_back are [T, n_head, d_head] with the cache's heads, d_head contiguous")
+    args = QuantWriteArgs(T, int(sinks), int(rolling))
+    args.in_stride[:] = stride[:2]
+    args.back_stride[:] = stride[:2] if back is None else back[:2]
+    return args
+
+
+def dsmoe_quant_cache_write(cache, k, v, tok_seq, pos, sinks=0, rolling=False, k_back=None, v_back=None, dev_status=None, stream=None):
+    """Writes tokens' keys and values [T, n_head, d_head] bf16 into a cache in 4 bits; k_back, v_back: the rows as the cache holds them, or ``None``."""
+    device, shape, stride = cache.device, k.shape, k.stride()
+    first = v_back if k_back is None else k_back
+    sizes = shape, stride, sinks, rolling, None if first is None else first.stride()
+    last, args = cache.write
+    if last != sizes:
+        args = _write_args(cache, *sizes)
+        cache.write = sizes, args
+    for t, layout in ((k, stride), (v, stride), (k_back, sizes[4]), (v_back, sizes[4])):
+        if t is not None and not (t.dtype is torch.bfloat16 and t.shape == shape and t.stride() == layout and t.get_device() == device):
+            raise ValueError("k and v, and k_back and v_back, are bf16 tensors of one shape and layout on the cache's device")
+    _check(lib().dsmoe_quant_cache_write(ctypes.byref(cache), ctypes.byref(args), k.data_ptr(), v.data_ptr(), _entries(tok_seq, torch.int32, shape[0], device),
+                                         _entries(pos, torch.int32, shape[0], device), None if k_back is None else k_back.data_ptr(),
+                                         None if v_back is None else v_back.data_ptr(), _entries(dev_status, torch.int32, 1, device),
+                                         _stream_of(device, stream)),
+           "dsmoe_quant_cache_write")
+
+
+def dsmoe_quant_cache_read(cache, length, K_out, V_out, first=0, stream=None):
+    """Reads slots ``first`` and the next ones back into K_out, V_out [n_seq, n_head, rows, d_head] bf16, of sequence s those below length[s] alone
+    (``None``: all)."""
+    shape, out_stride, device = K_out.shape, K_out.stride(), cache.device
+    if not (K_out.dtype == V_out.dtype == torch.bfloat16 and len(shape) == 4 and shape == V_out.shape == (cache.n_seq, cache.n_head, shape[2], cache.d_head)
+            and V_out.stride() == out_stride and out_stride[3] == 1 and K_out.get_device() == V_out.get_device() == device):
+        raise ValueError("K_out and V_out are bf16 tensors [n_seq, n_head, rows, d_head] of one layout, d_head contiguous, on the cache's device")
+    args = QuantReadArgs(int(first), shape[2])
+    args.out_stride[:] = out_stride[:3]
+    _check(lib().dsmoe_quant_cache_read(ctypes.byref(cache), ctypes.byref(args), _entries(length, torch.int32, cache.n_seq, device), K_out.data_ptr(),
+                                        V_out.data_ptr(), _stream_of(device, stream)),
+           "dsmoe_quant_cache_read")
+
+
+def dsmoe_quant_attention_workspace_size(desc: AttentionDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dsmoe_quant_attention_workspace_size(ctypes.byref(desc), ctypes.byref(n)), "dsmoe_quant_attention_workspace_size")
+    return n.value
+
+
+def dsmoe_quant_attention(desc, cache, window, sinks, rolling, q, tok_seq, pos, out, lse, workspace, dev_status=None, stream=None):
+    """``dsmoe_window_attention`` over a cache in 4 bits; window 2**31 - 1: all keys."""
+    device = cache.device
+    _check(lib().dsmoe_quant_attention(ctypes.byref(desc), ctypes.byref(cache), window, sinks, rolling,
+                                       *_query_ptrs(desc, q, tok_seq, pos, out, lse, device), *_room(workspace, device),
+                                       _entries(dev_status, torch.int32, 1, device), _stream_of(device, stream)),
+           "dsmoe_quant_attention")
 
 
 def dsmoe_timing_enable(n_pairs: int):

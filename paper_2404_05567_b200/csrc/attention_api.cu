@@ -4,7 +4,7 @@
 #include <algorithm>
 #include <climits>
 
-#include "cache_attention.cuh"
+#include "quant_cache.cuh"
 
 namespace dsmoe {
 
@@ -317,6 +317,103 @@ dsmoe_status check_prefix(const dsmoe_attention_desc* d, const dsmoe_prefix* p, 
     return DSMOE_OK;
 }
 
+// ---- caches in 4 bits
+
+// Rows of `row` bytes or elements at strides that are multiples of `unit`
+dsmoe_status check_rows(const int64_t* stride, const int64_t* n, int count, int64_t unit) {
+    for (int i = 0; i < count; ++i)
+        if (stride[i] < 0 || stride[i] % unit) return DSMOE_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i)
+        if (stride[i] > (1ll << 40)) return DSMOE_ERR_UNSUPPORTED;
+    return within_reach(stride, n, count) ? DSMOE_OK : DSMOE_ERR_UNSUPPORTED;
+}
+
+dsmoe_status check_quant_cache(const dsmoe_quant_cache* c) {
+    if (!c) return DSMOE_ERR_INVALID_ARG;
+    if (c->n_seq <= 0 || c->n_head <= 0 || c->L <= 0 || c->d_head <= 0) return DSMOE_ERR_INVALID_ARG;
+    if (c->d_head % 32 || c->d_head > 256) return DSMOE_ERR_UNSUPPORTED;
+    if (c->L > 1 << 30 || (long long)c->n_seq * c->n_head > INT_MAX / 4) return DSMOE_ERR_UNSUPPORTED;
+    if (!c->K || !c->V || !c->K_scale || !c->V_scale) return DSMOE_ERR_INVALID_ARG;
+    if (!aligned16(c->K) || !aligned16(c->V)) return DSMOE_ERR_INVALID_ARG;
+    const uintptr_t row = 2 * quant_scales(c->d_head);        // (a row of scales is one load)
+    if ((uintptr_t)c->K_scale % row || (uintptr_t)c->V_scale % row) return DSMOE_ERR_INVALID_ARG;
+    const int64_t n[3] = {c->n_seq, c->n_head, c->L};
+    DSMOE_TRY(check_rows(c->code_stride, n, 3, 16));
+    return check_rows(c->scale_stride, n, 3, quant_scales(c->d_head));
+}
+
+// The memory of a cache's four parts
+struct QuantExtents {
+    Extent e[4];
+    bool meets(const Extent& o) const { return e[0].meets(o) || e[1].meets(o) || e[2].meets(o) || e[3].meets(o); }
+};
+QuantExtents quant_extents(const dsmoe_quant_cache& c) {
+    const int64_t n[3] = {c.n_seq, c.n_head, c.L};
+    const int sc = quant_scales(c.d_head);
+    return QuantExtents{{extent(c.K, c.code_stride, n, c.d_head / 2, 1), extent(c.V, c.code_stride, n, c.d_head / 2, 1),
+                         extent(c.K_scale, c.scale_stride, n, sc, 2), extent(c.V_scale, c.scale_stride, n, sc, 2)}};
+}
+
+QuantView quant_view(const dsmoe_quant_cache& c) {
+    QuantView v{};
+    v.n_seq = c.n_seq, v.n_head = c.n_head, v.L = c.L, v.d_head = c.d_head;
+    v.K = static_cast<unsigned char*>(c.K);
+    v.V = static_cast<unsigned char*>(c.V);
+    v.K_scale = static_cast<__nv_bfloat16*>(c.K_scale);
+    v.V_scale = static_cast<__nv_bfloat16*>(c.V_scale);
+    v.c_s = c.code_stride[0], v.c_h = c.code_stride[1], v.c_p = c.code_stride[2];
+    v.s_s = c.scale_stride[0], v.s_h = c.scale_stride[1], v.s_p = c.scale_stride[2];
+    return v;
+}
+
+// Prompts are attended to from bf16 copies of what their tokens see, which are exact, on the 128-row kernel: reading back and reading that again moves 8
+// times the bytes that a token's own pass over the 4 bits does, so from eight tokens a sequence on.
+constexpr int kQuantTileTokens = 8;
+bool quant_on_tiles(const AttnView& A) { return own_on_tiles(A) && A.T >= (long long)kQuantTileTokens * A.n_seq; }
+// The copies as the cache of a view
+AttnView quant_copy_view(const AttnView& A, char* ws, size_t bytes) {
+    AttnView B = A;
+    B.K = reinterpret_cast<const __nv_bfloat16*>(ws);
+    B.V = reinterpret_cast<const __nv_bfloat16*>(ws + bytes);
+    B.kv_p = A.d_head;
+    B.kv_h = (long long)A.L * A.d_head;
+    B.kv_s = B.kv_h * A.n_head;
+    return B;
+}
+struct QuantAttnPlan {
+    bool tiles;
+    size_t copy, range, rest, total;      // tiles: bytes of a copy (K's and V's are first), where the ranges lie, where attend's workspace begins
+    size_t run_head;                      // otherwise: (the slots are first)
+    QuantPlan plan;
+    AttnPlan attn;
+    bool fits;
+};
+QuantAttnPlan quant_attention_plan(const AttnView& A) {
+    QuantAttnPlan w{};
+    w.tiles = quant_on_tiles(quant_copy_view(A, nullptr, 0));
+    if (w.tiles) {
+        w.copy = align_up((size_t)A.n_seq * A.n_head * A.L * A.d_head * 2, 256);
+        w.range = 2 * w.copy;
+        w.rest = w.range + align_up((size_t)A.n_seq * sizeof(int4), 256);
+        w.attn = attention_plan(quant_copy_view(A, nullptr, w.copy), SharedKeys{}, false, false);
+        w.total = w.rest + w.attn.total;
+        w.fits = w.attn.fits && w.copy < (size_t)1 << 40;
+    } else {
+        size_t slots, heads;
+        quant_plan_size(A, &w.plan, &slots, &heads);
+        w.run_head = align_up(slots, 256);
+        w.total = w.run_head + align_up(heads, 256);
+        w.fits = w.total < (size_t)1 << 36;
+    }
+    return w;
+}
+
+dsmoe_attention_desc quant_desc(const dsmoe_attention_desc& d) {         // (the strides of a cache in 16 bits are not looked at)
+    dsmoe_attention_desc q = d;
+    q.kv_stride[0] = q.kv_stride[1] = q.kv_stride[2] = 0;
+    return q;
+}
+
 }  // namespace
 
 }  // namespace dsmoe
@@ -473,6 +570,132 @@ dsmoe_status dsmoe_cache_evict(const dsmoe_attention_desc* desc, const dsmoe_evi
     E.count = static_cast<int32_t*>(workspace);
     E.dev_status = dev_status;
     return launch_evict(E, (cudaStream_t)stream);
+}
+
+dsmoe_status dsmoe_quant_cache_write(const dsmoe_quant_cache* cache, const dsmoe_quant_write_args* args, const void* k, const void* v,
+                                     const int32_t* tok_seq, const int32_t* pos, void* k_back, void* v_back, int32_t* dev_status, dsmoe_stream stream) {
+    DSMOE_TRY(check_quant_cache(cache));
+    if (!args) return DSMOE_ERR_INVALID_ARG;
+    const dsmoe_quant_write_args& a = *args;
+    const dsmoe_quant_cache& c = *cache;
+    if (a.T < 0 || a.sinks < 0 || (a.rolling != 0 && a.rolling != 1) || (a.rolling && a.sinks >= c.L)) return DSMOE_ERR_INVALID_ARG;
+    const int64_t in[3] = {a.in_stride[0], a.in_stride[1], 0}, back[3] = {a.back_stride[0], a.back_stride[1], 0}, n[3] = {a.T, c.n_head, 1};
+    DSMOE_TRY(check_rows(in, n, 2, 8));
+    if (k_back || v_back) DSMOE_TRY(check_rows(back, n, 2, 8));
+    if ((double)a.T * c.n_head > (double)INT_MAX / 2) return DSMOE_ERR_UNSUPPORTED;
+    // Each row of the cache is its own (slots that no token of the call goes to keep what they hold)
+    const int64_t places[3] = {c.n_seq, c.n_head, c.L};
+    const int64_t code = (intptr_t)c.V - (intptr_t)c.K, scale = ((intptr_t)c.V_scale - (intptr_t)c.K_scale) / 2;
+    const int sc = quant_scales(c.d_head);
+    if (!rows_apart(c.code_stride, places, c.d_head / 2) || rows_meet(code, c.code_stride, places, c.d_head / 2) ||
+        !rows_apart(c.scale_stride, places, sc) || rows_meet(scale, c.scale_stride, places, sc))
+        return DSMOE_ERR_INVALID_ARG;
+    const QuantExtents held = quant_extents(c);
+    if (held.e[0].meets(held.e[2]) || held.e[0].meets(held.e[3]) || held.e[1].meets(held.e[2]) || held.e[1].meets(held.e[3])) return DSMOE_ERR_INVALID_ARG;
+    if (a.T == 0) return DSMOE_OK;
+    if (!k || !v || !pos || !aligned16(k) || !aligned16(v) || !aligned16(k_back) || !aligned16(v_back)) return DSMOE_ERR_INVALID_ARG;
+    const Extent ek = extent(k, in, n, c.d_head, 2), ev = extent(v, in, n, c.d_head, 2);
+    if (held.meets(ek) || held.meets(ev)) return DSMOE_ERR_INVALID_ARG;
+    if (k_back || v_back) {
+        if (!rows_apart(back, n, c.d_head)) return DSMOE_ERR_INVALID_ARG;
+        for (const void* b : {k_back, v_back}) {
+            if (!b) continue;
+            const Extent eb = extent(b, back, n, c.d_head, 2);
+            if (held.meets(eb) || eb.meets(ek) || eb.meets(ev)) return DSMOE_ERR_INVALID_ARG;
+        }
+        if (k_back && v_back && rows_meet(((intptr_t)v_back - (intptr_t)k_back) / 2, back, n, c.d_head)) return DSMOE_ERR_INVALID_ARG;
+    }
+    QuantWrite W{};
+    W.T = a.T, W.sinks = a.sinks, W.ring = a.rolling ? c.L - a.sinks : 0;
+    W.k = static_cast<const __nv_bfloat16*>(k);
+    W.v = static_cast<const __nv_bfloat16*>(v);
+    W.i_t = in[0], W.i_h = in[1];
+    W.tok_seq = tok_seq;
+    W.pos = pos;
+    W.k_back = static_cast<__nv_bfloat16*>(k_back);
+    W.v_back = static_cast<__nv_bfloat16*>(v_back);
+    W.b_t = back[0], W.b_h = back[1];
+    W.dev_status = dev_status;
+    return launch_quant_write(quant_view(c), W, (cudaStream_t)stream);
+}
+
+dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_quant_read_args* args, const int32_t* len, void* K_out, void* V_out,
+                                    dsmoe_stream stream) {
+    DSMOE_TRY(check_quant_cache(cache));
+    if (!args) return DSMOE_ERR_INVALID_ARG;
+    const dsmoe_quant_read_args& a = *args;
+    const dsmoe_quant_cache& c = *cache;
+    if (a.first < 0 || a.rows < 0 || (long long)a.first + a.rows > c.L) return DSMOE_ERR_INVALID_ARG;
+    const int64_t n[3] = {c.n_seq, c.n_head, a.rows};
+    DSMOE_TRY(check_rows(a.out_stride, n, 3, 8));
+    if (a.rows == 0) return DSMOE_OK;
+    if (!K_out || !V_out || !aligned16(K_out) || !aligned16(V_out)) return DSMOE_ERR_INVALID_ARG;
+    if (!rows_apart(a.out_stride, n, c.d_head) || rows_meet(((intptr_t)V_out - (intptr_t)K_out) / 2, a.out_stride, n, c.d_head)) return DSMOE_ERR_INVALID_ARG;
+    const QuantExtents held = quant_extents(c);
+    if (held.meets(extent(K_out, a.out_stride, n, c.d_head, 2)) || held.meets(extent(V_out, a.out_stride, n, c.d_head, 2))) return DSMOE_ERR_INVALID_ARG;
+    QuantRead R{};
+    R.first = a.first, R.rows = a.rows;
+    R.len = len;
+    R.K = static_cast<__nv_bfloat16*>(K_out);
+    R.V = static_cast<__nv_bfloat16*>(V_out);
+    R.o_s = a.out_stride[0], R.o_h = a.out_stride[1], R.o_p = a.out_stride[2];
+    return launch_quant_read(quant_view(c), R, (cudaStream_t)stream);
+}
+
+dsmoe_status dsmoe_quant_attention_workspace_size(const dsmoe_attention_desc* desc, size_t* bytes) {
+    if (!desc || !bytes) return DSMOE_ERR_INVALID_ARG;
+    const dsmoe_attention_desc d = quant_desc(*desc);
+    DSMOE_TRY(check_attention(&d));
+    *bytes = 0;
+    if (d.T == 0) return DSMOE_OK;
+    // (with and without sequence numbers)
+    const QuantAttnPlan w = quant_attention_plan(view_of(d, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr));
+    if (!w.fits) return DSMOE_ERR_UNSUPPORTED;
+    *bytes = w.total;
+    return DSMOE_OK;
+}
+
+dsmoe_status dsmoe_quant_attention(const dsmoe_attention_desc* desc, const dsmoe_quant_cache* cache, int window, int sinks, int rolling, const void* q,
+                                   const int32_t* tok_seq, const int32_t* pos, void* out, float* lse, void* workspace, size_t ws_bytes,
+                                   int32_t* dev_status, dsmoe_stream stream) {
+    if (!desc) return DSMOE_ERR_INVALID_ARG;
+    const dsmoe_attention_desc d = quant_desc(*desc);
+    DSMOE_TRY(check_attention(&d));
+    DSMOE_TRY(check_quant_cache(cache));
+    const dsmoe_quant_cache& c = *cache;
+    if (c.n_seq != d.n_seq || c.n_head != d.n_head || c.L != d.L || c.d_head != d.d_head) return DSMOE_ERR_INVALID_ARG;
+    DSMOE_TRY(check_window(&d, window, sinks, rolling));
+    if (d.T == 0) return DSMOE_OK;
+    if (!q || !pos || !out || !aligned16(q) || !aligned16(out)) return DSMOE_ERR_INVALID_ARG;
+    const int64_t n[3] = {d.T, d.n_head, d.group};
+    const Extent o = extent(out, d.o_stride, n, d.d_head, 2);
+    if (o.meets(extent(q, d.q_stride, n, d.d_head, 2)) || quant_extents(c).meets(o)) return DSMOE_ERR_INVALID_ARG;
+    AttnView A = view_of(d, q, nullptr, nullptr, tok_seq, pos, out, lse, dev_status);
+    // (the workspace is that of a window as wide as the cache)
+    QuantAttnPlan w = quant_attention_plan(A);
+    if (!w.fits) return DSMOE_ERR_UNSUPPORTED;
+    if (!workspace || !aligned16(workspace) || ws_bytes < w.total) return DSMOE_ERR_WORKSPACE;
+    A.window = window;
+    A.sinks = sinks;
+    A.ring = rolling ? d.L - sinks : 0;
+    char* const ws = static_cast<char*>(workspace);
+    cudaStream_t s = (cudaStream_t)stream;
+    if (w.tiles) {
+        const AttnView B = quant_copy_view(A, ws, w.copy);
+        int4* const range = reinterpret_cast<int4*>(ws + w.range);
+        DSMOE_TRY(launch_quant_range(A, range, s));
+        QuantRead R{};
+        R.rows = A.L;
+        R.range = range;
+        R.K = const_cast<__nv_bfloat16*>(B.K);
+        R.V = const_cast<__nv_bfloat16*>(B.V);
+        R.o_s = B.kv_s, R.o_h = B.kv_h, R.o_p = B.kv_p;
+        DSMOE_TRY(launch_quant_read(quant_view(c), R, s));
+        return attend(B, SharedKeys{}, w.attn, ws + w.rest, s);
+    }
+    w.plan.slots = reinterpret_cast<float*>(ws);
+    w.plan.run_head = reinterpret_cast<int2*>(ws + w.run_head);
+    return launch_quant_attention(A, quant_view(c), w.plan, s);
 }
 
 }  // extern "C"

@@ -1,0 +1,644 @@
+// Attention of single tokens against their caches in 4 bits (see quant_cache.cuh for the format, cache_attention.cuh for what a row sees and what parts are).
+//
+// The keys of all (token, head, row tile) pairs, in units of 32, are one list, cut into equal runs, as in attention_stream_kernel: a run is a CTA's, whose
+// warps take its units in turn, or a warp's; a pair that several runs share leaves a part per run, added up by the next launch.
+//
+// A warp brings its units' codes and scales into a ring of its own (cp.async), and takes 16 keys at a time to its tensor instructions with the keys, not the rows, as
+// the 16-row operand: S^T = K q^T and O^T += V^T P^T.  Codes become bf16 numbers in registers, once for all of the pair's rows, of which 8 are the
+// narrow side of an instruction (two of those for groups of more than 8).
+//   K: 4 bits beside the exponent of 128 are 128 + 8 + c, exactly; a group's sum then begins with -136 times the sum of the row's queries there, and its
+//      scale multiplies it into the logit.  (Sums of up to 18 times the products' own magnitude: 2^-20 of that is lost instead of 2^-24.)
+//   V: 4 bits beside the exponent of 16 are 16 + 8 + c; times the scale, minus 24 times the scale, is s * c, exactly, in one packed operation, whose scales are
+//      the two keys' that share a register.
+// Weights are two bf16 numbers each, as good as 16 bits.  The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
+#include <algorithm>
+
+#include "quant_cache.cuh"
+#include "umma.cuh"
+
+namespace dsmoe {
+
+namespace {
+
+constexpr int kQuantUnit = 32;            // keys that a warp takes at a time
+
+__device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4], uint2 b, float c0, float c1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void mma_next(float (&d)[4], const uint32_t (&a)[4], uint2 b) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ float low_part(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float high_part(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ float exp2_fast(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// a * b + c, two bf16 numbers at a time
+__device__ __forceinline__ uint32_t fma_pair(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+// (x & mask) | bits
+__device__ __forceinline__ uint32_t masked(uint32_t x, uint32_t mask, uint32_t bits) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+    return r;
+}
+
+// N words from shared memory, at a multiple of N words
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&r)[N], uint32_t addr) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]) : "r"(addr + 4 * i));
+    } else if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r[i]), "=r"(r[i + 1]) : "r"(addr + 4 * i));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[i]) : "r"(addr + 4 * i));
+    }
+}
+// BYTES (4, 8, 16), or zeros
+template <int BYTES>
+__device__ __forceinline__ void copy_piece(uint32_t dst, const void* src, bool real) {
+    const uint32_t n = real ? BYTES : 0;
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(n) : "memory");
+}
+
+__host__ __device__ static inline int quant_units(const Sight& s) {
+    const int n = (s.sinks + kQuantUnit - 1) / kQuantUnit + (s.last >= s.first ? (s.last - s.first) / kQuantUnit + 1 : 0);
+    return n > 0 ? n : 1;                 // a token that sees nothing has one unit without keys, so that somebody writes its row
+}
+
+// NT: tiles of 8 rows that a pair has
+template <int DH, int NT>
+struct QuantGeo {
+    static constexpr int G = DH / kQuantGroup, ROW = 16 * G, SC = 2 * quant_scales(DH);
+    // bytes from one key's codes to the next in shared memory, with which neither the keys' nor the values' reads meet in a bank
+    static constexpr int KROW = ROW + (G == 8 ? 16 : 0), VROW = ROW + (G % 2 == 0 ? 16 : 0);
+    static constexpr int V = kQuantUnit * KROW, KS = V + kQuantUnit * VROW, VS = KS + kQuantUnit * SC, UNIT = VS + kQuantUnit * SC;
+    static constexpr int WARPS = DH <= 128 && NT == 1 ? 16 : 8;
+    static constexpr int FIT = 208 * 1024 / (WARPS * UNIT), BUFS = FIT > 4 ? 4 : FIT, SMEM = WARPS * BUFS * UNIT;
+    static constexpr int LDO = DH + 4;    // floats from one row of a warp's accumulators to the next, where they meet: eight rows take a unit's place
+    static_assert(BUFS >= 2 && 8 * LDO * 4 <= UNIT && UNIT % 16 == 0, "rings of two units and more");
+};
+
+template <int DH, int NT, bool BY_WARP>
+__global__ void __launch_bounds__(32 * QuantGeo<DH, NT>::WARPS, 1)
+attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant__ QuantView C, const __grid_constant__ QuantPlan P) {
+    using Geo = QuantGeo<DH, NT>;
+    constexpr int G = Geo::G, BUFS = Geo::BUFS, WARPS = Geo::WARPS, THREADS = 32 * WARPS, PER = kListTokens / THREADS, LDO = Geo::LDO;
+    constexpr int SW = quant_scales(DH) / 2;            // words of a key's scales
+    extern __shared__ __align__(16) unsigned char aq_smem[];
+    __shared__ long long base_s[kListTokens + 1];       // units before token e's
+    __shared__ long long warp_sum_s[WARPS];
+    __shared__ int longest_s[WARPS];
+    __shared__ float ms[WARPS][8 * NT], ls[WARPS][8 * NT];
+    __shared__ uint32_t at_s[WARPS];                    // where each warp's accumulators of the pair are
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q4 = lane & 3;
+    const int pairs_each = A.n_head * A.row_tiles;      // pairs of a token
+    const int places = BY_WARP ? WARPS : 1;             // runs of a CTA
+    chain_wait();
+    for (int i = tid; i < P.passes * places; i += THREADS) P.run_head[(long long)(i / places) * P.runs + blockIdx.x * places + i % places] = make_int2(0, 0);
+    if (blockIdx.x == 0) {
+        const int rest = P.runs - (int)gridDim.x * places;
+        for (int i = tid; i < P.passes * rest; i += THREADS) P.run_head[(long long)(i / rest + 1) * P.runs - 1 - i % rest] = make_int2(0, 0);
+    }
+
+    for (int pass = 0; pass < P.passes; ++pass) {
+    // ---- the pass's tokens and their units
+    const int n0 = pass * kListTokens, n = min(kListTokens, A.T - n0);
+    __syncthreads();
+    {
+        long long mine[PER], sum = 0;
+        int longest = 1;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = tid * PER + i;
+            mine[i] = 0;
+            if (e < n) {
+                bool bad = false;
+                const int units = quant_units(sight_of(A, n0 + e, &bad));
+                longest = max(longest, units);
+                mine[i] = (long long)units * pairs_each;
+                if (bad && blockIdx.x == 0) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
+            }
+            sum += mine[i];
+        }
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        long long incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 31) {
+            warp_sum_s[warp] = incl;
+            longest_s[warp] = longest;
+        }
+        __syncthreads();
+        long long before = incl - sum;
+        for (int w = 0; w < warp; ++w) before += warp_sum_s[w];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = tid * PER + i;
+            if (e < n) base_s[e] = before;
+            before += mine[i];
+        }
+        if (tid == THREADS - 1) base_s[n] = before;
+        __syncthreads();
+    }
+    const long long total = base_s[n];
+    // Equal runs, of at least a unit for each warp
+    long long wanted = min((long long)gridDim.x, (total + WARPS - 1) / WARPS);
+    if (BY_WARP) {
+        int longest = 1;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) longest = max(longest, longest_s[w]);
+        wanted = warp_runs(total, longest, (long long)gridDim.x * WARPS);
+    }
+    if (P.whole) wanted = (long long)n * pairs_each;
+    const int n_runs = (int)wanted, run_no = BY_WARP ? (int)blockIdx.x * WARPS + warp : (int)blockIdx.x;
+    if (run_no >= n_runs) {
+        __syncwarp();
+        continue;
+    }
+    const long long share = total / n_runs, extra = total - share * n_runs;
+    const auto run_start = [&](long long c) { return c * share + (c < extra ? c : extra); };
+    const auto run_of = [&](long long u) {              // the run that holds unit u
+        const long long cut = extra * (share + 1);
+        return u < cut ? u / (share + 1) : extra + (u - cut) / share;
+    };
+    long long u0, u1;
+    if (P.whole) {
+        const int e = run_no / pairs_each;
+        const long long units = (base_s[e + 1] - base_s[e]) / pairs_each;
+        u0 = base_s[e] + run_no % pairs_each * units;
+        u1 = u0 + units;
+    } else {
+        u0 = run_start(run_no);
+        u1 = run_start(run_no + 1);
+    }
+    const long long run = (long long)pass * P.runs + run_no;
+
+    // Where a unit lies: token, its (head, row tile), key block of it
+    struct Cursor {
+        int e, h, k, units;
+        Sight s;
+    };
+    const auto look = [&](Cursor& c) {
+        bool bad = false;
+        if (c.e >= n) return;
+        c.s = sight_of(A, n0 + c.e, &bad);
+        c.units = quant_units(c.s);
+    };
+    const auto settle = [&](Cursor& c) {                // k past the pair's units: on to the pair that holds it
+        while (c.e < n && c.k >= c.units) {
+            c.k -= c.units;
+            if (++c.h == pairs_each) {
+                c.h = 0;
+                ++c.e;
+                look(c);
+            }
+        }
+    };
+    Cursor seg;
+    {
+        int lo = 0, hi = n - 1;                         // the last token whose units begin at or before u0
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (base_s[mid] <= u0) lo = mid;
+            else hi = mid - 1;
+        }
+        seg.e = lo;
+        look(seg);
+        const long long in = u0 - base_s[lo];
+        seg.h = (int)(in / seg.units);
+        seg.k = (int)(in % seg.units);
+    }
+    Cursor ahead = seg;                                 // the next unit to fetch
+    const int hop = BY_WARP ? 1 : WARPS, begin = BY_WARP ? 0 : warp;
+    long long u_ahead = u0 + begin;
+    if (u_ahead < u1) {
+        ahead.k += begin;
+        settle(ahead);
+    }
+    const uint32_t ring0 = ptx::smem_u32(aq_smem) + (uint32_t)(warp * BUFS * Geo::UNIT);
+    const auto fetch = [&](int buf) {
+        if (u_ahead < u1) {
+            const Sight& s = ahead.s;
+            const int su = (s.sinks + kQuantUnit - 1) / kQuantUnit;
+            const int key0 = ahead.k < su ? ahead.k * kQuantUnit : s.first + (ahead.k - su) * kQuantUnit;
+            const int nk = ahead.k < su ? s.sinks - key0 : s.last + 1 - key0;       // keys of the unit, if fewer than kQuantUnit
+            const int slot0 = slot_of(A, key0), j = ahead.h / A.row_tiles;
+            const long long code = s.seq * C.c_s + j * C.c_h, sc = s.seq * C.s_s + j * C.s_h;
+            const uint32_t to = ring0 + (uint32_t)(buf * Geo::UNIT);
+            {                                           // a lane's key's scales
+                int slot = slot0 + (lane < nk ? lane : 0);
+                if (A.ring && slot >= A.L) slot -= A.ring;                           // in a unit across the end of the ring the slots are not neighbours
+                copy_piece<Geo::SC>(to + Geo::KS + lane * Geo::SC, C.K_scale + sc + slot * C.s_p, lane < nk);
+                copy_piece<Geo::SC>(to + Geo::VS + lane * Geo::SC, C.V_scale + sc + slot * C.s_p, lane < nk);
+            }
+            // a unit of neighbouring slots that is full: no piece needs a look at its row
+            if ((G & (G - 1)) == 0 && nk >= kQuantUnit && (!A.ring || slot0 + kQuantUnit <= A.L)) {
+                constexpr int ROWS = 32 / G;                                         // rows at a time
+                const long long from = code + (slot0 + lane / G) * C.c_p + lane % G * 16, down = ROWS * C.c_p;
+                const unsigned char *k = C.K + from, *v = C.V + from;
+                const uint32_t kd = to + lane / G * Geo::KROW + lane % G * 16, vd = to + Geo::V + lane / G * Geo::VROW + lane % G * 16;
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    ptx::cp_async16(kd + i * ROWS * Geo::KROW, k);
+                    ptx::cp_async16(vd + i * ROWS * Geo::VROW, v);
+                    k += down;
+                    v += down;
+                }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < G; ++i) {
+                    const int idx = lane + 32 * i, row = idx / G, ch = idx % G;
+                    int slot = slot0 + (row < nk ? row : 0);
+                    if (A.ring && slot >= A.L) slot -= A.ring;
+                    const long long src = code + slot * C.c_p + ch * 16;
+                    copy_piece<16>(to + row * Geo::KROW + ch * 16, C.K + src, row < nk);    // past the last key: zeros
+                    copy_piece<16>(to + Geo::V + row * Geo::VROW + ch * 16, C.V + src, row < nk);
+                }
+            }
+            u_ahead += hop;
+            if (u_ahead < u1) {                         // (settling may wait for a token's sequence and position)
+                ahead.k += hop;
+                settle(ahead);
+            }
+        }
+        ptx::cp_async_commit();
+    };
+    for (int b = 0; b < BUFS - 1; ++b) fetch(b);
+
+    const uint32_t kfrag = (uint32_t)(g8 * Geo::KROW + q4 * 4 * G), vfrag = (uint32_t)(Geo::V + 2 * q4 * Geo::VROW + (g8 >> 1) * 4 * G);
+    const uint32_t half = g8 & 1 ? 0x7632u : 0x5410u;   // which half of a word of the values' is this lane's
+    int buf = 0;
+    long long mine = u0 + begin;                        // this warp's next unit
+    for (long long at = u0; at < u1;) {
+        const int t = n0 + seg.e, units = seg.units, first_k = seg.k;
+        const long long end = min(u1, at + units - first_k);
+        const Sight& s = seg.s;
+        const int su = (s.sinks + kQuantUnit - 1) / kQuantUnit;
+        const int j = seg.h / A.row_tiles, row0 = seg.h % A.row_tiles * 16, rows = min(8 * NT, A.group - row0);
+        // queries as the narrow operand, in the order in which codes leave their words, and what a group's sum begins with
+        uint2 qf[NT][2 * G];
+        float init[NT][G][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const bool real = nt * 8 + g8 < rows;
+            const __nv_bfloat16* const q = A.q + t * A.q_t + j * A.q_h + (real ? row0 + nt * 8 + g8 : 0) * A.q_g + q4 * 8;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                uint4 x = *reinterpret_cast<const uint4*>(q + g * kQuantGroup);
+                if (!real) x = make_uint4(0u, 0u, 0u, 0u);
+                qf[nt][2 * g] = make_uint2(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
+                qf[nt][2 * g + 1] = make_uint2(__byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+                float sum = ((low_part(x.x) + high_part(x.x)) + (low_part(x.y) + high_part(x.y))) +
+                            ((low_part(x.z) + high_part(x.z)) + (low_part(x.w) + high_part(x.w)));
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                init[nt][g][0] = -136.f * __shfl_sync(0xffffffffu, sum, q4 * 8);
+                init[nt][g][1] = -136.f * __shfl_sync(0xffffffffu, sum, q4 * 8 + 4);
+            }
+        }
+        // rows 2 q4 and 2 q4 + 1 of each tile
+        float m[NT][2], l[NT][2], o[2 * G][NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2 * G; ++i) o[i][nt][0] = o[i][nt][1] = o[i][nt][2] = o[i][nt][3] = 0.f;
+        }
+        for (; mine < end; mine += hop) {
+            __syncwarp();                               // every lane is past its reads of the buffer that is filled again now
+            fetch((buf + BUFS - 1) % BUFS);
+            ptx::cp_async_wait<BUFS - 1>();
+            __syncwarp();
+            const uint32_t unit = ring0 + (uint32_t)(buf * Geo::UNIT);
+            // ---- logits of keys g8 and g8 + 8 of each half of the unit
+            float x[2][NT][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t w0[G], w1[G], s0[SW], s1[SW];
+                load_words<G>(w0, unit + kfrag + (uint32_t)(16 * h * Geo::KROW));
+                load_words<G>(w1, unit + kfrag + (uint32_t)((16 * h + 8) * Geo::KROW));
+                load_words<SW>(s0, unit + (uint32_t)(Geo::KS + (16 * h + g8) * Geo::SC));
+                load_words<SW>(s1, unit + (uint32_t)(Geo::KS + (16 * h + 8 + g8) * Geo::SC));
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    uint32_t a[4], b[4];
+                    a[0] = masked(w0[g], 0x000f000fu, 0x43004300u);
+                    a[1] = masked(w1[g], 0x000f000fu, 0x43004300u);
+                    a[2] = masked(w0[g] >> 4, 0x000f000fu, 0x43004300u);
+                    a[3] = masked(w1[g] >> 4, 0x000f000fu, 0x43004300u);
+                    b[0] = masked(w0[g] >> 8, 0x000f000fu, 0x43004300u);
+                    b[1] = masked(w1[g] >> 8, 0x000f000fu, 0x43004300u);
+                    b[2] = masked(w0[g] >> 12, 0x000f000fu, 0x43004300u);
+                    b[3] = masked(w1[g] >> 12, 0x000f000fu, 0x43004300u);
+                    const float sa = g & 1 ? high_part(s0[g / 2]) : low_part(s0[g / 2]), sb = g & 1 ? high_part(s1[g / 2]) : low_part(s1[g / 2]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float c[4];
+                        mma_first(c, a, qf[nt][2 * g], init[nt][g][0], init[nt][g][1]);
+                        mma_next(c, b, qf[nt][2 * g + 1]);
+                        x[h][nt][0] = g == 0 ? sa * c[0] : fmaf(sa, c[0], x[h][nt][0]);
+                        x[h][nt][1] = g == 0 ? sa * c[1] : fmaf(sa, c[1], x[h][nt][1]);
+                        x[h][nt][2] = g == 0 ? sb * c[2] : fmaf(sb, c[2], x[h][nt][2]);
+                        x[h][nt][3] = g == 0 ? sb * c[3] : fmaf(sb, c[3], x[h][nt][3]);
+                    }
+                }
+            }
+            // to base 2; what is no key is hidden
+            const int k = first_k + (int)(mine - at);
+            const int nk = k < su ? s.sinks - k * kQuantUnit : s.last + 1 - s.first - (k - su) * kQuantUnit;
+            float top[NT][2];
+            bool moves = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                top[nt][0] = top[nt][1] = -INFINITY;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        x[h][nt][c] *= A.scale_log2;
+                        if (nk < kQuantUnit && 16 * h + (c >> 1) * 8 + g8 >= nk) x[h][nt][c] = -INFINITY;
+                        top[nt][c & 1] = fmaxf(top[nt][c & 1], x[h][nt][c]);
+                    }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) moves = moves || top[nt][r] > m[nt][r] + kStreamMoves || (m[nt][r] == -INFINITY && top[nt][r] > m[nt][r]);
+            }
+            // (see kStreamMoves)
+            if (__any_sync(0xffffffffu, moves)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        float b = top[nt][r];
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, d));
+                        const float up = fmaxf(m[nt][r], b), f = up == -INFINITY ? 1.f : exp2_fast(m[nt][r] - up);
+                        m[nt][r] = up;
+                        l[nt][r] *= f;
+#pragma unroll
+                        for (int i = 0; i < 2 * G; ++i) {
+                            o[i][nt][r] *= f;
+                            o[i][nt][2 + r] *= f;
+                        }
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // ---- the weights as two bf16 numbers each, the second the first's rounding error, with two keys of a row side by side
+                uint2 pf[NT], pr[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float z0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], z1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+                    const float p0 = exp2_fast(x[h][nt][0] - z0), p1 = exp2_fast(x[h][nt][1] - z1);
+                    const float p2 = exp2_fast(x[h][nt][2] - z0), p3 = exp2_fast(x[h][nt][3] - z1);
+                    l[nt][0] += p0 + p2;
+                    l[nt][1] += p1 + p3;
+                    const uint32_t f0 = pack2(p0, p1), f1 = pack2(p2, p3);
+                    pf[nt] = make_uint2(transpose8(f0), transpose8(f1));
+                    pr[nt] = make_uint2(transpose8(pack2(p0 - low_part(f0), p1 - high_part(f0))), transpose8(pack2(p2 - low_part(f1), p3 - high_part(f1))));
+                }
+                // ---- values of keys 2 q4, 2 q4 + 1 and the same + 8
+                uint32_t v0[G], v1[G], v2[G], v3[G], s0[2 * SW], s1[2 * SW];
+                load_words<G>(v0, unit + vfrag + (uint32_t)(16 * h * Geo::VROW));
+                load_words<G>(v1, unit + vfrag + (uint32_t)((16 * h + 1) * Geo::VROW));
+                load_words<G>(v2, unit + vfrag + (uint32_t)((16 * h + 8) * Geo::VROW));
+                load_words<G>(v3, unit + vfrag + (uint32_t)((16 * h + 9) * Geo::VROW));
+                load_words<2 * SW>(s0, unit + (uint32_t)(Geo::VS + (16 * h + 2 * q4) * Geo::SC));
+                load_words<2 * SW>(s1, unit + (uint32_t)(Geo::VS + (16 * h + 8 + 2 * q4) * Geo::SC));
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const uint32_t w0 = __byte_perm(v0[g], v1[g], half), w1 = __byte_perm(v2[g], v3[g], half);
+                    const uint32_t sa = __byte_perm(s0[g / 2], s0[SW + g / 2], g & 1 ? 0x7632 : 0x5410);
+                    const uint32_t sb = __byte_perm(s1[g / 2], s1[SW + g / 2], g & 1 ? 0x7632 : 0x5410);
+                    const uint32_t na = fma_pair(sa, 0xc1c0c1c0u, 0x80008000u), nb = fma_pair(sb, 0xc1c0c1c0u, 0x80008000u);     // -24 s
+                    uint32_t a[4], b[4];
+                    a[0] = fma_pair(masked(w0 << 3, 0x00780078u, 0x41804180u), sa, na);
+                    a[1] = fma_pair(masked(w0 >> 1, 0x00780078u, 0x41804180u), sa, na);
+                    b[0] = fma_pair(masked(w0 >> 5, 0x00780078u, 0x41804180u), sa, na);
+                    b[1] = fma_pair(masked(w0 >> 9, 0x00780078u, 0x41804180u), sa, na);
+                    a[2] = fma_pair(masked(w1 << 3, 0x00780078u, 0x41804180u), sb, nb);
+                    a[3] = fma_pair(masked(w1 >> 1, 0x00780078u, 0x41804180u), sb, nb);
+                    b[2] = fma_pair(masked(w1 >> 5, 0x00780078u, 0x41804180u), sb, nb);
+                    b[3] = fma_pair(masked(w1 >> 9, 0x00780078u, 0x41804180u), sb, nb);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma_next(o[2 * g][nt], a, pf[nt]);
+                        mma_next(o[2 * g + 1][nt], b, pf[nt]);
+                        mma_next(o[2 * g][nt], a, pr[nt]);
+                        mma_next(o[2 * g + 1][nt], b, pr[nt]);
+                    }
+                }
+            }
+            buf = buf + 1 == BUFS ? 0 : buf + 1;
+        }
+        Cursor next = seg;
+        if (end < u1) {
+            next.k += (int)(end - at);
+            settle(next);
+        } else if (pass + 1 == P.passes) {
+            chain_next();
+        }
+        const bool whole = end - at == units, begins = first_k == 0;
+        if (begins && !whole && (BY_WARP ? lane : tid) == 0)
+            P.run_head[run] = make_int2(t * pairs_each + seg.h, parts_word((int)(run_of(at + units - 1) - run_no + 1), 1));
+        float* const slot = P.slots + part_slot(run, begins, 1, 0) * 16 * (DH + 2);
+        // ---- sums over the keys that the lanes of a row had
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[nt][r] += __shfl_xor_sync(0xffffffffu, l[nt][r], d);
+        const auto write_lse = [&](long long r, float M, float den) {
+            if (A.lse) A.lse[r] = ((M == -INFINITY ? 0.f : M) + log2f(den)) * 0.6931471805599453f;
+        };
+        if (BY_WARP) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int row = nt * 8 + 2 * q4 + r, member = row0 + row;
+                    if (row >= rows) continue;
+                    const float den = l[nt][r], inv = den == 0.f ? 0.f : 1.f / den;       // no key: zeros
+                    __nv_bfloat16* const out = A.out + t * A.o_t + j * A.o_h + member * A.o_g + g8 * 4;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const float4 v = make_float4(o[2 * g][nt][r], o[2 * g][nt][2 + r], o[2 * g + 1][nt][r], o[2 * g + 1][nt][2 + r]);
+                        // (a slot's rows begin at multiples of 8 bytes)
+                        if (whole) {
+                            *reinterpret_cast<uint2*>(out + g * kQuantGroup) = make_uint2(pack2(v.x * inv, v.y * inv), pack2(v.z * inv, v.w * inv));
+                        } else {
+                            float2* const to = reinterpret_cast<float2*>(slot + row * DH + g * kQuantGroup + g8 * 4);
+                            to[0] = make_float2(v.x, v.y);
+                            to[1] = make_float2(v.z, v.w);
+                        }
+                    }
+                    if (g8 != 0) continue;
+                    if (whole) write_lse(row_at(A, t, j, member), m[nt][r], den);
+                    else *reinterpret_cast<float2*>(slot + 16 * DH + row * 2) = make_float2(m[nt][r], den);
+                }
+            seg = next;
+            at = end;
+            continue;
+        }
+        // ---- the warps' triples of the pair, through the buffer that each has just finished (the next fetch would fill it)
+        const uint32_t free_at = (uint32_t)((warp * BUFS + (buf + BUFS - 1) % BUFS) * Geo::UNIT);
+        __syncwarp();
+        if (lane == 0) at_s[warp] = free_at;
+        if (g8 == 0)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    ms[warp][nt * 8 + 2 * q4 + r] = m[nt][r];
+                    ls[warp][nt * 8 + 2 * q4 + r] = l[nt][r];
+                }
+        float* const acc = reinterpret_cast<float*>(aq_smem + free_at);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    *reinterpret_cast<float4*>(acc + (2 * q4 + r) * LDO + g * kQuantGroup + g8 * 4) =
+                        make_float4(o[2 * g][nt][r], o[2 * g][nt][2 + r], o[2 * g + 1][nt][r], o[2 * g + 1][nt][2 + r]);
+            __syncthreads();
+            for (int idx = tid; idx < min(8, rows - nt * 8) * (DH / 2); idx += THREADS) {
+                const int in = idx / (DH / 2), row = nt * 8 + in, col = idx % (DH / 2) * 2, member = row0 + row;
+                float M = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w) M = fmaxf(M, ms[w][row]);
+                const float z = M == -INFINITY ? 0.f : M;
+                float nx = 0.f, ny = 0.f, den = 0.f;
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w) {
+                    const float wgt = exp2_fast(ms[w][row] - z);          // 0 for a warp that saw no key
+                    const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(aq_smem + at_s[w]) + in * LDO + col);
+                    nx = fmaf(wgt, v.x, nx);
+                    ny = fmaf(wgt, v.y, ny);
+                    den = fmaf(wgt, ls[w][row], den);
+                }
+                if (whole) {
+                    const float inv = den == 0.f ? 0.f : 1.f / den;
+                    *reinterpret_cast<uint32_t*>(A.out + t * A.o_t + j * A.o_h + member * A.o_g + col) = pack2(nx * inv, ny * inv);
+                    if (col == 0) write_lse(row_at(A, t, j, member), M, den);
+                } else {
+                    *reinterpret_cast<float2*>(slot + row * DH + col) = make_float2(nx, ny);
+                    if (col == 0) *reinterpret_cast<float2*>(slot + 16 * DH + row * 2) = make_float2(M, den);
+                }
+            }
+            __syncthreads();                            // the warps' triples are read before they are overwritten, by the next rows' or the next fetch
+        }
+        seg = next;
+        at = end;
+    }
+    ptx::cp_async_wait<0>();
+    }
+}
+
+template <int DH, int NT>
+struct QuantLaunch {
+    using Geo = QuantGeo<DH, NT>;
+    template <bool BY_WARP>
+    static dsmoe_status go(const AttnView& A, const QuantView& C, const QuantPlan& P, int ctas, cudaStream_t s) {
+        auto* kernel = attention_quant_kernel<DH, NT, BY_WARP>;
+        static bool attr[kMaxDeviceSlots] = {};
+        int dev = 0;
+        DeviceState* st = nullptr;
+        DSMOE_TRY(device_state(&st, &dev));
+        if (!attr[dev]) {
+            DSMOE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo::SMEM));
+            attr[dev] = true;
+        }
+        DSMOE_CUDA_TRY(launch_chained(kernel, (unsigned)ctas, 32 * Geo::WARPS, Geo::SMEM, s, A, C, P));
+        return DSMOE_OK;
+    }
+};
+
+int quant_warps(const AttnView& A) { return A.d_head <= 128 && A.group <= 8 ? 16 : 8; }
+
+// Keys that a token sees at most
+long long quant_seen(const AttnView& A) { return A.window < A.L ? std::min((long long)A.window + A.sinks, (long long)A.L) : A.L; }
+
+// CTAs: one an SM, as far as each has a unit per warp in the longest case
+int quant_ctas(const AttnView& A) {
+    const long long units = ((quant_seen(A) + kQuantUnit - 1) / kQuantUnit + 1) * A.T * A.n_head * A.row_tiles, warps = quant_warps(A);
+    return (int)std::min((units + warps - 1) / warps, (long long)std::min(sm_count(), kMostStreamCtas));
+}
+
+}  // namespace
+
+// The runs are numbered as attention_sum_kernel takes those of single warps: stream_warps of them to a CTA
+void quant_plan_size(const AttnView& A, QuantPlan* plan, size_t* slots, size_t* run_head) {
+    plan->passes = ceil_div(A.T, kListTokens);
+    plan->runs = (int)align_up((size_t)quant_ctas(A) * quant_warps(A), stream_warps(A.d_head));
+    *run_head = (size_t)plan->passes * plan->runs * sizeof(int2);
+    *slots = 2 * (size_t)plan->passes * plan->runs * part_bytes(A.d_head);
+}
+
+dsmoe_status launch_quant_attention(const AttnView& A, const QuantView& C, const QuantPlan& plan, cudaStream_t s) {
+    QuantPlan P = plan;
+    const long long pairs = (long long)A.T * A.n_head * A.row_tiles;
+    const int sms = std::min(sm_count(), kMostStreamCtas), warps = quant_warps(A);
+    int ctas = std::min(quant_ctas(A), sms);
+    // A CTA takes all of a pair's keys, and no part is left to add up, where the CTAs that stay idle would save less than the second launch costs
+    P.whole = pairs <= sms && quant_seen(A) * (sms - pairs) <= 3ll * kQuantUnit * warps * sms;
+    P.by_warp = !P.whole && pairs >= (long long)ctas * warps;
+    if (P.whole) ctas = (int)pairs;
+    P.runs = (int)align_up((size_t)ctas * (P.by_warp ? warps : 1), stream_warps(A.d_head));      // (no more than there is room for)
+#define DSMOE_CALL(DH)                                                                                                                               \
+    (A.group <= 8 ? P.by_warp ? QuantLaunch<DH, 1>::go<true>(A, C, P, ctas, s) : QuantLaunch<DH, 1>::go<false>(A, C, P, ctas, s)                       \
+                  : P.by_warp ? QuantLaunch<DH, 2>::go<true>(A, C, P, ctas, s) : QuantLaunch<DH, 2>::go<false>(A, C, P, ctas, s))
+    switch (A.d_head) {
+        case 32: DSMOE_TRY(DSMOE_CALL(32)); break;
+        case 64: DSMOE_TRY(DSMOE_CALL(64)); break;
+        case 96: DSMOE_TRY(DSMOE_CALL(96)); break;
+        case 128: DSMOE_TRY(DSMOE_CALL(128)); break;
+        case 160: DSMOE_TRY(DSMOE_CALL(160)); break;
+        case 192: DSMOE_TRY(DSMOE_CALL(192)); break;
+        case 224: DSMOE_TRY(DSMOE_CALL(224)); break;
+        case 256: DSMOE_TRY(DSMOE_CALL(256)); break;
+        default: return DSMOE_ERR_UNSUPPORTED;
+    }
+#undef DSMOE_CALL
+    if (P.whole) return DSMOE_OK;
+    StreamPlan sum{};
+    sum.passes = P.passes;
+    sum.ctas = P.runs / stream_warps(A.d_head);
+    sum.by_warp = true;
+    sum.heads_at_once = 1;
+    sum.slots = P.slots;
+    sum.run_head = P.run_head;
+    return launch_attention_sum(A, sum, RowParts{}, s);
+}
+
+}  // namespace dsmoe

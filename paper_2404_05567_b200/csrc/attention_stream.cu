@@ -39,28 +39,11 @@ __device__ __forceinline__ float exp2_fast(float v) {
     return r;
 }
 
-// Where the part of pair p of a group of HB lies that a run leaves: a run has room for the parts of the pairs that began before it and for those
-// of the pairs that begin in it
-__device__ __forceinline__ long long part_slot(long long run, bool begins, int HB, int p) { return (2 * run + (begins ? 1 : 0)) * HB + p; }
-// What is said of a pair's parts beside its first run: their number, and how many runs there are from one to the next
-__device__ __forceinline__ int parts_word(int parts, int stride) { return parts == 0 ? 0 : parts | stride << 16; }
-
 // Row `at`'s largest logit z (0 if it sees nothing) and sum, for whoever asks
 __device__ __forceinline__ void write_sums(const AttnView& A, size_t at, float z, float den) {
     if (A.lse) A.lse[at] = (z + log2f(den)) * 0.6931471805599453f;
     if (A.ml) A.ml[at] = make_float2(z, den == 0.f ? 0.f : 1.f / den);
 }
-
-// BY_WARP: runs that `total` units are cut into, `most` at most.  None is shorter than a kPartsAtMost-th of the longest pair's units, so that no pair lies in
-// more than kPartsAtMost + 1 runs.
-constexpr int kPartsAtMost = 200;
-__host__ __device__ constexpr long long warp_runs(long long total, long long longest, long long most) {
-    const long long least = (longest + kPartsAtMost - 1) / kPartsAtMost, runs = total / least;
-    return runs < 1 ? 1 : runs < most ? runs : most;
-}
-// (runs are of total / runs units and more: 250 units beside 159 and 1183 pairs of one)
-static_assert(250 <= (kPartsAtMost - 1) * (409 / warp_runs(409, 250, 1184)) + 1 && 250 <= (kPartsAtMost - 1) * (1433 / warp_runs(1433, 250, 1184)) + 1);
-static_assert(warp_runs(1, 1, 1184) == 1 && warp_runs(100000, 400, 1184) == 1184 && warp_runs(800, 800, 1184) == 200);
 
 template <int DH>
 struct StreamGeo {

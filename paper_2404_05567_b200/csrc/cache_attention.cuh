@@ -126,6 +126,23 @@ struct StreamPlan {
 __host__ __device__ static constexpr int stream_warps(int d_head) { return d_head <= 128 ? 8 : 4; }       // of a CTA
 static inline size_t part_bytes(int d_head) { return (size_t)16 * (d_head + 2) * 4; }
 
+// Where the part of pair p of a group of HB lies that a run leaves: a run has room for the parts of the pairs that began before it and for those
+// of the pairs that begin in it
+__device__ static __forceinline__ long long part_slot(long long run, bool begins, int HB, int p) { return (2 * run + (begins ? 1 : 0)) * HB + p; }
+// What is said of a pair's parts beside its first run: their number, and how many runs there are from one to the next
+__device__ static __forceinline__ int parts_word(int parts, int stride) { return parts == 0 ? 0 : parts | stride << 16; }
+
+// Runs of single warps that `total` units are cut into, `most` at most.  None is shorter than a kPartsAtMost-th of the longest pair's units, so that no pair lies in
+// more than kPartsAtMost + 1 runs.
+constexpr int kPartsAtMost = 200;
+__host__ __device__ static constexpr long long warp_runs(long long total, long long longest, long long most) {
+    const long long least = (longest + kPartsAtMost - 1) / kPartsAtMost, runs = total / least;
+    return runs < 1 ? 1 : runs < most ? runs : most;
+}
+// (runs are of total / runs units and more: 250 units beside 159 and 1183 pairs of one)
+static_assert(250 <= (kPartsAtMost - 1) * (409 / warp_runs(409, 250, 1184)) + 1 && 250 <= (kPartsAtMost - 1) * (1433 / warp_runs(1433, 250, 1184)) + 1);
+static_assert(warp_runs(1, 1, 1184) == 1 && warp_runs(100000, 400, 1184) == 1184 && warp_runs(800, 800, 1184) == 200);
+
 // The 128-row kernel: heads of 64, 96 and 128, caches that a tensor map describes.  Its rows' keys are cut into `splits`; o, ml: where their parts
 // go (TileParts), or nullptr with one split: out and lse are written.
 struct TilePlan {
