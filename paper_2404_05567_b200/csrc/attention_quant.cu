@@ -91,6 +91,12 @@ __host__ __device__ static inline int quant_units(const Sight& s) {
     return n > 0 ? n : 1;                 // a token that sees nothing has one unit without keys, so that somebody writes its row
 }
 
+// Warps of a CTA: as many as their registers and rings allow
+__host__ __device__ static constexpr int quant_warps(int d_head, int nt) { return d_head <= 128 ? nt == 1 ? 12 : 8 : nt == 1 ? 6 : 4; }
+
+// The natural logarithm of a row's sum
+__device__ __forceinline__ float row_lse(float M, float den) { return ((M == -INFINITY ? 0.f : M) + log2f(den)) * 0.6931471805599453f; }
+
 // NT: tiles of 8 rows that a pair has
 template <int DH, int NT>
 struct QuantGeo {
@@ -98,33 +104,47 @@ struct QuantGeo {
     // bytes from one key's codes to the next in shared memory, with which neither the keys' nor the values' reads meet in a bank
     static constexpr int KROW = ROW + (G == 8 ? 16 : 0), VROW = ROW + (G % 2 == 0 ? 16 : 0);
     static constexpr int V = kQuantUnit * KROW, KS = V + kQuantUnit * VROW, VS = KS + kQuantUnit * SC, UNIT = VS + kQuantUnit * SC;
-    static constexpr int WARPS = DH <= 128 && NT == 1 ? 16 : 8;
-    static constexpr int FIT = 208 * 1024 / (WARPS * UNIT), BUFS = FIT > 4 ? 4 : FIT, SMEM = WARPS * BUFS * UNIT;
-    static constexpr int LDO = DH + 4;    // floats from one row of a warp's accumulators to the next, where they meet: eight rows take a unit's place
-    static_assert(BUFS >= 2 && 8 * LDO * 4 <= UNIT && UNIT % 16 == 0, "rings of two units and more");
+    static constexpr int WARPS = quant_warps(DH, NT);
+    static constexpr int LDO = DH + 4;    // floats from one row of a warp's sums to the next, where they meet
+    static constexpr int SUMS = 8 * NT * LDO * 4;
+    static constexpr int FIT = (216 * 1024 / WARPS - SUMS) / UNIT, BUFS = FIT > 4 ? 4 : FIT;
+    static constexpr int OWN = BUFS * UNIT + SUMS, SMEM = WARPS * OWN;       // a warp's: its ring, and the sums of the pair that began before its run
+    static_assert(BUFS >= 2 && SUMS <= BUFS * UNIT && UNIT % 16 == 0, "rings of two units and more, in which a warp's last sums find a place");
 };
 
-template <int DH, int NT, bool BY_WARP>
+// What a warp leaves of a pair that is not its alone: rows' largest logits and sums beside the values' sums
+template <int ROWS>
+struct Piece {
+    int there, begins, ends;              // whether there is one; begins or ends with the pair
+    int e, h, units;                      // the pair: token, (head, row tile), units
+    uint32_t sums;                        // where they lie
+    float m[ROWS], l[ROWS];
+};
+
+// HB: neighbouring pairs that a CTA takes at a time, a warp each.  Where the heads of a position lie side by side they are so read side by side, and rows of
+// one head beyond 16 read its keys out of L2 or nearer.
+//
+// A CTA's run of the list is cut into equal runs of its warps (of each of the HB pairs), which take their units one after the other and owe the others
+// nothing until the end.  What a warp has of a pair that began before its run or goes on behind it is a piece; the CTA's pieces of a pair are added up once all
+// are there, and a pair that several CTAs share leaves a part per CTA.
+template <int DH, int NT, int HB>
 __global__ void __launch_bounds__(32 * QuantGeo<DH, NT>::WARPS, 1)
 attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant__ QuantView C, const __grid_constant__ QuantPlan P) {
     using Geo = QuantGeo<DH, NT>;
-    constexpr int G = Geo::G, BUFS = Geo::BUFS, WARPS = Geo::WARPS, THREADS = 32 * WARPS, PER = kListTokens / THREADS, LDO = Geo::LDO;
+    constexpr int G = Geo::G, BUFS = Geo::BUFS, WARPS = Geo::WARPS, THREADS = 32 * WARPS, PER = (kListTokens + THREADS - 1) / THREADS, LDO = Geo::LDO;
     constexpr int SW = quant_scales(DH) / 2;            // words of a key's scales
+    constexpr int KW = WARPS / HB;                      // runs of a CTA
     extern __shared__ __align__(16) unsigned char aq_smem[];
     __shared__ long long base_s[kListTokens + 1];       // units before token e's
     __shared__ long long warp_sum_s[WARPS];
-    __shared__ int longest_s[WARPS];
-    __shared__ float ms[WARPS][8 * NT], ls[WARPS][8 * NT];
-    __shared__ uint32_t at_s[WARPS];                    // where each warp's accumulators of the pair are
+    __shared__ Piece<8 * NT> piece_s[HB][2 * KW];       // of each run: what began before it, what goes on behind it
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q4 = lane & 3;
-    const int pairs_each = A.n_head * A.row_tiles;      // pairs of a token
-    const int places = BY_WARP ? WARPS : 1;             // runs of a CTA
+    const int hb = warp % HB, kw = warp / HB;
+    const int groups = A.n_head * A.row_tiles / HB;     // of a token, HB pairs each
     chain_wait();
-    for (int i = tid; i < P.passes * places; i += THREADS) P.run_head[(long long)(i / places) * P.runs + blockIdx.x * places + i % places] = make_int2(0, 0);
-    if (blockIdx.x == 0) {
-        const int rest = P.runs - (int)gridDim.x * places;
-        for (int i = tid; i < P.passes * rest; i += THREADS) P.run_head[(long long)(i / rest + 1) * P.runs - 1 - i % rest] = make_int2(0, 0);
-    }
+    // (runs beyond the grid's are the last CTA's)
+    for (int i = tid; i < P.passes * P.runs; i += THREADS)
+        if (min(i % P.runs, (int)gridDim.x - 1) == (int)blockIdx.x) P.run_head[i] = make_int2(0, 0);
 
     for (int pass = 0; pass < P.passes; ++pass) {
     // ---- the pass's tokens and their units
@@ -132,77 +152,54 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
     __syncthreads();
     {
         long long mine[PER], sum = 0;
-        int longest = 1;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = tid * PER + i;
             mine[i] = 0;
             if (e < n) {
                 bool bad = false;
-                const int units = quant_units(sight_of(A, n0 + e, &bad));
-                longest = max(longest, units);
-                mine[i] = (long long)units * pairs_each;
+                mine[i] = (long long)quant_units(sight_of(A, n0 + e, &bad)) * groups;
                 if (bad && blockIdx.x == 0) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
             }
             sum += mine[i];
         }
-        longest = __reduce_max_sync(0xffffffffu, longest);
         long long incl = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long up = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += up;
         }
-        if (lane == 31) {
-            warp_sum_s[warp] = incl;
-            longest_s[warp] = longest;
-        }
+        if (lane == 31) warp_sum_s[warp] = incl;
+        if (lane < 2) piece_s[hb][2 * kw + lane].there = 0;
         __syncthreads();
         long long before = incl - sum;
         for (int w = 0; w < warp; ++w) before += warp_sum_s[w];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = tid * PER + i;
-            if (e < n) base_s[e] = before;
+            if (e < n && e < kListTokens) base_s[e] = before;
             before += mine[i];
         }
         if (tid == THREADS - 1) base_s[n] = before;
         __syncthreads();
     }
-    const long long total = base_s[n];
-    // Equal runs, of at least a unit for each warp
-    long long wanted = min((long long)gridDim.x, (total + WARPS - 1) / WARPS);
-    if (BY_WARP) {
-        int longest = 1;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) longest = max(longest, longest_s[w]);
-        wanted = warp_runs(total, longest, (long long)gridDim.x * WARPS);
+    // Equal runs of the CTAs, of at least a unit for each warp
+    const int n_runs = P.whole ? n * groups : (int)min((long long)gridDim.x, (base_s[n] + KW - 1) / KW);
+    if ((int)blockIdx.x >= n_runs) continue;
+    long long u0, left;                                 // the first unit of this warp's run, and the number of those that are still to be taken
+    {
+        const long long share = base_s[n] / n_runs, extra = base_s[n] - share * n_runs;
+        long long first = blockIdx.x * share + min((long long)blockIdx.x, extra), units = share + (blockIdx.x < extra ? 1 : 0);
+        if (P.whole) {
+            const int e = (int)blockIdx.x / groups;
+            units = (base_s[e + 1] - base_s[e]) / groups;
+            first = base_s[e] + (int)blockIdx.x % groups * units;
+        }
+        u0 = first + units * kw / KW;
+        left = first + units * (kw + 1) / KW - u0;
     }
-    if (P.whole) wanted = (long long)n * pairs_each;
-    const int n_runs = (int)wanted, run_no = BY_WARP ? (int)blockIdx.x * WARPS + warp : (int)blockIdx.x;
-    if (run_no >= n_runs) {
-        __syncwarp();
-        continue;
-    }
-    const long long share = total / n_runs, extra = total - share * n_runs;
-    const auto run_start = [&](long long c) { return c * share + (c < extra ? c : extra); };
-    const auto run_of = [&](long long u) {              // the run that holds unit u
-        const long long cut = extra * (share + 1);
-        return u < cut ? u / (share + 1) : extra + (u - cut) / share;
-    };
-    long long u0, u1;
-    if (P.whole) {
-        const int e = run_no / pairs_each;
-        const long long units = (base_s[e + 1] - base_s[e]) / pairs_each;
-        u0 = base_s[e] + run_no % pairs_each * units;
-        u1 = u0 + units;
-    } else {
-        u0 = run_start(run_no);
-        u1 = run_start(run_no + 1);
-    }
-    const long long run = (long long)pass * P.runs + run_no;
 
-    // Where a unit lies: token, its (head, row tile), key block of it
+    // Where a unit lies: token, its group of pairs, key block of it
     struct Cursor {
         int e, h, k, units;
         Sight s;
@@ -214,14 +211,14 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
         c.units = quant_units(c.s);
     };
     const auto settle = [&](Cursor& c) {                // k past the pair's units: on to the pair that holds it
-        while (c.e < n && c.k >= c.units) {
-            c.k -= c.units;
-            if (++c.h == pairs_each) {
-                c.h = 0;
-                ++c.e;
-                look(c);
-            }
+        if (c.k < c.units) return false;
+        c.k = 0;
+        if (++c.h == groups) {
+            c.h = 0;
+            ++c.e;
+            look(c);
         }
+        return true;
     };
     Cursor seg;
     {
@@ -238,27 +235,27 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
         seg.k = (int)(in % seg.units);
     }
     Cursor ahead = seg;                                 // the next unit to fetch
-    const int hop = BY_WARP ? 1 : WARPS, begin = BY_WARP ? 0 : warp;
-    long long u_ahead = u0 + begin;
-    if (u_ahead < u1) {
-        ahead.k += begin;
-        settle(ahead);
-    }
-    const uint32_t ring0 = ptx::smem_u32(aq_smem) + (uint32_t)(warp * BUFS * Geo::UNIT);
+    long long to_fetch = left, code = 0, scales = 0;    // ... where its pair's codes and scales begin
+    const auto aim = [&]() {
+        const int j = (ahead.h * HB + hb) / A.row_tiles;
+        code = ahead.s.seq * C.c_s + j * C.c_h;
+        scales = ahead.s.seq * C.s_s + j * C.s_h;
+    };
+    aim();
+    const uint32_t ring0 = ptx::smem_u32(aq_smem) + (uint32_t)(warp * Geo::OWN);
     const auto fetch = [&](int buf) {
-        if (u_ahead < u1) {
+        if (to_fetch > 0) {
             const Sight& s = ahead.s;
             const int su = (s.sinks + kQuantUnit - 1) / kQuantUnit;
             const int key0 = ahead.k < su ? ahead.k * kQuantUnit : s.first + (ahead.k - su) * kQuantUnit;
             const int nk = ahead.k < su ? s.sinks - key0 : s.last + 1 - key0;       // keys of the unit, if fewer than kQuantUnit
-            const int slot0 = slot_of(A, key0), j = ahead.h / A.row_tiles;
-            const long long code = s.seq * C.c_s + j * C.c_h, sc = s.seq * C.s_s + j * C.s_h;
+            const int slot0 = slot_of(A, key0);
             const uint32_t to = ring0 + (uint32_t)(buf * Geo::UNIT);
             {                                           // a lane's key's scales
                 int slot = slot0 + (lane < nk ? lane : 0);
                 if (A.ring && slot >= A.L) slot -= A.ring;                           // in a unit across the end of the ring the slots are not neighbours
-                copy_piece<Geo::SC>(to + Geo::KS + lane * Geo::SC, C.K_scale + sc + slot * C.s_p, lane < nk);
-                copy_piece<Geo::SC>(to + Geo::VS + lane * Geo::SC, C.V_scale + sc + slot * C.s_p, lane < nk);
+                copy_piece<Geo::SC>(to + Geo::KS + lane * Geo::SC, C.K_scale + scales + slot * C.s_p, lane < nk);
+                copy_piece<Geo::SC>(to + Geo::VS + lane * Geo::SC, C.V_scale + scales + slot * C.s_p, lane < nk);
             }
             // a unit of neighbouring slots that is full: no piece needs a look at its row
             if ((G & (G - 1)) == 0 && nk >= kQuantUnit && (!A.ring || slot0 + kQuantUnit <= A.L)) {
@@ -284,11 +281,8 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                     copy_piece<16>(to + Geo::V + row * Geo::VROW + ch * 16, C.V + src, row < nk);
                 }
             }
-            u_ahead += hop;
-            if (u_ahead < u1) {                         // (settling may wait for a token's sequence and position)
-                ahead.k += hop;
-                settle(ahead);
-            }
+            ++ahead.k;
+            if (--to_fetch > 0 && settle(ahead)) aim(); // (which may wait for a token's sequence and position)
         }
         ptx::cp_async_commit();
     };
@@ -297,13 +291,11 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
     const uint32_t kfrag = (uint32_t)(g8 * Geo::KROW + q4 * 4 * G), vfrag = (uint32_t)(Geo::V + 2 * q4 * Geo::VROW + (g8 >> 1) * 4 * G);
     const uint32_t half = g8 & 1 ? 0x7632u : 0x5410u;   // which half of a word of the values' is this lane's
     int buf = 0;
-    long long mine = u0 + begin;                        // this warp's next unit
-    for (long long at = u0; at < u1;) {
-        const int t = n0 + seg.e, units = seg.units, first_k = seg.k;
-        const long long end = min(u1, at + units - first_k);
+    while (left > 0) {
+        const int t = n0 + seg.e, units = seg.units, first_k = seg.k, end_k = (int)min((long long)units, first_k + left);
         const Sight& s = seg.s;
         const int su = (s.sinks + kQuantUnit - 1) / kQuantUnit;
-        const int j = seg.h / A.row_tiles, row0 = seg.h % A.row_tiles * 16, rows = min(8 * NT, A.group - row0);
+        const int pair = seg.h * HB + hb, j = pair / A.row_tiles, row0 = pair % A.row_tiles * 16, rows = min(8 * NT, A.group - row0);
         // queries as the narrow operand, in the order in which codes leave their words, and what a group's sum begins with
         uint2 qf[NT][2 * G];
         float init[NT][G][2];
@@ -334,7 +326,7 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
 #pragma unroll
             for (int i = 0; i < 2 * G; ++i) o[i][nt][0] = o[i][nt][1] = o[i][nt][2] = o[i][nt][3] = 0.f;
         }
-        for (; mine < end; mine += hop) {
+        for (int k = first_k; k < end_k; ++k) {
             __syncwarp();                               // every lane is past its reads of the buffer that is filled again now
             fetch((buf + BUFS - 1) % BUFS);
             ptx::cp_async_wait<BUFS - 1>();
@@ -374,8 +366,22 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                 }
             }
             // to base 2; what is no key is hidden
-            const int k = first_k + (int)(mine - at);
             const int nk = k < su ? s.sinks - k * kQuantUnit : s.last + 1 - s.first - (k - su) * kQuantUnit;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) x[h][nt][c] *= A.scale_log2;
+            if (nk < kQuantUnit) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (16 * h + (c >> 1) * 8 + g8 >= nk) x[h][nt][c] = -INFINITY;
+            }
             float top[NT][2];
             bool moves = false;
 #pragma unroll
@@ -385,8 +391,6 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        x[h][nt][c] *= A.scale_log2;
-                        if (nk < kQuantUnit && 16 * h + (c >> 1) * 8 + g8 >= nk) x[h][nt][c] = -INFINITY;
                         top[nt][c & 1] = fmaxf(top[nt][c & 1], x[h][nt][c]);
                     }
 #pragma unroll
@@ -460,17 +464,6 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             }
             buf = buf + 1 == BUFS ? 0 : buf + 1;
         }
-        Cursor next = seg;
-        if (end < u1) {
-            next.k += (int)(end - at);
-            settle(next);
-        } else if (pass + 1 == P.passes) {
-            chain_next();
-        }
-        const bool whole = end - at == units, begins = first_k == 0;
-        if (begins && !whole && (BY_WARP ? lane : tid) == 0)
-            P.run_head[run] = make_int2(t * pairs_each + seg.h, parts_word((int)(run_of(at + units - 1) - run_no + 1), 1));
-        float* const slot = P.slots + part_slot(run, begins, 1, 0) * 16 * (DH + 2);
         // ---- sums over the keys that the lanes of a row had
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -478,99 +471,129 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             for (int r = 0; r < 2; ++r)
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[nt][r] += __shfl_xor_sync(0xffffffffu, l[nt][r], d);
-        const auto write_lse = [&](long long r, float M, float den) {
-            if (A.lse) A.lse[r] = ((M == -INFINITY ? 0.f : M) + log2f(den)) * 0.6931471805599453f;
-        };
-        if (BY_WARP) {
+        if (end_k - first_k == units) {                        // the pair is this warp's
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const int row = nt * 8 + 2 * q4 + r, member = row0 + row;
-                    if (row >= rows) continue;
+                    const int member = row0 + nt * 8 + 2 * q4 + r;
+                    if (nt * 8 + 2 * q4 + r >= rows) continue;
                     const float den = l[nt][r], inv = den == 0.f ? 0.f : 1.f / den;       // no key: zeros
                     __nv_bfloat16* const out = A.out + t * A.o_t + j * A.o_h + member * A.o_g + g8 * 4;
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        const float4 v = make_float4(o[2 * g][nt][r], o[2 * g][nt][2 + r], o[2 * g + 1][nt][r], o[2 * g + 1][nt][2 + r]);
-                        // (a slot's rows begin at multiples of 8 bytes)
-                        if (whole) {
-                            *reinterpret_cast<uint2*>(out + g * kQuantGroup) = make_uint2(pack2(v.x * inv, v.y * inv), pack2(v.z * inv, v.w * inv));
-                        } else {
-                            float2* const to = reinterpret_cast<float2*>(slot + row * DH + g * kQuantGroup + g8 * 4);
-                            to[0] = make_float2(v.x, v.y);
-                            to[1] = make_float2(v.z, v.w);
-                        }
-                    }
-                    if (g8 != 0) continue;
-                    if (whole) write_lse(row_at(A, t, j, member), m[nt][r], den);
-                    else *reinterpret_cast<float2*>(slot + 16 * DH + row * 2) = make_float2(m[nt][r], den);
+                    for (int g = 0; g < G; ++g)
+                        *reinterpret_cast<uint2*>(out + g * kQuantGroup) = make_uint2(pack2(o[2 * g][nt][r] * inv, o[2 * g][nt][2 + r] * inv),
+                                                                                      pack2(o[2 * g + 1][nt][r] * inv, o[2 * g + 1][nt][2 + r] * inv));
+                    if (g8 == 0 && A.lse) A.lse[row_at(A, t, j, member)] = row_lse(m[nt][r], den);
                 }
-            seg = next;
-            at = end;
-            continue;
-        }
-        // ---- the warps' triples of the pair, through the buffer that each has just finished (the next fetch would fill it)
-        const uint32_t free_at = (uint32_t)((warp * BUFS + (buf + BUFS - 1) % BUFS) * Geo::UNIT);
-        __syncwarp();
-        if (lane == 0) at_s[warp] = free_at;
-        if (g8 == 0)
+        } else {
+            // what goes on behind the run lies where the ring was, as nothing is fetched any more
+            const bool begins = first_k == 0;
+            Piece<8 * NT>& piece = piece_s[hb][2 * kw + (begins ? 1 : 0)];
+            const uint32_t sums = (uint32_t)(warp * Geo::OWN + (begins ? 0 : BUFS * Geo::UNIT));
+            if (begins) ptx::cp_async_wait<0>();
+            __syncwarp();
+            if (lane == 0) {
+                piece.there = 1;
+                piece.begins = begins;
+                piece.ends = end_k == units;
+                piece.e = seg.e, piece.h = pair, piece.units = units;
+                piece.sums = sums;
+            }
+            float* const to = reinterpret_cast<float*>(aq_smem + sums);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    ms[warp][nt * 8 + 2 * q4 + r] = m[nt][r];
-                    ls[warp][nt * 8 + 2 * q4 + r] = l[nt][r];
+                    const int row = nt * 8 + 2 * q4 + r;
+                    if (g8 == 0) {
+                        piece.m[row] = m[nt][r];
+                        piece.l[row] = l[nt][r];
+                    }
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+                        *reinterpret_cast<float4*>(to + row * LDO + g * kQuantGroup + g8 * 4) =
+                            make_float4(o[2 * g][nt][r], o[2 * g][nt][2 + r], o[2 * g + 1][nt][r], o[2 * g + 1][nt][2 + r]);
                 }
-        float* const acc = reinterpret_cast<float*>(aq_smem + free_at);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-                    *reinterpret_cast<float4*>(acc + (2 * q4 + r) * LDO + g * kQuantGroup + g8 * 4) =
-                        make_float4(o[2 * g][nt][r], o[2 * g][nt][2 + r], o[2 * g + 1][nt][r], o[2 * g + 1][nt][2 + r]);
-            __syncthreads();
-            for (int idx = tid; idx < min(8, rows - nt * 8) * (DH / 2); idx += THREADS) {
-                const int in = idx / (DH / 2), row = nt * 8 + in, col = idx % (DH / 2) * 2, member = row0 + row;
+        }
+        left -= end_k - first_k;
+        seg.k = end_k;
+        if (left > 0) settle(seg);
+    }
+    ptx::cp_async_wait<0>();
+    if (pass + 1 == P.passes) chain_next();
+    __syncthreads();
+
+    // ---- the CTA's pieces of a pair follow one another: what goes on behind a run, and what began before the next ones, up to its end.  A chain of them may
+    // also begin before the CTA's first run, or go on behind its last.  The warps of a pair of the HB share out its chains, or the columns of one.
+    {
+        const Piece<8 * NT>* const pieces = piece_s[hb];
+        int first = 0;                                  // (if it does not begin its pair, an earlier CTA does)
+        while (first < 2 * KW && !pieces[first].there) ++first;
+        const auto heads_chain = [&](int i) { return pieces[i].there && (pieces[i].begins || i == first); };
+        const auto goes_on = [&](int i) { return pieces[i].there && !pieces[i].begins; };
+        int chains = 0;
+        for (int i = 0; i < 2 * KW; ++i) chains += heads_chain(i) ? 1 : 0;
+        const int slices = chains == 0 ? 1 : max(1, KW / chains), slice = kw % slices;
+        const long long run = (long long)pass * P.runs + blockIdx.x;
+        for (int c = kw / slices; c < chains; c += KW / slices) {
+            int head = 0;
+            for (int before = 0;; ++head)
+                if (heads_chain(head) && before++ == c) break;
+            int last = head;                            // the last piece of the chain
+            for (int i = head + 1; i < 2 * KW && !pieces[last].ends; ++i)
+                if (goes_on(i)) last = i;
+            const Piece<8 * NT>& f = pieces[head];
+            const int t = n0 + f.e, j = f.h / A.row_tiles, row0 = f.h % A.row_tiles * 16, rows = min(8 * NT, A.group - row0);
+            const bool begins = f.begins, ends = pieces[last].ends, whole = begins && ends;
+            float* const slot = P.slots + part_slot(run, begins, HB, hb) * 16 * (DH + 2);
+            if (begins && !ends && hb == 0 && slice == 0 && lane == 0) {
+                // the run that holds the pair's last unit
+                const long long u = base_s[f.e] + (long long)(f.h / HB + 1) * f.units - 1, share = base_s[n] / n_runs, extra = base_s[n] - share * n_runs;
+                const long long cut = extra * (share + 1), end = u < cut ? u / (share + 1) : extra + (u - cut) / share;
+                P.run_head[run] = make_int2(t * A.n_head * A.row_tiles + f.h, parts_word((int)end - (int)blockIdx.x + 1, 1));
+            }
+            for (int idx = lane + 32 * slice; idx < rows * (DH / 4); idx += 32 * slices) {
+                const int row = idx / (DH / 4), col = idx % (DH / 4) * 4, member = row0 + row;
                 float M = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < WARPS; ++w) M = fmaxf(M, ms[w][row]);
+                for (int i = head; i <= last; ++i)
+                    if (i == head || goes_on(i)) M = fmaxf(M, pieces[i].m[row]);
                 const float z = M == -INFINITY ? 0.f : M;
-                float nx = 0.f, ny = 0.f, den = 0.f;
-#pragma unroll
-                for (int w = 0; w < WARPS; ++w) {
-                    const float wgt = exp2_fast(ms[w][row] - z);          // 0 for a warp that saw no key
-                    const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(aq_smem + at_s[w]) + in * LDO + col);
-                    nx = fmaf(wgt, v.x, nx);
-                    ny = fmaf(wgt, v.y, ny);
-                    den = fmaf(wgt, ls[w][row], den);
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                float den = 0.f;
+                for (int i = head; i <= last; ++i) {
+                    if (i != head && !goes_on(i)) continue;
+                    const float wgt = exp2_fast(pieces[i].m[row] - z);    // 0 for a piece that saw no key
+                    const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(aq_smem + pieces[i].sums) + row * LDO + col);
+                    sum.x = fmaf(wgt, v.x, sum.x);
+                    sum.y = fmaf(wgt, v.y, sum.y);
+                    sum.z = fmaf(wgt, v.z, sum.z);
+                    sum.w = fmaf(wgt, v.w, sum.w);
+                    den = fmaf(wgt, pieces[i].l[row], den);
                 }
                 if (whole) {
                     const float inv = den == 0.f ? 0.f : 1.f / den;
-                    *reinterpret_cast<uint32_t*>(A.out + t * A.o_t + j * A.o_h + member * A.o_g + col) = pack2(nx * inv, ny * inv);
-                    if (col == 0) write_lse(row_at(A, t, j, member), M, den);
+                    *reinterpret_cast<uint2*>(A.out + t * A.o_t + j * A.o_h + member * A.o_g + col) =
+                        make_uint2(pack2(sum.x * inv, sum.y * inv), pack2(sum.z * inv, sum.w * inv));
+                    if (col == 0 && A.lse) A.lse[row_at(A, t, j, member)] = row_lse(M, den);
                 } else {
-                    *reinterpret_cast<float2*>(slot + row * DH + col) = make_float2(nx, ny);
+                    float2* const to = reinterpret_cast<float2*>(slot + row * DH + col);          // (multiples of 8 bytes)
+                    to[0] = make_float2(sum.x, sum.y);
+                    to[1] = make_float2(sum.z, sum.w);
                     if (col == 0) *reinterpret_cast<float2*>(slot + 16 * DH + row * 2) = make_float2(M, den);
                 }
             }
-            __syncthreads();                            // the warps' triples are read before they are overwritten, by the next rows' or the next fetch
         }
-        seg = next;
-        at = end;
     }
-    ptx::cp_async_wait<0>();
     }
 }
 
 template <int DH, int NT>
 struct QuantLaunch {
     using Geo = QuantGeo<DH, NT>;
-    template <bool BY_WARP>
-    static dsmoe_status go(const AttnView& A, const QuantView& C, const QuantPlan& P, int ctas, cudaStream_t s) {
-        auto* kernel = attention_quant_kernel<DH, NT, BY_WARP>;
+    template <int HB>
+    static dsmoe_status heads(const AttnView& A, const QuantView& C, const QuantPlan& P, int ctas, cudaStream_t s) {
+        auto* kernel = attention_quant_kernel<DH, NT, HB>;
         static bool attr[kMaxDeviceSlots] = {};
         int dev = 0;
         DeviceState* st = nullptr;
@@ -582,42 +605,46 @@ struct QuantLaunch {
         DSMOE_CUDA_TRY(launch_chained(kernel, (unsigned)ctas, 32 * Geo::WARPS, Geo::SMEM, s, A, C, P));
         return DSMOE_OK;
     }
+    static dsmoe_status go(const AttnView& A, const QuantView& C, const QuantPlan& P, int hb, int ctas, cudaStream_t s) {
+        if constexpr (Geo::WARPS % 4 == 0)
+            if (hb == 4) return heads<4>(A, C, P, ctas, s);
+        return hb == 2 ? heads<2>(A, C, P, ctas, s) : heads<1>(A, C, P, ctas, s);
+    }
 };
 
-int quant_warps(const AttnView& A) { return A.d_head <= 128 && A.group <= 8 ? 16 : 8; }
+int quant_warps_of(const AttnView& A) { return quant_warps(A.d_head, A.group <= 8 ? 1 : 2); }
 
 // Keys that a token sees at most
 long long quant_seen(const AttnView& A) { return A.window < A.L ? std::min((long long)A.window + A.sinks, (long long)A.L) : A.L; }
 
 // CTAs: one an SM, as far as each has a unit per warp in the longest case
 int quant_ctas(const AttnView& A) {
-    const long long units = ((quant_seen(A) + kQuantUnit - 1) / kQuantUnit + 1) * A.T * A.n_head * A.row_tiles, warps = quant_warps(A);
+    const long long units = ((quant_seen(A) + kQuantUnit - 1) / kQuantUnit + 1) * A.T * A.n_head * A.row_tiles, warps = quant_warps_of(A);
     return (int)std::min((units + warps - 1) / warps, (long long)std::min(sm_count(), kMostStreamCtas));
 }
 
+constexpr int kMostHeadsAtOnce = 4;
+
 }  // namespace
 
-// The runs are numbered as attention_sum_kernel takes those of single warps: stream_warps of them to a CTA
+// The runs are numbered as attention_sum_kernel takes those of single warps, of which stream_warps are a CTA's there
 void quant_plan_size(const AttnView& A, QuantPlan* plan, size_t* slots, size_t* run_head) {
     plan->passes = ceil_div(A.T, kListTokens);
-    plan->runs = (int)align_up((size_t)quant_ctas(A) * quant_warps(A), stream_warps(A.d_head));
+    plan->runs = (int)align_up(std::min((long long)A.T * A.n_head * A.row_tiles + quant_ctas(A), (long long)std::min(sm_count(), kMostStreamCtas)), 8);
     *run_head = (size_t)plan->passes * plan->runs * sizeof(int2);
-    *slots = 2 * (size_t)plan->passes * plan->runs * part_bytes(A.d_head);
+    *slots = 2 * (size_t)plan->passes * plan->runs * kMostHeadsAtOnce * part_bytes(A.d_head);
 }
 
 dsmoe_status launch_quant_attention(const AttnView& A, const QuantView& C, const QuantPlan& plan, cudaStream_t s) {
     QuantPlan P = plan;
     const long long pairs = (long long)A.T * A.n_head * A.row_tiles;
-    const int sms = std::min(sm_count(), kMostStreamCtas), warps = quant_warps(A);
-    int ctas = std::min(quant_ctas(A), sms);
+    const int sms = std::min(sm_count(), kMostStreamCtas), warps = quant_warps_of(A), each = A.n_head * A.row_tiles;
     // A CTA takes all of a pair's keys, and no part is left to add up, where the CTAs that stay idle would save less than the second launch costs
     P.whole = pairs <= sms && quant_seen(A) * (sms - pairs) <= 3ll * kQuantUnit * warps * sms;
-    P.by_warp = !P.whole && pairs >= (long long)ctas * warps;
-    if (P.whole) ctas = (int)pairs;
-    P.runs = (int)align_up((size_t)ctas * (P.by_warp ? warps : 1), stream_warps(A.d_head));      // (no more than there is room for)
-#define DSMOE_CALL(DH)                                                                                                                               \
-    (A.group <= 8 ? P.by_warp ? QuantLaunch<DH, 1>::go<true>(A, C, P, ctas, s) : QuantLaunch<DH, 1>::go<false>(A, C, P, ctas, s)                       \
-                  : P.by_warp ? QuantLaunch<DH, 2>::go<true>(A, C, P, ctas, s) : QuantLaunch<DH, 2>::go<false>(A, C, P, ctas, s))
+    const bool side_by_side = A.row_tiles > 1 || (A.n_head > 1 && C.c_h < C.c_p);
+    const int hb = P.whole || !side_by_side ? 1 : each % 4 == 0 && warps % 4 == 0 ? 4 : each % 2 == 0 ? 2 : 1;
+    const int ctas = P.whole ? (int)pairs : quant_ctas(A);
+#define DSMOE_CALL(DH) (A.group <= 8 ? QuantLaunch<DH, 1>::go(A, C, P, hb, ctas, s) : QuantLaunch<DH, 2>::go(A, C, P, hb, ctas, s))
     switch (A.d_head) {
         case 32: DSMOE_TRY(DSMOE_CALL(32)); break;
         case 64: DSMOE_TRY(DSMOE_CALL(64)); break;
@@ -633,9 +660,9 @@ dsmoe_status launch_quant_attention(const AttnView& A, const QuantView& C, const
     if (P.whole) return DSMOE_OK;
     StreamPlan sum{};
     sum.passes = P.passes;
-    sum.ctas = P.runs / stream_warps(A.d_head);
+    sum.ctas = P.runs * hb / stream_warps(A.d_head);
     sum.by_warp = true;
-    sum.heads_at_once = 1;
+    sum.heads_at_once = hb;
     sum.slots = P.slots;
     sum.run_head = P.run_head;
     return launch_attention_sum(A, sum, RowParts{}, s);

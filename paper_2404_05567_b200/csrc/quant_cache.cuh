@@ -50,9 +50,9 @@ dsmoe_status launch_quant_range(const AttnView& A, int4* range, cudaStream_t s);
 
 // Attention of all tokens (A.K, A.V and kv_ unused)
 struct QuantPlan {
-    int runs, passes;                     // places for runs of each pass
-    bool whole, by_warp;                  // see the kernel
-    float* slots;                         // [passes][runs][2][16][d_head + 2]
+    int runs, passes;                     // places for runs of each pass, a multiple of 8
+    bool whole;                           // each CTA's run is a pair's units: no parts
+    float* slots;                         // [passes][runs][2][up to 4 pairs][16][d_head + 2]
     int2* run_head;                       // [passes][runs]
 };
 // The most runs that any window needs (A has none), and the bytes of `slots` and `run_head`
