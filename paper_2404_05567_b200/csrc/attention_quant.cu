@@ -6,11 +6,16 @@
 // A warp brings its units' codes and scales into a ring of its own (cp.async), and takes 16 keys at a time to its tensor instructions with the keys, not the rows, as
 // the 16-row operand: S^T = K q^T and O^T += V^T P^T.  Codes become bf16 numbers in registers, once for all of the pair's rows, of which 8 are the
 // narrow side of an instruction (two of those for groups of more than 8).
-//   K: 4 bits beside the exponent of 128 are 128 + 8 + c, exactly; a group's sum then begins with -136 times the sum of the row's queries there, and its
-//      scale multiplies it into the logit.  (Sums of up to 18 times the products' own magnitude: 2^-20 of that is lost instead of 2^-24.)
+//   K: a code's 4 bits at the lower end of a half word are an fp16 number as they are, (8 + c) 2^-24, and 16 times that four bits further up: half a word of
+//      codes is an operand of masks alone.  A row's queries are multiplied by the power of two that makes the largest 2^14 to 2^15 (and 1 / 16 in the
+//      second kind of place) and so are fp16 numbers exactly, down to 2^-28 of the largest.  A group's sum begins with -8 times the sum of the row's queries
+//      there, and its scale multiplies it into the logit.  (With e4m3 operands, for which whole words of codes would do, the tensor instructions cost twice
+//      as much and others beside: 62 tokens with up to 8192 keys 77.9 us instead of 70.6 with bf16 operands.)
 //   V: 4 bits beside the exponent of 16 are 16 + 8 + c; times the scale, minus 24 times the scale, is s * c, exactly, in one packed operation, whose scales are
 //      the two keys' that share a register.
 // Weights are two bf16 numbers each, as good as 16 bits.  The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "quant_cache.cuh"
@@ -22,11 +27,17 @@ namespace {
 
 constexpr int kQuantUnit = 32;            // keys that a warp takes at a time
 
-__device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4], uint2 b, float c0, float c1) {
+__device__ __forceinline__ void mma_codes_first(float (&d)[4], const uint32_t (&a)[4], uint2 b, float c0, float c1) {
     asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void mma_codes_next(float (&d)[4], const uint32_t (&a)[4], uint2 b) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
 }
 __device__ __forceinline__ void mma_next(float (&d)[4], const uint32_t (&a)[4], uint2 b) {
     asm volatile(
@@ -49,6 +60,10 @@ __device__ __forceinline__ float exp2_fast(float v) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+__device__ __forceinline__ uint32_t pack2_half(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
 }
 // a * b + c, two bf16 numbers at a time
 __device__ __forceinline__ uint32_t fma_pair(uint32_t a, uint32_t b, uint32_t c) {
@@ -296,26 +311,47 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
         const Sight& s = seg.s;
         const int su = (s.sinks + kQuantUnit - 1) / kQuantUnit;
         const int pair = seg.h * HB + hb, j = pair / A.row_tiles, row0 = pair % A.row_tiles * 16, rows = min(8 * NT, A.group - row0);
-        // queries as the narrow operand, in the order in which codes leave their words, and what a group's sum begins with
+        // queries as the narrow operand, in the order in which codes leave their words; what a group's sum begins with; and what makes a row's sums logits in
+        // base 2
         uint2 qf[NT][2 * G];
-        float init[NT][G][2];
+        float init[NT][G][2], to_logit[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const bool real = nt * 8 + g8 < rows;
             const __nv_bfloat16* const q = A.q + t * A.q_t + j * A.q_h + (real ? row0 + nt * 8 + g8 : 0) * A.q_g + q4 * 8;
+            uint4 in[G];
+            uint32_t top = 0;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                uint4 x = *reinterpret_cast<const uint4*>(q + g * kQuantGroup);
-                if (!real) x = make_uint4(0u, 0u, 0u, 0u);
-                qf[nt][2 * g] = make_uint2(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
-                qf[nt][2 * g + 1] = make_uint2(__byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
-                float sum = ((low_part(x.x) + high_part(x.x)) + (low_part(x.y) + high_part(x.y))) +
-                            ((low_part(x.z) + high_part(x.z)) + (low_part(x.w) + high_part(x.w)));
+                in[g] = *reinterpret_cast<const uint4*>(q + g * kQuantGroup);
+                if (!real) in[g] = make_uint4(0u, 0u, 0u, 0u);
+                const uint32_t w[4] = {in[g].x, in[g].y, in[g].z, in[g].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+            }
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // the power of two (2^126 at most), and the inverse of 2^-24 times it
+            const int exponent = min(max((int)(top >> 7), 15), 254);
+            const float up = __uint_as_float((uint32_t)(268 - exponent) << 23);
+            float down = __uint_as_float((uint32_t)(exponent - 14) << 23) * (0x1p24f * A.scale_log2);
+            if (top >= 0x7f80u) down = __uint_as_float(0x7fffffffu);              // a query that is no number: the row is none
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const uint32_t w[4] = {in[g].x, in[g].y, in[g].z, in[g].w};
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = (i & 1 ? high_part(w[i / 2]) : low_part(w[i / 2])) * up;
+                qf[nt][2 * g] = make_uint2(pack2_half(x[0], x[4]), pack2_half(x[1] * 0.0625f, x[5] * 0.0625f));
+                qf[nt][2 * g + 1] = make_uint2(pack2_half(x[2], x[6]), pack2_half(x[3] * 0.0625f, x[7] * 0.0625f));
+                float sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                init[nt][g][0] = -136.f * __shfl_sync(0xffffffffu, sum, q4 * 8);
-                init[nt][g][1] = -136.f * __shfl_sync(0xffffffffu, sum, q4 * 8 + 4);
+                init[nt][g][0] = -0x1p-21f * __shfl_sync(0xffffffffu, sum, q4 * 8);
+                init[nt][g][1] = -0x1p-21f * __shfl_sync(0xffffffffu, sum, q4 * 8 + 4);
             }
+            to_logit[nt][0] = __shfl_sync(0xffffffffu, down, q4 * 8);
+            to_logit[nt][1] = __shfl_sync(0xffffffffu, down, q4 * 8 + 4);
         }
         // rows 2 q4 and 2 q4 + 1 of each tile
         float m[NT][2], l[NT][2], o[2 * G][NT][4];
@@ -343,21 +379,15 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                 load_words<SW>(s1, unit + (uint32_t)(Geo::KS + (16 * h + 8 + g8) * Geo::SC));
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    uint32_t a[4], b[4];
-                    a[0] = masked(w0[g], 0x000f000fu, 0x43004300u);
-                    a[1] = masked(w1[g], 0x000f000fu, 0x43004300u);
-                    a[2] = masked(w0[g] >> 4, 0x000f000fu, 0x43004300u);
-                    a[3] = masked(w1[g] >> 4, 0x000f000fu, 0x43004300u);
-                    b[0] = masked(w0[g] >> 8, 0x000f000fu, 0x43004300u);
-                    b[1] = masked(w1[g] >> 8, 0x000f000fu, 0x43004300u);
-                    b[2] = masked(w0[g] >> 12, 0x000f000fu, 0x43004300u);
-                    b[3] = masked(w1[g] >> 12, 0x000f000fu, 0x43004300u);
+                    const uint32_t v0 = w0[g] >> 8, v1 = w1[g] >> 8;
+                    const uint32_t a[4] = {w0[g] & 0x000f000fu, w1[g] & 0x000f000fu, w0[g] & 0x00f000f0u, w1[g] & 0x00f000f0u};
+                    const uint32_t b[4] = {v0 & 0x000f000fu, v1 & 0x000f000fu, v0 & 0x00f000f0u, v1 & 0x00f000f0u};
                     const float sa = g & 1 ? high_part(s0[g / 2]) : low_part(s0[g / 2]), sb = g & 1 ? high_part(s1[g / 2]) : low_part(s1[g / 2]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float c[4];
-                        mma_first(c, a, qf[nt][2 * g], init[nt][g][0], init[nt][g][1]);
-                        mma_next(c, b, qf[nt][2 * g + 1]);
+                        mma_codes_first(c, a, qf[nt][2 * g], init[nt][g][0], init[nt][g][1]);
+                        mma_codes_next(c, b, qf[nt][2 * g + 1]);
                         x[h][nt][0] = g == 0 ? sa * c[0] : fmaf(sa, c[0], x[h][nt][0]);
                         x[h][nt][1] = g == 0 ? sa * c[1] : fmaf(sa, c[1], x[h][nt][1]);
                         x[h][nt][2] = g == 0 ? sb * c[2] : fmaf(sb, c[2], x[h][nt][2]);
@@ -372,7 +402,7 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) x[h][nt][c] *= A.scale_log2;
+                    for (int c = 0; c < 4; ++c) x[h][nt][c] *= to_logit[nt][c & 1];
             if (nk < kQuantUnit) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)

@@ -69,14 +69,16 @@ def tensors(code, scale, by_token=False, device="cuda", fill=0.0):
     return held.to(device), sc.to(device)
 
 
-# Logits: c + 136 (an integer below 2^8) times a query is exact; a group's sum begins with -136 times the sum of its queries and takes two tensor
-# instructions of 16 products each, that may cut each of their 17 terms 2^-23 below the largest, at most 136 sum |q|; the sum of 32 queries is off by
-# at most 32 2^-24 of sum |q|.  Then the scales multiply and G sums are added, as the other attention kernels' d products are.
+# Logits: a row's queries are fp16 numbers scaled so that the largest is 2^14 or more, in half of the places 2^10: exact, or rounded by 2^-25 at most, 2^-35 of the
+# largest.  Times |s c| <= 7 s that is what 32 values add to a group's sum.  The sum itself begins with -8 times the sum of the queries, which is off by 32 2^-24
+# of sum |q|, and takes two tensor instructions of 16 products of at most 15 |q|, that may cut each of their 17 terms 2^-23 below the largest, at most
+# 8 sum |q| + 15 max |q|.  Then the scales multiply and G sums are added, as the other attention kernels' d products are.
 def quant_logit_error(q, scale, K_scale, spread, d):
     """q [g, d], K_scale [n, d / 32]: for every row of q."""
-    sums = np.abs(q).reshape(q.shape[0], -1, GROUP).sum(-1)                        # [g, d / 32]
-    cut = (2 * 17 * 2.0 ** -23 + 32 * 2.0 ** -24) * 136
-    return abs(scale) * cut * (sums @ K_scale.T).max(1, initial=0.0) + logit_error(spread, d)
+    q = np.abs(q)
+    sums, top = q.reshape(q.shape[0], -1, GROUP).sum(-1), q.max(-1, keepdims=True)          # [g, d / 32], [g, 1]
+    group = 7 * GROUP * 2.0 ** -35 * top + 8 * 32 * 2.0 ** -24 * sums + 2 * 17 * 2.0 ** -23 * (8 * sums + 15 * top)
+    return abs(scale) * (group @ K_scale.T).max(1, initial=0.0) + logit_error(spread, d)
 
 
 def quant_out_tolerance(out, absolute, error, prompt):

@@ -120,8 +120,10 @@ def test_many_short_pairs(by_token):
 
 
 def test_one_long_pair_beside_many_short_ones():
+    """600 tokens of two sequences: with heads of 64 taken as prompts, with heads of 32 as single tokens."""
     tokens = [(0, 20000)] + [(1, i % 5) for i in range(1, 600)]
-    run(QuantCase(tokens, 2, 2, 64, 2, 20001, seed=20))
+    run(QuantCase(tokens, 2, 2, 64, 2, 20001, seed=20), prompt=True)
+    run(QuantCase(tokens, 2, 2, 32, 2, 20001, seed=20))
 
 
 def test_parts_of_larger_tensors():
