@@ -11,9 +11,11 @@
 //      second kind of place) and so are fp16 numbers exactly, down to 2^-28 of the largest.  A group's sum begins with -8 times the sum of the row's queries
 //      there, and its scale multiplies it into the logit.  (With e4m3 operands, for which whole words of codes would do, the tensor instructions cost twice
 //      as much and others beside: 62 tokens with up to 8192 keys 77.9 us instead of 70.6 with bf16 operands.)
-//   V: 4 bits beside the exponent of 16 are 16 + 8 + c; times the scale, minus 24 times the scale, is s * c, exactly, in one packed operation, whose scales are
-//      the two keys' that share a register.
-// Weights are two bf16 numbers each, as good as 16 bits.  The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
+//   V: operands of masks alone too.  The scales multiply the weights instead, as fp16 numbers, a weight and group at a time (rounded to 11 bits), and the sum
+//      of a group's weights, from one more instruction, is taken away eight times.  The scales are relative to a power of two near the largest that the
+//      warp has met, which moves as the maximum of the logits does.  Units with scales 2^8 below it (or that are no numbers) go another way: 4 bits beside the
+//      exponent of 16 are 16 + 8 + c; times the scale, minus 24 times the scale, is s * c, exactly, in one packed operation; and weights are two bf16 numbers each.
+// The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -26,14 +28,15 @@ namespace dsmoe {
 namespace {
 
 constexpr int kQuantUnit = 32;            // keys that a warp takes at a time
+constexpr float kRaise = 6.f;             // weights of up to 2^(kStreamMoves + kRaise), times scales below 2, are fp16 numbers
 
-__device__ __forceinline__ void mma_codes_first(float (&d)[4], const uint32_t (&a)[4], uint2 b, float c0, float c1) {
+__device__ __forceinline__ void mma_half_first(float (&d)[4], const uint32_t (&a)[4], uint2 b, float c0, float c1) {
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "f"(c0), "f"(c1));
 }
-__device__ __forceinline__ void mma_codes_next(float (&d)[4], const uint32_t (&a)[4], uint2 b) {
+__device__ __forceinline__ void mma_half(float (&d)[4], const uint32_t (&a)[4], uint2 b) {
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -71,6 +74,23 @@ __device__ __forceinline__ uint32_t fma_pair(uint32_t a, uint32_t b, uint32_t c)
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
+// The larger ones of two numbers of 16 bits each
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_half_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }        // -126 <= e <= 127
 // (x & mask) | bits
 __device__ __forceinline__ uint32_t masked(uint32_t x, uint32_t mask, uint32_t bits) {
     uint32_t r;
@@ -93,6 +113,19 @@ __device__ __forceinline__ void load_words(uint32_t (&r)[N], uint32_t addr) {
         for (int i = 0; i < N; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[i]) : "r"(addr + 4 * i));
     }
 }
+template <int N>
+__device__ __forceinline__ void store_words(uint32_t addr, const uint32_t (&r)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            asm volatile("st.shared.v4.b32 [%4], {%0, %1, %2, %3};" ::"r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(addr + 4 * i) : "memory");
+    } else if constexpr (N == 2) {
+        asm volatile("st.shared.v2.b32 [%2], {%0, %1};" ::"r"(r[0]), "r"(r[1]), "r"(addr) : "memory");
+    } else {
+        static_assert(N == 1, "a word, two, or fours");
+        asm volatile("st.shared.b32 [%1], %0;" ::"r"(r[0]), "r"(addr) : "memory");
+    }
+}
 // BYTES (4, 8, 16), or zeros
 template <int BYTES>
 __device__ __forceinline__ void copy_piece(uint32_t dst, const void* src, bool real) {
@@ -109,6 +142,18 @@ __host__ __device__ static inline int quant_units(const Sight& s) {
 // Warps of a CTA: as many as their registers and rings allow
 __host__ __device__ static constexpr int quant_warps(int d_head, int nt) { return d_head <= 128 ? nt == 1 ? 12 : 8 : nt == 1 ? 6 : 4; }
 
+// a / b of numbers that are not negative, which nearly always are small
+__device__ __forceinline__ long long divide(long long a, int b) { return a >> 32 == 0 ? (uint32_t)a / (uint32_t)b : a / b; }
+// The first unit of run c of n equal ones (the first ones a unit longer), and the run that holds unit u
+__device__ __forceinline__ long long run_start(long long total, int n, int c) {
+    const long long share = divide(total, n);
+    return c * share + min((long long)c, total - share * n);
+}
+__device__ __forceinline__ int run_of(long long total, int n, long long u) {
+    const long long share = divide(total, n), extra = total - share * n, cut = extra * (share + 1);
+    return (int)(u < cut ? u / (share + 1) : extra + (u - cut) / share);
+}
+
 // The natural logarithm of a row's sum
 __device__ __forceinline__ float row_lse(float M, float den) { return ((M == -INFINITY ? 0.f : M) + log2f(den)) * 0.6931471805599453f; }
 
@@ -118,7 +163,7 @@ struct QuantGeo {
     static constexpr int G = DH / kQuantGroup, ROW = 16 * G, SC = 2 * quant_scales(DH);
     // bytes from one key's codes to the next in shared memory, with which neither the keys' nor the values' reads meet in a bank
     static constexpr int KROW = ROW + (G == 8 ? 16 : 0), VROW = ROW + (G % 2 == 0 ? 16 : 0);
-    static constexpr int V = kQuantUnit * KROW, KS = V + kQuantUnit * VROW, VS = KS + kQuantUnit * SC, UNIT = VS + kQuantUnit * SC;
+    static constexpr int V = kQuantUnit * KROW, KS = V + kQuantUnit * VROW, VS = KS + kQuantUnit * 2 * SC, UNIT = VS + kQuantUnit * SC;
     static constexpr int WARPS = quant_warps(DH, NT);
     static constexpr int LDO = DH + 4;    // floats from one row of a warp's sums to the next, where they meet
     static constexpr int SUMS = 8 * NT * LDO * 4;
@@ -151,6 +196,7 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
     constexpr int KW = WARPS / HB;                      // runs of a CTA
     extern __shared__ __align__(16) unsigned char aq_smem[];
     __shared__ long long base_s[kListTokens + 1];       // units before token e's
+    __shared__ Sight sight_s[kListTokens];
     __shared__ long long warp_sum_s[WARPS];
     __shared__ Piece<8 * NT> piece_s[HB][2 * KW];       // of each run: what began before it, what goes on behind it
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q4 = lane & 3;
@@ -173,7 +219,9 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             mine[i] = 0;
             if (e < n) {
                 bool bad = false;
-                mine[i] = (long long)quant_units(sight_of(A, n0 + e, &bad)) * groups;
+                const Sight s = sight_of(A, n0 + e, &bad);
+                sight_s[e] = s;
+                mine[i] = (long long)quant_units(s) * groups;
                 if (bad && blockIdx.x == 0) report_status(A.dev_status, DSMOE_ERR_INVALID_ARG);
             }
             sum += mine[i];
@@ -199,19 +247,22 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
         __syncthreads();
     }
     // Equal runs of the CTAs, of at least a unit for each warp
-    const int n_runs = P.whole ? n * groups : (int)min((long long)gridDim.x, (base_s[n] + KW - 1) / KW);
+    const int n_runs = P.whole ? n * groups : (int)min((long long)gridDim.x, divide(base_s[n] + KW - 1, KW));
     if ((int)blockIdx.x >= n_runs) continue;
     long long u0, left;                                 // the first unit of this warp's run, and the number of those that are still to be taken
     {
-        const long long share = base_s[n] / n_runs, extra = base_s[n] - share * n_runs;
-        long long first = blockIdx.x * share + min((long long)blockIdx.x, extra), units = share + (blockIdx.x < extra ? 1 : 0);
+        long long first, units;
         if (P.whole) {
             const int e = (int)blockIdx.x / groups;
-            units = (base_s[e + 1] - base_s[e]) / groups;
+            units = quant_units(sight_s[e]);
             first = base_s[e] + (int)blockIdx.x % groups * units;
+        } else {
+            first = run_start(base_s[n], n_runs, blockIdx.x);
+            units = run_start(base_s[n], n_runs, blockIdx.x + 1) - first;
         }
-        u0 = first + units * kw / KW;
-        left = first + units * (kw + 1) / KW - u0;
+        const long long a = divide(units * kw, KW), b = divide(units * (kw + 1), KW);
+        u0 = first + a;
+        left = b - a;
     }
 
     // Where a unit lies: token, its group of pairs, key block of it
@@ -220,9 +271,8 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
         Sight s;
     };
     const auto look = [&](Cursor& c) {
-        bool bad = false;
         if (c.e >= n) return;
-        c.s = sight_of(A, n0 + c.e, &bad);
+        c.s = sight_s[c.e];
         c.units = quant_units(c.s);
     };
     const auto settle = [&](Cursor& c) {                // k past the pair's units: on to the pair that holds it
@@ -237,17 +287,15 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
     };
     Cursor seg;
     {
-        int lo = 0, hi = n - 1;                         // the last token whose units begin at or before u0
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (base_s[mid] <= u0) lo = mid;
-            else hi = mid - 1;
-        }
+        // the last token whose units begin at or before u0: its 16, then which of them
+        static_assert(kListTokens <= 32 * 16, "two looks of a warp");
+        int lo = 16 * (__popc(__ballot_sync(0xffffffffu, 16 * lane < n && base_s[min(16 * lane, n)] <= u0)) - 1);
+        lo += __popc(__ballot_sync(0xffffffffu, lane < 16 && lo + lane < n && base_s[min(lo + lane, n)] <= u0)) - 1;
         seg.e = lo;
         look(seg);
         const long long in = u0 - base_s[lo];
-        seg.h = (int)(in / seg.units);
-        seg.k = (int)(in % seg.units);
+        seg.h = (int)divide(in, seg.units);
+        seg.k = (int)(in - (long long)seg.h * seg.units);
     }
     Cursor ahead = seg;                                 // the next unit to fetch
     long long to_fetch = left, code = 0, scales = 0;    // ... where its pair's codes and scales begin
@@ -269,7 +317,7 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             {                                           // a lane's key's scales
                 int slot = slot0 + (lane < nk ? lane : 0);
                 if (A.ring && slot >= A.L) slot -= A.ring;                           // in a unit across the end of the ring the slots are not neighbours
-                copy_piece<Geo::SC>(to + Geo::KS + lane * Geo::SC, C.K_scale + scales + slot * C.s_p, lane < nk);
+                copy_piece<Geo::SC>(to + Geo::KS + lane * 2 * Geo::SC, C.K_scale + scales + slot * C.s_p, lane < nk);
                 copy_piece<Geo::SC>(to + Geo::VS + lane * Geo::SC, C.V_scale + scales + slot * C.s_p, lane < nk);
             }
             // a unit of neighbouring slots that is full: no piece needs a look at its row
@@ -297,15 +345,14 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                 }
             }
             ++ahead.k;
-            if (--to_fetch > 0 && settle(ahead)) aim(); // (which may wait for a token's sequence and position)
+            if (--to_fetch > 0 && settle(ahead)) aim();
         }
         ptx::cp_async_commit();
     };
-    for (int b = 0; b < BUFS - 1; ++b) fetch(b);
 
     const uint32_t kfrag = (uint32_t)(g8 * Geo::KROW + q4 * 4 * G), vfrag = (uint32_t)(Geo::V + 2 * q4 * Geo::VROW + (g8 >> 1) * 4 * G);
     const uint32_t half = g8 & 1 ? 0x7632u : 0x5410u;   // which half of a word of the values' is this lane's
-    int buf = 0;
+    int buf = 0, fetched = 0;                           // (the first unit is preceded by BUFS - 1 of them)
     while (left > 0) {
         const int t = n0 + seg.e, units = seg.units, first_k = seg.k, end_k = (int)min((long long)units, first_k + left);
         const Sight& s = seg.s;
@@ -333,8 +380,8 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             // the power of two (2^126 at most), and the inverse of 2^-24 times it
             const int exponent = min(max((int)(top >> 7), 15), 254);
-            const float up = __uint_as_float((uint32_t)(268 - exponent) << 23);
-            float down = __uint_as_float((uint32_t)(exponent - 14) << 23) * (0x1p24f * A.scale_log2);
+            const float up = copysignf(power_of_two(141 - exponent), A.scale_log2);       // (a negative scale: the queries' signs)
+            float down = power_of_two(exponent - 141) * (0x1p24f * fabsf(A.scale_log2));
             if (top >= 0x7f80u) down = __uint_as_float(0x7fffffffu);              // a query that is no number: the row is none
 #pragma unroll
             for (int g = 0; g < G; ++g) {
@@ -353,41 +400,111 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             to_logit[nt][0] = __shfl_sync(0xffffffffu, down, q4 * 8);
             to_logit[nt][1] = __shfl_sync(0xffffffffu, down, q4 * 8 + 4);
         }
-        // rows 2 q4 and 2 q4 + 1 of each tile
-        float m[NT][2], l[NT][2], o[2 * G][NT][4];
+        // Rows 2 q4 and 2 q4 + 1 of each tile.  The largest sum m so far, as it was when it last moved, and the sum beyond which it moves; weights are
+        // 2^(to_logit x - z), 2^kRaise times those relative to the largest logit, so that small ones are fp16 numbers.
+        float m[NT][2], limit[NT][2], z[NT][2], l[NT][2];
+        // Sums of values in units of 2^(base - 88), each second one 16 times as large; and what is to be added to group g8's
+        float o[2 * G][NT][4], shift[NT][4];
+        int base = 0;                                   // the exponent (of a bf16) whose scales' exponent as an fp16 is 0
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            m[nt][0] = m[nt][1] = -INFINITY;
-            l[nt][0] = l[nt][1] = 0.f;
+            m[nt][0] = m[nt][1] = limit[nt][0] = limit[nt][1] = -INFINITY;
+            z[nt][0] = z[nt][1] = l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
             for (int i = 0; i < 2 * G; ++i) o[i][nt][0] = o[i][nt][1] = o[i][nt][2] = o[i][nt][3] = 0.f;
+            shift[nt][0] = shift[nt][1] = shift[nt][2] = shift[nt][3] = 0.f;
         }
         for (int k = first_k; k < end_k; ++k) {
             __syncwarp();                               // every lane is past its reads of the buffer that is filled again now
-            fetch((buf + BUFS - 1) % BUFS);
+#pragma unroll 1
+            for (;; ++fetched) {
+                const int to = buf + fetched;
+                fetch(to < BUFS ? to : to - BUFS);
+                if (fetched == BUFS - 1) break;
+            }
             ptx::cp_async_wait<BUFS - 1>();
-            __syncwarp();
             const uint32_t unit = ring0 + (uint32_t)(buf * Geo::UNIT);
-            // ---- logits of keys g8 and g8 + 8 of each half of the unit
+            // ---- a lane's key's scales (it has copied them itself): K's to fp32; V's to fp16, relative to base, with two keys' side by side
+            bool plain;
+            {
+                const uint32_t k_at = unit + (uint32_t)(Geo::KS + lane * 2 * Geo::SC), v_at = unit + (uint32_t)(Geo::VS + lane * Geo::SC);
+                uint32_t ks[SW], wide[2 * SW], vs[SW], top = 0, low = 0xffffffffu;
+                bool bad = false;
+                load_words<SW>(ks, k_at);
+                load_words<SW>(vs, v_at);
+#pragma unroll
+                for (int i = 0; i < SW; ++i) {
+                    wide[2 * i] = ks[i] << 16;
+                    wide[2 * i + 1] = ks[i] & 0xffff0000u;
+                }
+                store_words<2 * SW>(k_at, wide);
+#pragma unroll
+                for (int g = 0; g < G; ++g) {           // (places behind the last group may hold anything)
+                    const uint32_t v = g & 1 ? vs[g / 2] >> 16 : vs[g / 2] & 0xffffu, size = v & 0x7fffu;
+                    if (size < 0x7f80u) top = max(top, size);
+                    low = min(low, v - 1u);             // (zeros: the largest)
+                    bad = bad || v >= 0x7f80u;          // (also what is below zero)
+                }
+                // scales of a bf16's exponents base + 6 to base + 15, and zeros
+                if (__any_sync(0xffffffffu, top >= (uint32_t)(base + 16) << 7)) {
+                    const uint32_t most = __reduce_max_sync(0xffffffffu, top);
+                    const int next = max((int)(most >> 7) - 14, 0);
+                    const float f = exp2_fast((float)(base - next));
+                    base = next;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                            for (int i = 0; i < 2 * G; ++i) o[i][nt][c] *= f;
+                            shift[nt][c] *= f;
+                        }
+                }
+                bad = bad || low < ((uint32_t)(base + 6) << 7) - 1u;
+                plain = !__any_sync(0xffffffffu, bad);
+                if (plain) {
+                    const uint32_t none = (uint32_t)base << 7 | (uint32_t)base << 23;
+                    uint32_t pairs[SW];
+#pragma unroll
+                    for (int i = 0; i < SW; ++i) vs[i] = max_pair(vs[i], none) * 8u - none * 8u;      // (mantissas of 7 and 10 bits)
+                    // of keys 2 i and 2 i + 1: one group's of both in a word; the even key's lane writes the first half of the groups
+                    if constexpr (SW == 1) {
+                        const uint32_t other = __shfl_xor_sync(0xffffffffu, vs[0], 1);
+                        pairs[0] = lane & 1 ? __byte_perm(other, vs[0], 0x7632) : __byte_perm(vs[0], other, 0x5410);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < SW / 2; ++i) {
+                            const uint32_t mine = lane & 1 ? vs[SW / 2 + i] : vs[i];
+                            const uint32_t other = __shfl_xor_sync(0xffffffffu, lane & 1 ? vs[i] : vs[SW / 2 + i], 1);
+                            const uint32_t even = lane & 1 ? other : mine, odd = lane & 1 ? mine : other;
+                            pairs[2 * i] = __byte_perm(even, odd, 0x5410);
+                            pairs[2 * i + 1] = __byte_perm(even, odd, 0x7632);
+                        }
+                    }
+                    store_words<SW>(v_at, pairs);
+                }
+            }
+            __syncwarp();
+            // ---- sums of keys g8 and g8 + 8 of each half of the unit
             float x[2][NT][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                uint32_t w0[G], w1[G], s0[SW], s1[SW];
+                uint32_t w0[G], w1[G], s0[2 * SW], s1[2 * SW];
                 load_words<G>(w0, unit + kfrag + (uint32_t)(16 * h * Geo::KROW));
                 load_words<G>(w1, unit + kfrag + (uint32_t)((16 * h + 8) * Geo::KROW));
-                load_words<SW>(s0, unit + (uint32_t)(Geo::KS + (16 * h + g8) * Geo::SC));
-                load_words<SW>(s1, unit + (uint32_t)(Geo::KS + (16 * h + 8 + g8) * Geo::SC));
+                load_words<2 * SW>(s0, unit + (uint32_t)(Geo::KS + (16 * h + g8) * 2 * Geo::SC));
+                load_words<2 * SW>(s1, unit + (uint32_t)(Geo::KS + (16 * h + 8 + g8) * 2 * Geo::SC));
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const uint32_t v0 = w0[g] >> 8, v1 = w1[g] >> 8;
                     const uint32_t a[4] = {w0[g] & 0x000f000fu, w1[g] & 0x000f000fu, w0[g] & 0x00f000f0u, w1[g] & 0x00f000f0u};
                     const uint32_t b[4] = {v0 & 0x000f000fu, v1 & 0x000f000fu, v0 & 0x00f000f0u, v1 & 0x00f000f0u};
-                    const float sa = g & 1 ? high_part(s0[g / 2]) : low_part(s0[g / 2]), sb = g & 1 ? high_part(s1[g / 2]) : low_part(s1[g / 2]);
+                    const float sa = __uint_as_float(s0[g]), sb = __uint_as_float(s1[g]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float c[4];
-                        mma_codes_first(c, a, qf[nt][2 * g], init[nt][g][0], init[nt][g][1]);
-                        mma_codes_next(c, b, qf[nt][2 * g + 1]);
+                        mma_half_first(c, a, qf[nt][2 * g], init[nt][g][0], init[nt][g][1]);
+                        mma_half(c, b, qf[nt][2 * g + 1]);
                         x[h][nt][0] = g == 0 ? sa * c[0] : fmaf(sa, c[0], x[h][nt][0]);
                         x[h][nt][1] = g == 0 ? sa * c[1] : fmaf(sa, c[1], x[h][nt][1]);
                         x[h][nt][2] = g == 0 ? sb * c[2] : fmaf(sb, c[2], x[h][nt][2]);
@@ -395,14 +512,8 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                     }
                 }
             }
-            // to base 2; what is no key is hidden
+            // what is no key is hidden
             const int nk = k < su ? s.sinks - k * kQuantUnit : s.last + 1 - s.first - (k - su) * kQuantUnit;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) x[h][nt][c] *= to_logit[nt][c & 1];
             if (nk < kQuantUnit) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -415,17 +526,12 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             float top[NT][2];
             bool moves = false;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                top[nt][0] = top[nt][1] = -INFINITY;
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        top[nt][c & 1] = fmaxf(top[nt][c & 1], x[h][nt][c]);
-                    }
-#pragma unroll
-                for (int r = 0; r < 2; ++r) moves = moves || top[nt][r] > m[nt][r] + kStreamMoves || (m[nt][r] == -INFINITY && top[nt][r] > m[nt][r]);
-            }
+                for (int r = 0; r < 2; ++r) {
+                    top[nt][r] = max3(fmaxf(x[0][nt][r], x[0][nt][2 + r]), x[1][nt][r], x[1][nt][2 + r]);
+                    moves = moves || top[nt][r] > limit[nt][r];
+                }
             // (see kStreamMoves)
             if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
@@ -435,64 +541,142 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                         float b = top[nt][r];
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, d));
-                        const float up = fmaxf(m[nt][r], b), f = up == -INFINITY ? 1.f : exp2_fast(m[nt][r] - up);
-                        m[nt][r] = up;
+                        if (!(b > m[nt][r])) continue;  // (the row's lanes agree)
+                        const float before = z[nt][r];
+                        z[nt][r] = fmaf(b, to_logit[nt][r], -kRaise);
+                        limit[nt][r] = b + kStreamMoves / to_logit[nt][r];
+                        const float f = m[nt][r] == -INFINITY ? 1.f : exp2_fast(before - z[nt][r]);
+                        m[nt][r] = b;
                         l[nt][r] *= f;
 #pragma unroll
                         for (int i = 0; i < 2 * G; ++i) {
                             o[i][nt][r] *= f;
                             o[i][nt][2 + r] *= f;
                         }
+                        shift[nt][r] *= f;
                     }
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                // ---- the weights as two bf16 numbers each, the second the first's rounding error, with two keys of a row side by side
-                uint2 pf[NT], pr[NT];
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float z0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], z1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
-                    const float p0 = exp2_fast(x[h][nt][0] - z0), p1 = exp2_fast(x[h][nt][1] - z1);
-                    const float p2 = exp2_fast(x[h][nt][2] - z0), p3 = exp2_fast(x[h][nt][3] - z1);
-                    l[nt][0] += p0 + p2;
-                    l[nt][1] += p1 + p3;
-                    const uint32_t f0 = pack2(p0, p1), f1 = pack2(p2, p3);
-                    pf[nt] = make_uint2(transpose8(f0), transpose8(f1));
-                    pr[nt] = make_uint2(transpose8(pack2(p0 - low_part(f0), p1 - high_part(f0))), transpose8(pack2(p2 - low_part(f1), p3 - high_part(f1))));
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) x[h][nt][c] = exp2_fast(fmaf(x[h][nt][c], to_logit[nt][c & 1], -z[nt][c & 1]));
+            if (nk < kQuantUnit) {                      // (a scale of 0 makes hidden logits no numbers)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (16 * h + (c >> 1) * 8 + g8 >= nk) x[h][nt][c] = 0.f;
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) l[nt][r] += (x[0][nt][r] + x[0][nt][2 + r]) + (x[1][nt][r] + x[1][nt][2 + r]);
+            // ---- values of keys 2 q4, 2 q4 + 1 and the same + 8 of each half
+            if (plain) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t v0[G], v1[G], v2[G], v3[G], s0[2 * SW], s1[2 * SW];
+                    load_words<G>(v0, unit + vfrag + (uint32_t)(16 * h * Geo::VROW));
+                    load_words<G>(v1, unit + vfrag + (uint32_t)((16 * h + 1) * Geo::VROW));
+                    load_words<G>(v2, unit + vfrag + (uint32_t)((16 * h + 8) * Geo::VROW));
+                    load_words<G>(v3, unit + vfrag + (uint32_t)((16 * h + 9) * Geo::VROW));
+                    load_words<2 * SW>(s0, unit + (uint32_t)(Geo::VS + (16 * h + 2 * q4) * Geo::SC));
+                    load_words<2 * SW>(s1, unit + (uint32_t)(Geo::VS + (16 * h + 8 + 2 * q4) * Geo::SC));
+                    uint2 pf[NT];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        pf[nt] = make_uint2(transpose8(pack2_half(x[h][nt][0], x[h][nt][1])), transpose8(pack2_half(x[h][nt][2], x[h][nt][3])));
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const uint32_t w0 = __byte_perm(v0[g], v1[g], half), w1 = __byte_perm(v2[g], v3[g], half), u0 = w0 >> 8, u1 = w1 >> 8;
+                        const uint32_t a[4] = {w0 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x000f000fu, w1 & 0x00f000f0u};
+                        const uint32_t b[4] = {u0 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x000f000fu, u1 & 0x00f000f0u};
+                        const uint32_t eights = g8 == g ? 0x80088008u : 0u, c[4] = {eights, 0u, eights, 0u};         // -8 2^-24 in row g
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint2 w = make_uint2(mul_half_pair(pf[nt].x, s0[g]), mul_half_pair(pf[nt].y, s1[g]));
+                            mma_half(o[2 * g][nt], a, w);
+                            mma_half(o[2 * g + 1][nt], b, w);
+                            mma_half(shift[nt], c, w);
+                        }
+                    }
                 }
-                // ---- values of keys 2 q4, 2 q4 + 1 and the same + 8
-                uint32_t v0[G], v1[G], v2[G], v3[G], s0[2 * SW], s1[2 * SW];
-                load_words<G>(v0, unit + vfrag + (uint32_t)(16 * h * Geo::VROW));
-                load_words<G>(v1, unit + vfrag + (uint32_t)((16 * h + 1) * Geo::VROW));
-                load_words<G>(v2, unit + vfrag + (uint32_t)((16 * h + 8) * Geo::VROW));
-                load_words<G>(v3, unit + vfrag + (uint32_t)((16 * h + 9) * Geo::VROW));
-                load_words<2 * SW>(s0, unit + (uint32_t)(Geo::VS + (16 * h + 2 * q4) * Geo::SC));
-                load_words<2 * SW>(s1, unit + (uint32_t)(Geo::VS + (16 * h + 8 + 2 * q4) * Geo::SC));
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const uint32_t w0 = __byte_perm(v0[g], v1[g], half), w1 = __byte_perm(v2[g], v3[g], half);
-                    const uint32_t sa = __byte_perm(s0[g / 2], s0[SW + g / 2], g & 1 ? 0x7632 : 0x5410);
-                    const uint32_t sb = __byte_perm(s1[g / 2], s1[SW + g / 2], g & 1 ? 0x7632 : 0x5410);
-                    const uint32_t na = fma_pair(sa, 0xc1c0c1c0u, 0x80008000u), nb = fma_pair(sb, 0xc1c0c1c0u, 0x80008000u);     // -24 s
-                    uint32_t a[4], b[4];
-                    a[0] = fma_pair(masked(w0 << 3, 0x00780078u, 0x41804180u), sa, na);
-                    a[1] = fma_pair(masked(w0 >> 1, 0x00780078u, 0x41804180u), sa, na);
-                    b[0] = fma_pair(masked(w0 >> 5, 0x00780078u, 0x41804180u), sa, na);
-                    b[1] = fma_pair(masked(w0 >> 9, 0x00780078u, 0x41804180u), sa, na);
-                    a[2] = fma_pair(masked(w1 << 3, 0x00780078u, 0x41804180u), sb, nb);
-                    a[3] = fma_pair(masked(w1 >> 1, 0x00780078u, 0x41804180u), sb, nb);
-                    b[2] = fma_pair(masked(w1 >> 5, 0x00780078u, 0x41804180u), sb, nb);
-                    b[3] = fma_pair(masked(w1 >> 9, 0x00780078u, 0x41804180u), sb, nb);
+            } else {
+                // the scales in the sums' units
+                const int e = 88 - base;
+                const uint32_t f0 = pack2(power_of_two(e / 2), power_of_two(e / 2)), f1 = pack2(power_of_two(e - e / 2), power_of_two(e - e / 2));
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    uint2 pf[NT], pr[NT];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        mma_next(o[2 * g][nt], a, pf[nt]);
-                        mma_next(o[2 * g + 1][nt], b, pf[nt]);
-                        mma_next(o[2 * g][nt], a, pr[nt]);
-                        mma_next(o[2 * g + 1][nt], b, pr[nt]);
+                        float p[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) p[c] = h == 0 ? x[0][nt][c] : x[1][nt][c];
+                        const uint32_t w0 = pack2(p[0], p[1]), w1 = pack2(p[2], p[3]);
+                        pf[nt] = make_uint2(transpose8(w0), transpose8(w1));
+                        pr[nt] = make_uint2(transpose8(pack2(p[0] - low_part(w0), p[1] - high_part(w0))), transpose8(pack2(p[2] - low_part(w1), p[3] - high_part(w1))));
+                    }
+                    const uint32_t at = unit + vfrag + (uint32_t)(16 * h * Geo::VROW), s_at = unit + (uint32_t)(Geo::VS + (16 * h + 2 * q4) * Geo::SC);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        uint32_t v0[1], v1[1], v2[1], v3[1], s0[1], s1[1], s2[1], s3[1];
+                        load_words<1>(v0, at + 4 * g);
+                        load_words<1>(v1, at + 4 * g + Geo::VROW);
+                        load_words<1>(v2, at + 4 * g + 8 * Geo::VROW);
+                        load_words<1>(v3, at + 4 * g + 9 * Geo::VROW);
+                        load_words<1>(s0, s_at + g / 2 * 4);
+                        load_words<1>(s1, s_at + g / 2 * 4 + Geo::SC);
+                        load_words<1>(s2, s_at + g / 2 * 4 + 8 * Geo::SC);
+                        load_words<1>(s3, s_at + g / 2 * 4 + 9 * Geo::SC);
+                        const uint32_t w0 = __byte_perm(v0[0], v1[0], half), w1 = __byte_perm(v2[0], v3[0], half), side = g & 1 ? 0x7632 : 0x5410;
+                        const uint32_t sa = fma_pair(fma_pair(__byte_perm(s0[0], s1[0], side), f0, 0x80008000u), f1, 0x80008000u);
+                        const uint32_t sb = fma_pair(fma_pair(__byte_perm(s2[0], s3[0], side), f0, 0x80008000u), f1, 0x80008000u);
+                        const uint32_t na = fma_pair(sa, 0xc1c0c1c0u, 0x80008000u), nb = fma_pair(sb, 0xc1c0c1c0u, 0x80008000u);     // -24 s
+                        const uint32_t sa16 = fma_pair(sa, 0x41804180u, 0x80008000u), sb16 = fma_pair(sb, 0x41804180u, 0x80008000u);
+                        const uint32_t na16 = fma_pair(na, 0x41804180u, 0x80008000u), nb16 = fma_pair(nb, 0x41804180u, 0x80008000u);
+                        uint32_t a[4], b[4];
+                        a[0] = fma_pair(masked(w0 << 3, 0x00780078u, 0x41804180u), sa, na);
+                        a[1] = fma_pair(masked(w0 >> 1, 0x00780078u, 0x41804180u), sa16, na16);
+                        b[0] = fma_pair(masked(w0 >> 5, 0x00780078u, 0x41804180u), sa, na);
+                        b[1] = fma_pair(masked(w0 >> 9, 0x00780078u, 0x41804180u), sa16, na16);
+                        a[2] = fma_pair(masked(w1 << 3, 0x00780078u, 0x41804180u), sb, nb);
+                        a[3] = fma_pair(masked(w1 >> 1, 0x00780078u, 0x41804180u), sb16, nb16);
+                        b[2] = fma_pair(masked(w1 >> 5, 0x00780078u, 0x41804180u), sb, nb);
+                        b[3] = fma_pair(masked(w1 >> 9, 0x00780078u, 0x41804180u), sb16, nb16);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma_next(o[2 * g][nt], a, pf[nt]);
+                            mma_next(o[2 * g + 1][nt], b, pf[nt]);
+                            mma_next(o[2 * g][nt], a, pr[nt]);
+                            mma_next(o[2 * g + 1][nt], b, pr[nt]);
+                        }
                     }
                 }
             }
             buf = buf + 1 == BUFS ? 0 : buf + 1;
+        }
+        // ---- the sums as numbers, relative to the largest logit
+        {
+            const int e = base - 88 - (int)kRaise;
+            const float f0 = power_of_two(e / 2), f1 = power_of_two(e - e / 2);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    l[nt][r] *= exp2_fast(-kRaise);
+                    m[nt][r] = m[nt][r] == -INFINITY ? -INFINITY : m[nt][r] * to_logit[nt][r];
+#pragma unroll
+                    for (int i = 0; i < 2 * G; ++i) {
+                        const float add = __shfl_sync(0xffffffffu, shift[nt][r], i / 2 * 4 + q4);
+                        o[i][nt][r] = (o[i][nt][r] + add) * f0 * f1;
+                        o[i][nt][2 + r] = fmaf(o[i][nt][2 + r], 0.0625f, add) * f0 * f1;
+                    }
+                }
         }
         // ---- sums over the keys that the lanes of a row had
 #pragma unroll
@@ -554,52 +738,44 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
     if (pass + 1 == P.passes) chain_next();
     __syncthreads();
 
-    // ---- the CTA's pieces of a pair follow one another: what goes on behind a run, and what began before the next ones, up to its end.  A chain of them may
-    // also begin before the CTA's first run, or go on behind its last.  The warps of a pair of the HB share out its chains, or the columns of one.
+    // ---- the CTA's pieces of a pair follow one another, a chain: what goes on behind a run, and what began before the next ones, up to its end.  A chain may
+    // also begin before the CTA's first run, or go on behind its last.  The threads of a pair of the HB share out its rows and columns.
     {
         const Piece<8 * NT>* const pieces = piece_s[hb];
-        int first = 0;                                  // (if it does not begin its pair, an earlier CTA does)
-        while (first < 2 * KW && !pieces[first].there) ++first;
-        const auto heads_chain = [&](int i) { return pieces[i].there && (pieces[i].begins || i == first); };
-        const auto goes_on = [&](int i) { return pieces[i].there && !pieces[i].begins; };
-        int chains = 0;
-        for (int i = 0; i < 2 * KW; ++i) chains += heads_chain(i) ? 1 : 0;
-        const int slices = chains == 0 ? 1 : max(1, KW / chains), slice = kw % slices;
+        static_assert(2 * KW <= 32, "a lane for each piece");
+        const bool there = lane < 2 * KW && pieces[lane].there;
+        const uint32_t all = __ballot_sync(0xffffffffu, there), ends = __ballot_sync(0xffffffffu, there && pieces[lane].ends);
+        // (if the first one does not begin its pair, an earlier CTA does)
+        uint32_t heads = __ballot_sync(0xffffffffu, there && pieces[lane].begins) | (all & (0u - all));
         const long long run = (long long)pass * P.runs + blockIdx.x;
-        for (int c = kw / slices; c < chains; c += KW / slices) {
-            int head = 0;
-            for (int before = 0;; ++head)
-                if (heads_chain(head) && before++ == c) break;
-            int last = head;                            // the last piece of the chain
-            for (int i = head + 1; i < 2 * KW && !pieces[last].ends; ++i)
-                if (goes_on(i)) last = i;
+        for (; heads; heads &= heads - 1) {
+            const int head = __ffs(heads) - 1, next = (heads & (heads - 1)) ? __ffs(heads & (heads - 1)) - 1 : 2 * KW;
+            const uint32_t chain = all & (next == 32 ? ~0u : (1u << next) - 1u) & (~0u << head);
             const Piece<8 * NT>& f = pieces[head];
             const int t = n0 + f.e, j = f.h / A.row_tiles, row0 = f.h % A.row_tiles * 16, rows = min(8 * NT, A.group - row0);
-            const bool begins = f.begins, ends = pieces[last].ends, whole = begins && ends;
+            const bool begins = f.begins, whole = begins && (ends & chain) != 0;
             float* const slot = P.slots + part_slot(run, begins, HB, hb) * 16 * (DH + 2);
-            if (begins && !ends && hb == 0 && slice == 0 && lane == 0) {
-                // the run that holds the pair's last unit
-                const long long u = base_s[f.e] + (long long)(f.h / HB + 1) * f.units - 1, share = base_s[n] / n_runs, extra = base_s[n] - share * n_runs;
-                const long long cut = extra * (share + 1), end = u < cut ? u / (share + 1) : extra + (u - cut) / share;
-                P.run_head[run] = make_int2(t * A.n_head * A.row_tiles + f.h, parts_word((int)end - (int)blockIdx.x + 1, 1));
-            }
-            for (int idx = lane + 32 * slice; idx < rows * (DH / 4); idx += 32 * slices) {
+            if (begins && !whole && hb == 0 && kw == 0 && lane == 0)
+                P.run_head[run] = make_int2(t * A.n_head * A.row_tiles + f.h,
+                                            parts_word(run_of(base_s[n], n_runs, base_s[f.e] + (long long)(f.h / HB + 1) * f.units - 1) - (int)blockIdx.x + 1, 1));
+            for (int idx = kw * 32 + lane; idx < rows * (DH / 4); idx += KW * 32) {
                 const int row = idx / (DH / 4), col = idx % (DH / 4) * 4, member = row0 + row;
                 float M = -INFINITY;
-                for (int i = head; i <= last; ++i)
-                    if (i == head || goes_on(i)) M = fmaxf(M, pieces[i].m[row]);
+#pragma unroll 4
+                for (int i = head; i < next; ++i) M = fmaxf(M, chain >> i & 1u ? pieces[i].m[row] : -INFINITY);
                 const float z = M == -INFINITY ? 0.f : M;
                 float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
                 float den = 0.f;
-                for (int i = head; i <= last; ++i) {
-                    if (i != head && !goes_on(i)) continue;
-                    const float wgt = exp2_fast(pieces[i].m[row] - z);    // 0 for a piece that saw no key
-                    const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(aq_smem + pieces[i].sums) + row * LDO + col);
-                    sum.x = fmaf(wgt, v.x, sum.x);
-                    sum.y = fmaf(wgt, v.y, sum.y);
-                    sum.z = fmaf(wgt, v.z, sum.z);
-                    sum.w = fmaf(wgt, v.w, sum.w);
-                    den = fmaf(wgt, pieces[i].l[row], den);
+#pragma unroll 4
+                for (int i = head; i < next; ++i) {
+                    if (!(chain >> i & 1u)) continue;
+                    const float w = exp2_fast(pieces[i].m[row] - z);      // 0 for a piece that saw no key
+                    const float4 v = *reinterpret_cast<const float4*>(aq_smem + pieces[i].sums + row * LDO * 4 + col * 4);
+                    sum.x = fmaf(w, v.x, sum.x);
+                    sum.y = fmaf(w, v.y, sum.y);
+                    sum.z = fmaf(w, v.z, sum.z);
+                    sum.w = fmaf(w, v.w, sum.w);
+                    den = fmaf(w, pieces[i].l[row], den);
                 }
                 if (whole) {
                     const float inv = den == 0.f ? 0.f : 1.f / den;

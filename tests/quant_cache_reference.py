@@ -81,10 +81,15 @@ def quant_logit_error(q, scale, K_scale, spread, d):
     return abs(scale) * (group @ K_scale.T).max(1, initial=0.0) + logit_error(spread, d)
 
 
-def quant_out_tolerance(out, absolute, error, prompt):
-    """Weights are off by exp(+-2 error) and 2^-20, as two bf16 numbers by 2^-16, or (prompts) as one by 2^-8; the output is rounded to bf16."""
+def quant_out_tolerance(out, absolute, error, prompt, n, V_scale):
+    """`absolute`: the weighted sum of |V|; n keys; V_scale: the largest of their values' scales.  Weights are off by exp(+-2 error) and 2^-20.  Prompts: rounded to
+    bf16, 2^-8.  Otherwise: rounded to fp16 before and behind the product with a scale, 2^-11 each; products of less than 2^-14 by 2^-25, in units in which the
+    largest weight is 2^6 and the largest scale 1 / 2 or more, and their codes' magnitudes are 7 at most: n 2^-31 14 V_scale.  The sums hold 8 + c instead of c, up
+    to 15 / 7 of what 7 scales are, and so do those that are taken away: at most 2^8 additions each that cut 2^-23.  The output is rounded to bf16."""
     e = np.expm1(2 * error)[..., None] + 2.0 ** -20
-    return BF16_HALF_STEP * (np.abs(out) + (absolute if prompt else 0.0)) * 1.01 + absolute * (e + 2.0 ** -15) + 1e-30
+    if prompt:
+        return BF16_HALF_STEP * (np.abs(out) + absolute) * 1.01 + absolute * (e + 2.0 ** -16) + 1e-30
+    return BF16_HALF_STEP * np.abs(out) * 1.01 + absolute * (e + 2.0 ** -10 * 1.01) + V_scale * (n * 2.0 ** -31 * 14 + 2 * 2.0 ** 8 * 2.0 ** -23 * 15) + 1e-30
 
 
 class QuantCase:
@@ -137,7 +142,8 @@ class QuantCase:
                 o, x, _, absolute, spread = attention(q, K[s, j], V[s, j], self.scale, at)
                 error = quant_logit_error(q, self.scale, self.scales_np[0][s, j][at], spread, d)
                 out[t, j], lse[t, j] = o, x
-                out_tol[t, j], lse_tol[t, j] = quant_out_tolerance(o, absolute, error, prompt), error + lse_tolerance(x, spread, d)
+                largest = self.scales_np[1][s, j][at].max(initial=0.0)
+                out_tol[t, j], lse_tol[t, j] = quant_out_tolerance(o, absolute, error, prompt, len(at), largest), error + lse_tolerance(x, spread, d)
         return out, lse, out_tol, lse_tol
 
     def check(self, want):
