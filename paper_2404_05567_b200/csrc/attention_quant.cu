@@ -13,8 +13,8 @@
 //      as much and others beside: 62 tokens with up to 8192 keys 77.9 us instead of 70.6 with bf16 operands.)
 //   V: operands of masks alone too.  The scales multiply the weights instead, as fp16 numbers, a weight and group at a time (rounded to 11 bits), and the sum
 //      of a group's weights, from one more instruction, is taken away eight times.  The scales are relative to a power of two near the largest that the
-//      warp has met, which moves as the maximum of the logits does.  Units with scales 2^8 below it (or that are no numbers) go another way: 4 bits beside the
-//      exponent of 16 are 16 + 8 + c; times the scale, minus 24 times the scale, is s * c, exactly, in one packed operation; and weights are two bf16 numbers each.
+//      warp has met, which moves as the maximum of the logits does.  Units with scales 2^8 below it (or that are no numbers) go another way: values
+//      are bf16 numbers s * c and weights two bf16 numbers each.
 // The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
 #include <cuda_fp16.h>
 
@@ -636,18 +636,12 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                         const uint32_t w0 = __byte_perm(v0[0], v1[0], half), w1 = __byte_perm(v2[0], v3[0], half), side = g & 1 ? 0x7632 : 0x5410;
                         const uint32_t sa = fma_pair(fma_pair(__byte_perm(s0[0], s1[0], side), f0, 0x80008000u), f1, 0x80008000u);
                         const uint32_t sb = fma_pair(fma_pair(__byte_perm(s2[0], s3[0], side), f0, 0x80008000u), f1, 0x80008000u);
-                        const uint32_t na = fma_pair(sa, 0xc1c0c1c0u, 0x80008000u), nb = fma_pair(sb, 0xc1c0c1c0u, 0x80008000u);     // -24 s
                         const uint32_t sa16 = fma_pair(sa, 0x41804180u, 0x80008000u), sb16 = fma_pair(sb, 0x41804180u, 0x80008000u);
-                        const uint32_t na16 = fma_pair(na, 0x41804180u, 0x80008000u), nb16 = fma_pair(nb, 0x41804180u, 0x80008000u);
-                        uint32_t a[4], b[4];
-                        a[0] = fma_pair(masked(w0 << 3, 0x00780078u, 0x41804180u), sa, na);
-                        a[1] = fma_pair(masked(w0 >> 1, 0x00780078u, 0x41804180u), sa16, na16);
-                        b[0] = fma_pair(masked(w0 >> 5, 0x00780078u, 0x41804180u), sa, na);
-                        b[1] = fma_pair(masked(w0 >> 9, 0x00780078u, 0x41804180u), sa16, na16);
-                        a[2] = fma_pair(masked(w1 << 3, 0x00780078u, 0x41804180u), sb, nb);
-                        a[3] = fma_pair(masked(w1 >> 1, 0x00780078u, 0x41804180u), sb16, nb16);
-                        b[2] = fma_pair(masked(w1 >> 5, 0x00780078u, 0x41804180u), sb, nb);
-                        b[3] = fma_pair(masked(w1 >> 9, 0x00780078u, 0x41804180u), sb16, nb16);
+                        const auto value = [](uint32_t x, uint32_t s) {            // 4 bits beside the exponent of 16 are 24 + c
+                            return fma_pair(fma_pair(masked(x, 0x00780078u, 0x41804180u), 0x3f803f80u, 0xc1c0c1c0u), s, 0x80008000u);
+                        };
+                        const uint32_t a[4] = {value(w0 << 3, sa), value(w0 >> 1, sa16), value(w1 << 3, sb), value(w1 >> 1, sb16)};
+                        const uint32_t b[4] = {value(w0 >> 5, sa), value(w0 >> 9, sa16), value(w1 >> 5, sb), value(w1 >> 9, sb16)};
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             mma_next(o[2 * g][nt], a, pf[nt]);

@@ -8,83 +8,125 @@ namespace {
 
 constexpr int kThreads = 256, kReadRows = 4;      // kReadRows: rows a thread of the reading kernel has under way
 
-// (a scale that is no number makes all of the group's values none)
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+// a * b + c, two bf16 numbers at a time
+__device__ __forceinline__ uint32_t fma_pair(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 
-// Eight values of a word
-__device__ __forceinline__ uint4 values_of(uint32_t word, float scale) {
-    uint32_t r[4];
+// Eight values of a word.  4 bits beside the exponent of 16 are 16 + 8 + c, for values i and i + 4 at a time; less 24 they are c, and the product with the scale is
+// exact (it is rounded to bf16 where somebody else has left a scale of more than four significant bits).
+__device__ __forceinline__ uint4 values_of(uint32_t word, uint32_t scale) {
+    const uint32_t s = scale | scale << 16;
+    uint32_t v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float lo = (float)((int)(word >> (8 * i) & 15u) - 8), hi = (float)((int)(word >> (8 * i + 4) & 15u) - 8);
-        r[i] = bf16_pair(lo * scale, hi * scale);                     // (exact)
+        const uint32_t x = ((i == 0 ? word << 3 : word >> (4 * i - 3)) & 0x00780078u) | 0x41804180u;
+        v[i] = fma_pair(fma_pair(x, 0x3f803f80u, 0xc1c0c1c0u), s, 0x80008000u);
     }
-    return make_uint4(r[0], r[1], r[2], r[3]);
+    return make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
 }
 
-// The word of eight values whose group's other values the three neighbouring lanes have; all lanes of the warp call it
-__device__ __forceinline__ uint32_t quantise(const uint4 in, float* scale_out) {
+// A word of eight values, their scale and, with BACK, what it stands for; the three neighbouring lanes have the group's other values, and all lanes of the
+// warp call it
+struct Quantised {
+    uint32_t word;
+    uint16_t scale;
+    uint4 back;
+};
+template <bool BACK>
+__device__ __forceinline__ Quantised quantise(const uint4 in) {
     const uint32_t w[4] = {in.x, in.y, in.z, in.w};
-    uint32_t top = 0;                                                 // magnitudes in order, as integers: what is no finite number is above all
+    // magnitudes in order, as integers: what is no finite number is above all
+    uint32_t top = max_pair(max_pair(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max_pair(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+    top = max_pair(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max_pair(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    top = max(top & 0xffffu, top >> 16);
+    float x[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    // Up to four significant bits (or a multiple of 2^-129), 2^122 at most (24 s is a number then).  The quotient is rounded to 24 bits first, which
-    // moves it over no border: between a bf16 number / 7 and a border lie 2^-10 of it or more, or nothing.
-    const uint32_t raw = (__float_as_uint(__fdiv_rn(__uint_as_float(top << 16), 7.f)) + 0xfffffu) & ~0xfffffu;
-    const float s = top >= 0x7f80u ? __uint_as_float(0x7fff0000u) : fminf(__uint_as_float(raw), 0x1p122f);
-    *scale_out = s;
-    if (top == 0u || top >= 0x7f80u) return 0x88888888u;
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    // A seventh of the largest, up to four significant bits (or a multiple of 2^-129).  The product is a little small, by 2^-23 of it at most, so that what is
+    // a border does not pass it; between a bf16 number / 7 that is none and a border lie 2^-10 of it.
+    float s = __uint_as_float((__float_as_uint(__uint_as_float(top << 16) * 0x1.249248p-3f) + 0xfffffu) & ~0xfffffu), times = s;
+    // Groups of the smallest numbers (whose scale has no reciprocal), of the largest (beyond 7 2^122), of zeros, and with what is no number
+    if (s < 0x1p-64f || top > 0x7de0u) {
+        const bool number = top < 0x7f80u;
+        s = number ? fminf(s, 0x1p122f) : 0.f;
+        const float up = s < 0x1p-64f ? 0x1p64f : 1.f, most = 7.f * s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = s > 0.f ? fminf(fmaxf(x[i], -most), most) * up : 0.f;
+        times = s > 0.f ? s * up : 1.f;
+        if (!number) s = __uint_as_float(0x7fff0000u);
+    }
     // x / s as x * (1 / s): a little off, but halves have to be halves.  With eight and four bits x / s is a half or further than 2^-11 from one, so it
-    // is rounded to a multiple of 2^-13 first.  (For scales whose reciprocal may overflow both are multiplied by 2^64.)
-    const float up = s < 0x1p-64f ? 0x1p64f : 1.f, inv = __frcp_rn(s * up);
+    // is rounded to a multiple of 2^-13 first (beside 1.5 2^10), then to an integer (beside 1.5 2^23, whose lowest bits it then is).
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(times));
+    float n[8];
     uint32_t word = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float x = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-        const float fine = __fsub_rn(__fadd_rn(__fmul_rn(x * up, inv), 0x1.8p10f), 0x1.8p10f);
-        const int c = min(max(__float2int_rn(fine), -7), 7);         // (rounds what is too large to the largest integer)
-        word |= (uint32_t)(c + 8) << (4 * i);
+    for (int i = 7; i >= 0; --i) {
+        n[i] = __fadd_rn(__fsub_rn(__fmaf_rn(x[i], inv, 0x1.8p10f), 0x1.8p10f), 0x1.8p23f);
+        word = word * 16u + __float_as_uint(n[i]);
     }
-    return word;
+    Quantised q;
+    q.word = word - 0x4b400000u * 0x11111111u + 0x88888888u;          // (modulo 2^32; c + 8)
+    q.scale = (uint16_t)(__float_as_uint(s) >> 16);
+    if (BACK) {
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = bf16_pair(__fsub_rn(n[2 * i], 0x1.8p23f) * s, __fsub_rn(n[2 * i + 1], 0x1.8p23f) * s);       // (exact)
+        q.back = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    return q;
 }
 
+template <bool BACK>
 __global__ void __launch_bounds__(kThreads) quant_write_kernel(const __grid_constant__ QuantView C, const __grid_constant__ QuantWrite W) {
     chain_wait();
     chain_next();
     const int words = C.d_head / 8, G = C.d_head / kQuantGroup, at_once = kThreads / words;
     // (a group's four lanes are neighbours in a warp: words is a multiple of 4)
     const int x = (int)threadIdx.x % words, r = (int)threadIdx.x / words, g = x / 4, t = x % 4;
-    const long long row = (long long)blockIdx.x * at_once + r;
-    const bool real = r < at_once && row < (long long)W.T * C.n_head;
-    const int token = real ? (int)(row / C.n_head) : 0, head = real ? (int)(row % C.n_head) : 0;
+    const uint32_t row = blockIdx.x * (uint32_t)at_once + r;          // (T * n_head is below 2^30)
+    const bool real = r < at_once && row < (uint32_t)W.T * C.n_head;
+    const int token = real ? (int)(row / (uint32_t)C.n_head) : 0, head = real ? (int)(row - (uint32_t)token * C.n_head) : 0;
     const int p = W.pos[token], seq = W.tok_seq ? W.tok_seq[token] : 0;
     const uint4 k = *reinterpret_cast<const uint4*>(W.k + token * W.i_t + head * W.i_h + 8 * x);
     const uint4 v = *reinterpret_cast<const uint4*>(W.v + token * W.i_t + head * W.i_h + 8 * x);
     // a token that a later one of the call takes the slot of
     const bool has_later = W.ring > 0 && token + (long long)W.ring < W.T;
     const int p_later = has_later ? W.pos[token + W.ring] : -1, seq_later = has_later && W.tok_seq ? W.tok_seq[token + W.ring] : 0;
-    float ks, vs;
-    const uint32_t kw = quantise(k, &ks), vw = quantise(v, &vs);
+    const Quantised kq = quantise<BACK>(k), vq = quantise<BACK>(v);
     if (!real || p == -1) return;
     if (seq < 0 || seq >= C.n_seq || p < 0 || (W.ring ? p == 0x7fffffff : p >= C.L)) {
         if (x == 0 && head == 0) report_status(W.dev_status, DSMOE_ERR_INVALID_ARG);
         return;
     }
-    if (W.k_back) *reinterpret_cast<uint4*>(W.k_back + token * W.b_t + head * W.b_h + 8 * x) = values_of(kw, ks);
-    if (W.v_back) *reinterpret_cast<uint4*>(W.v_back + token * W.b_t + head * W.b_h + 8 * x) = values_of(vw, vs);
+    if (BACK) {
+        const long long to = token * W.b_t + head * W.b_h + 8 * x;
+        if (W.k_back) *reinterpret_cast<uint4*>(W.k_back + to) = kq.back;
+        if (W.v_back) *reinterpret_cast<uint4*>(W.v_back + to) = vq.back;
+    }
     if (has_later && p >= W.sinks && seq_later == seq && p_later == (long long)p + W.ring) return;
     const int slot = !W.ring || p < W.sinks ? p : W.sinks + (p - W.sinks) % W.ring;
-    const long long at = seq * C.c_s + head * C.c_h + slot * C.c_p + (t * G + g) * 4, s_at = seq * C.s_s + head * C.s_h + slot * C.s_p + g;
-    *reinterpret_cast<uint32_t*>(C.K + at) = kw;
-    *reinterpret_cast<uint32_t*>(C.V + at) = vw;
+    const long long at = seq * C.c_s + head * C.c_h + slot * C.c_p + (t * G + g) * 4;
+    *reinterpret_cast<uint32_t*>(C.K + at) = kq.word;
+    *reinterpret_cast<uint32_t*>(C.V + at) = vq.word;
     if (t == 0) {
-        C.K_scale[s_at] = __float2bfloat16_rn(ks);                    // (exact)
-        C.V_scale[s_at] = __float2bfloat16_rn(vs);
+        const long long s_at = seq * C.s_s + head * C.s_h + slot * C.s_p + g;
+        reinterpret_cast<uint16_t*>(C.K_scale)[s_at] = kq.scale;
+        reinterpret_cast<uint16_t*>(C.V_scale)[s_at] = vq.scale;
     }
 }
 
@@ -94,31 +136,33 @@ __global__ void __launch_bounds__(kThreads) quant_read_kernel(const __grid_const
     chain_next();
     const int words = C.d_head / 8, G = C.d_head / kQuantGroup, at_once = kThreads / words;
     const int x = (int)threadIdx.x % words, r = (int)threadIdx.x / words, g = x / 4, t = x % 4;
-    const unsigned inner = by_slot ? C.n_head : R.rows;
+    const uint32_t inner = by_slot ? C.n_head : R.rows;
     const long long rows = (long long)R.rows * C.n_head, tile = at_once * kReadRows, per_seq = (rows + tile - 1) / tile, all = per_seq * C.n_seq;
     if (r >= at_once) return;
+    const int word_at = (t * G + g) * 4;
     for (long long b = blockIdx.x; b < all; b += gridDim.x) {
         const int seq = (int)(b / per_seq);
-        const long long base = b % per_seq * tile;
+        const long long base = (b - seq * per_seq) * tile;
         const int outer0 = (int)(base / inner);
-        const unsigned inner0 = (unsigned)(base % inner) + r;         // (below 2^31)
+        const uint32_t inner0 = (uint32_t)(base - (long long)outer0 * inner) + r;                // (below 2^31)
         const int len = R.len ? R.len[seq] : INT_MAX;
         const int4 range = R.range ? R.range[seq] : make_int4(INT_MAX, 0, 0, 0);
-        uint32_t kw[kReadRows], vw[kReadRows];
-        float ks[kReadRows], vs[kReadRows];
+        const unsigned char *const K = C.K + seq * C.c_s + word_at, *const V = C.V + seq * C.c_s + word_at;
+        const uint16_t* const Ks = reinterpret_cast<const uint16_t*>(C.K_scale) + seq * C.s_s + g;
+        const uint16_t* const Vs = reinterpret_cast<const uint16_t*>(C.V_scale) + seq * C.s_s + g;
+        uint32_t kw[kReadRows], vw[kReadRows], ks[kReadRows], vs[kReadRows];
         long long to[kReadRows];
 #pragma unroll
         for (int u = 0; u < kReadRows; ++u) {
-            const unsigned in = inner0 + u * at_once, over = in / inner;
-            const int outer = outer0 + (int)over, rest = (int)(in - over * inner), head = by_slot ? rest : outer, n = by_slot ? outer : rest;
-            const long long slot = (long long)R.first + n;
+            const uint32_t in = inner0 + u * at_once, over = in / inner, rest = in - over * inner;
+            const int outer = outer0 + (int)over, head = by_slot ? (int)rest : outer, n = by_slot ? outer : (int)rest, slot = R.first + n;
             to[u] = -1;
             if (base + r + u * at_once >= rows || slot >= len || (slot >= range.x && (slot < range.y || slot >= range.z))) continue;
-            const long long at = seq * C.c_s + head * C.c_h + slot * C.c_p + (t * G + g) * 4, s_at = seq * C.s_s + head * C.s_h + slot * C.s_p + g;
-            kw[u] = *reinterpret_cast<const uint32_t*>(C.K + at);
-            vw[u] = *reinterpret_cast<const uint32_t*>(C.V + at);
-            ks[u] = __bfloat162float(C.K_scale[s_at]);
-            vs[u] = __bfloat162float(C.V_scale[s_at]);
+            const long long at = head * C.c_h + slot * C.c_p, s_at = head * C.s_h + slot * C.s_p;
+            kw[u] = *reinterpret_cast<const uint32_t*>(K + at);
+            vw[u] = *reinterpret_cast<const uint32_t*>(V + at);
+            ks[u] = Ks[s_at];
+            vs[u] = Vs[s_at];
             to[u] = seq * R.o_s + head * R.o_h + n * R.o_p + 8 * x;
         }
 #pragma unroll
@@ -169,7 +213,7 @@ __global__ void __launch_bounds__(512) quant_range_kernel(const __grid_constant_
 dsmoe_status launch_quant_write(const QuantView& C, const QuantWrite& W, cudaStream_t s) {
     const long long at_once = kThreads / (C.d_head / 8), blocks = ((long long)W.T * C.n_head + at_once - 1) / at_once;
     if (blocks > 0x7fffffffll) return DSMOE_ERR_UNSUPPORTED;
-    DSMOE_CUDA_TRY(launch_chained(quant_write_kernel, (unsigned)blocks, kThreads, 0, s, C, W));
+    DSMOE_CUDA_TRY(launch_chained(W.k_back || W.v_back ? quant_write_kernel<true> : quant_write_kernel<false>, (unsigned)blocks, kThreads, 0, s, C, W));
     return DSMOE_OK;
 }
 
