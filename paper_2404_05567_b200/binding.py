@@ -480,7 +480,7 @@ def make_quant_cache(K, V, K_scale, V_scale) -> QuantCache:
     cache = QuantCache(n_seq, n_head, L, 2 * row, K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr())
     cache.code_stride[:], cache.scale_stride[:] = K.stride()[:3], K_scale.stride()[:3]
     cache.tensors, cache.device = (K, V, K_scale, V_scale), device
-    cache.write = None, None             # the last write's shapes, and the arguments they make
+    cache.write = cache.read = None, None        # the last write's and read's shapes, and the arguments they make
     return cache
 
 
@@ -496,46 +496,67 @@ def make_quant_attention_desc(q, cache: QuantCache, scale=1.0, out=None) -> Atte
     return desc
 
 
-def _write_args(cache, shape, stride, sinks, rolling, back):
+def _write_args(cache, shape, stride, back, sinks, rolling):
     T = shape[0]
-    if shape != (T, cache.n_head, cache.d_head) or stride[2] != 1 or not (back is None or back[2] == 1):
+    if shape != (T, cache.n_head, cache.d_head) or stride[2] != 1 or back[2] != 1:
         raise ValueError("k, v, k_back and v_back are [T, n_head, d_head] with the cache's heads, d_head contiguous")
-    args = QuantWriteArgs(T, int(sinks), int(rolling))
-    args.in_stride[:] = stride[:2]
-    args.back_stride[:] = stride[:2] if back is None else back[:2]
+    args = QuantWriteArgs(int(T), int(sinks), int(rolling))
+    args.in_stride[:], args.back_stride[:] = stride[:2], back[:2]
     return args
+
+
+def _bf16_pair(a, b, shape, stride, device):
+    """Addresses of two bf16 tensors of this shape and layout on this device."""
+    if not (a.dtype is torch.bfloat16 and b.dtype is torch.bfloat16 and a.shape == shape and b.shape == shape and a.stride() == stride
+            and b.stride() == stride and a.get_device() == device and b.get_device() == device):
+        raise ValueError("expected bf16 tensors of one shape and layout on the cache's device")
+    return a.data_ptr(), b.data_ptr()
 
 
 def dsmoe_quant_cache_write(cache, k, v, tok_seq, pos, sinks=0, rolling=False, k_back=None, v_back=None, dev_status=None, stream=None):
     """Writes tokens' keys and values [T, n_head, d_head] bf16 into a cache in 4 bits; k_back, v_back: the rows as the cache holds them, or ``None``."""
+    # (small calls are as long as the host takes: shapes and layouts like the last call's are not laid out for the library again)
     device, shape, stride = cache.device, k.shape, k.stride()
-    first = v_back if k_back is None else k_back
-    sizes = shape, stride, sinks, rolling, None if first is None else first.stride()
+    back, k_to, v_to = stride, None, None
+    if k_back is not None:
+        back = k_back.stride()
+        k_to, v_to = _bf16_pair(k_back, k_back if v_back is None else v_back, shape, back, device)
+        if v_back is None:
+            v_to = None
+    elif v_back is not None:
+        back = v_back.stride()
+        v_to = _bf16_pair(v_back, v_back, shape, back, device)[0]
+    sizes = shape, stride, back, sinks, rolling
     last, args = cache.write
     if last != sizes:
         args = _write_args(cache, *sizes)
         cache.write = sizes, args
-    for t, layout in ((k, stride), (v, stride), (k_back, sizes[4]), (v_back, sizes[4])):
-        if t is not None and not (t.dtype is torch.bfloat16 and t.shape == shape and t.stride() == layout and t.get_device() == device):
-            raise ValueError("k and v, and k_back and v_back, are bf16 tensors of one shape and layout on the cache's device")
-    _check(lib().dsmoe_quant_cache_write(ctypes.byref(cache), ctypes.byref(args), k.data_ptr(), v.data_ptr(), _entries(tok_seq, torch.int32, shape[0], device),
-                                         _entries(pos, torch.int32, shape[0], device), None if k_back is None else k_back.data_ptr(),
-                                         None if v_back is None else v_back.data_ptr(), _entries(dev_status, torch.int32, 1, device),
+    T = shape[0]
+    _check(lib().dsmoe_quant_cache_write(ctypes.byref(cache), ctypes.byref(args), *_bf16_pair(k, v, shape, stride, device), _entries(tok_seq, torch.int32, T, device),
+                                         _entries(pos, torch.int32, T, device), k_to, v_to, _entries(dev_status, torch.int32, 1, device),
                                          _stream_of(device, stream)),
            "dsmoe_quant_cache_write")
+
+
+def _read_args(cache, shape, stride, first):
+    if len(shape) != 4 or shape != (cache.n_seq, cache.n_head, shape[2], cache.d_head) or stride[3] != 1:
+        raise ValueError("K_out and V_out are bf16 tensors [n_seq, n_head, rows, d_head] of one layout, d_head contiguous")
+    args = QuantReadArgs(int(first), shape[2])
+    args.out_stride[:] = stride[:3]
+    return args
 
 
 def dsmoe_quant_cache_read(cache, length, K_out, V_out, first=0, stream=None):
     """Reads slots ``first`` and the next ones back into K_out, V_out [n_seq, n_head, rows, d_head] bf16, of sequence s those below length[s] alone
     (``None``: all)."""
     shape, out_stride, device = K_out.shape, K_out.stride(), cache.device
-    if not (K_out.dtype == V_out.dtype == torch.bfloat16 and len(shape) == 4 and shape == V_out.shape == (cache.n_seq, cache.n_head, shape[2], cache.d_head)
-            and V_out.stride() == out_stride and out_stride[3] == 1 and K_out.get_device() == V_out.get_device() == device):
-        raise ValueError("K_out and V_out are bf16 tensors [n_seq, n_head, rows, d_head] of one layout, d_head contiguous, on the cache's device")
-    args = QuantReadArgs(int(first), shape[2])
-    args.out_stride[:] = out_stride[:3]
-    _check(lib().dsmoe_quant_cache_read(ctypes.byref(cache), ctypes.byref(args), _entries(length, torch.int32, cache.n_seq, device), K_out.data_ptr(),
-                                        V_out.data_ptr(), _stream_of(device, stream)),
+    sizes = shape, out_stride, first
+    last, args = cache.read
+    if last != sizes:
+        args = _read_args(cache, *sizes)
+        cache.read = sizes, args
+    _check(lib().dsmoe_quant_cache_read(ctypes.byref(cache), ctypes.byref(args), _entries(length, torch.int32, cache.n_seq, device),
+                                        *_bf16_pair(K_out, V_out, shape, out_stride, device), _stream_of(device, stream)),
            "dsmoe_quant_cache_read")
 
 
