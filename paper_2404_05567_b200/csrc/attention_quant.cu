@@ -11,8 +11,8 @@
 //      second kind of place) and so are fp16 numbers exactly, down to 2^-28 of the largest.  A group's sum begins with -8 times the sum of the row's queries
 //      there, and its scale multiplies it into the logit.  (With e4m3 operands, for which whole words of codes would do, the tensor instructions cost twice
 //      as much and others beside: 62 tokens with up to 8192 keys 77.9 us instead of 70.6 with bf16 operands.)
-//   V: operands of masks alone too.  The scales multiply the weights instead, as fp16 numbers, a weight and group at a time (rounded to 11 bits), and the sum
-//      of a group's weights, from one more instruction, is taken away eight times.  The scales are relative to a power of two near the largest that the
+//   V: operands of masks too, less 8 2^-24, or 16 times that.  The scales multiply the weights instead, as fp16 numbers, a weight and group at a time (rounded to
+//      11 bits).  The scales are relative to a power of two near the largest that the
 //      warp has met, which moves as the maximum of the logits does.  Units with scales 2^8 below it (or that are no numbers) go another way: values
 //      are bf16 numbers s * c and weights two bf16 numbers each.
 // The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
@@ -83,6 +83,11 @@ __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t mul_half_pair(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t add_half_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -403,8 +408,8 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
         // Rows 2 q4 and 2 q4 + 1 of each tile.  The largest sum m so far, as it was when it last moved, and the sum beyond which it moves; weights are
         // 2^(to_logit x - z), 2^kRaise times those relative to the largest logit, so that small ones are fp16 numbers.
         float m[NT][2], limit[NT][2], z[NT][2], l[NT][2];
-        // Sums of values in units of 2^(base - 88), each second one 16 times as large; and what is to be added to group g8's
-        float o[2 * G][NT][4], shift[NT][4];
+        // Sums of values in units of 2^(base - 88), each second one 16 times as large
+        float o[2 * G][NT][4];
         int base = 0;                                   // the exponent (of a bf16) whose scales' exponent as an fp16 is 0
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -412,7 +417,6 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             z[nt][0] = z[nt][1] = l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
             for (int i = 0; i < 2 * G; ++i) o[i][nt][0] = o[i][nt][1] = o[i][nt][2] = o[i][nt][3] = 0.f;
-            shift[nt][0] = shift[nt][1] = shift[nt][2] = shift[nt][3] = 0.f;
         }
         for (int k = first_k; k < end_k; ++k) {
             __syncwarp();                               // every lane is past its reads of the buffer that is filled again now
@@ -454,11 +458,9 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
+                        for (int c = 0; c < 4; ++c)
 #pragma unroll
                             for (int i = 0; i < 2 * G; ++i) o[i][nt][c] *= f;
-                            shift[nt][c] *= f;
-                        }
                 }
                 bad = bad || low < ((uint32_t)(base + 6) << 7) - 1u;
                 plain = !__any_sync(0xffffffffu, bad);
@@ -553,7 +555,6 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                             o[i][nt][r] *= f;
                             o[i][nt][2 + r] *= f;
                         }
-                        shift[nt][r] *= f;
                     }
             }
 #pragma unroll
@@ -593,15 +594,16 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
                         const uint32_t w0 = __byte_perm(v0[g], v1[g], half), w1 = __byte_perm(v2[g], v3[g], half), u0 = w0 >> 8, u1 = w1 >> 8;
-                        const uint32_t a[4] = {w0 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x000f000fu, w1 & 0x00f000f0u};
-                        const uint32_t b[4] = {u0 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x000f000fu, u1 & 0x00f000f0u};
-                        const uint32_t eights = g8 == g ? 0x80088008u : 0u, c[4] = {eights, 0u, eights, 0u};         // -8 2^-24 in row g
+                        // (0x8008: -8 2^-24)
+                        const uint32_t a[4] = {add_half_pair(w0 & 0x000f000fu, 0x80088008u), add_half_pair(w0 & 0x00f000f0u, 0x80808080u),
+                                               add_half_pair(w1 & 0x000f000fu, 0x80088008u), add_half_pair(w1 & 0x00f000f0u, 0x80808080u)};
+                        const uint32_t b[4] = {add_half_pair(u0 & 0x000f000fu, 0x80088008u), add_half_pair(u0 & 0x00f000f0u, 0x80808080u),
+                                               add_half_pair(u1 & 0x000f000fu, 0x80088008u), add_half_pair(u1 & 0x00f000f0u, 0x80808080u)};
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             const uint2 w = make_uint2(mul_half_pair(pf[nt].x, s0[g]), mul_half_pair(pf[nt].y, s1[g]));
                             mma_half(o[2 * g][nt], a, w);
                             mma_half(o[2 * g + 1][nt], b, w);
-                            mma_half(shift[nt], c, w);
                         }
                     }
                 }
@@ -666,9 +668,8 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                     m[nt][r] = m[nt][r] == -INFINITY ? -INFINITY : m[nt][r] * to_logit[nt][r];
 #pragma unroll
                     for (int i = 0; i < 2 * G; ++i) {
-                        const float add = __shfl_sync(0xffffffffu, shift[nt][r], i / 2 * 4 + q4);
-                        o[i][nt][r] = (o[i][nt][r] + add) * f0 * f1;
-                        o[i][nt][2 + r] = fmaf(o[i][nt][2 + r], 0.0625f, add) * f0 * f1;
+                        o[i][nt][r] = o[i][nt][r] * f0 * f1;
+                        o[i][nt][2 + r] = o[i][nt][2 + r] * (f0 * 0.0625f) * f1;
                     }
                 }
         }
