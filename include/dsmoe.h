@@ -478,8 +478,8 @@ typedef struct dsmoe_quant_cache {
  *   many positions further on, so that a prompt longer than the ring leaves its latest keys.  (Otherwise a slot's row may hold pieces of several tokens.)
  *   k_back, v_back: NULL, or bf16 [T][n_head][d_head] by back_stride: the tokens' rows as the cache holds them (also of tokens passed over), for callers
  *   that go on with those, as a prompt's own attention does.
- * Rows of the cache must not overlap; the memory of k, v, k_back and v_back must not overlap the cache's, nor k's and v's that of k_back and v_back; no row of
- * k_back may overlap one of v_back.
+ * Rows of the cache must not overlap, and the memory from the first code to the last must not overlap that of the scales; the memory of k, v, k_back and v_back must
+ * not overlap the cache's, nor k's and v's that of k_back and v_back; no row of k_back may overlap one of v_back.
  */
 typedef struct dsmoe_quant_write_args {
     int32_t T, sinks, rolling;
@@ -504,11 +504,11 @@ dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_
 /*
  * dsmoe_window_attention over a cache in 4 bits: the same queries, windows, sinks, rolling caches, outputs, limits, and clamping and reporting of
  * tok_seq and pos (desc->kv_stride is not looked at; its other sizes must be the cache's).  window 2^31 - 1: all keys.  The weights that multiply the
- * values are two bf16 numbers each, or one in calls of prompts.
+ * values have 11 bits behind their product with a scale (16 bits beside values with scales that are more than 2^8 apart), or, in calls of prompts, 8.
  *   A call of eight tokens or more a sequence of the cache (T >= 8 * n_seq), T * group >= 64, d_head 64, 96 or 128 and scale > 0 is taken as one of prompts:
  *   what its tokens see is read back into the workspace, 4 * d_head bytes a slot and head of the cache, and attended to as by
  *   dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences alone.  Other calls read the 4 bits once per token.
- *   Magnitudes of queries up to 2^114 (other calls; a group's queries times 136 are added in fp32).
+ *   scale times the largest query is below 2^117 (other calls).
  * workspace: dsmoe_quant_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one call to the next.  Results do not change from
  * run to run.
  */

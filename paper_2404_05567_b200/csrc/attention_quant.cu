@@ -175,6 +175,7 @@ struct QuantGeo {
     static constexpr int FIT = (216 * 1024 / WARPS - SUMS) / UNIT, BUFS = FIT > 4 ? 4 : FIT;
     static constexpr int OWN = BUFS * UNIT + SUMS, SMEM = WARPS * OWN;       // a warp's: its ring, and the sums of the pair that began before its run
     static_assert(BUFS >= 2 && SUMS <= BUFS * UNIT && UNIT % 16 == 0, "rings of two units and more, in which a warp's last sums find a place");
+    static_assert(SMEM + 20 * 1024 <= 227 * 1024, "and the lists");
 };
 
 // What a warp leaves of a pair that is not its alone: rows' largest logits and sums beside the values' sums
@@ -204,6 +205,7 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
     __shared__ Sight sight_s[kListTokens];
     __shared__ long long warp_sum_s[WARPS];
     __shared__ Piece<8 * NT> piece_s[HB][2 * KW];       // of each run: what began before it, what goes on behind it
+    __shared__ int head_s[WARPS][2 * KW + 1];           // first pieces of pairs
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q4 = lane & 3;
     const int hb = warp % HB, kw = warp / HB;
     const int groups = A.n_head * A.row_tiles / HB;     // of a token, HB pairs each
@@ -741,20 +743,31 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
         const bool there = lane < 2 * KW && pieces[lane].there;
         const uint32_t all = __ballot_sync(0xffffffffu, there), ends = __ballot_sync(0xffffffffu, there && pieces[lane].ends);
         // (if the first one does not begin its pair, an earlier CTA does)
-        uint32_t heads = __ballot_sync(0xffffffffu, there && pieces[lane].begins) | (all & (0u - all));
+        const uint32_t heads = __ballot_sync(0xffffffffu, there && pieces[lane].begins) | (all & (0u - all));
+        const int chains = __popc(heads);
+        if (heads >> lane & 1u) head_s[warp][__popc(heads & ((1u << lane) - 1u))] = lane;
+        if (lane == 0) head_s[warp][chains] = 2 * KW;
+        __syncwarp();
         const long long run = (long long)pass * P.runs + blockIdx.x;
-        for (; heads; heads &= heads - 1) {
-            const int head = __ffs(heads) - 1, next = (heads & (heads - 1)) ? __ffs(heads & (heads - 1)) - 1 : 2 * KW;
-            const uint32_t chain = all & (next == 32 ? ~0u : (1u << next) - 1u) & (~0u << head);
+        if (hb == 0 && kw == 0 && lane == 0 && chains > 0) {
+            // the last chain may go on: the run that holds its pair's last unit
+            const int head = head_s[warp][chains - 1];
             const Piece<8 * NT>& f = pieces[head];
-            const int t = n0 + f.e, j = f.h / A.row_tiles, row0 = f.h % A.row_tiles * 16, rows = min(8 * NT, A.group - row0);
+            if (f.begins && (ends >> head) == 0)
+                P.run_head[run] = make_int2((n0 + f.e) * A.n_head * A.row_tiles + f.h,
+                                            parts_word(run_of(base_s[n], n_runs, base_s[f.e] + (long long)(f.h / HB + 1) * f.units - 1) - (int)blockIdx.x + 1, 1));
+        }
+        const int most = min(8 * NT, A.group) * (DH / 4);
+        for (int item = kw * 32 + lane; item < chains * most; item += KW * 32) {
+            const int c = item / most, idx = item - c * most, row = idx / (DH / 4), col = idx % (DH / 4) * 4;
+            const int head = head_s[warp][c], next = head_s[warp][c + 1];
+            const Piece<8 * NT>& f = pieces[head];
+            const int t = n0 + f.e, j = f.h / A.row_tiles, row0 = f.h % A.row_tiles * 16, member = row0 + row;
+            if (member >= A.group) continue;
+            const uint32_t chain = all & (next == 32 ? ~0u : (1u << next) - 1u) & (~0u << head);
             const bool begins = f.begins, whole = begins && (ends & chain) != 0;
             float* const slot = P.slots + part_slot(run, begins, HB, hb) * 16 * (DH + 2);
-            if (begins && !whole && hb == 0 && kw == 0 && lane == 0)
-                P.run_head[run] = make_int2(t * A.n_head * A.row_tiles + f.h,
-                                            parts_word(run_of(base_s[n], n_runs, base_s[f.e] + (long long)(f.h / HB + 1) * f.units - 1) - (int)blockIdx.x + 1, 1));
-            for (int idx = kw * 32 + lane; idx < rows * (DH / 4); idx += KW * 32) {
-                const int row = idx / (DH / 4), col = idx % (DH / 4) * 4, member = row0 + row;
+            {
                 float M = -INFINITY;
 #pragma unroll 4
                 for (int i = head; i < next; ++i) M = fmaxf(M, chain >> i & 1u ? pieces[i].m[row] : -INFINITY);

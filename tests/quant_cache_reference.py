@@ -84,12 +84,12 @@ def quant_logit_error(q, scale, K_scale, spread, d):
 def quant_out_tolerance(out, absolute, error, prompt, n, V_scale):
     """`absolute`: the weighted sum of |V|; n keys; V_scale: the largest of their values' scales.  Weights are off by exp(+-2 error) and 2^-20.  Prompts: rounded to
     bf16, 2^-8.  Otherwise: rounded to fp16 before and behind the product with a scale, 2^-11 each; products of less than 2^-14 by 2^-25, in units in which the
-    largest weight is 2^6 and the largest scale 1 / 2 or more, and their codes' magnitudes are 7 at most: n 2^-31 14 V_scale.  The sums hold 8 + c instead of c, up
-    to 15 / 7 of what 7 scales are, and so do those that are taken away: at most 2^8 additions each that cut 2^-23.  The output is rounded to bf16."""
+    largest weight is 2^6 and the largest scale 1 / 2 or more, and their codes' magnitudes are 7 at most: n 2^-31 14 V_scale.  Sums in fp32: chains of at most 2^8
+    additions, 2^-24 each.  The output is rounded to bf16."""
     e = np.expm1(2 * error)[..., None] + 2.0 ** -20
     if prompt:
         return BF16_HALF_STEP * (np.abs(out) + absolute) * 1.01 + absolute * (e + 2.0 ** -16) + 1e-30
-    return BF16_HALF_STEP * np.abs(out) * 1.01 + absolute * (e + 2.0 ** -10 * 1.01) + V_scale * (n * 2.0 ** -31 * 14 + 2 * 2.0 ** 8 * 2.0 ** -23 * 15) + 1e-30
+    return BF16_HALF_STEP * np.abs(out) * 1.01 + absolute * (e + 2.0 ** -10 * 1.01 + 2.0 ** -16) + V_scale * n * 2.0 ** -31 * 14 + 1e-30
 
 
 class QuantCase:
