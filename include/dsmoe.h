@@ -504,7 +504,8 @@ dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_
 /*
  * dsmoe_window_attention over a cache in 4 bits: the same queries, windows, sinks, rolling caches, outputs, limits, and clamping and reporting of
  * tok_seq and pos (desc->kv_stride is not looked at; its other sizes must be the cache's).  window 2^31 - 1: all keys.  The weights that multiply the
- * values have 11 bits behind their product with a scale (16 bits beside values with scales that are more than 2^8 apart), or, in calls of prompts, 8.
+ * values have 11 bits behind their product with a scale, and those of 2^-31 of a row's largest or less count for nothing (16 bits, and all count, where
+ * neighbouring keys' scales of values are more than 2^7 apart); or, in calls of prompts, 8.
  *   A call of eight tokens or more a sequence of the cache (T >= 8 * n_seq), T * group >= 64, d_head 64, 96 or 128 and scale > 0 is taken as one of prompts:
  *   what its tokens see is read back into the workspace, 4 * d_head bytes a slot and head of the cache, and attended to as by
  *   dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences alone.  Other calls read the 4 bits once per token.

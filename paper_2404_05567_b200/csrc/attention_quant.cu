@@ -1,10 +1,10 @@
 // Attention of single tokens against their caches in 4 bits (see quant_cache.cuh for the format, cache_attention.cuh for what a row sees and what parts are).
 //
-// The keys of all (token, head, row tile) pairs, in units of 32, are one list, cut into equal runs, as in attention_stream_kernel: a run is a CTA's, whose
-// warps take its units in turn, or a warp's; a pair that several runs share leaves a part per run, added up by the next launch.
+// The keys of all (token, head, row tile) pairs, in units of 32, are one list, cut into equal runs of the CTAs and those into equal runs of their warps; a pair that
+// several CTAs share leaves a part per CTA, added up by the next launch.
 //
 // A warp brings its units' codes and scales into a ring of its own (cp.async), and takes 16 keys at a time to its tensor instructions with the keys, not the rows, as
-// the 16-row operand: S^T = K q^T and O^T += V^T P^T.  Codes become bf16 numbers in registers, once for all of the pair's rows, of which 8 are the
+// the 16-row operand: S^T = K q^T and O^T += V^T P^T.  Codes become operands in registers, once for all of the pair's rows, of which 8 are the
 // narrow side of an instruction (two of those for groups of more than 8).
 //   K: a code's 4 bits at the lower end of a half word are an fp16 number as they are, (8 + c) 2^-24, and 16 times that four bits further up: half a word of
 //      codes is an operand of masks alone.  A row's queries are multiplied by the power of two that makes the largest 2^14 to 2^15 (and 1 / 16 in the
@@ -12,9 +12,9 @@
 //      there, and its scale multiplies it into the logit.  (With e4m3 operands, for which whole words of codes would do, the tensor instructions cost twice
 //      as much and others beside: 62 tokens with up to 8192 keys 77.9 us instead of 70.6 with bf16 operands.)
 //   V: operands of masks too, less 8 2^-24, or 16 times that.  The scales multiply the weights instead, as fp16 numbers, a weight and group at a time (rounded to
-//      11 bits).  The scales are relative to a power of two near the largest that the
-//      warp has met, which moves as the maximum of the logits does.  Units with scales 2^8 below it (or that are no numbers) go another way: values
-//      are bf16 numbers s * c and weights two bf16 numbers each.
+//      11 bits).  The scales are relative to a power of two near the largest that the warp has met, which moves as the maximum of the logits does.  A weight of
+//      2^-31 or less of the row's largest then counts for nothing beside scales of the same kind; so once the warp has met scales of a pair that are more than 2^7
+//      apart, or no numbers, it goes another way: values are bf16 numbers s * c and weights two bf16 numbers each.
 // The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
 #include <cuda_fp16.h>
 
@@ -412,7 +412,8 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
         float m[NT][2], limit[NT][2], z[NT][2], l[NT][2];
         // Sums of values in units of 2^(base - 88), each second one 16 times as large
         float o[2 * G][NT][4];
-        int base = 0;                                   // the exponent (of a bf16) whose scales' exponent as an fp16 is 0
+        int base = 0, first_base = 0;                   // the exponent (of a bf16) whose scales' exponent as an fp16 is 0; what it was at first
+        bool plain = true;                              // so far all scales are near one another
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             m[nt][0] = m[nt][1] = limit[nt][0] = limit[nt][1] = -INFINITY;
@@ -431,7 +432,6 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
             ptx::cp_async_wait<BUFS - 1>();
             const uint32_t unit = ring0 + (uint32_t)(buf * Geo::UNIT);
             // ---- a lane's key's scales (it has copied them itself): K's to fp32; V's to fp16, relative to base, with two keys' side by side
-            bool plain;
             {
                 const uint32_t k_at = unit + (uint32_t)(Geo::KS + lane * 2 * Geo::SC), v_at = unit + (uint32_t)(Geo::VS + lane * Geo::SC);
                 uint32_t ks[SW], wide[2 * SW], vs[SW], top = 0, low = 0xffffffffu;
@@ -451,10 +451,18 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                     low = min(low, v - 1u);             // (zeros: the largest)
                     bad = bad || v >= 0x7f80u;          // (also what is below zero)
                 }
-                // scales of a bf16's exponents base + 6 to base + 15, and zeros
-                if (__any_sync(0xffffffffu, top >= (uint32_t)(base + 16) << 7)) {
-                    const uint32_t most = __reduce_max_sync(0xffffffffu, top);
-                    const int next = max((int)(most >> 7) - 14, 0);
+                // Plain: scales of a bf16's exponents base + 8 to base + 15, and zeros; base does not rise far.  Otherwise they may reach to base + 95, and so may values
+                // of all kinds be bf16 numbers.
+                int next = base;
+                if (__any_sync(0xffffffffu, top >= (uint32_t)(base + (plain ? 16 : 96)) << 7)) {
+                    next = max((int)(__reduce_max_sync(0xffffffffu, top) >> 7) - (plain ? 14 : 94), 0);
+                    if (base == 0) first_base = next;
+                }
+                if (plain && __any_sync(0xffffffffu, bad || low < ((uint32_t)(next + 8) << 7) - 1u || next > first_base + 6)) {
+                    plain = false;
+                    next = max(next - 80, 0);
+                }
+                if (next != base) {
                     const float f = exp2_fast((float)(base - next));
                     base = next;
 #pragma unroll
@@ -464,8 +472,6 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
 #pragma unroll
                             for (int i = 0; i < 2 * G; ++i) o[i][nt][c] *= f;
                 }
-                bad = bad || low < ((uint32_t)(base + 6) << 7) - 1u;
-                plain = !__any_sync(0xffffffffu, bad);
                 if (plain) {
                     const uint32_t none = (uint32_t)base << 7 | (uint32_t)base << 23;
                     uint32_t pairs[SW];

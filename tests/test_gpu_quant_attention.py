@@ -210,3 +210,66 @@ def test_without_lse_and_status():
     ws = torch.empty(dm.dsmoe_quant_attention_workspace_size(desc), dtype=torch.uint8, device="cuda")
     dm.dsmoe_quant_attention(desc, cache, ALL, 0, False, c.q, c.tok_seq, c.pos, c.out, None, ws)
     assert (np.abs(c.out.double().cpu().numpy() - want[0]) <= want[2]).all()
+
+
+@pytest.mark.parametrize("far", [2.0 ** 96, 2.0 ** 12, 2.0 ** -12, 2.0 ** -96])
+def test_values_of_magnitudes_far_apart(far):
+    """Keys whose values are far larger than others', with weights so small that both count; or far smaller, with weights so large."""
+    from cache_attention_reference import attention
+    from quant_cache_reference import quant_logit_error, quant_out_tolerance, quantise, tensors, values
+    rng = np.random.default_rng(21)
+    n, d, L = 500, 128, 777
+    c = QuantCase([(0, n - 1)], 1, 3, d, 1, L, seed=21)
+    c.q_np[:, :, :] = c.q_np[:, :, :1]                                   # members alike, so that a key's weight is as small for all
+    c.q = torch.from_numpy(c.q_np).to(torch.bfloat16).cuda()
+    q = c.q_np[0, 0, 0]
+    K, V = rng.standard_normal((1, 1, L, d)), rng.standard_normal((1, 1, L, d))
+    at = [5, 40, 41, 100, 333] + list(range(400, 440))
+    rare = np.zeros(L, dtype=bool)
+    rare[at] = True
+    K[0, 0, rare] = q * -np.log(far) / (c.scale * (q @ q))
+    kc, ks = quantise(K)
+    # by what the keys have become: values in the opposite proportion of the weights
+    logit = c.scale * (values(kc, ks)[0, 0] @ q)
+    V[0, 0, rare] *= np.exp(np.log(np.exp(logit[:n][~rare[:n]]).sum()) - logit[rare] - 3.0)[:, None]
+    V = torch.from_numpy(V).to(torch.bfloat16).double().numpy()
+    vc, vs = quantise(V)
+    (c.K, c.K_scale), (c.V, c.V_scale) = tensors(kc, ks), tensors(vc, vs)
+    K, V = values(kc, ks)[0, 0, :n], values(vc, vs)[0, 0, :n]
+    want, lse, weight, absolute, spread = attention(c.q_np[0, 0], K, V, c.scale, np.arange(n))
+    rare = rare[:n]
+    error = quant_logit_error(c.q_np[0, 0], c.scale, ks[0, 0, :n], spread, d)
+    # (what products of less than 2^-14 lose is beside the weights of the keys of one kind, in units of their own scales)
+    tol = quant_out_tolerance(want, absolute, error, False, 0, 0.0)
+    tol += sum(n * 2.0 ** -31 * 14 * vs[0, 0, :n][kind].max() * weight[:, kind].max() for kind in (rare, ~rare))
+    part = V.copy()
+    part[~rare] = 0.0
+    part = attention(c.q_np[0, 0], K, part, c.scale, np.arange(n))[0]
+    assert (np.abs(part).max(-1) > 0.1 * np.abs(want).max(-1)).all() and (np.abs(want - part).max(-1) > 0.1 * np.abs(want).max(-1)).all()
+    call(c)
+    got = c.out.double().cpu().numpy()[0, 0]
+    assert (np.abs(want) > 10 * tol).mean() > 0.5                        # (the tolerance says something)
+    assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+    assert (np.abs(c.lse.double().cpu().numpy()[0, 0] - lse) <= error + 1e-4).all()
+
+
+def test_scales_that_a_writer_never_leaves():
+    """Zero bytes, scales below zero, of eight significant bits, of the smallest numbers: values as they read back."""
+    from cache_attention_reference import attention
+    rng = np.random.default_rng(22)
+    n, d = 300, 96
+    c = QuantCase([(0, n - 1), (1, n - 1)], 2, 4, d, 2, n, seed=22)
+    c.V[0, :, 40:60], c.V_scale[0, :, 40:60] = 0, 0
+    c.V_scale[0, :, 100:140, 1] *= -1
+    c.V_scale[1] *= torch.from_numpy(rng.uniform(1, 1.9, c.V_scale[1].shape)).cuda().to(torch.bfloat16)
+    c.V_scale[1, :, 200:] *= 2.0 ** -100
+    cache = c.cache()
+    V = torch.empty((2, 2, n, d), dtype=torch.bfloat16, device="cuda")
+    dm.dsmoe_quant_cache_read(cache, None, torch.empty_like(V), V)
+    call(c)
+    V = V.double().cpu().numpy()
+    for t in range(2):
+        for j in range(2):
+            o, _, _, absolute, _ = attention(c.q_np[t, j], c.values_np[0][t, j], V[t, j], c.scale, np.arange(n))
+            # (scales of eight bits: the values that are read back are rounded once more, by 2^-8)
+            assert (np.abs(c.out.double().cpu().numpy()[t, j] - o) <= 2.0 ** -8 * 1.01 * np.abs(o) + absolute * (2.0 ** -8 + 2.0 ** -8)).all()
