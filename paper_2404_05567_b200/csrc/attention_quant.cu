@@ -453,16 +453,17 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                 }
                 // Plain: scales of a bf16's exponents base + 8 to base + 15, and zeros; base does not rise far.  Otherwise they may reach to base + 95, and so may values
                 // of all kinds be bf16 numbers.
-                int next = base;
-                if (__any_sync(0xffffffffu, top >= (uint32_t)(base + (plain ? 16 : 96)) << 7)) {
-                    next = max((int)(__reduce_max_sync(0xffffffffu, top) >> 7) - (plain ? 14 : 94), 0);
-                    if (base == 0) first_base = next;
-                }
-                if (plain && __any_sync(0xffffffffu, bad || low < ((uint32_t)(next + 8) << 7) - 1u || next > first_base + 6)) {
-                    plain = false;
-                    next = max(next - 80, 0);
-                }
-                if (next != base) {
+                const auto near = [&](int b) { return !bad && top < (uint32_t)(b + 16) << 7 && low >= ((uint32_t)(b + 8) << 7) - 1u; };
+                if (!plain || __any_sync(0xffffffffu, !near(base))) {
+                    int next = base;
+                    if (__any_sync(0xffffffffu, top >= (uint32_t)(base + (plain ? 16 : 96)) << 7)) {
+                        next = max((int)(__reduce_max_sync(0xffffffffu, top) >> 7) - (plain ? 14 : 94), 0);
+                        if (base == 0) first_base = next;
+                    }
+                    if (plain && (next > first_base + 6 || __any_sync(0xffffffffu, !near(next)))) {
+                        plain = false;
+                        next = max(next - 80, 0);
+                    }
                     const float f = exp2_fast((float)(base - next));
                     base = next;
 #pragma unroll
