@@ -147,8 +147,6 @@ __host__ __device__ static inline int quant_units(const Sight& s) {
 // Warps of a CTA: as many as their registers and rings allow
 __host__ __device__ static constexpr int quant_warps(int d_head, int nt) { return d_head <= 128 ? nt == 1 ? 12 : 8 : nt == 1 ? 6 : 4; }
 
-// a / b of numbers that are not negative, which nearly always are small
-__device__ __forceinline__ long long divide(long long a, int b) { return a >> 32 == 0 ? (uint32_t)a / (uint32_t)b : a / b; }
 // The first unit of run c of n equal ones (the first ones a unit longer), and the run that holds unit u
 __device__ __forceinline__ long long run_start(long long total, int n, int c) {
     const long long share = divide(total, n);

@@ -17,6 +17,9 @@ constexpr int kQuantGroup = 32;
 // Places for scales in a row: as many as one load takes
 __host__ __device__ static constexpr int quant_scales(int d_head) { return d_head <= 64 ? 2 : d_head <= 128 ? 4 : 8; }
 
+// a / b of numbers that are not negative, which nearly always are small
+__device__ __forceinline__ long long divide(long long a, long long b) { return (a | b) >> 32 == 0 ? (uint32_t)a / (uint32_t)b : a / b; }
+
 struct QuantView {
     int n_seq, n_head, L, d_head;
     unsigned char *K, *V;                 // codes
