@@ -506,9 +506,10 @@ dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_
  * tok_seq and pos (desc->kv_stride is not looked at; its other sizes must be the cache's).  window 2^31 - 1: all keys.  The weights that multiply the
  * values have 11 bits behind their product with a scale, and those of 2^-31 of a row's largest or less count for nothing (16 bits, and all count, where
  * neighbouring keys' scales of values are more than 2^7 apart); or, in calls of prompts, 8.
- *   A call of eight tokens or more a sequence of the cache (T >= 8 * n_seq), T * group >= 64, d_head 64, 96 or 128 and scale > 0 is taken as one of prompts:
- *   what its tokens see is read back into the workspace, 4 * d_head bytes a slot and head of the cache, and attended to as by
- *   dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences alone.  Other calls read the 4 bits once per token.
+ *   A call of T >= 8 * n_seq tokens, T * group >= 64 rows, d_head 64, 96 or 128, scale > 0 and T * n_head * (group + 15) / 16 * (L / 32 + 1) * (group > 8 ? 4 : 1) (whole
+ *   numbers) of 8192 or more, or 32768 if n_seq > 1 and T < 48 * n_seq, is taken as one of prompts: what its tokens see is read back into the workspace, 4 * d_head
+ *   bytes a slot and head of the cache, and attended to as by dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences
+ *   alone.  Other calls read the 4 bits once per token, and
  *   scale times the largest query is below 2^117 (other calls).
  * workspace: dsmoe_quant_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one call to the next.  Results do not change from
  * run to run.

@@ -366,10 +366,16 @@ QuantView quant_view(const dsmoe_quant_cache& c) {
     return v;
 }
 
-// Prompts are attended to from bf16 copies of what their tokens see, which are exact, on the 128-row kernel: reading back and reading that again moves 8
-// times the bytes that a token's own pass over the 4 bits does, so from eight tokens a sequence on.
-constexpr int kQuantTileTokens = 8;
-bool quant_on_tiles(const AttnView& A) { return own_on_tiles(A) && A.T >= (long long)kQuantTileTokens * A.n_seq; }
+// Prompts are attended to from bf16 copies of what their tokens see, which are exact, on the 128-row kernel.  Reading back and reading that again moves 8 times the
+// bytes that a token's own pass over the 4 bits does, so from eight tokens a sequence on; and finding out what is to be read, reading it and that kernel's own
+// launches take longer than single tokens do where there is little to do.  us of single tokens and of prompts, 4 x 5 heads of 128: 16 tokens of one cache of 200
+// 9.8, 17.0, of 4000 23, 27 (8064 units); 64 of 1000 24, 22 (8192); 256 of 300 26, 19; 16 of each of 16 caches of 300 27, 45 (10240), 64 of 100 44, 21; 32 of each of 4
+// of 200 19, 29, 128 30, 23 (14336).  Groups of more than 8, whose units cost twice as much and fill tiles better: 16 heads on one, 64 of 1000 19, 22 (2048),
+// 256 of 300 29, 18 (2560).
+bool quant_on_tiles(const AttnView& A) {
+    const double units = (double)A.T * A.n_head * A.row_tiles * (A.L / 32 + 1) * (A.group <= 8 ? 1 : 4);
+    return own_on_tiles(A) && A.T >= 8ll * A.n_seq && units >= (A.n_seq == 1 || A.T >= 48ll * A.n_seq ? 8192 : 32768);
+}
 // The copies as the cache of a view
 AttnView quant_copy_view(const AttnView& A, char* ws, size_t bytes) {
     AttnView B = A;

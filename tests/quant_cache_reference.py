@@ -92,6 +92,12 @@ def quant_out_tolerance(out, absolute, error, prompt, n, V_scale):
     return BF16_HALF_STEP * np.abs(out) * 1.01 + absolute * (e + 2.0 ** -10 * 1.01 + 2.0 ** -16) + V_scale * n * 2.0 ** -31 * 14 + 1e-30
 
 
+def taken_as_prompts(T, n_seq, n_head, group, L, d, scale):
+    units = T * n_head * ((group + 15) // 16) * (L // 32 + 1) * (4 if group > 8 else 1)
+    return (d in (64, 96, 128) and scale > 0 and T * group >= 64 and T >= 8 * n_seq
+            and units >= (8192 if n_seq == 1 or T >= 48 * n_seq else 32768))
+
+
 class QuantCase:
     """Inputs of one attention call on the GPU and what it should return.  tokens: a list of (sequence, position)."""
 
@@ -130,8 +136,11 @@ class QuantCase:
         import paper_2404_05567_b200 as dm
         return dm.make_quant_cache(self.K, self.V, self.K_scale, self.V_scale)
 
-    def expected(self, window=None, sinks=0, rolling=False, prompt=False, seen_at=visible):
-        T, d = len(self.tokens), self.d
+    def prompts(self):
+        return taken_as_prompts(len(self.tokens), self.n_seq, self.n_head, self.group, self.L, self.d, self.scale)
+
+    def expected(self, window=None, sinks=0, rolling=False, seen_at=visible):
+        T, d, prompt = len(self.tokens), self.d, self.prompts()
         out, lse = np.zeros((T, self.n_head, self.group, d)), np.zeros((T, self.n_head, self.group))
         out_tol, lse_tol = np.zeros_like(out), np.zeros_like(lse)
         K, V = self.values_np

@@ -23,8 +23,10 @@ def call(c, window=ALL, sinks=0, rolling=False, stream=None, ws=None):
 
 
 def run(c, window=ALL, sinks=0, rolling=False, prompt=False, seen_at=visible):
+    """`prompt`: how the call is meant to be taken."""
+    assert c.prompts() == prompt
     call(c, window, sinks, rolling)
-    c.check(c.expected(window, sinks, rolling, prompt, seen_at))
+    c.check(c.expected(window, sinks, rolling, seen_at))
     assert c.status.item() == 0
 
 
@@ -66,21 +68,20 @@ def test_prompts(d, group, by_token):
     """Neighbouring tokens of prompts, one that continues a context, two of few tokens; what none of them sees is anything."""
     tokens = [(0, p) for p in range(150)] + [(1, p) for p in range(70, 130)] + [(2, 0), (3, 158), (3, 159), (2, -1)]
     prompt = d <= 128                              # (wider heads are taken as single tokens)
-    run(QuantCase(tokens, 2, group, d, 4, 160, seed=9, by_token=by_token, hide=unseen(tokens, 50, 3)), 50, 3, prompt=prompt)
+    run(QuantCase(tokens, 8, group, d, 4, 160, seed=9, by_token=by_token, hide=unseen(tokens, 50, 3)), 50, 3, prompt=prompt)
     one = [(0, p) for p in range(300)]
-    c = QuantCase(one, 2, group, d, 1, 310, seed=10, by_token=by_token, hide=unseen(one, ALL, 0))
+    c = QuantCase(one, 4, group, d, 1, 310, seed=10, by_token=by_token, hide=unseen(one, ALL, 0))
     c.tok_seq = None
     run(c, prompt=prompt)
 
 
 def test_prompts_of_rolling_caches():
-    tokens = [(s, p) for s, last in ((0, 90), (1, 12), (2, 500), (3, 2 ** 31 - 2)) for p in range(max(0, last - 30), last + 1)]
-
     def seen_at(p, w, k):
         return sorted(set(range(max(0, p - w + 1), p + 1)) | set(range(min(k, p + 1))))
-    run(QuantCase(tokens, 4, 5, 128, 4, 40 + 3 + 30, seed=5), 40, 3, True, prompt=True, seen_at=seen_at)
-    few = [(s, p) for s, last in ((0, 90), (1, 12), (2, 500)) for p in range(last - 3, last + 1)]
-    run(QuantCase(few, 4, 5, 128, 3, 40 + 3 + 30, seed=6), 40, 3, True, seen_at=seen_at)
+    tokens = [(s, p) for s, last in ((0, 190), (1, 62), (2, 2 ** 31 - 2)) for p in range(max(0, last - 59), last + 1)]
+    run(QuantCase(tokens, 15, 5, 128, 3, 40 + 3 + 60, seed=5), 40, 3, True, prompt=True, seen_at=seen_at)
+    few = [(s, p) for s, last in ((0, 90), (1, 12), (2, 500), (3, 2 ** 31 - 2)) for p in range(max(0, last - 30), last + 1)]
+    run(QuantCase(few, 4, 5, 128, 4, 40 + 3 + 31, seed=6), 40, 3, True, seen_at=seen_at)
 
 
 def test_rows_that_see_nothing():
@@ -88,6 +89,7 @@ def test_rows_that_see_nothing():
     run(QuantCase(tokens, 2, 3, 64, 2, 41, seed=3, hide=unseen(tokens, 1000, 0)), 1000)
     run(QuantCase([(0, -1)] * 3, 2, 3, 64, 2, 41, seed=3, hide=lambda s, l: True), 7, 2)
     run(QuantCase([(0, -1)] * 40, 2, 3, 64, 2, 41, seed=3, hide=lambda s, l: True), 7, 2)
+    run(QuantCase([(0, -1)] * 100, 42, 3, 64, 2, 41, seed=3, hide=lambda s, l: True), 7, 2, prompt=True)
 
 
 def test_one_sequence_without_its_numbers():
@@ -178,19 +180,21 @@ def test_keys_and_values_that_are_no_numbers():
 
 def test_out_of_range():
     """Clamped and reported, as by the other attention steps."""
-    for n in (1, 30):
+    for n, n_head in ((1, 2), (30, 2), (150, 30)):
         tokens = [(0, 30)] * n + [(5, 20), (-1, 3), (1, 100), (0, -7)]
-        c = QuantCase([(0, 30)] * n + [(1, 20), (0, 3), (1, 40), (0, -1)], 2, 5, 64, 2, 41, seed=13)
+        c = QuantCase([(0, 30)] * n + [(1, 20), (0, 3), (1, 40), (0, -1)], n_head, 5, 64, 2, 41, seed=13)
+        assert c.prompts() == (n == 150)
         c.tok_seq = torch.tensor([s for s, _ in tokens], dtype=torch.int32, device="cuda")
         c.pos = torch.tensor([p for _, p in tokens], dtype=torch.int32, device="cuda")
         call(c)
-        c.check(c.expected(prompt=n > 1))
+        c.check(c.expected())
         assert c.status.item() == 1
 
 
 def test_same_results_every_time_and_on_another_stream():
     for tokens in ([(s, 1000 + 77 * s) for s in range(9)], [(0, p) for p in range(200)] + [(1, p) for p in range(300, 500)]):
         c = QuantCase(tokens, 4, 5, 128, 9, 2000, seed=14)
+        assert c.prompts() == (len(tokens) > 9)
         call(c, 900, 4)
         first, lse = c.out.clone(), c.lse.clone()
         for i in range(3):

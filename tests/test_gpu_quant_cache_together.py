@@ -7,7 +7,7 @@ import torch
 
 import paper_2404_05567_b200 as dm
 from cache_attention_reference import attention, lse_tolerance, visible
-from quant_cache_reference import GROUP, quant_logit_error, quant_out_tolerance, quantise, scales_of, slot_of, unpack, values
+from quant_cache_reference import GROUP, quant_logit_error, quant_out_tolerance, quantise, scales_of, slot_of, taken_as_prompts, unpack, values
 
 pytestmark = pytest.mark.gpu
 
@@ -96,11 +96,13 @@ class Server:
 @pytest.mark.parametrize("rolling", [False, True])
 @pytest.mark.parametrize("n_head,group,d", [(4, 5, 128), (2, 6, 64), (3, 12, 96), (2, 3, 160)])
 def test_prompt_then_tokens(n_head, group, d, rolling):
-    n_seq, prompt, steps = 3, 70, 40
-    s = Server(n_seq, n_head, group, d, WINDOW + SINKS + prompt if rolling else 128, prompt, steps, rolling, seed=d + group)
+    n_seq, prompt, steps = 3, 150, 40
+    s = Server(n_seq, n_head, group, d, WINDOW + SINKS + prompt if rolling else 256, prompt, steps, rolling, seed=d + group)
+    as_prompts = taken_as_prompts(n_seq * prompt, n_seq, n_head, group, s.L, d, s.scale)
+    assert as_prompts == (n_head > 2)
     rows = s.rows(steps)
     s.take_prompt()
-    s.check(rows, s.prompt_q, s.prompt_out, s.prompt_lse, [(i, p) for i in range(n_seq) for p in range(prompt)], d <= 128)
+    s.check(rows, s.prompt_q, s.prompt_out, s.prompt_lse, [(i, p) for i in range(n_seq) for p in range(prompt)], as_prompts)
     s.check_cache(rows, prompt - 1)
     s.feed(0)
     s.step()

@@ -153,13 +153,17 @@ def test_attention_calls_that_are_refused():
 
 
 def test_workspaces_of_prompts_hold_what_they_read_back():
-    """Eight tokens a sequence and more: 4 d_head bytes a slot and head; the cache's 16-bit strides are not looked at."""
+    """4 d_head bytes a slot and head where a call is taken as one of prompts; the cache's 16-bit strides are not looked at."""
+    from quant_cache_reference import taken_as_prompts
+    a = dict(n_seq=2, n_head=2, d_head=64, scale=0.125, L=200000, group=8)
     copies = 4 * 64 * 2 * 2 * 200000
-    size = lambda **kw: _size(_desc(**{"T": 16, "group": 8, "L": 200000, **kw}))
-    assert size()[1] >= copies and size(T=15)[1] < copies / 4
-    for kw in (dict(d_head=160), dict(scale=-0.1), dict(group=2)):        # of the kinds that are taken otherwise
-        assert size(**kw)[1] < copies / 2
-    assert size(T=15, kv_stride=(1, -3, 2 ** 60)) == size(T=15)
+    for T, kw, prompts in ((16, {}, True), (15, {}, False), (16, dict(group=2), False), (64, dict(d_head=160), False), (64, dict(scale=-0.1), False)):
+        got = {**a, **kw, "T": T}
+        assert taken_as_prompts(got["T"], got["n_seq"], got["n_head"], got["group"], got["L"], got["d_head"], got["scale"]) == prompts
+        size = _size(_desc(**got))[1]
+        assert size >= copies if prompts else size < copies / 2, (T, kw)
+    d = dict(T=15, group=8, L=200000)
+    assert _size(_desc(**d, kv_stride=(1, -3, 2 ** 60))) == _size(_desc(**d))
 
 
 def _tensors(n_seq=2, n_head=3, L=40, d=128, by_token=False):
