@@ -509,8 +509,7 @@ dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_
  *   A call of T >= 8 * n_seq tokens, T * group >= 64 rows, d_head 64, 96 or 128, scale > 0 and T * n_head * (group + 15) / 16 * (L / 32 + 1) * (group > 8 ? 4 : 1) (whole
  *   numbers) of 8192 or more, or 32768 if n_seq > 1 and T < 48 * n_seq, is taken as one of prompts: what its tokens see is read back into the workspace, 4 * d_head
  *   bytes a slot and head of the cache, and attended to as by dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences
- *   alone.  Other calls read the 4 bits once per token, and
- *   scale times the largest query is below 2^117 (other calls).
+ *   alone.  Other calls read the 4 bits once per token; in them scale times the largest query must be below 2^117.
  * workspace: dsmoe_quant_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one call to the next.  Results do not change from
  * run to run.
  */
