@@ -277,3 +277,24 @@ def test_scales_that_a_writer_never_leaves():
             o, _, _, absolute, _ = attention(c.q_np[t, j], c.values_np[0][t, j], V[t, j], c.scale, np.arange(n))
             # (scales of eight bits: the values that are read back are rounded once more, by 2^-8)
             assert (np.abs(c.out.double().cpu().numpy()[t, j] - o) <= 2.0 ** -8 * 1.01 * np.abs(o) + absolute * (2.0 ** -8 + 2.0 ** -8)).all()
+
+
+@pytest.mark.parametrize("T,L,prompt", [(3, 400, False), (90, 1500, True)])
+def test_offsets_beyond_32_bits(T, L, prompt):
+    """The same keys at the end of a cache whose codes, and whose copies in 16 bits, reach beyond 2^32 bytes: as at that of a short one."""
+    n_seq, n_head, d, room = 3, 8, 128, 2_900_000
+    tokens = [(t % n_seq, L - 1 - t // n_seq) if not prompt else (t // 30, L - 30 + t % 30) for t in range(T)]
+    c = QuantCase(tokens, n_head, 5, d, n_seq, L, seed=23)
+    want = c.expected(200, 0)
+    assert c.prompts() == prompt and n_seq * n_head * room * d // 2 > 2 ** 32
+    for name in ("K", "V", "K_scale", "V_scale"):
+        x = getattr(c, name)
+        wide = torch.full((n_seq, n_head, room, x.shape[3]), 0 if x.dtype == torch.uint8 else float("nan"), dtype=x.dtype, device="cuda")
+        wide[:, :, room - L:] = x
+        setattr(c, name, wide)
+    c.pos += room - L
+    c.L = room
+    assert c.prompts() == prompt
+    call(c, 200, 0)
+    c.check(want)
+    assert c.status.item() == 0
