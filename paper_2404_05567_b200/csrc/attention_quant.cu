@@ -147,7 +147,8 @@ __host__ __device__ static inline int quant_units(const Sight& s) {
     return n > 0 ? n : 1;                 // a token that sees nothing has one unit without keys, so that somebody writes its row
 }
 
-// Warps of a CTA: as many as their registers and rings allow
+// Warps of a CTA: as many as their registers and rings allow.  With 12 and with 8, us: 62 tokens with up to 8192 keys 66, 74; 2 with 131072 75, 87; 256 with up to 500
+// 17.6, 18.9; one token with 512 10.5, 10.1.
 __host__ __device__ static constexpr int quant_warps(int d_head, int nt) { return d_head <= 128 ? nt == 1 ? 12 : 8 : nt == 1 ? 6 : 4; }
 
 // The first unit of run c of n equal ones (the first ones a unit longer), and the run that holds unit u
@@ -189,7 +190,7 @@ struct Piece {
 };
 
 // HB: neighbouring pairs that a CTA takes at a time, a warp each.  Where the heads of a position lie side by side they are so read side by side, and rows of
-// one head beyond 16 read its keys out of L2 or nearer.
+// one head beyond 16 read its keys out of L2 or nearer.  62 tokens with up to 8192 keys, 4 heads side by side: 66 us with 4 at a time, 69 with 2, 83 with 1.
 //
 // A CTA's run of the list is cut into equal runs of its warps (of each of the HB pairs), which take their units one after the other and owe the others
 // nothing until the end.  What a warp has of a pair that began before its run or goes on behind it is a piece; the CTA's pieces of a pair are added up once all
@@ -861,7 +862,8 @@ dsmoe_status launch_quant_attention(const AttnView& A, const QuantView& C, const
     QuantPlan P = plan;
     const long long pairs = (long long)A.T * A.n_head * A.row_tiles;
     const int sms = std::min(sm_count(), kMostStreamCtas), warps = quant_warps_of(A), each = A.n_head * A.row_tiles;
-    // A CTA takes all of a pair's keys, and no part is left to add up, where the CTAs that stay idle would save less than the second launch costs
+    // A CTA takes all of a pair's keys, and no part is left to add up, where the CTAs that stay idle would save less than the second launch
+    // costs (one token, 4 x 5 heads of 128, 512 keys: 10.5 us, 13.5 in two launches)
     P.whole = pairs <= sms && quant_seen(A) * (sms - pairs) <= 3ll * kQuantUnit * warps * sms;
     const bool side_by_side = A.row_tiles > 1 || (A.n_head > 1 && C.c_h < C.c_p);
     const int hb = P.whole || !side_by_side ? 1 : each % 4 == 0 && warps % 4 == 0 ? 4 : each % 2 == 0 ? 2 : 1;
