@@ -504,8 +504,9 @@ dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_
 /*
  * dsmoe_window_attention over a cache in 4 bits: the same queries, windows, sinks, rolling caches, outputs, limits, and clamping and reporting of
  * tok_seq and pos (desc->kv_stride is not looked at; its other sizes must be the cache's).  window 2^31 - 1: all keys.  The weights that multiply the
- * values have 11 bits behind their product with a scale, and those of 2^-31 of a row's largest or less count for nothing (16 bits, and all count, where
- * neighbouring keys' scales of values are more than 2^7 apart); or, in calls of prompts, 8.
+ * values have 11 bits behind their product with a value's scale, if that is 2^-23 of the row's largest weight times the largest scale that it sees or more;
+ * smaller products are off by up to 2^-33 of that each (16 bits, and all count, where scales of values that follow one another are more than 2^8 apart); or, in calls
+ * of prompts, 8.
  *   A call of T >= 8 * n_seq tokens, T * group >= 64 rows, d_head 64, 96 or 128, scale > 0 and T * n_head * (group + 15) / 16 * (L / 32 + 1) * (group > 8 ? 4 : 1) (whole
  *   numbers) of 8192 or more, or 32768 if n_seq > 1 and T < 48 * n_seq, is taken as one of prompts: what its tokens see is read back into the workspace, 4 * d_head
  *   bytes a slot and head of the cache, and attended to as by dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences

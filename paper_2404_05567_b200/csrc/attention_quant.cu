@@ -12,9 +12,11 @@
 //      there, and its scale multiplies it into the logit.  (With e4m3 operands, for which whole words of codes would do, the tensor instructions cost twice
 //      as much and others beside: 62 tokens with up to 8192 keys 77.9 us instead of 70.6 with bf16 operands.)
 //   V: operands of masks too, less 8 2^-24, or 16 times that.  The scales multiply the weights instead, as fp16 numbers, a weight and group at a time (rounded to
-//      11 bits).  The scales are relative to a power of two near the largest that the warp has met, which moves as the maximum of the logits does.  A weight of
-//      2^-31 or less of the row's largest then counts for nothing beside scales of the same kind; so once the warp has met scales of a pair that are more than 2^7
-//      apart, or no numbers, it goes another way: values are bf16 numbers s * c and weights two bf16 numbers each.
+//      11 bits).  The scales are relative to a power of two near the largest that the warp has met, 1/2 to 2 times it, which moves as the maximum of the logits does.
+//      A product is a multiple of 2^-34 of that (2^-24, and kRaise): it has 11 bits where the weight is 2^-23 of the row's largest or more beside scales like the
+//      largest, 2^-17 beside the smallest, 2^-7; it is nothing below 2^-35 and 2^-28.  So once the warp has met scales of a pair that are further apart (2^6 to
+//      2^8), or no numbers, it goes another way: values are bf16 numbers s * c and weights two bf16 numbers each (62 tokens with up to 8192 keys, of which the first
+//      four have values 2^-9 as large: 70.7 us instead of 65.6).
 // The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
 // What bounds it: 62 tokens with up to 8192 keys, 4 x 5 heads of 128 by position, take 66 us (their 4.5 bits a value at 6.45 TB/s 34): the copies alone 50, of which 35
 // at 6.3 TB/s and the rest before the first key and behind the last one; a unit's chain of scales, products, maximum, exponentials, transposition and products,
@@ -31,7 +33,10 @@ namespace dsmoe {
 namespace {
 
 constexpr int kQuantUnit = 32;            // keys that a warp takes at a time
-constexpr float kRaise = 6.f;             // weights of up to 2^(kStreamMoves + kRaise), times scales below 2, are fp16 numbers
+// The maximum that weights are relative to moves when a logit passes it by more than kQuantMoves.  Weights of up to 2^(kQuantMoves + kRaise), times scales
+// below 2, are fp16 numbers; each of the 14 that the moves do not take keeps products of small weights and small scales one bit longer.  With moves of 8, 4, 2 and 1,
+// us: 62 tokens with up to 8192 keys 65.8, 65.6, 65.8, 66.6; 48 tokens of 4 x 16 heads of 96, window 4090 55.6, 56.1, 57.7, 59.3; 62 of 4 x 16 of 256, 4096 keys 252, 262, 279, 294.
+constexpr float kQuantMoves = 4.f, kRaise = 10.f;
 
 __device__ __forceinline__ void mma_half_first(float (&d)[4], const uint32_t (&a)[4], uint2 b, float c0, float c1) {
     asm volatile(
@@ -545,7 +550,7 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                     top[nt][r] = max3(fmaxf(x[0][nt][r], x[0][nt][2 + r]), x[1][nt][r], x[1][nt][2 + r]);
                     moves = moves || top[nt][r] > limit[nt][r];
                 }
-            // (see kStreamMoves)
+            // (see kQuantMoves)
             if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -557,7 +562,7 @@ attention_quant_kernel(const __grid_constant__ AttnView A, const __grid_constant
                         if (!(b > m[nt][r])) continue;  // (the row's lanes agree)
                         const float before = z[nt][r];
                         z[nt][r] = fmaf(b, to_logit[nt][r], -kRaise);
-                        limit[nt][r] = b + kStreamMoves / to_logit[nt][r];
+                        limit[nt][r] = b + kQuantMoves / to_logit[nt][r];
                         const float f = m[nt][r] == -INFINITY ? 1.f : exp2_fast(before - z[nt][r]);
                         m[nt][r] = b;
                         l[nt][r] *= f;
