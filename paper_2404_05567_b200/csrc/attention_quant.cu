@@ -845,6 +845,8 @@ int quant_warps_of(const AttnView& A) { return quant_warps(A.d_head, A.group <= 
 // Keys that a token sees at most
 long long quant_seen(const AttnView& A) { return A.window < A.L ? std::min((long long)A.window + A.sinks, (long long)A.L) : A.L; }
 
+constexpr int kWholeUnits = 6;            // of a warp, at most, where a CTA takes all of a pair's keys
+
 // CTAs: one an SM, as far as each has a unit per warp in the longest case
 int quant_ctas(const AttnView& A) {
     const long long units = ((quant_seen(A) + kQuantUnit - 1) / kQuantUnit + 1) * A.T * A.n_head * A.row_tiles, warps = quant_warps_of(A);
@@ -854,6 +856,18 @@ int quant_ctas(const AttnView& A) {
 constexpr int kMostHeadsAtOnce = 4;
 
 }  // namespace
+
+// Whether a CTA takes all of a pair's keys, `seen` at most, so that no part is left to add up: where the CTAs that stay idle would save less than the second launch
+// costs, as long as one pair of all keys beside others of few holds up the call by no more than that launch.  One launch and two, us, with 4 x 5 heads of 128:
+//   one token    512 keys 10.1, 12.6; 1024 12.4, 13.1; 1536 14.6, 13.1; 2048 17.2, 13.1 (two from 1185 on)
+//   32 tokens    512 keys 10.8, 16.1; 1024 13.1, 18.7; 2048 18.6, 22.3; 4096 28.0, 31.8; 8192 46.2, 47.3
+//   the same, but a tenth of the keys to all of them: 512 11.2, 14.0; 1024 13.2, 17.1; 2048 18.4, 18.8; 4096 26.9, 24.5; 8192 44.3, 34.0
+//   the same, by position: 1024 13.5, 18.0; 2048 18.7, 20.6; 4096 27.5, 25.9; 8192 45.1, 36.7 (neighbouring heads are read side by side in runs alone)
+//   37 tokens, one of 131072 keys and the others of 200: 560, 42.4
+// 4 x 16 heads of 96, 32 tokens, a tenth to all: 1024 keys 15.1, 24.4; 2048 21.2, 27.4; 4096 33.3, 33.6; 8192 58.6, 46.1.
+bool quant_whole(long long pairs, long long seen, int warps, int sms) {
+    return pairs <= sms && seen <= (long long)kWholeUnits * kQuantUnit * warps && seen * (sms - pairs) <= 3ll * kQuantUnit * warps * sms;
+}
 
 // The runs are numbered as attention_sum_kernel takes those of single warps, of which stream_warps are a CTA's there
 void quant_plan_size(const AttnView& A, QuantPlan* plan, size_t* slots, size_t* run_head) {
@@ -866,10 +880,8 @@ void quant_plan_size(const AttnView& A, QuantPlan* plan, size_t* slots, size_t* 
 dsmoe_status launch_quant_attention(const AttnView& A, const QuantView& C, const QuantPlan& plan, cudaStream_t s) {
     QuantPlan P = plan;
     const long long pairs = (long long)A.T * A.n_head * A.row_tiles;
-    const int sms = std::min(sm_count(), kMostStreamCtas), warps = quant_warps_of(A), each = A.n_head * A.row_tiles;
-    // A CTA takes all of a pair's keys, and no part is left to add up, where the CTAs that stay idle would save less than the second launch
-    // costs (one token, 4 x 5 heads of 128, 512 keys: 10.5 us, 13.5 in two launches)
-    P.whole = pairs <= sms && quant_seen(A) * (sms - pairs) <= 3ll * kQuantUnit * warps * sms;
+    const int warps = quant_warps_of(A), each = A.n_head * A.row_tiles;
+    P.whole = quant_whole(pairs, quant_seen(A), warps, std::min(sm_count(), kMostStreamCtas));
     const bool side_by_side = A.row_tiles > 1 || (A.n_head > 1 && C.c_h < C.c_p);
     const int hb = P.whole || !side_by_side ? 1 : each % 4 == 0 && warps % 4 == 0 ? 4 : each % 2 == 0 ? 2 : 1;
     const int ctas = P.whole ? (int)pairs : quant_ctas(A);
