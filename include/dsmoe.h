@@ -507,10 +507,13 @@ dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_
  * values have 11 bits behind their product with a value's scale, if that is 2^-23 of the row's largest weight times the largest scale that it sees or more;
  * smaller products are off by up to 2^-33 of that each (16 bits, and all count, where scales of values that follow one another are more than 2^8 apart); or, in calls
  * of prompts, 8.
- *   A call of T >= 8 * n_seq tokens, T * group >= 64 rows, d_head 64, 96 or 128, scale > 0 and T * n_head * (group + 15) / 16 * (L / 32 + 1) * (group > 8 ? 4 : 1) (whole
- *   numbers) of 8192 or more, or 32768 if n_seq > 1 and T < 48 * n_seq, is taken as one of prompts: what its tokens see is read back into the workspace, 4 * d_head
- *   bytes a slot and head of the cache, and attended to as by dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences
- *   alone.  Other calls read the 4 bits once per token; in them scale times the largest query must be below 2^117.
+ *   Some calls are taken as ones of prompts: what their tokens see is read back into the workspace, 4 * d_head bytes a slot and head of the cache, and attended to
+ * as by dsmoe_window_attention.  Prompts of few of a cache's sequences are better given those sequences alone.  They are (n = T * n_head * ((group + 15) / 16), whole
+ * numbers, W = 12 for groups up to 8 and 8 for others) calls with d_head 64, 96 or 128, scale > 0, T * group >= 64,
+ *     T >= 8 * n_seq, and T * group >= 64 * n_seq or both T >= 16 * n_seq and T * group >= 32 * n_seq,
+ *     n * (L / 32 + 1) * (group > 8 ? 4 : 1) of 8192 or more, or 32768 if n_seq > 1 and T < 48 * n_seq,
+ *     and either n > S or L > 192 * W or L * (S - n) > 96 * W * S, on a GPU of S SMs.
+ *   Other calls read the 4 bits once per token; in them scale times the largest query must be below 2^117.
  * workspace: dsmoe_quant_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one call to the next.  Results do not change from
  * run to run.
  */

@@ -368,13 +368,18 @@ QuantView quant_view(const dsmoe_quant_cache& c) {
 
 // Prompts are attended to from bf16 copies of what their tokens see, which are exact, on the 128-row kernel.  Reading back and reading that again moves 8 times the
 // bytes that a token's own pass over the 4 bits does, so from eight tokens a sequence on; and finding out what is to be read, reading it and that kernel's own
-// launches take longer than single tokens do where there is little to do.  us of single tokens and of prompts, 4 x 5 heads of 128: 16 tokens of one cache of 200
-// 9.8, 17.0, of 4000 23, 27 (8064 units); 64 of 1000 24, 22 (8192); 256 of 300 26, 19; 16 of each of 16 caches of 300 27, 45 (10240), 64 of 100 44, 21; 32 of each of 4
-// of 200 19, 29, 128 30, 23 (14336).  Groups of more than 8, whose units cost twice as much and fill tiles better: 16 heads on one, 64 of 1000 19, 22 (2048),
-// 256 of 300 29, 18 (2560).
+// launches take longer than single tokens do where there is little to do.  us of single tokens and of prompts, 4 x 5 heads of 128: 16 tokens of one cache of 4000
+// 23, 27 (8064 units); 64 of 1000 23, 20 (8192); 128 of 1000 31, 22; 32 of each of 4 of 1000 31, 36 (16384), of 2000 46, 39 (32256).  Groups of more than 8, whose
+// units cost twice as much and fill tiles better: 16 heads on one, 200 of 350 26, 16 (2200 units).  What single tokens do in one launch they do in less than prompts
+// take: 16 heads on one, 64 of 1000 18, 21 (2048), of 1200 19.5, 20.6; 4 x 16 heads, 32 of 1000 18, 21 (4096).
+// A sequence's rows have to fill half of a tile, or a quarter with 16 tokens and more: what fills less is left to the streaming kernel, which reads the copies once
+// a token.  32 caches of 4000: 4 x 1 heads of 64, 8 tokens 92, 240, 24 255, 616, 32 332, 124; 4 x 2 of 64, 12 131, 327, 16 170, 118; 4 x 5 of 128, 8 132, 192, 12 190, 197,
+// 16 248, 189; 4 x 16, 8 216, 167.
 bool quant_on_tiles(const AttnView& A) {
     const double units = (double)A.T * A.n_head * A.row_tiles * (A.L / 32 + 1) * (A.group <= 8 ? 1 : 4);
-    return own_on_tiles(A) && A.T >= 8ll * A.n_seq && units >= (A.n_seq == 1 || A.T >= 48ll * A.n_seq ? 8192 : 32768);
+    const long long rows = (long long)A.T * A.group, n_seq = A.n_seq;
+    return own_on_tiles(A) && !quant_whole(A) && A.T >= 8 * n_seq && (rows >= 64 * n_seq || (A.T >= 16 * n_seq && rows >= 32 * n_seq)) &&
+           units >= (n_seq == 1 || A.T >= 48 * n_seq ? 8192 : 32768);
 }
 // The copies as the cache of a view
 AttnView quant_copy_view(const AttnView& A, char* ws, size_t bytes) {

@@ -868,6 +868,9 @@ constexpr int kMostHeadsAtOnce = 4;
 bool quant_whole(long long pairs, long long seen, int warps, int sms) {
     return pairs <= sms && seen <= (long long)kWholeUnits * kQuantUnit * warps && seen * (sms - pairs) <= 3ll * kQuantUnit * warps * sms;
 }
+bool quant_whole(const AttnView& A) {
+    return quant_whole((long long)A.T * A.n_head * A.row_tiles, quant_seen(A), quant_warps_of(A), std::min(sm_count(), kMostStreamCtas));
+}
 
 // The runs are numbered as attention_sum_kernel takes those of single warps, of which stream_warps are a CTA's there
 void quant_plan_size(const AttnView& A, QuantPlan* plan, size_t* slots, size_t* run_head) {
@@ -881,7 +884,7 @@ dsmoe_status launch_quant_attention(const AttnView& A, const QuantView& C, const
     QuantPlan P = plan;
     const long long pairs = (long long)A.T * A.n_head * A.row_tiles;
     const int warps = quant_warps_of(A), each = A.n_head * A.row_tiles;
-    P.whole = quant_whole(pairs, quant_seen(A), warps, std::min(sm_count(), kMostStreamCtas));
+    P.whole = quant_whole(A);
     const bool side_by_side = A.row_tiles > 1 || (A.n_head > 1 && C.c_h < C.c_p);
     const int hb = P.whole || !side_by_side ? 1 : each % 4 == 0 && warps % 4 == 0 ? 4 : each % 2 == 0 ? 2 : 1;
     const int ctas = P.whole ? (int)pairs : quant_ctas(A);

@@ -62,6 +62,7 @@ struct QuantPlan {
 void quant_plan_size(const AttnView& A, QuantPlan* plan, size_t* slots, size_t* run_head);
 // Whether it takes one launch, a CTA for each of the pairs (token, head, 16 rows) that see `seen` keys at most, with so many warps a CTA, on so many SMs
 bool quant_whole(long long pairs, long long seen, int warps, int sms);
+bool quant_whole(const AttnView& A);
 dsmoe_status launch_quant_attention(const AttnView& A, const QuantView& C, const QuantPlan& plan, cudaStream_t s);
 
 }  // namespace dsmoe

@@ -31,3 +31,26 @@ def test_a_cta_per_pair_takes_few_keys_of_any_number_of_pairs(warps, sms):
 def test_a_cta_per_pair_of_many_keys_only_where_few_ctas_stay_idle():
     assert _whole(148, 2304) and _whole(128, 2304) and not _whole(128, 2305) and not _whole(64, 2304) and _whole(64, 2029) and not _whole(64, 2030)
     assert _whole(4, 1184) and not _whole(4, 1185)
+
+
+def _size(T, n_seq, n_head, group, d_head, L, scale):
+    desc = dm.AttentionDesc(T, n_head, group, d_head, n_seq, L, scale)
+    desc.q_stride[:] = desc.o_stride[:] = (n_head * group * d_head, group * d_head, d_head)
+    return dm.dsmoe_quant_attention_workspace_size(desc)
+
+
+def _as_prompts(*sizes):
+    """Calls with a negative scale are never taken as prompts; the others' workspaces differ from theirs if they are."""
+    return _size(*sizes, 0.1) != _size(*sizes, -0.1)
+
+
+@pytest.mark.parametrize("T,n_head,group,d,L", [(64, 1, 16, 128, 1000), (64, 1, 16, 128, 1200), (32, 4, 16, 128, 1000), (128, 1, 12, 96, 640), (148, 1, 5, 128, 2000)])
+def test_what_one_launch_takes_is_not_taken_as_a_prompt(T, n_head, group, d, L):
+    assert not _as_prompts(T, 1, n_head, group, d, L)
+    assert _as_prompts(2 * T + 100, 1, n_head, group, d, L)
+
+
+@pytest.mark.parametrize("group,d,few,many", [(1, 64, 31, 32), (2, 64, 15, 16), (3, 128, 15, 16), (4, 128, 15, 16), (5, 128, 12, 13), (6, 96, 10, 11), (8, 128, 7, 8), (16, 128, 7, 8)])
+def test_tokens_of_a_sequence_that_fill_little_of_a_tile_are_not_taken_as_prompts(group, d, few, many):
+    for n_seq in (2, 32):
+        assert not _as_prompts(few * n_seq, n_seq, 4, group, d, 24000) and _as_prompts(many * n_seq, n_seq, 4, group, d, 24000)
