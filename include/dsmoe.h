@@ -512,7 +512,8 @@ dsmoe_status dsmoe_quant_cache_read(const dsmoe_quant_cache* cache, const dsmoe_
  * numbers, W = 12 for groups up to 8 and 8 for others) calls with d_head 64, 96 or 128, scale > 0, T * group >= 64,
  *     T >= 8 * n_seq, and T * group >= 64 * n_seq or both T >= 16 * n_seq and T * group >= 32 * n_seq,
  *     n * (L / 32 + 1) * (group > 8 ? 4 : 1) of 8192 or more, or 32768 if n_seq > 1 and T < 48 * n_seq,
- *     and either n > S or L > 192 * W or L * (S - n) > 96 * W * S, on a GPU of S SMs.
+ *     either n > S or L > 192 * W or L * (S - n) > 96 * W * S, on a GPU of S SMs,
+ *     and copies of K of less than 2^40 bytes.
  *   Other calls read the 4 bits once per token; in them scale times the largest query must be below 2^117.
  * workspace: dsmoe_quant_attention_workspace_size bytes, 16-byte aligned; nothing in it is kept from one call to the next.  Results do not change from
  * run to run.

@@ -372,13 +372,14 @@ QuantView quant_view(const dsmoe_quant_cache& c) {
 // 23, 27 (8064 units); 64 of 1000 23, 20 (8192); 128 of 1000 31, 22; 32 of each of 4 of 1000 31, 36 (16384), of 2000 46, 39 (32256).  Groups of more than 8, whose
 // units cost twice as much and fill tiles better: 16 heads on one, 200 of 350 26, 16 (2200 units).  What single tokens do in one launch they do in less than prompts
 // take: 16 heads on one, 64 of 1000 18, 21 (2048), of 1200 19.5, 20.6; 4 x 16 heads, 32 of 1000 18, 21 (4096).
-// A sequence's rows have to fill half of a tile, or a quarter with 16 tokens and more: what fills less is left to the streaming kernel, which reads the copies once
+// Where the copies are larger than a workspace may be, single tokens it is.  A sequence's rows have to fill half of a tile, or a quarter with 16 tokens and more: what fills less is left to the streaming kernel, which reads the copies once
 // a token.  32 caches of 4000: 4 x 1 heads of 64, 8 tokens 92, 240, 24 255, 616, 32 332, 124; 4 x 2 of 64, 12 131, 327, 16 170, 118; 4 x 5 of 128, 8 132, 192, 12 190, 197,
 // 16 248, 189; 4 x 16, 8 216, 167.
 bool quant_on_tiles(const AttnView& A) {
     const double units = (double)A.T * A.n_head * A.row_tiles * (A.L / 32 + 1) * (A.group <= 8 ? 1 : 4);
     const long long rows = (long long)A.T * A.group, n_seq = A.n_seq;
-    return own_on_tiles(A) && !quant_whole(A) && A.T >= 8 * n_seq && (rows >= 64 * n_seq || (A.T >= 16 * n_seq && rows >= 32 * n_seq)) &&
+    const double copy = (double)A.n_seq * A.n_head * A.L * A.d_head * 2;                  // bytes (beyond 64 bits, with strides of 0)
+    return copy < 0x1p40 && own_on_tiles(A) && !quant_whole(A) && A.T >= 8 * n_seq && (rows >= 64 * n_seq || (A.T >= 16 * n_seq && rows >= 32 * n_seq)) &&
            units >= (n_seq == 1 || A.T >= 48 * n_seq ? 8192 : 32768);
 }
 // The copies as the cache of a view
@@ -408,14 +409,15 @@ QuantAttnPlan quant_attention_plan(const AttnView& A) {
         w.rest = w.range + align_up((size_t)A.n_seq * sizeof(int4), 256);
         w.attn = attention_plan(quant_copy_view(A, nullptr, w.copy), SharedKeys{}, false, false);
         w.total = w.rest + w.attn.total;
-        w.fits = w.attn.fits && w.copy < (size_t)1 << 40;
-    } else {
-        size_t slots, heads;
-        quant_plan_size(A, &w.plan, &slots, &heads);
-        w.run_head = align_up(slots, 256);
-        w.total = w.run_head + align_up(heads, 256);
-        w.fits = w.total < (size_t)1 << 36;
+        w.fits = w.attn.fits;
+        if (w.fits) return w;
+        w = QuantAttnPlan{};
     }
+    size_t slots, heads;
+    quant_plan_size(A, &w.plan, &slots, &heads);
+    w.run_head = align_up(slots, 256);
+    w.total = w.run_head + align_up(heads, 256);
+    w.fits = w.total < (size_t)1 << 36;
     return w;
 }
 

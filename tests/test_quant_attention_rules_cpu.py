@@ -54,3 +54,11 @@ def test_what_one_launch_takes_is_not_taken_as_a_prompt(T, n_head, group, d, L):
 def test_tokens_of_a_sequence_that_fill_little_of_a_tile_are_not_taken_as_prompts(group, d, few, many):
     for n_seq in (2, 32):
         assert not _as_prompts(few * n_seq, n_seq, 4, group, d, 24000) and _as_prompts(many * n_seq, n_seq, 4, group, d, 24000)
+
+
+@pytest.mark.parametrize("T,n_seq,n_head,group,d,L", [(1024, 64, 64, 5, 128, 1 << 20), (64, 1, 512, 5, 128, 1 << 23), (1 << 17, 1 << 12, (1 << 13) - 1, 1, 128, 1 << 30)])
+def test_copies_beyond_any_workspace_are_not_made(T, n_seq, n_head, group, d, L):
+    """Rows of a cache may be shared (strides of 0), so that sizes go further than memory does: such calls are taken as single tokens, not refused."""
+    size = _size(T, n_seq, n_head, group, d, L, 0.1)
+    assert size == _size(T, n_seq, n_head, group, d, L, -0.1) < 2 ** 36
+    assert _as_prompts(T, n_seq, min(n_head, 8), group, d, min(L, 1 << 12))
