@@ -133,23 +133,23 @@ __global__ void __launch_bounds__(kThreads) quant_write_kernel(const __grid_cons
     }
 }
 
-// by_slot: the heads of a slot lie side by side in the cache, and are read side by side
-__global__ void __launch_bounds__(kThreads) quant_read_kernel(const __grid_constant__ QuantView C, const __grid_constant__ QuantRead R, int by_slot) {
+// by_slot: the heads of a slot lie side by side in the cache, and are read side by side.  What there is to read of each sequence the host does not know, only how many
+// slots there are.  COUNTED: the sequences' tiles of rows are counted first, kThreads sequences at a time, and a CTA takes each gridDim.x-th of them.  Otherwise all
+// slots' tiles are looked at (see launch_quant_read).
+template <bool COUNTED>
+__global__ void __launch_bounds__(kThreads, 8) quant_read_kernel(const __grid_constant__ QuantView C, const __grid_constant__ QuantRead R, int by_slot) {
     chain_wait();
     chain_next();
     const int words = C.d_head / 8, G = C.d_head / kQuantGroup, at_once = kThreads / words;
     const int x = (int)threadIdx.x % words, r = (int)threadIdx.x / words, g = x / 4, t = x % 4;
-    const uint32_t inner = by_slot ? C.n_head : R.rows;
-    const long long rows = (long long)R.rows * C.n_head, tile = at_once * kReadRows, per_seq = (rows + tile - 1) / tile, all = per_seq * C.n_seq;
-    if (r >= at_once) return;
     const int word_at = (t * G + g) * 4;
-    for (long long b = blockIdx.x; b < all; b += gridDim.x) {
-        const int seq = (int)divide(b, per_seq);
-        const long long base = (b - seq * per_seq) * tile;
+    const long long tile = at_once * kReadRows;
+    // kReadRows times the CTA's rows from the base-th of the sequence's n * n_head on; slot_of_nth(i): where the i-th slot of those n lies from R.first on, or less than 0
+    const auto read = [&](int seq, long long base, int n, const auto& slot_of_nth) {
+        const long long rows = (long long)n * C.n_head;
+        const uint32_t inner = by_slot ? C.n_head : n;
         const int outer0 = (int)divide(base, inner);
         const uint32_t inner0 = (uint32_t)(base - (long long)outer0 * inner) + r;                // (below 2^31)
-        const int len = R.len ? R.len[seq] : INT_MAX;
-        const int4 range = R.range ? R.range[seq] : make_int4(INT_MAX, 0, 0, 0);
         const unsigned char *const K = C.K + seq * C.c_s + word_at, *const V = C.V + seq * C.c_s + word_at;
         const uint16_t* const Ks = reinterpret_cast<const uint16_t*>(C.K_scale) + seq * C.s_s + g;
         const uint16_t* const Vs = reinterpret_cast<const uint16_t*>(C.V_scale) + seq * C.s_s + g;
@@ -158,21 +158,78 @@ __global__ void __launch_bounds__(kThreads) quant_read_kernel(const __grid_const
 #pragma unroll
         for (int u = 0; u < kReadRows; ++u) {
             const uint32_t in = inner0 + u * at_once, over = in / inner, rest = in - over * inner;
-            const int outer = outer0 + (int)over, head = by_slot ? (int)rest : outer, n = by_slot ? outer : (int)rest, slot = R.first + n;
+            const int outer = outer0 + (int)over, head = by_slot ? (int)rest : outer, at_n = slot_of_nth(by_slot ? outer : (int)rest), slot = R.first + at_n;
             to[u] = -1;
-            if (base + r + u * at_once >= rows || slot >= len || (slot >= range.x && (slot < range.y || slot >= range.z))) continue;
+            if (base + r + u * at_once >= rows || at_n < 0) continue;
             const long long at = head * C.c_h + slot * C.c_p, s_at = head * C.s_h + slot * C.s_p;
             kw[u] = *reinterpret_cast<const uint32_t*>(K + at);
             vw[u] = *reinterpret_cast<const uint32_t*>(V + at);
             ks[u] = Ks[s_at];
             vs[u] = Vs[s_at];
-            to[u] = seq * R.o_s + head * R.o_h + n * R.o_p + 8 * x;
+            to[u] = seq * R.o_s + head * R.o_h + at_n * R.o_p + 8 * x;
         }
 #pragma unroll
         for (int u = 0; u < kReadRows; ++u) {
             if (to[u] < 0) continue;
             *reinterpret_cast<uint4*>(R.K + to[u]) = values_of(kw[u], ks[u]);
             *reinterpret_cast<uint4*>(R.V + to[u]) = values_of(vw[u], vs[u]);
+        }
+    };
+    if constexpr (COUNTED) {
+        __shared__ long long end_s[kThreads];           // tiles up to this sequence and with it
+        __shared__ int3 part_s[kThreads];               // of its slots: .x from the first on, then those from .y on, .z in all
+        __shared__ long long warp_sum_s[kThreads / 32];
+        const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+        long long b = blockIdx.x, before = 0;           // the next tile of this CTA; tiles of earlier sequences
+        for (int seq0 = 0; seq0 < C.n_seq; seq0 += kThreads) {
+            const int mine = seq0 + tid;
+            int3 part = make_int3(0, 0, 0);
+            if (mine < C.n_seq) {
+                if (R.range) {
+                    const int4 range = R.range[mine];
+                    part.x = range.x;
+                    part.y = max(range.y, range.x);
+                    part.z = range.x + max(range.z - part.y, 0);
+                } else {
+                    part.x = part.z = R.len ? min(max(R.len[mine], R.first) - R.first, R.rows) : R.rows;
+                }
+            }
+            long long end = ((long long)part.z * C.n_head + tile - 1) / tile;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long up = __shfl_up_sync(0xffffffffu, end, o);
+                if (lane >= o) end += up;
+            }
+            __syncthreads();                            // (everybody is past the tiles of the last ones)
+            if (lane == 31) warp_sum_s[warp] = end;
+            __syncthreads();
+            end += before;
+            for (int w = 0; w < warp; ++w) end += warp_sum_s[w];
+            end_s[tid] = end;
+            part_s[tid] = part;
+            __syncthreads();
+            const long long last = end_s[kThreads - 1];
+            for (; b < last; b += gridDim.x) {
+                int i = 0;                              // the sequences that end at or before tile b
+#pragma unroll
+                for (int k = 0; k < kThreads; k += 32) i += __popc(__ballot_sync(0xffffffffu, end_s[k + lane] <= b));
+                if (r >= at_once) continue;
+                const int3 p = part_s[i];
+                read(seq0 + i, (b - (i > 0 ? end_s[i - 1] : before)) * tile, p.z, [&](int n) { return n < p.x ? n : p.y + (n - p.x); });
+            }
+            before = last;
+        }
+    } else {
+        const long long per_seq = ((long long)R.rows * C.n_head + tile - 1) / tile, all = per_seq * C.n_seq;
+        if (r >= at_once) return;
+        for (long long b = blockIdx.x; b < all; b += gridDim.x) {
+            const int seq = (int)divide(b, per_seq);
+            const int len = R.len ? R.len[seq] : INT_MAX;
+            const int4 range = R.range ? R.range[seq] : make_int4(INT_MAX, 0, 0, 0);
+            read(seq, (b - seq * per_seq) * tile, R.rows, [&](int n) {
+                const int slot = R.first + n;
+                return slot >= len || (slot >= range.x && (slot < range.y || slot >= range.z)) ? -1 : n;
+            });
         }
     }
 }
@@ -220,10 +277,14 @@ dsmoe_status launch_quant_write(const QuantView& C, const QuantWrite& W, cudaStr
     return DSMOE_OK;
 }
 
+// Counting the sequences' tiles costs 1 us, and 3 for each kThreads sequences more; looking at slots that hold nothing takes far longer where caches are large and hold little.
+// So they are counted where all slots are more than four rounds of the grid.  Counted and not, us: 32 caches of 131072 slots that hold 200 9.7, 596 (and 32 prompts of 16 tokens on
+// them, 4 x 5 heads of 128, 43, 628); 32 of 819 to 8192 of 8192, 4 heads of 128 66, 81, full 116, 117 (6.9 rounds); 8 of 400 to 4000, heads of 96 10.8, 11.8, full 17.2, 15.6 (0.7);
+// 256 of 500, 2 heads of 64 23.2, 18.5 (0.9); 1000 of 300, one head of 128 63, 37 (2.1).
 dsmoe_status launch_quant_read(const QuantView& C, const QuantRead& R, cudaStream_t s) {
     const long long tile = kThreads / (C.d_head / 8) * kReadRows, all = ((long long)R.rows * C.n_head + tile - 1) / tile * C.n_seq;
     const long long most = 32ll * sm_count(), grid = all < most ? all : most;
-    DSMOE_CUDA_TRY(launch_chained(quant_read_kernel, (unsigned)grid, kThreads, 0, s, C, R, (int)(C.n_head > 1 && C.c_h < C.c_p)));
+    DSMOE_CUDA_TRY(launch_chained(all > 4 * most ? quant_read_kernel<true> : quant_read_kernel<false>, (unsigned)grid, kThreads, 0, s, C, R, (int)(C.n_head > 1 && C.c_h < C.c_p)));
     return DSMOE_OK;
 }
 

@@ -42,7 +42,7 @@ dsmoe_status launch_quant_write(const QuantView& C, const QuantWrite& W, cudaStr
 struct QuantRead {
     int first, rows;                      // slots first .. first + rows - 1
     const int32_t* len;                   // nullable: slots below len[sequence] alone
-    const int4* range;                    // nullable: of each sequence, slots below .x and those from .y to .z - 1 alone
+    const int4* range;                    // nullable (first 0, no len): of each sequence, slots below .x and those from .y to .z - 1 alone
     __nv_bfloat16 *K, *V;
     long long o_s, o_h, o_p;
 };
