@@ -1,5 +1,5 @@
 // Writing a cache in 4 bits and reading it back (see quant_cache.cuh for the format): a thread has a word of a row of K and the same one of V, 16 bytes of each as
-// bf16, and the threads of a warp follow the rows as they lie there.  Reading 32 caches of up to 8192 slots of 4 heads of 128 takes 96 us, 5.4 TB/s, of which three
+// bf16, and the threads of a warp follow the rows as they lie there.  Reading 32 caches of up to 8192 slots of 4 heads of 128 takes 88 us, 5.9 TB/s, of which three
 // quarters are writes.  Writing 4 x 8192 tokens takes 31 us, 5 TB/s, and is bound by instructions (410 a warp of 512 values; issue slots 84 %).
 #include "quant_cache.cuh"
 
@@ -7,8 +7,8 @@ namespace dsmoe {
 
 namespace {
 
-// kReadRows: rows that a thread of the reading kernel has under way.  32 caches of up to 8192 slots of 4 heads of 128, us: 96 with 4 of them and 128 threads (5.4 TB/s),
-// with 2 122, with 8 112, with 256 threads 102, with 512 109; with addresses that are steps apart instead of products 100.
+// kReadRows: rows that a thread of the reading kernel has under way.  32 caches of up to 8192 slots of 4 heads of 128, us: 88 with 4 of them and 128 threads (5.9 TB/s),
+// with 2 99, with 8 95, with 256 threads 102, with 512 112.
 constexpr int kThreads = 128, kReadRows = 4;
 
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
@@ -278,13 +278,13 @@ dsmoe_status launch_quant_write(const QuantView& C, const QuantWrite& W, cudaStr
 }
 
 // Counting the sequences' tiles costs 1 us, and 3 for each kThreads sequences more; looking at slots that hold nothing takes far longer where caches are large and hold little.
-// So they are counted where all slots are more than four rounds of the grid.  Counted and not, us: 32 caches of 131072 slots that hold 200 9.7, 596 (and 32 prompts of 16 tokens on
+// So they are counted where all slots are more than four rounds of the grid, and one more for each kThreads sequences.  Counted and not, us: 32 caches of 131072 slots that hold 200 9.7, 596 (and 32 prompts of 16 tokens on
 // them, 4 x 5 heads of 128, 43, 628); 32 of 819 to 8192 of 8192, 4 heads of 128 66, 81, full 116, 117 (6.9 rounds); 8 of 400 to 4000, heads of 96 10.8, 11.8, full 17.2, 15.6 (0.7);
 // 256 of 500, 2 heads of 64 23.2, 18.5 (0.9); 1000 of 300, one head of 128 63, 37 (2.1).
 dsmoe_status launch_quant_read(const QuantView& C, const QuantRead& R, cudaStream_t s) {
     const long long tile = kThreads / (C.d_head / 8) * kReadRows, all = ((long long)R.rows * C.n_head + tile - 1) / tile * C.n_seq;
     const long long most = 32ll * sm_count(), grid = all < most ? all : most;
-    DSMOE_CUDA_TRY(launch_chained(all > 4 * most ? quant_read_kernel<true> : quant_read_kernel<false>, (unsigned)grid, kThreads, 0, s, C, R, (int)(C.n_head > 1 && C.c_h < C.c_p)));
+    DSMOE_CUDA_TRY(launch_chained(all > most * (4 + C.n_seq / kThreads) ? quant_read_kernel<true> : quant_read_kernel<false>, (unsigned)grid, kThreads, 0, s, C, R, (int)(C.n_head > 1 && C.c_h < C.c_p)));
     return DSMOE_OK;
 }
 

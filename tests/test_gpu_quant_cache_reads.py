@@ -13,10 +13,10 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("by_token", [False, True])
 @pytest.mark.parametrize("n_seq,n_head,L,d,first,rows", [(300, 2, 70, 96, 3, 60), (129, 1, 90, 32, 0, 90), (128, 3, 33, 256, 32, 1), (5, 4, 700, 64, 100, 555),
                                                          (1, 1, 1, 32, 0, 1), (1000, 1, 7, 160, 1, 5),
-                                                         (300, 2, 530, 256, 7, 520), (3, 2, 52000, 224, 1, 51999)])
+                                                         (300, 2, 530, 256, 7, 520), (3, 2, 52000, 224, 1, 51999), (257, 2, 900, 224, 7, 890)])
 def test_what_is_held_of_many_sequences(n_seq, n_head, L, d, first, rows, by_token):
-    """Lengths below nothing, of nothing, before the first slot that is asked for, within them, and beyond; all of a sequence beside none of its neighbours.  The last two
-    sizes are more than four times what a grid takes at once."""
+    """Lengths below nothing, of nothing, before the first slot that is asked for, within them, and beyond; all of a sequence beside none of its neighbours.  The last
+    sizes are more than four to six times what a grid takes at once."""
     rng = np.random.default_rng(n_seq + d)
     parts = []
     for _ in range(2):                             # (rows out of 1009, in another order for each sequence and head)
