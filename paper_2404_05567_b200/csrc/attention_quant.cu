@@ -16,11 +16,11 @@
 //      A product is a multiple of 2^-34 of that (2^-24, and kRaise): it has 11 bits where the weight is 2^-23 of the row's largest or more beside scales like the
 //      largest, 2^-17 beside the smallest, 2^-7; it is nothing below 2^-35 and 2^-28.  So once the warp has met scales of a pair that are further apart (2^6 to
 //      2^8), or no numbers, it goes another way: values are bf16 numbers s * c and weights two bf16 numbers each (62 tokens with up to 8192 keys, of which the first
-//      four have values 2^-9 as large: 70.7 us instead of 65.6).
+//      four have values 2^-9 as large: 69 us instead of 66).
 // The logits' layout holds two rows of a key side by side, the weights' two keys of a row: movmatrix.
 // What bounds it: 62 tokens with up to 8192 keys, 4 x 5 heads of 128 by position, take 66 us (their 4.5 bits a value at 6.45 TB/s 34): the copies alone 50, of which 35
 // at 6.3 TB/s and the rest before the first key and behind the last one; a unit's chain of scales, products, maximum, exponentials, transposition and products,
-// with three warps a scheduler to cover it, 16 more (ALU 52 %, tensor pipe 20 %, issue slots 56 % of the cycles).  2 tokens with 131072 keys, 8 x 4 heads: 76 (44).
+// with three warps a scheduler to cover it, 16 more (ALU 52 %, tensor pipe 20 %, issue slots 56 % of the cycles).  2 tokens with 131072 keys, 8 x 4 heads: 74 (44).
 #include <cuda_fp16.h>
 
 #include <algorithm>
